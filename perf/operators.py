@@ -1,0 +1,575 @@
+"""Performance cases of the operators that evaluate and retrain a DARB layer.
+
+After a language model has been pruned, a program scores texts with it (log probabilities of
+the given tokens, with their entropy and the most likely alternatives) and retrains the
+retained weights (the same loss with its gradient, the gradients of the DARB product and of
+the layer norm before it, and an AdamW step over all tensors).  Activations are [features x
+batch], as the DARB products read and write them: feature-major ("features", a feature's
+values contiguous), or token-major ("tokens"), which reaches the calls as a transposed view.
+
+``own`` false computes each operator in elementary torch operations, in 32 bits; true calls
+the framework.  Sizes are those of the workloads (4096 x 9216 head, 1024-wide LSTM with 200
+steps of 32, the 1500-wide language model of the paper with its vocabulary of 10 000 words)
+and generic ones around them.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda"
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+SIZE = {"f32": 4, "f16": 2, "bf16": 2}
+BLOCK = 256          # elements of an 8-bit state that share a scale
+LR, BETA1, BETA2, EPS, DECAY = 1e-3, 0.9, 0.999, 1e-8, 0.01
+LN_EPS = 1e-5
+
+
+# ---------------------------------------------------------------------------------------
+# cases
+# ---------------------------------------------------------------------------------------
+
+def _logprob(op, V, B, dtype, order, top=0, masked=False, entropy=True):
+    return dict(op=op, V=V, B=B, dtype=dtype, order=order, top=top, masked=masked,
+                entropy=entropy)
+
+
+def _norm(op, H, B, dtype, order, wdtype="f32"):
+    return dict(op=op, H=H, B=B, dtype=dtype, order=order, wdtype=wdtype)
+
+
+def _adamw(count, total, dtype, gdtype, bits, masters):
+    return dict(op="adamw", count=count, total=total, dtype=dtype, gdtype=gdtype, bits=bits,
+                masters=masters)
+
+
+def _grad(M, N, B, wdtype, xdtype, b_min, b_max):
+    return dict(op="spmm_grad", M=M, N=N, B=B, wdtype=wdtype, xdtype=xdtype, b_min=b_min,
+                b_max=b_max)
+
+
+def listed():
+    cases = {
+        # one generated token: its log probability and five alternatives, some words ruled out
+        "logprob_next_token": _logprob("logprobs", 10000, 1, "f32", "features", 5, masked=True),
+        # perplexity of 35 steps of a batch of 20 (some places padded), straight from the
+        # product that made the logits
+        "logprob_eval_lm": _logprob("logprobs", 10000, 700, "f32", "features"),
+        # the loss's gradient on the same batch, entropy term included
+        "logprob_grad_lm": _logprob("logprobs_grad", 10000, 700, "f32", "features"),
+        # scoring with a wide vocabulary in bf16, token by token, with 20 alternatives
+        "logprob_wide_bf16": _logprob("logprobs", 131072, 512, "bf16", "tokens", 20),
+        # a gradient whose rows are odd in length and in number, fp16
+        "logprob_grad_odd_f16": _logprob("logprobs_grad", 50001, 1023, "f16", "tokens",
+                                         entropy=False),
+        # layer norm of one step of the 1024-wide LSTM's batch of 32 (latency)
+        "norm_step": _norm("norm", 1024, 32, "f32", "features"),
+        # its gradients over the whole sequence of 200 steps
+        "norm_grad_seq": _norm("norm_grad", 1024, 6400, "f32", "features"),
+        # gradients of a wide layer, token-major bf16, an odd number of tokens
+        "norm_grad_wide_bf16": _norm("norm_grad", 9216, 2047, "bf16", "tokens", "bf16"),
+        # retraining the retained weights of a small language model: 14 fp32 tensors
+        "adamw_lm": _adamw(14, 4_000_000, "f32", "f32", 32, False),
+        # many fp16 tensors with fp32 masters and states in 8 bits, moments exported
+        "adamw_many_8bit": _adamw(96, 64_000_000, "f16", "f32", 8, True),
+        # gradients of the 4096 x 9216 head at the metric's batch of 64
+        "grad_fc_b64": _grad(4096, 9216, 64, "f32", "f32", 8, 128),
+        # gradients of the language model's output layer: 10 000 words, fp16 weights
+        "grad_lm_b700": _grad(10000, 1500, 700, "f16", "f32", 4, 64),
+    }
+    return [dict(c, name=n) for n, c in cases.items()]
+
+
+def _log_int(rng, lo, hi):
+    v = int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    step = rng.choice([1, 1, 4, 16, 64])     # most sizes are multiples of something
+    return max(lo, min(hi, v // step * step))
+
+
+def draw(rng):
+    kind = rng.choice(["logprobs", "logprobs_grad", "norm", "norm_grad", "adamw", "spmm_grad"])
+    dtype = rng.choice(["f32", "f16", "bf16"])
+    order = rng.choice(["features", "tokens"])
+    if kind.startswith("logprobs"):
+        V = _log_int(rng, 200, 131072)
+        B = _log_int(rng, 1, max(1, min(4096, 60_000_000 // V)))
+        top = rng.choice([0, 1, 5, 20, 50]) if kind == "logprobs" else 0
+        return _logprob(kind, V, B, dtype, order, top, masked=rng.random() < 0.3,
+                        entropy=rng.random() < 0.7)
+    if kind.startswith("norm"):
+        H = _log_int(rng, 16, 9216)
+        B = _log_int(rng, 1, max(1, min(16384, 18_000_000 // H)))
+        return _norm(kind, H, B, dtype, order, rng.choice(["f32", dtype]))
+    if kind == "adamw":
+        count = _log_int(rng, 1, 120)
+        total = max(count, _log_int(rng, 10_000, 60_000_000))
+        return _adamw(count, total, dtype, rng.choice(["f32", dtype]), rng.choice([32, 8]),
+                      dtype != "f32" and rng.random() < 0.6)
+    N = _log_int(rng, 200, 9216)
+    M = _log_int(rng, 256, 10000)
+    B = _log_int(rng, 1, max(1, min(1024, 10_000_000_000 // (M * N))))
+    wdtype = rng.choice(["f32", "f16"])
+    xdtype = rng.choice(["f32", "f16"]) if wdtype == "f16" else "f32"
+    return _grad(M, N, B, wdtype, xdtype, rng.choice([4, 8]), rng.choice([32, 64, 128]))
+
+
+# ---------------------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------------------
+
+def _generator(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed) * 2 + 1)
+    return g
+
+
+def _activations(g, F, B, dtype, order, spread=1.0, shift=0.0):
+    """[F, B] in the memory order asked for."""
+    shape = (F, B) if order == "features" else (B, F)
+    t = (torch.randn(shape, generator=g, device=DEV) * spread + shift).to(TYPES[dtype])
+    return t if order == "features" else t.t()
+
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    op = case["op"]
+    if op.startswith("logprobs"):
+        return _prepare_logprobs(case, g)
+    if op.startswith("norm"):
+        return _prepare_norm(case, g)
+    if op == "adamw":
+        return _prepare_adamw(case, g)
+    return _prepare_grad(case, g)
+
+
+def _prepare_logprobs(case, g):
+    V, B = case["V"], case["B"]
+    z = _activations(g, V, B, case["dtype"], case["order"], spread=2.5)
+    t = torch.randint(0, V, (B,), generator=g, device=DEV)
+    if case["masked"]:                       # words that a grammar rules out everywhere
+        out = torch.rand(V, generator=g, device=DEV) < 0.3
+        out[t] = False
+        z.masked_fill_(out[:, None], -math.inf)
+    t[torch.rand(B, generator=g, device=DEV) < 1 / 16] = -1          # padded places
+    s = dict(case=case, z=z, t=t)
+    if case["op"] == "logprobs_grad":
+        f = z.float()
+        m = f.amax(0)
+        e = torch.exp(f - m)
+        S = e.sum(0)
+        s["lse"] = m + torch.log(S)
+        scale = 1024.0 if case["dtype"] == "f16" else 1.0            # a loss scale
+        s["g"] = -scale / B * (0.5 + torch.rand(B, generator=g, device=DEV))
+        if case["entropy"]:
+            d = torch.where(e > 0, f - m, 0.0)
+            s["entropy"] = torch.log(S) - (e * d).sum(0) / S
+            s["ge"] = torch.full((B,), -0.05 * scale / B, device=DEV)
+    return s
+
+
+def _prepare_norm(case, g):
+    H, B = case["H"], case["B"]
+    x = _activations(g, H, B, case["dtype"], case["order"], 0.7, 0.1)
+    w = (1 + 0.2 * torch.randn(H, generator=g, device=DEV)).to(TYPES[case["wdtype"]])
+    b = (0.1 * torch.randn(H, generator=g, device=DEV)).to(TYPES[case["wdtype"]])
+    s = dict(case=case, x=x, w=w, b=b)
+    if case["op"] == "norm_grad":
+        s["dy"] = _activations(g, H, B, case["dtype"], case["order"], 0.3)
+        f = x.float()
+        s["mean"] = f.mean(0)
+        s["rstd"] = 1 / torch.sqrt((f - s["mean"]).square().mean(0) + LN_EPS)
+    return s
+
+
+def _tensor_sizes(case):
+    """Sizes of a model's tensors: large matrices and small vectors, adding up to the total."""
+    r = np.random.default_rng(case["count"])
+    share = np.exp(r.normal(0.0, 1.2, case["count"]))
+    return [max(1, int(n)) for n in share / share.sum() * case["total"]]
+
+
+def _prepare_adamw(case, g):
+    # the tensors lie in one buffer of each kind, each starting on a whole block
+    sizes = _tensor_sizes(case)
+    rooms = [-(-n // BLOCK) * BLOCK for n in sizes]
+    starts = np.concatenate([[0], np.cumsum(rooms)])
+    total = int(starts[-1])
+    live = torch.zeros(total, dtype=torch.bool, device=DEV)
+    for n, a in zip(sizes, starts):
+        live[a:a + n] = True
+
+    def draw_flat(spread):
+        return torch.where(live, torch.randn(total, generator=g, device=DEV) * spread, 0.0)
+
+    scale = torch.exp(1.5 * torch.randn(total // BLOCK, 1, generator=g, device=DEV)).expand(
+        -1, BLOCK).reshape(-1)
+    p = draw_flat(0.05)
+    s = dict(case=case, t=10, p=p.to(TYPES[case["dtype"]]),
+             g=(draw_flat(1e-2) * scale).to(TYPES[case["gdtype"]]))
+    if case["masters"]:
+        s["master"] = p
+    m, v = draw_flat(3e-3) * scale, (draw_flat(1e-2) * scale).square() + live * 1e-9
+    if case["bits"] == 32:
+        s["m"], s["v"] = m, v
+    else:
+        # element's counter of the random numbers that round the states
+        at = torch.arange(total, device=DEV) - torch.as_tensor(
+            np.repeat(starts[:-1], rooms), device=DEV)
+        key = torch.as_tensor(np.repeat(np.arange(len(sizes)) * 0xBB67AE85, rooms), device=DEV)
+        s["counter"] = (at + key).to(torch.int32)          # modulo 2^32
+        s["mc"], s["ms"] = _to_codes(m, torch.zeros_like(s["counter"]), 20, 889, 127)
+        s["vc"], s["vs"] = _to_codes(v, torch.zeros_like(s["counter"]), 19, 1777, 255)
+    if own:
+        import paper_1911_08020_amd as darb
+        cut = lambda flat: [flat[a:a + n] for n, a in zip(sizes, starts)]       # noqa: E731
+        blocks = lambda flat: [flat[a // BLOCK:(a + r) // BLOCK]                # noqa: E731
+                               for r, a in zip(rooms, starts)]
+        if case["bits"] == 32:
+            state = list(zip(cut(s["m"]), cut(s["v"])))
+        else:
+            state = list(zip(cut(s["mc"]), cut(s["vc"]), blocks(s["ms"]), blocks(s["vs"])))
+            s["m"], s["v"] = torch.zeros(total, device=DEV), torch.zeros(total, device=DEV)
+            s["moments"] = (cut(s["m"]), cut(s["v"]))
+        s["optimizer"] = darb.AdamW(cut(s["p"]), lr=LR, betas=(BETA1, BETA2), eps=EPS,
+                                    weight_decay=DECAY, state_bits=case["bits"],
+                                    masters=cut(s["master"]) if case["masters"] else None,
+                                    state=state, steps=s["t"])
+        s["grads"] = cut(s["g"])
+    return s
+
+
+def _rows_of_sizes(case):
+    """Block sizes (log2) and the rows of each; the sparsest rows are the most."""
+    l2 = np.arange(int(math.log2(case["b_min"])), int(math.log2(case["b_max"])) + 1)
+    rows = np.full(len(l2), int(case["M"] / (1.6 * len(l2))))
+    rows[-1] += case["M"] - rows.sum()
+    return l2, rows
+
+
+def _prepare_grad(case, g):
+    M, N, B = case["M"], case["N"], case["B"]
+    l2 = torch.as_tensor(np.repeat(*_rows_of_sizes(case)), device=DEV)
+    l2 = l2[torch.randperm(M, generator=g, device=DEV)]
+    # storage order: rows by block size, then by number; a row's blocks in order
+    order = torch.sort(l2, stable=True).indices
+    b = 1 << l2[order]
+    blocks = (N + b - 1) // b
+    row = torch.repeat_interleave(order, blocks)
+    width = torch.repeat_interleave(b, blocks)
+    first = torch.cumsum(blocks, 0) - blocks
+    col0 = (torch.arange(len(row), device=DEV) - torch.repeat_interleave(first, blocks)) * width
+    room = torch.minimum(width, N - col0)
+    off = (torch.rand(len(row), generator=g, device=DEV) * room).long().clamp_(max=room - 1)
+    s = dict(case=case, row=row, col=col0 + off, offsets=off.to(torch.uint8),
+             values=(0.1 * torch.randn(len(row), generator=g, device=DEV)).to(
+                 TYPES[case["wdtype"]]),
+             X=_activations(g, N, B, case["xdtype"], "features"),
+             dY=_activations(g, M, B, "f32", "features", 0.1))
+    s["at"] = s["row"] * N + s["col"]
+    if own:
+        import paper_1911_08020_amd as darb
+        density = 1.0 / (1 << l2).double().cpu().numpy()
+        s["plan"] = darb.Plan(M, N, density, 0.5, darb.ROUND_FLOOR, case["b_min"],
+                              case["b_max"]).upload()
+        # the columns' index lasts as long as the mask: a program keeps it while it retrains
+        s["index"] = s["plan"].transpose(s["offsets"])
+    return s
+
+
+# ---------------------------------------------------------------------------------------
+# one pass
+# ---------------------------------------------------------------------------------------
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return PLAIN[state["case"]["op"]](state)
+
+
+def _run_own(s):
+    import paper_1911_08020_amd as darb
+    op = s["case"]["op"]
+    if op == "logprobs":
+        r = darb.token_logprobs(s["z"], s["t"], top=s["case"]["top"])
+        out = dict(logprob=r.logprob, entropy=r.entropy, lse=r.lse)
+        if s["case"]["top"]:
+            out.update(top_logprob=r.top_logprob, top_index=r.top_index)
+        return out
+    if op == "logprobs_grad":
+        return dict(dz=darb.token_logprobs_grad(s["z"], s["t"], s["lse"], s["g"],
+                                                entropy=s.get("entropy"),
+                                                grad_entropy=s.get("ge")))
+    if op == "norm":
+        y, mean, rstd = darb.layer_norm(s["x"], s["w"], s["b"], eps=LN_EPS)
+        return dict(y=y, mean=mean, rstd=rstd)
+    if op == "norm_grad":
+        dx, dw, db = darb.layer_norm_grad(s["dy"], s["x"], s["mean"], s["rstd"], s["w"])
+        return dict(dx=dx, dw=dw, db=db)
+    if op == "adamw":
+        s["optimizer"].step(s["grads"])
+        if s["case"]["bits"] == 8:
+            s["optimizer"].moments(out=s["moments"])
+        return _adamw_outputs(s)
+    dv, dX = s["plan"].spmm_grad(s["index"], s["values"], s["X"], s["dY"])
+    return dict(dvalues=dv, dX=dX)
+
+
+def _adamw_outputs(s):
+    out = dict(p=s["p"], m=s["m"], v=s["v"])
+    if s["case"]["masters"]:
+        out["master"] = s["master"]
+    return out
+
+
+# ---------------------------------------------------------------------------------------
+# the plain forms
+# ---------------------------------------------------------------------------------------
+
+def _plain_logprobs(s):
+    z, t, top = s["z"].float(), s["t"], s["case"]["top"]
+    m = z.amax(0)
+    d = z - torch.where(m == -math.inf, 0.0, m)
+    e = torch.exp(d)
+    S = e.sum(0)
+    lse = m + torch.log(torch.where(m == -math.inf, 1.0, S))
+    # a probability of zero adds nothing to the entropy
+    entropy = torch.log(S) - torch.where(e > 0, e * d, 0.0).sum(0) / S
+    entropy = torch.where(m == -math.inf, 0.0, entropy)
+    given = z.gather(0, t.clamp(min=0)[None])[0] - lse
+    logprob = torch.where(t < 0, 0.0, torch.where(m == -math.inf, -math.inf, given))
+    out = dict(logprob=logprob, entropy=entropy, lse=lse)
+    if top:
+        # the value's order in the upper half, the lowest index first below it
+        i = (z + 0.0).view(torch.int32)
+        key = torch.where(i < 0, i ^ 0x7FFFFFFF, i).long() << 32
+        key += (0x7FFFFFFF - torch.arange(z.shape[0], device=DEV))[:, None]
+        index = torch.topk(key, top, dim=0).indices
+        out["top_logprob"] = (z.gather(0, index) - lse).t().contiguous()
+        out["top_index"] = index.t().contiguous()
+    return out
+
+
+def _plain_logprobs_grad(s):
+    z, t = s["z"].float(), s["t"]
+    lp = z - s["lse"]
+    p = torch.exp(lp)
+    dz = -p * s["g"]
+    hit = torch.arange(z.shape[0], device=DEV)[:, None] == t
+    dz = torch.where(hit, dz + s["g"], dz)
+    dz = torch.where(t < 0, 0.0, dz)          # no given token, no gradient of it
+    if s["case"]["entropy"]:
+        dz = dz - torch.where(p > 0, s["ge"] * p * (lp + s["entropy"]), 0.0)
+    return dict(dz=dz.to(s["z"].dtype))
+
+
+def _plain_norm(s):
+    x = s["x"].float()
+    mean = x.mean(0)
+    c = x - mean
+    rstd = 1 / torch.sqrt(c.square().mean(0) + LN_EPS)
+    y = c * rstd * s["w"].float()[:, None] + s["b"].float()[:, None]
+    return dict(y=y.to(s["x"].dtype), mean=mean, rstd=rstd)
+
+
+def _plain_norm_grad(s):
+    x, dy, rstd = s["x"].float(), s["dy"].float(), s["rstd"]
+    xh = (x - s["mean"]) * rstd
+    a = dy * s["w"].float()[:, None]
+    dx = rstd * (a - a.mean(0) - xh * (a * xh).mean(0))
+    return dict(dx=dx.to(s["x"].dtype), dw=(dy * xh).sum(1), db=dy.sum(1))
+
+
+def _random_bits(counter):
+    """32 mixed bits of each 32-bit counter (multiplications modulo 2^32)."""
+    x = counter ^ ((counter >> 16) & 0xFFFF)
+    x = x * -1640531527                      # 0x9E3779B9, of the golden ratio
+    x = x ^ ((x >> 15) & 0x1FFFF)
+    x = x * -1257966797                      # 0xB504F333, of the square root of a half
+    return x ^ ((x >> 16) & 0xFFFF)
+
+
+def _to_codes(x, random, shift, low, top):
+    """Codes and block scales of x: the scale is the block's greatest magnitude a, the code the
+    leading bits of |x| / a after ``random`` (below 2^shift) was added to its bits.  Codes of 7
+    bits carry a sign; those of 8 bits stand for values that are not negative, and one that is
+    not zero keeps at least the lowest code."""
+    x = x.view(-1, BLOCK)
+    a = x.abs().amax(1, keepdim=True)
+    a = torch.where(a < 2.0 ** -120, 0.0, a)
+    q = x.abs() * torch.where(a > 0, 1 / a, 0.0)
+    c = ((q.view(torch.int32) + random.view(-1, BLOCK)) >> shift) - low
+    c = c.clamp(0, top)
+    if top == 255:
+        c = torch.where((x > 0) & (a > 0), c.clamp(min=1), torch.where(a > 0, c, 0))
+    else:
+        c = torch.where(c > 0, c + 128 * (x < 0), 0)
+    return c.to(torch.uint8).view(-1), a.view(-1)
+
+
+def _from_codes(code, scale, shift, low, top):
+    c = code.view(-1, BLOCK).int()
+    mag = c & top
+    x = torch.where(mag > 0, ((mag + low) << shift).view(torch.float32), 0.0) * scale[:, None]
+    return (x if top == 255 else torch.where(c > 127, -x, x)).view(-1)
+
+
+def _plain_adamw(s):
+    c = s["case"]
+    s["t"] += 1
+    t, g = s["t"], s["g"].float()
+    p = s["master"] if c["masters"] else s["p"].float()
+    if c["bits"] == 32:
+        m, v = s["m"], s["v"]
+    else:
+        m = _from_codes(s["mc"], s["ms"], 20, 889, 127)
+        v = _from_codes(s["vc"], s["vs"], 19, 1777, 255)
+    m = m * BETA1 + g * (1 - BETA1)
+    v = v * BETA2 + (g * g) * (1 - BETA2)
+    d = torch.sqrt(v) * (1 / math.sqrt(1 - BETA2 ** t)) + EPS
+    p = p * (1 - LR * DECAY) - (m / d) * (LR / (1 - BETA1 ** t))
+    if c["masters"]:
+        s["master"].copy_(p)
+    s["p"].copy_(p)
+    if c["bits"] == 8:
+        # the step's own random numbers: a stream per step
+        step = (t * 0x6A09E667) & 0xFFFFFFFF
+        x = _random_bits(s["counter"] + (step - (1 << 32) if step >> 31 else step))
+        s["mc"], s["ms"] = _to_codes(m, (x & 0xFFFF) << 4, 20, 889, 127)
+        s["vc"], s["vs"] = _to_codes(v, ((x >> 16) & 0xFFFF) << 3, 19, 1777, 255)
+        s["m"] = _from_codes(s["mc"], s["ms"], 20, 889, 127)
+        s["v"] = _from_codes(s["vc"], s["vs"], 19, 1777, 255)
+    else:
+        s["m"].copy_(m)
+        s["v"].copy_(v)
+    return _adamw_outputs(s)
+
+
+def _plain_spmm_grad(s):
+    # the dense products: by the decoded matrix, and of all pairs of rows
+    M, N = s["case"]["M"], s["case"]["N"]
+    W = torch.zeros(M * N, device=DEV)
+    W[s["at"]] = s["values"].float()
+    dX = W.view(M, N).t() @ s["dY"]
+    every = s["dY"] @ s["X"].float().t()
+    return dict(dvalues=every.view(-1)[s["at"]], dX=dX)
+
+
+PLAIN = {"logprobs": _plain_logprobs, "logprobs_grad": _plain_logprobs_grad,
+         "norm": _plain_norm, "norm_grad": _plain_norm_grad, "adamw": _plain_adamw,
+         "spmm_grad": _plain_spmm_grad}
+
+
+# ---------------------------------------------------------------------------------------
+# what a pass cannot do without
+# ---------------------------------------------------------------------------------------
+
+def work(case):
+    op = case["op"]
+    if op.startswith("logprobs"):
+        n, z = case["V"] * case["B"], SIZE[case["dtype"]]
+        if op == "logprobs":
+            return dict(bytes=n * z + case["B"] * (8 + 12 + 12 * case["top"]), flops=6 * n)
+        return dict(bytes=2 * n * z + 24 * case["B"], flops=6 * n)
+    if op.startswith("norm"):
+        n, z = case["H"] * case["B"], SIZE[case["dtype"]]
+        w = SIZE[case["wdtype"]] * case["H"]
+        if op == "norm":
+            return dict(bytes=2 * n * z + 2 * w + 8 * case["B"], flops=7 * n)
+        return dict(bytes=3 * n * z + w + 8 * case["H"] + 8 * case["B"], flops=13 * n)
+    if op == "adamw":
+        n, z = case["total"], SIZE[case["dtype"]]
+        each = SIZE[case["gdtype"]] + z + (8 if case["masters"] else z)
+        # 8 bits: two codes read and written, two scales a block, the moments exported
+        each += 16 if case["bits"] == 32 else 4 + 16 / BLOCK + 8
+        return dict(bytes=n * each, flops=16 * n)
+    M, N, B = case["M"], case["N"], case["B"]
+    nnz = sum(int(rows) * -(-N // (1 << int(l2))) for l2, rows in zip(*_rows_of_sizes(case)))
+    # values and offsets, both operands, both gradients, the row order
+    return dict(bytes=nnz * (SIZE[case["wdtype"]] + 1 + 4) + 4 * M +
+                (N * SIZE[case["xdtype"]] + 4 * M + 4 * N) * B, flops=4 * nnz * B)
+
+
+# ---------------------------------------------------------------------------------------
+# the definitions in 64 bits
+# ---------------------------------------------------------------------------------------
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    op = case["op"]
+    if op.startswith("logprobs"):
+        z, t = s["z"].t().double(), s["t"]                          # [B, V]
+        lse = torch.logsumexp(z, 1)
+        lp = z - lse[:, None]
+        p = lp.exp()
+        rows = torch.arange(len(t), device=DEV)
+        if op == "logprobs":
+            out = dict(lse=lse, entropy=torch.special.entr(p).sum(1),
+                       logprob=torch.where(t < 0, 0.0, lp[rows, t.clamp(min=0)]))
+            if case["top"]:
+                index = torch.sort(s["z"].t().float(), dim=1, descending=True,
+                                   stable=True).indices[:, :case["top"]]
+                out.update(top_index=index, top_logprob=lp.gather(1, index))
+            return out
+        # the gradient runs from the log sum and the entropy that the first pass handed on
+        lp = z - s["lse"].double()[:, None]
+        p = lp.exp()
+        given = torch.zeros_like(p)
+        given[rows, t.clamp(min=0)] = 1.0
+        dz = torch.where(t < 0, 0.0, s["g"].double())[:, None] * (given - p)
+        if case["entropy"]:
+            both = torch.xlogy(p, p) + p * s["entropy"].double()[:, None]
+            dz = dz - s["ge"].double()[:, None] * both
+        return dict(dz=dz.t())
+    if op.startswith("norm"):
+        x, w = s["x"].t().double(), s["w"].double()                 # [B, H]
+        if op == "norm":
+            var, mean = torch.var_mean(x, dim=1, correction=0, keepdim=True)
+            rstd = (var + LN_EPS).rsqrt()
+            return dict(y=((x - mean) * rstd * w + s["b"].double()).t(), mean=mean[:, 0],
+                        rstd=rstd[:, 0])
+        dy = s["dy"].t().double()
+        rstd = s["rstd"].double()[:, None]
+        xh = (x - s["mean"].double()[:, None]) * rstd
+        a = dy * w
+        n = x.shape[1]
+        dx = rstd / n * (n * a - a.sum(1, keepdim=True) -
+                         xh * torch.linalg.vecdot(a, xh)[:, None])
+        return dict(dx=dx.t(), dw=torch.linalg.vecdot(dy, xh, dim=0), db=dy.sum(0))
+    if op == "adamw":
+        t, g = s["t"] + 1, s["g"].double()
+        p = (s["master"] if case["masters"] else s["p"]).double()
+        if case["bits"] == 32:
+            m, v = s["m"].double(), s["v"].double()
+        else:
+            m, v = _values_of(s["mc"], s["ms"], 3), _values_of(s["vc"], s["vs"], 4)
+        m = torch.lerp(g, m, BETA1)
+        v = torch.lerp(g.square(), v, BETA2)
+        step = (m / (1 - BETA1 ** t)) / ((v / (1 - BETA2 ** t)).sqrt() + EPS)
+        p = p - LR * DECAY * p - LR * step
+        # states in 8 bits are rounded by random numbers: they have no exact value
+        return dict(p=p, m=m if case["bits"] == 32 else None, v=v if case["bits"] == 32 else None,
+                    **(dict(master=p) if case["masters"] else {}))
+    dX = torch.zeros(case["N"], case["B"], dtype=torch.float64, device=DEV)
+    dv = torch.zeros(len(s["row"]), dtype=torch.float64, device=DEV)
+    part = max(1, 100_000_000 // case["B"])
+    for a in range(0, len(dv), part):
+        r, c = s["row"][a:a + part], s["col"][a:a + part]
+        dy = s["dY"][r].double()
+        dv[a:a + part] = (dy * s["X"][c].double()).sum(1)
+        dX.index_add_(0, c, dy * s["values"][a:a + part].double()[:, None])
+    return dict(dvalues=dv, dX=dX)
+
+
+def _values_of(code, scale, mantissa):
+    """Code by code through a table: 2^e (1 + f / 2^mantissa), the greatest code being 1."""
+    n = 1 << (7 if mantissa == 3 else 8)
+    table = [0.0]
+    for c in range(1, n):
+        e, f = divmod(c + 1 - n, 1 << mantissa)       # the greatest code is 2^0
+        table.append(2.0 ** e * (1 + f / (1 << mantissa)))
+    table = torch.tensor(table + ([-x for x in table] if n == 128 else []), dtype=torch.float64,
+                         device=DEV)
+    return (table[code.long()].view(-1, BLOCK) * scale.double()[:, None]).view(-1)
