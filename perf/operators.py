@@ -132,7 +132,6 @@ def _activations(g, F, B, dtype, order, spread=1.0, shift=0.0):
     return t if order == "features" else t.t()
 
 
-
 def prepare(case, seed):
     g = _generator(seed)
     op = case["op"]
