@@ -55,7 +55,9 @@ extern "C" {
 #define DARB_E_NOMEM (-5)        /* host allocation failed */
 #define DARB_E_WORKSPACE (-6)    /* workspace too small */
 
-typedef enum { DARB_F32 = 0, DARB_F16 = 1 } darb_dtype;
+/* DARB_BF16 is taken by the evaluation and retraining calls only (logits, layer norm,
+ * parameters and their gradients); the format and its products are fp32 or fp16. */
+typedef enum { DARB_F32 = 0, DARB_F16 = 1, DARB_BF16 = 2 } darb_dtype;
 
 /* Rounding of a row density to a power-of-two fraction (section 3.2). */
 typedef enum {
@@ -355,6 +357,183 @@ int darb_lstm_layer(const darb_plan *wih_plan, const void *wih_values,
 
 /* Workspace floats darb_lstm_layer needs for (H, T, batch).  Errors: DARB_E_INVALID. */
 int darb_lstm_workspace(int64_t H, int64_t T, int64_t batch, int64_t *floats);
+
+/* ------------------------------------------------------------------------------------
+ * Evaluating and retraining a DARB layer (section 4.1 retrains the retained weights after
+ * pruning): log probabilities with their gradient, layer norm, the product's gradients and
+ * the optimizer's step.
+ *
+ * Activations are [features x batch] as everywhere here.  The first two take either memory
+ * order: element (f, b) lies at f * feature_stride + b * batch_stride (elements), and one of
+ * the two strides is 1 (batch_stride: the order of the products' X and Y; feature_stride: a
+ * batch of rows).  Along an axis of size 1 the stride is not used and may be anything.  The
+ * other stride is at least the unit axis' length.  Sums and statistics are fp32; results of
+ * a 16-bit type are rounded once, to nearest even.  All calls are deterministic.
+ */
+
+/*
+ * Log probabilities of given tokens under logits z [V x B]: per column (token),
+ *   lse = log sum_v e^z[v],  logprob = z[target] - lse,
+ *   entropy = - sum_v p_v log p_v,  p_v = e^(z[v] - lse),
+ * and the `top` greatest logits' log probabilities and classes, greatest first, equal ones
+ * by the lower class.  A logit of -inf has probability 0 and adds nothing to the entropy.
+ * A column of nothing but -inf has lse and log probabilities -inf and entropy 0; one that
+ * holds a NaN or +inf has NaN for all three (its alternatives are still ordered, NaN first).
+ * A negative target means that the column has none: logprob 0.  A target of V or more: NaN.
+ *   zdtype       DARB_F32, DARB_F16 or DARB_BF16
+ *   z            device [V x B], 1 <= V < 2^31, 1 <= B < 2^31
+ *   targets      device int64 [B], or NULL (no column has a target)
+ *   top          0 ... 64, at most V
+ *   logprob, entropy, lse      device fp32 [B]
+ *   top_logprob  device fp32 [B x top]; top_index device int64 [B x top] (NULL if top is 0)
+ *   workspace    device, 256-byte aligned, >= darb_token_logprobs_workspace's bytes
+ * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_WORKSPACE, DARB_E_HIP.
+ */
+int darb_token_logprobs_workspace(int64_t V, int64_t B, int64_t top, int64_t *bytes);
+int darb_token_logprobs(int zdtype, int64_t V, int64_t B, const void *z, int64_t z_feature_stride,
+                        int64_t z_batch_stride, const int64_t *targets, int64_t top,
+                        float *logprob, float *entropy, float *lse, float *top_logprob,
+                        int64_t *top_index, void *workspace, int64_t workspace_bytes,
+                        void *stream);
+
+/*
+ * The gradient of sum_b (grad_logprob[b] logprob[b] + grad_entropy[b] entropy[b]):
+ *   dz[v] = grad_logprob (1[v = target] - p_v) - grad_entropy p_v (log p_v + entropy),
+ * from the lse (and entropy) of darb_token_logprobs; p_v log p_v is zero where p_v is.  A
+ * column without a target gets none of the first part, one of nothing but -inf (lse = -inf) is zero
+ * altogether, and one whose target is V or more is NaN.
+ *   grad_logprob  device fp32 [B] or NULL (zeros)
+ *   entropy, grad_entropy  device fp32 [B], both or neither NULL; not all three NULL
+ *   dz            device [V x B] of zdtype, the unit stride along z's axis; may be z itself
+ * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_HIP.
+ */
+int darb_token_logprobs_grad(int zdtype, int64_t V, int64_t B, const void *z,
+                             int64_t z_feature_stride, int64_t z_batch_stride,
+                             const int64_t *targets, const float *lse, const float *grad_logprob,
+                             const float *entropy, const float *grad_entropy, void *dz,
+                             int64_t dz_feature_stride, int64_t dz_batch_stride, void *stream);
+
+/*
+ * Layer norm of the columns of x [H x B]:
+ *   mean = sum_h x / H,  rstd = 1 / sqrt(sum_h (x - mean)^2 / H + eps),
+ *   y = (x - mean) rstd weight + bias.
+ *   xdtype        type of x and y: DARB_F32, DARB_F16 or DARB_BF16
+ *   wdtype        type of weight and bias: DARB_F32 or xdtype
+ *   weight, bias  device [H], each may be NULL (ones, zeros)
+ *   eps           >= 0 (0: a constant column divides by zero)
+ *   y             device [H x B], the unit stride along x's axis; may be x itself
+ *   mean, rstd    device fp32 [B], each may be NULL
+ * 1 <= H < 2^31, 1 <= B < 2^31.
+ * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_HIP.
+ */
+int darb_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const void *x,
+                    int64_t x_feature_stride, int64_t x_batch_stride, const void *weight,
+                    const void *bias, double eps, void *y, int64_t y_feature_stride,
+                    int64_t y_batch_stride, float *mean, float *rstd, void *stream);
+
+/*
+ * Its gradients from dy [H x B] (type and axis of x), x, and the mean and rstd it returned:
+ * with xh = (x - mean) rstd and a = dy weight,
+ *   dx = rstd (a - sum_h a / H - xh sum_h a xh / H),
+ *   dweight = sum_b dy xh,  dbias = sum_b dy   (fp32 [H], in an order that H and B fix).
+ *   dx            device [H x B] of xdtype, the unit stride along x's axis; may be dy itself
+ *                 or x itself
+ *   weight        as given to darb_layer_norm (NULL: ones)
+ *   dx, dweight, dbias   each may be NULL (not computed), not all three
+ *   workspace     device, 256-byte aligned, >= darb_layer_norm_workspace's bytes
+ * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_WORKSPACE, DARB_E_HIP.
+ */
+int darb_layer_norm_workspace(int64_t H, int64_t B, int64_t *bytes);
+int darb_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, const void *dy,
+                         int64_t dy_feature_stride, int64_t dy_batch_stride, const void *x,
+                         int64_t x_feature_stride, int64_t x_batch_stride, const float *mean,
+                         const float *rstd, const void *weight, void *dx,
+                         int64_t dx_feature_stride, int64_t dx_batch_stride, float *dweight,
+                         float *dbias, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * The gradients of Y = W_darb X (darb_spmm; darb_spmv with B = 1) with the mask fixed:
+ *   dvalues[s] = sum_b dY[r, b] X[c, b]   for the slot s that keeps column c of row r,
+ *   dX[c, b]   = sum over the slots s of column c of values[s] dY[r, b].
+ * They run over an index of the retained weights by column, which darb_transpose makes from
+ * the byte offsets (the same index for the same offsets, bit for bit).  It stays valid as long
+ * as the offsets do: a program that retrains the values makes it once.
+ *   index     device, 256-byte aligned, >= darb_transpose_bytes bytes; the plan must keep
+ *             fewer than 2^31 weights
+ * darb_spmm_grad:
+ *   wdtype, values, xdtype, B, X, ldx   as for darb_spmm
+ *   dY        device fp32 [M x B], leading dimension ldy >= B
+ *   dvalues   device fp32 [nnz], overwritten, or NULL
+ *   dX        device fp32 [N x B], leading dimension lddx >= B, overwritten (a column that no
+ *             row keeps: zeros), or NULL; not both NULL
+ * values may be NULL if dX is, X if dvalues is.
+ * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_NOT_UPLOADED, DARB_E_WORKSPACE, DARB_E_HIP.
+ */
+int darb_transpose_bytes(const darb_plan *plan, int64_t *bytes);
+int darb_transpose(const darb_plan *plan, const uint8_t *offsets, void *index,
+                   int64_t index_bytes, void *stream);
+int darb_spmm_grad(const darb_plan *plan, const void *index, int wdtype, const void *values,
+                   int xdtype, int64_t B, const void *X, int64_t ldx, const float *dY,
+                   int64_t ldy, float *dvalues, float *dX, int64_t lddx, void *stream);
+
+/*
+ * AdamW with decoupled weight decay over many tensors at once.  Step t >= 1:
+ *   m = m b1 + g (1 - b1),  v = v b2 + g g (1 - b2),
+ *   p = p (1 - lr decay) - (m / (sqrt(v) rs + eps)) (lr / (1 - b1^t)),
+ *   rs = 1 / sqrt(1 - b2^t),
+ * each operation one correctly rounded fp32 operation in this order, the scalars computed in
+ * fp64 and rounded to fp32; g is the gradient times *grad_scale.  Where a tensor has a
+ * master, p is the master and the parameter receives its rounding.
+ *
+ * States in 8 bits: blocks of 256 consecutive elements share an fp32 scale, the greatest
+ * magnitude of the block.  A code c > 0 of m (7 bits, and the sign in bit 7) stands for the
+ * fp32 number with the bits (c + 889) << 20 times the scale, one of v (8 bits) for the bits
+ * (c + 1777) << 19; code 0 stands for 0.  A step rounds the new state x with random bits:
+ * with q = |x| (1 / scale) the code is (bits of q + r) >> 20 (19), less 889 (1777), from 0
+ * (v > 0: 1) to 127 (255), where r has its upper 16 bits below the shift from a hash of the
+ * element's number, the tensor's and the seed: h is x0 = element + tensor * 0xBB67AE85 + seed
+ * after x ^= x >> 16, x *= 0x9E3779B9, x ^= x >> 15, x *= 0xB504F333, x ^= x >> 16 (modulo
+ * 2^32); m takes its low half, v its high half.  A block whose greatest magnitude is below
+ * 2^-120 becomes 0; one that holds an infinity or NaN gets scale NaN.
+ *
+ * darb_adamw_create copies the table of tensors into the caller's workspace (on `stream`,
+ * waiting for it); the tensors and the workspace stay allocated while the handle is used, and
+ * no tensor's memory may overlap another's.  The handle is host memory; release it with
+ * darb_adamw_destroy.
+ *   bits        32 (m, v: fp32 [n]) or 8 (m, v: uint8 [n]; m_scale, v_scale: fp32
+ *               [ceil(n / 256)]); all zeros is the initial state
+ *   n           0 <= n < 2^39
+ *   decay       the tensor's weight decay, >= 0
+ * darb_adamw_step:
+ *   grads       host array of `count` device pointers, [n] of the type in gdtypes; NULL: the
+ *               tensor is left as it is
+ *   grad_scale  device fp32 [1] or NULL (1)
+ *   lr >= 0, 0 <= beta1, beta2 < 1, eps >= 0, step >= 1
+ * darb_adamw_moments writes the values that the states stand for: host arrays of `count`
+ * device pointers to fp32 [n]; either array, or any pointer in it, may be NULL.
+ * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_WORKSPACE, DARB_E_NOMEM, DARB_E_HIP.
+ */
+typedef struct darb_adamw darb_adamw;
+typedef struct {
+    void *param;       /* device [n] of dtype */
+    float *master;     /* device [n], or NULL */
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t n;
+    double decay;
+    int32_t dtype;     /* DARB_F32, DARB_F16 or DARB_BF16 */
+    int32_t reserved;  /* 0 */
+} darb_adamw_tensor;
+
+int darb_adamw_workspace(const darb_adamw_tensor *tensors, int64_t count, int64_t *bytes);
+int darb_adamw_create(const darb_adamw_tensor *tensors, int64_t count, int bits, void *workspace,
+                      int64_t workspace_bytes, void *stream, darb_adamw **out);
+int darb_adamw_step(const darb_adamw *adamw, const void *const *grads, const int *gdtypes,
+                    int64_t count, double lr, double beta1, double beta2, double eps,
+                    int64_t step, const float *grad_scale, uint32_t seed, void *stream);
+int darb_adamw_moments(const darb_adamw *adamw, float *const *m, float *const *v, int64_t count,
+                       void *stream);
+void darb_adamw_destroy(darb_adamw *adamw);
 
 /*
  * Measurement helpers (not part of DARB).  darb_stream_read reads `bytes`

@@ -14,6 +14,15 @@ arrays are accepted for host-side inputs (row densities).
     packed = plan.pack_offsets(offsets)     # log2 b bits per weight (section 4.2)
     y = plan.spmv_packed(values, packed, x) # same result, bit for bit
 
+Evaluating and retraining a layer (``training``; activations are [features, batch]):
+
+    lp = token_logprobs(Y, targets, top=5)  # logprob, entropy, lse, alternatives
+    dY = token_logprobs_grad(Y, targets, lp.lse, grad_logprob)
+    index = plan.transpose(offsets)         # once per mask
+    dvalues, dX = plan.spmm_grad(index, values, X, dY)
+    opt = AdamW([values, ...], lr=1e-3, state_bits=8)
+    opt.step([dvalues, ...])
+
 The library must have been built (``python paper_1911_08020_amd/build.py`` or
 ``__graft_entry__.build()``); importing this package fails loudly otherwise.
 """
@@ -38,6 +47,7 @@ E_WORKSPACE = -6
 
 F32 = 0
 F16 = 1
+BF16 = 2                # logits, layer norm, parameters and gradients only
 ROUND_FLOOR = 0
 ROUND_PAPER = 1
 
@@ -60,6 +70,14 @@ class _Info(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_int64), ("packed_words", ctypes.c_int64),
                 ("nbins", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("bins", _Bin * 8)]
+
+
+class _AdamTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("decay", ctypes.c_double), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 def _load_library():
@@ -101,6 +119,22 @@ def _load_library():
         "darb_spmm_i8": ([P, P, P, P, P, I, I64, P, I64, P, I64, P], I),
         "darb_lstm_layer": ([P, P, P, P, P, P, I, I64, I64, I64, P, P, P, P, P, I64, P], I),
         "darb_lstm_workspace": ([I64, I64, I64, ctypes.POINTER(I64)], I),
+        "darb_token_logprobs_workspace": ([I64, I64, I64, ctypes.POINTER(I64)], I),
+        "darb_token_logprobs": ([I, I64, I64, P, I64, I64, P, I64, P, P, P, P, P, P, I64, P], I),
+        "darb_token_logprobs_grad": ([I, I64, I64, P, I64, I64, P, P, P, P, P, P, I64, I64, P], I),
+        "darb_layer_norm": ([I, I, I64, I64, P, I64, I64, P, P, ctypes.c_double, P, I64, I64, P,
+                             P, P], I),
+        "darb_layer_norm_workspace": ([I64, I64, ctypes.POINTER(I64)], I),
+        "darb_layer_norm_grad": ([I, I, I64, I64, P, I64, I64, P, I64, I64, P, P, P, P, I64, I64,
+                                  P, P, P, I64, P], I),
+        "darb_transpose_bytes": ([P, ctypes.POINTER(I64)], I),
+        "darb_transpose": ([P, P, P, I64, P], I),
+        "darb_spmm_grad": ([P, P, I, P, I, I64, P, I64, P, I64, P, P, I64, P], I),
+        "darb_adamw_workspace": ([P, I64, ctypes.POINTER(I64)], I),
+        "darb_adamw_create": ([P, I64, I, P, I64, P, ctypes.POINTER(P)], I),
+        "darb_adamw_step": ([P, P, P, I64] + [ctypes.c_double] * 4 + [I64, P, ctypes.c_uint32, P], I),
+        "darb_adamw_moments": ([P, P, P, I64, P], I),
+        "darb_adamw_destroy": ([P], None),
         "darb_stream_read": ([P, I64, P, P], I),
         "darb_stream_read_shape": ([P, I64, I, I, P, P], I),
         "darb_stream_copy": ([P, P, I64, P], I),
@@ -121,7 +155,11 @@ EXPORTED = ("darb_plan_create", "darb_plan_create_counts", "darb_plan_device_wor
             "darb_plan_destroy", "darb_encode", "darb_decode", "darb_spmv", "darb_spmm",
             "darb_pack_offsets", "darb_unpack_offsets", "darb_spmv_packed", "darb_spmm_packed",
             "darb_quantize_i8", "darb_spmv_i8", "darb_spmm_i8", "darb_lstm_layer",
-            "darb_lstm_workspace", "darb_stream_read", "darb_stream_read_shape", "darb_stream_copy", "darb_strerror",
+            "darb_lstm_workspace", "darb_token_logprobs_workspace", "darb_token_logprobs",
+            "darb_token_logprobs_grad", "darb_layer_norm", "darb_layer_norm_workspace",
+            "darb_layer_norm_grad", "darb_transpose_bytes", "darb_transpose", "darb_spmm_grad",
+            "darb_adamw_workspace", "darb_adamw_create", "darb_adamw_step", "darb_adamw_moments",
+            "darb_adamw_destroy", "darb_stream_read", "darb_stream_read_shape", "darb_stream_copy", "darb_strerror",
             "darb_last_error", "darb_version")
 
 
@@ -481,6 +519,68 @@ class Plan:
                "darb_spmm_i8")
         return Y
 
+    # -- gradients ----------------------------------------------------------------------
+    def transpose(self, offsets, index=None, stream=None):
+        """The retained weights by column, which ``spmm_grad`` runs over: a device buffer that
+        stays valid as long as the offsets do (make it once per mask)."""
+        torch = _torch()
+        _require_cuda(offsets)
+        _check_format(offsets, self.nnz, "offsets", (torch.uint8,))
+        need = ctypes.c_int64()
+        _check(_lib.darb_transpose_bytes(self._h, ctypes.byref(need)), "darb_transpose_bytes")
+        if index is None:
+            index = torch.empty(need.value, dtype=torch.uint8, device=offsets.device)
+        _require_cuda(index)
+        _check_format(index, need.value, "index", (torch.uint8,))
+        _check(_lib.darb_transpose(self._h, _ptr(offsets), _ptr(index), index.numel(),
+                                   _stream_ptr(stream)), "darb_transpose")
+        return index
+
+    def spmm_grad(self, index, values, X, dY, dvalues=None, dX=None, need_values=True,
+                  need_X=True, stream=None):
+        """(dvalues fp32 [nnz], dX fp32 [N, B]) of Y = W_darb X for dY fp32 [M, B]; None in the
+        place of a gradient that is not needed (``values`` may then be None for dX, ``X`` for
+        dvalues).  ``index``: ``transpose``'s of the format's offsets."""
+        torch = _torch()
+        _require_cuda(index, dY)
+        need = ctypes.c_int64()
+        _check(_lib.darb_transpose_bytes(self._h, ctypes.byref(need)), "darb_transpose_bytes")
+        _check_format(index, need.value, "index", (torch.uint8,))
+        if dY.dtype != torch.float32:
+            raise TypeError("dY must be fp32")
+        if dY.dim() != 2:
+            raise ValueError(f"dY must be [{self.M}, B]")
+        B = dY.shape[1]
+        ldy = _row_major_ld(dY, self.M, B, "dY")
+        wcode = xcode = F32
+        ldx = lddx = B
+        if need_X:
+            _require_cuda(values)
+            self._check_values(values)
+            wcode = _dtype_code(values)
+            if dX is None:
+                dX = torch.empty((self.N, B), dtype=torch.float32, device=dY.device)
+            _require_cuda(dX)
+            if dX.dtype != torch.float32:
+                raise TypeError("dX must be fp32")
+            lddx = _row_major_ld(dX, self.N, B, "dX")
+        if need_values:
+            _require_cuda(X)
+            ldx = _row_major_ld(X, self.N, B, "X")
+            xcode = _dtype_code(X)
+            if not need_X and xcode == F16:
+                wcode = F16                 # the values' type does not matter
+            if dvalues is None:
+                dvalues = torch.empty(self.nnz, dtype=torch.float32, device=dY.device)
+            _require_cuda(dvalues)
+            _check_format(dvalues, self.nnz, "dvalues", (torch.float32,))
+        _check(_lib.darb_spmm_grad(self._h, _ptr(index), wcode, _ptr(values) if need_X else None,
+                                   xcode, B, _ptr(X) if need_values else None, ldx, _ptr(dY), ldy,
+                                   _ptr(dvalues) if need_values else None,
+                                   _ptr(dX) if need_X else None, lddx, _stream_ptr(stream)),
+               "darb_spmm_grad")
+        return (dvalues if need_values else None), (dX if need_X else None)
+
     # -- argument checks --------------------------------------------------------------
     def _check_i8(self, codes, scales):
         torch = _torch()
@@ -605,3 +705,7 @@ def stream_copy(dst, src, stream=None):
         raise ValueError("dst smaller than src")
     _check(_lib.darb_stream_copy(_ptr(dst), _ptr(src), nbytes, _stream_ptr(stream)),
            "darb_stream_copy")
+
+
+from .training import (AdamW, TokenLogprobs, layer_norm, layer_norm_grad,  # noqa: E402,F401
+                       token_logprobs, token_logprobs_grad)

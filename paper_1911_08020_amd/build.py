@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdarb.so")
 CALL_MODULE = os.path.join(HERE, "_darbcall.so")
 SOURCES = ["api.cpp", "encode.hip", "product.hip", "product_i8.hip", "lstm_seq.hip",
-           "packed.hip", "prune.hip", "plan.hip", "misc.hip"]
+           "packed.hip", "prune.hip", "plan.hip", "misc.hip", "api_train.cpp", "logprobs.hip",
+           "layer_norm.hip", "adamw.hip", "spmm_grad.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -466,7 +466,9 @@ int darb_plan_create_device(int64_t M, int64_t N, const int64_t *row_count, int6
 // device entry points
 // ---------------------------------------------------------------------------
 
-static int check_uploaded(const darb_plan *p) {
+namespace darb {
+
+int check_uploaded(const darb_plan *p) {
     if (!p) return fail(DARB_E_INVALID, "plan is NULL");
     if (!p->d_perm) return fail(DARB_E_NOT_UPLOADED, "plan was not uploaded");
     int dev = -1;
@@ -478,14 +480,16 @@ static int check_uploaded(const darb_plan *p) {
     return DARB_OK;
 }
 
-static bool valid_dtype(int t) { return t == DARB_F32 || t == DARB_F16; }
-
-static int launched(hipError_t e, const char *what) {
+int launched(hipError_t e, const char *what) {
     if (e == hipSuccess) e = hipGetLastError();
     else (void)hipGetLastError();
     if (e != hipSuccess) return fail(DARB_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
     return DARB_OK;
 }
+
+}  // namespace darb
+
+static bool valid_dtype(int t) { return t == DARB_F32 || t == DARB_F16; }
 
 static int check_product_dtypes(int wdtype, int xdtype) {
     if (!valid_dtype(wdtype) || !valid_dtype(xdtype)) return fail(DARB_E_DTYPE, "unknown dtype");

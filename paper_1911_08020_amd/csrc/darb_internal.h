@@ -83,6 +83,9 @@ namespace darb {
 // error reporting (thread-local detail string)
 int fail(int code, const std::string &detail);
 void clear_error();
+// the plan has its device tables on the current device; the outcome of a launch
+int check_uploaded(const darb_plan *p);
+int launched(hipError_t e, const char *what);
 
 // kernel launchers (return hipError_t of the launch)
 hipError_t launch_encode(const darb_plan &p, int wdtype, const void *W, int64_t ldw,
@@ -161,6 +164,68 @@ hipError_t launch_plan_one(int64_t M, int64_t N, const int64_t *counts, int64_t 
 hipError_t launch_plan_device(int64_t M, int64_t N, const int64_t *counts, int64_t kept, int mode,
                               int lmin, int lmax, int32_t *perm, int64_t *rowinfo, void *scratch,
                               hipStream_t s);
+// ---- evaluating and retraining a layer ----
+// Log probabilities and their gradient.  One of the strides of z is 1 (the class stride, or
+// else the token stride), and dz's is the same one; V = 1 and B = 1 go either way.
+int64_t logprobs_max_top();
+int64_t logprobs_workspace_bytes(int64_t V, int64_t B, int64_t top);
+hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64_t class_stride,
+                           int64_t token_stride, const int64_t *targets, int64_t top,
+                           float *logprob, float *entropy, float *lse, float *top_logprob,
+                           int64_t *top_index, void *workspace, hipStream_t s);
+hipError_t launch_logprobs_grad(int dtype, int64_t V, int64_t B, const void *z,
+                                int64_t class_stride, int64_t token_stride,
+                                const int64_t *targets, const float *lse,
+                                const float *grad_logprob, const float *entropy,
+                                const float *grad_entropy, void *dz, int64_t out_class_stride,
+                                int64_t out_token_stride, hipStream_t s);
+int64_t layer_norm_workspace_bytes(int64_t H, int64_t B);
+hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const void *x,
+                             int64_t x_feature, int64_t x_token, const void *weight,
+                             const void *bias, float eps, void *y, int64_t y_feature,
+                             int64_t y_token, float *mean, float *rstd, hipStream_t s);
+hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, const void *dy,
+                                  int64_t dy_feature, int64_t dy_token, const void *x,
+                                  int64_t x_feature, int64_t x_token, const float *mean,
+                                  const float *rstd, const void *weight, void *dx,
+                                  int64_t dx_feature, int64_t dx_token, float *dweight,
+                                  float *dbias, void *workspace, hipStream_t s);
+// The column index of a plan's weights, and the products' gradients over it.
+int64_t transpose_bytes(const darb_plan &p);
+hipError_t launch_transpose(const darb_plan &p, const uint8_t *offsets, void *index, hipStream_t s);
+hipError_t launch_spmm_grad(const darb_plan &p, const void *index, int wdtype, const void *values,
+                            int xdtype, int64_t B, const void *X, int64_t ldx, const float *dY,
+                            int64_t ldy, float *dvalues, float *dX, int64_t lddx, hipStream_t s);
+// AdamW: the tensors' table and, for every tile of adam_tile_elements() elements, whose it is;
+// both in the caller's workspace.  A launch takes `count` (at most kAdamGrads, or half of it
+// for the moments) consecutive tensors, whose gradients' addresses travel with it.
+constexpr int kAdamBlock = 256;         // elements that share a scale in 8 bits
+constexpr int kAdamGrads = 384;
+struct AdamTensor {
+    void *param;
+    float *master;
+    void *m, *v;                        // fp32, or codes of 8 bits
+    float *m_scale, *v_scale;
+    int64_t n;
+    double decay;
+    int32_t dtype, reserved;
+};
+struct AdamTile {
+    uint32_t tensor, index;
+};
+struct AdamScalars {
+    double lr, beta1, beta2, eps;
+    int64_t step;
+    const float *grad_scale;
+    uint32_t seed;
+};
+int64_t adam_tile_elements();
+hipError_t launch_adamw(int bits, const AdamTensor *tensors, const AdamTile *tiles, int64_t ntiles,
+                        int first_tensor, int count, const void *const *grads, const int *types,
+                        const AdamScalars &c, hipStream_t s);
+hipError_t launch_moments(int bits, const AdamTensor *tensors, const AdamTile *tiles,
+                          int64_t ntiles, int first_tensor, int count, float *const *m,
+                          float *const *v, hipStream_t s);
 hipError_t launch_stream_read(const void *buf, int64_t bytes, float *sink, hipStream_t s);
 hipError_t launch_stream_read_shape(const void *buf, int64_t bytes, int threads, int vectors,
                                    float *sink, hipStream_t s);

@@ -1,0 +1,68 @@
+// Wave-wide (64 lanes) sums, maxima and scans of the training operators, in a fixed order.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace darb {
+
+// The value of another lane by a DPP pattern; lanes outside the row mask get `other`.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float dpp(float x, float other) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(x),
+                                                      CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t dpp(uint32_t x, uint32_t other) {
+    return uint32_t(__builtin_amdgcn_update_dpp(int(other), int(x), CTRL, ROWS, 0xf, false));
+}
+
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140;
+constexpr int kDppBcast15 = 0x142, kDppBcast31 = 0x143;
+
+struct AddOp {
+    __device__ static float of(float a, float b) { return a + b; }
+    __device__ static float none() { return 0.0f; }
+};
+struct MaxOp {  // a NaN is left out
+    __device__ static float of(float a, float b) { return fmaxf(a, b); }
+    __device__ static float none() { return -__builtin_inff(); }
+};
+
+// Over each aligned group of LANES (1 ... 64, a power of two) lanes; every lane of a group of
+// up to 16 gets the result, lane 63 that of 64, lanes 16 ... 31 and 48 ... 63 that of 32.
+template <int LANES, typename Op> __device__ __forceinline__ float group_reduce(float x) {
+    if (LANES >= 2) x = Op::of(x, dpp<kDppXor1>(x, x));
+    if (LANES >= 4) x = Op::of(x, dpp<kDppXor2>(x, x));
+    if (LANES >= 8) x = Op::of(x, dpp<kDppHalfMirror>(x, x));
+    if (LANES >= 16) x = Op::of(x, dpp<kDppMirror>(x, x));
+    if (LANES >= 32) x = Op::of(x, dpp<kDppBcast15, 0xa>(x, Op::none()));
+    if (LANES >= 64) x = Op::of(x, dpp<kDppBcast31, 0xc>(x, Op::none()));
+    return x;
+}
+
+__device__ __forceinline__ float lane_of(float x, int lane) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+}
+
+// The whole wave's result, the same in every lane (in a scalar register).
+__device__ __forceinline__ float wave_sum(float x) { return lane_of(group_reduce<64, AddOp>(x), 63); }
+__device__ __forceinline__ float wave_max(float x) { return lane_of(group_reduce<64, MaxOp>(x), 63); }
+
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) {
+    auto of = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+    x = of(x, dpp<kDppXor1>(x, x));
+    x = of(x, dpp<kDppXor2>(x, x));
+    x = of(x, dpp<kDppHalfMirror>(x, x));
+    x = of(x, dpp<kDppMirror>(x, x));
+    x = of(x, dpp<kDppBcast15, 0xa>(x, 0u));
+    x = of(x, dpp<kDppBcast31, 0xc>(x, 0u));
+    return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
+}
+
+__device__ __forceinline__ int lane_id() {
+    return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+}
+
+}  // namespace darb
