@@ -33,6 +33,20 @@ template <typename T, int V> __device__ __forceinline__ Loaded<T, V> load_vec(co
     return {*reinterpret_cast<const typename VecOf<T, V>::Type *>(p)};
 }
 
+// Keeps the compiler from holding what it has computed from x so far (fp32 values of 16-bit
+// elements, say) until x is used again: x itself takes the fewest registers.
+template <typename T, int V> __device__ __forceinline__ void forget_uses(Loaded<T, V> &x) {
+    if constexpr (sizeof(x.raw) == 16) {
+        typedef uint32_t U __attribute__((ext_vector_type(4)));
+        U u;
+        __builtin_memcpy(&u, &x.raw, 16);
+        asm volatile("" : "+v"(u));
+        __builtin_memcpy(&x.raw, &u, 16);
+    } else if constexpr (sizeof(x.raw) == 4) {
+        asm volatile("" : "+v"(x.raw));
+    }
+}
+
 template <typename T, int V> __device__ __forceinline__ void store_vec(T *p, const float (&f)[V]) {
     typename VecOf<T, V>::Type t;
     if constexpr (V == 1) {

@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kMaxThreads = 1024;
 constexpr int kMaxWaves = kMaxThreads / kWave;
-constexpr int kAnyThreads = 256;
+constexpr int kGradThreads = 512;       // twice the registers a thread: x, dy and the sums
 
 struct Matrix {                         // element (h, b) at h * feature + b * token
     void *p;
@@ -42,6 +42,24 @@ __device__ __forceinline__ float weight_at(const Args &a, const void *w, int64_t
     return a.w_f32 ? static_cast<const float *>(w)[h] : float(static_cast<const T *>(w)[h]);
 }
 
+// V weights from feature h on; `none` where there are no weights.
+template <typename T, int V>
+__device__ __forceinline__ void weights(const Args &a, const void *w, int64_t h, float none,
+                                        float (&f)[V]) {
+    if (!w) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = none;
+    } else if (a.w_f32) {
+        const Loaded<float, V> x = load_vec<float, V>(static_cast<const float *>(w) + h);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = x[j];
+    } else {
+        const Loaded<T, V> x = load_vec<T, V>(static_cast<const T *>(w) + h);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = x[j];
+    }
+}
+
 // The workgroup's sum of s[0 .. N), each in every thread; scratch: N * kMaxWaves floats.
 template <int N> __device__ __forceinline__ void block_sum(float (&s)[N], float *scratch) {
     const int waves = blockDim.x / kWave, w = threadIdx.x / kWave;
@@ -60,70 +78,381 @@ template <int N> __device__ __forceinline__ void block_sum(float (&s)[N], float 
     }
 }
 
-// ---- any strides and lengths: a workgroup per column, one element at a time ------------
+// A vector that would pass the end of its axis starts V before it instead, and leaves out its
+// first `skip` elements, which belong to others: no access is partial or divergent but the last
+// vector's store.
+template <int V> __device__ __forceinline__ int64_t back_from_end(int64_t at, int64_t end, int &skip) {
+    const int64_t own = at + V <= end ? at : end - V;
+    skip = at - own < V ? int(at - own) : V;
+    return own;
+}
 
-template <typename T>
-__global__ __launch_bounds__(kAnyThreads) void any_norm_kernel(Args a) {
+template <typename T, int V> __device__ __forceinline__ void store_own(T *p, int skip, const float (&f)[V]) {
+    if (skip == 0) {
+        store_vec<T, V>(p, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i >= skip) p[i] = T(f[i]);
+    }
+}
+
+// ---- token-major: a token's features are contiguous -----------------------------------
+//
+// A workgroup per token; a thread holds N vectors of the row, a workgroup's width apart.  N = 0:
+// a row longer than the registers of 1024 threads, read again for every sum.
+
+template <typename T, int V, int N> struct Row {
+    Loaded<T, V> held[N ? N : 1];
+    const T *p;
+    int64_t H;
+
+    // f(vector's place in the thread, its first feature, elements to leave out, vector)
+    template <typename F> __device__ __forceinline__ void each(F &&f) const {
+        int skip;
+        if constexpr (N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int64_t at = (int64_t(i) * blockDim.x + threadIdx.x) * V;
+                if (at >= H) break;
+                const int64_t h = back_from_end<V>(at, H, skip);
+                f(i, h, skip, held[i]);
+            }
+        } else {
+            for (int64_t at = int64_t(threadIdx.x) * V; at < H; at += int64_t(blockDim.x) * V) {
+                const int64_t h = back_from_end<V>(at, H, skip);
+                f(0, h, skip, load_vec<T, V>(p + h));
+            }
+        }
+    }
+    __device__ __forceinline__ void forget() {
+        if constexpr (N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) forget_uses(held[i]);
+        }
+    }
+    __device__ __forceinline__ void open(const T *row, int64_t len) {
+        p = row;
+        H = len;
+        if constexpr (N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                int skip;
+                const int64_t at = (int64_t(i) * blockDim.x + threadIdx.x) * V;
+                held[i] = load_vec<T, V>(p + back_from_end<V>(at, H, skip));
+            }
+        }
+    }
+};
+
+template <typename T, int V, int N>
+__global__ __launch_bounds__(kMaxThreads) void norm_rows_kernel(Args a) {
     __shared__ float scratch[kMaxWaves];
-    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
-        const T *x = static_cast<const T *>(a.x.p) + b * a.x.token;
-        T *y = static_cast<T *>(a.y.p) + b * a.y.token;
-        float s[1] = {0.0f};
-        for (int64_t h = threadIdx.x; h < a.H; h += kAnyThreads) s[0] += float(x[h * a.x.feature]);
-        block_sum(s, scratch);
-        const float mean = s[0] / float(a.H);
-        s[0] = 0.0f;
-        for (int64_t h = threadIdx.x; h < a.H; h += kAnyThreads) {
-            const float d = float(x[h * a.x.feature]) - mean;
+    const int64_t b = blockIdx.x;
+    Row<T, V, N> x;
+    x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H);
+    T *y = static_cast<T *>(a.y.p) + b * a.y.token;
+    float s[1] = {0.0f};
+    x.each([&](int, int64_t, int skip, const Loaded<T, V> &v) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[0] += j >= skip ? v[j] : 0.0f;
+    });
+    block_sum(s, scratch);
+    x.forget();
+    const float mean = s[0] / float(a.H);
+    s[0] = 0.0f;
+    x.each([&](int, int64_t, int skip, const Loaded<T, V> &v) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float d = j >= skip ? v[j] - mean : 0.0f;
             s[0] = fmaf(d, d, s[0]);
         }
+    });
+    block_sum(s, scratch);
+    x.forget();
+    const float rstd = 1.0f / sqrtf(s[0] / float(a.H) + a.eps);
+    x.each([&](int, int64_t h, int skip, const Loaded<T, V> &v) {
+        float w[V], c[V], out[V];
+        weights<T, V>(a, a.w, h, 1.0f, w);
+        weights<T, V>(a, a.b, h, 0.0f, c);
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] = fmaf((v[j] - mean) * rstd, w[j], c[j]);
+        store_own<T, V>(y + h, skip, out);
+    });
+    if (threadIdx.x == 0) {
+        if (a.mean) a.mean[b] = mean;
+        if (a.rstd) a.rstd[b] = rstd;
+    }
+}
+
+// The workgroup takes every gridDim.x-th token.  Held rows: dw and db sum in registers; longer
+// ones: in the workgroup's row of the workspace.
+template <typename T, int V, int N>
+__global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
+    constexpr int kHeld = N ? N : 1;
+    __shared__ float scratch[2 * kMaxWaves];
+    float *dw = a.dw ? a.dw + blockIdx.x * a.H : nullptr;
+    float *db = a.db ? a.db + blockIdx.x * a.H : nullptr;
+    float sw[kHeld][V], sb[kHeld][V];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) sw[i][j] = sb[i][j] = 0.0f;
+    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
+        Row<T, V, N> x, dy;
+        x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H);
+        dy.open(static_cast<const T *>(a.dy.p) + b * a.dy.token, a.H);
+        T *dx = static_cast<T *>(a.y.p) + b * a.y.token;
+        const float mean = a.mean[b], rstd = a.rstd[b];
+        float s[2] = {0.0f, 0.0f};
+        x.each([&](int i, int64_t h, int skip, const Loaded<T, V> &v) {
+            const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h);
+            float w[V];
+            weights<T, V>(a, a.w, h, 1.0f, w);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const bool own = j >= skip;
+                const float gj = own ? g[j] : 0.0f, xh = own ? (v[j] - mean) * rstd : 0.0f;
+                const float c = gj * w[j];
+                s[0] += c;
+                s[1] = fmaf(c, xh, s[1]);
+                if constexpr (N) {
+                    sw[i][j] = fmaf(gj, xh, sw[i][j]);
+                    sb[i][j] += gj;
+                } else if (own) {
+                    const bool first = b == blockIdx.x;
+                    if (dw) dw[h + j] = first ? gj * xh : fmaf(gj, xh, dw[h + j]);
+                    if (db) db[h + j] = first ? gj : db[h + j] + gj;
+                }
+            }
+        });
+        if (!a.y.p) continue;
         block_sum(s, scratch);
-        const float rstd = 1.0f / sqrtf(s[0] / float(a.H) + a.eps);
-        for (int64_t h = threadIdx.x; h < a.H; h += kAnyThreads) {
-            float v = (float(x[h * a.x.feature]) - mean) * rstd;
-            if (a.w) v *= weight_at<T>(a, a.w, h);
-            if (a.b) v += weight_at<T>(a, a.b, h);
-            y[h * a.y.feature] = T(v);
-        }
-        if (threadIdx.x == 0) {
-            if (a.mean) a.mean[b] = mean;
-            if (a.rstd) a.rstd[b] = rstd;
+        x.forget();
+        dy.forget();
+        const float m0 = s[0] / float(a.H), m1 = s[1] / float(a.H);
+        x.each([&](int i, int64_t h, int skip, const Loaded<T, V> &v) {
+            const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h);
+            float w[V], out[V];
+            weights<T, V>(a, a.w, h, 1.0f, w);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float xh = (v[j] - mean) * rstd;
+                out[j] = rstd * (g[j] * w[j] - m0 - xh * m1);
+            }
+            store_own<T, V>(dx + h, skip, out);
+        });
+    }
+    if constexpr (N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int64_t at = (int64_t(i) * blockDim.x + threadIdx.x) * V;
+            if (at >= a.H) break;
+            int skip;
+            const int64_t h = back_from_end<V>(at, a.H, skip);
+            if (dw) store_own<float, V>(dw + h, skip, sw[i]);
+            if (db) store_own<float, V>(db + h, skip, sb[i]);
         }
     }
 }
 
-// The workgroup's columns' dw and db go to its row of the partial sums, element by element.
-template <typename T>
-__global__ __launch_bounds__(kAnyThreads) void any_norm_grad_kernel(Args a) {
-    __shared__ float scratch[2 * kMaxWaves];
+// ---- feature-major: a feature's tokens are contiguous ---------------------------------
+//
+// A workgroup takes a tile of `lanes` * V tokens: a thread V tokens of every rows-th feature,
+// N of them in registers.  N = 0: more features than that, read again for every sum.
+
+template <typename T, int V, int N> struct Tile {
+    Loaded<T, V> held[N ? N : 1];
+    const T *p;
+    int64_t H, stride;
+    int first, rows;
+
+    // f(feature's place in the thread, feature, vector)
+    template <typename F> __device__ __forceinline__ void each(F &&f) const {
+        if constexpr (N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int64_t h = first + int64_t(i) * rows;
+                if (h < H) f(i, h, held[i]);
+            }
+        } else {
+            for (int64_t h = first; h < H; h += rows) f(0, h, load_vec<T, V>(p + h * stride));
+        }
+    }
+    __device__ __forceinline__ void forget() {
+        if constexpr (N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) forget_uses(held[i]);
+        }
+    }
+    __device__ __forceinline__ void open(const T *at, int64_t H_, int64_t stride_, int first_, int rows_) {
+        p = at;
+        H = H_;
+        stride = stride_;
+        first = first_;
+        rows = rows_;
+        if constexpr (N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int64_t h = first + int64_t(i) * rows;
+                held[i] = load_vec<T, V>(p + (h < H ? h : H - 1) * stride);
+            }
+        }
+    }
+};
+
+// s summed over the threads with the same tokens (lanes of them side by side), in each of them;
+// scratch: kMaxWaves * lanes * K floats.
+template <int K> __device__ __forceinline__ void tile_sum(float (&s)[K], int lanes, float *scratch) {
+    const int waves = blockDim.x / kWave, w = threadIdx.x / kWave, lane = lane_id();
+#pragma unroll
+    for (int j = 0; j < K; ++j)
+        for (int d = lanes; d < kWave; d <<= 1) s[j] += __shfl_xor(s[j], d, kWave);
+    if (waves == 1) return;
+    __syncthreads();                                 // the scratch's last use
+    if (lane < lanes)
+#pragma unroll
+        for (int j = 0; j < K; ++j) scratch[(w * K + j) * lanes + lane] = s[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        s[j] = 0.0f;
+        for (int k = 0; k < waves; ++k) s[j] += scratch[(k * K + j) * lanes + lane % lanes];
+    }
+}
+
+constexpr int kMaxLanes = 8;
+
+template <typename T, int V, int N>
+__global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int lanes) {
+    __shared__ float scratch[kMaxWaves * kMaxLanes * V];
+    const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes, rows = blockDim.x / lanes;
+    int skip;
+    const int64_t b = back_from_end<V>((int64_t(blockIdx.x) * lanes + tx) * V, a.B, skip);
+    Tile<T, V, N> x;
+    x.open(static_cast<const T *>(a.x.p) + b, a.H, a.x.feature, ty, rows);
+    T *y = static_cast<T *>(a.y.p) + b;
+    float mean[V], rstd[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) mean[j] = rstd[j] = 0.0f;
+    x.each([&](int, int64_t, const Loaded<T, V> &v) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) mean[j] += v[j];
+    });
+    tile_sum(mean, lanes, scratch);
+    x.forget();
+#pragma unroll
+    for (int j = 0; j < V; ++j) mean[j] /= float(a.H);
+    x.each([&](int, int64_t, const Loaded<T, V> &v) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float d = v[j] - mean[j];
+            rstd[j] = fmaf(d, d, rstd[j]);
+        }
+    });
+    tile_sum(rstd, lanes, scratch);
+    x.forget();
+#pragma unroll
+    for (int j = 0; j < V; ++j) rstd[j] = 1.0f / sqrtf(rstd[j] / float(a.H) + a.eps);
+    x.each([&](int, int64_t h, const Loaded<T, V> &v) {
+        const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f, c = a.b ? weight_at<T>(a, a.b, h) : 0.0f;
+        float out[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) out[j] = fmaf((v[j] - mean[j]) * rstd[j], w, c);
+        store_own<T, V>(y + h * a.y.feature, skip, out);
+    });
+    if (ty == 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (j >= skip && a.mean) a.mean[b + j] = mean[j];
+            if (j >= skip && a.rstd) a.rstd[b + j] = rstd[j];
+        }
+    }
+}
+
+template <typename T, int V, int N>
+__global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a, int lanes) {
+    constexpr int kHeld = N ? N : 1;
+    __shared__ float scratch[kMaxWaves * kMaxLanes * 2 * V];
+    const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes, rows = blockDim.x / lanes;
+    const int64_t tiles = (a.B + lanes * V - 1) / (lanes * V);
     float *dw = a.dw ? a.dw + blockIdx.x * a.H : nullptr;
     float *db = a.db ? a.db + blockIdx.x * a.H : nullptr;
-    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
-        const T *x = static_cast<const T *>(a.x.p) + b * a.x.token;
-        const T *dy = static_cast<const T *>(a.dy.p) + b * a.dy.token;
-        T *dx = static_cast<T *>(a.y.p) + b * a.y.token;
-        const float mean = a.mean[b], rstd = a.rstd[b];
-        const bool first = b == blockIdx.x;
-        float s[2] = {0.0f, 0.0f};
-        for (int64_t h = threadIdx.x; h < a.H; h += kAnyThreads) {
-            const float g = float(dy[h * a.dy.feature]);
-            const float xh = (float(x[h * a.x.feature]) - mean) * rstd;
-            const float v = a.w ? g * weight_at<T>(a, a.w, h) : g;
-            s[0] += v;
-            s[1] = fmaf(v, xh, s[1]);
-            if (dw) dw[h] = first ? g * xh : fmaf(g, xh, dw[h]);
-            if (db) db[h] = first ? g : db[h] + g;
+    float sw[kHeld], sb[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) sw[i] = sb[i] = 0.0f;
+    // over the lanes that share a feature's tokens; whole waves come here
+    auto across = [&](float s) {
+        for (int d = 1; d < lanes; d <<= 1) s += __shfl_xor(s, d, kWave);
+        return s;
+    };
+    for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        int skip;
+        const int64_t b = back_from_end<V>((tile * lanes + tx) * V, a.B, skip);
+        Tile<T, V, N> x, dy;
+        x.open(static_cast<const T *>(a.x.p) + b, a.H, a.x.feature, ty, rows);
+        dy.open(static_cast<const T *>(a.dy.p) + b, a.H, a.dy.feature, ty, rows);
+        T *dx = static_cast<T *>(a.y.p) + b;
+        float mean[V], rstd[V], s[2 * V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            mean[j] = a.mean[b + j];
+            rstd[j] = a.rstd[b + j];
+            s[j] = s[V + j] = 0.0f;
         }
+        x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
+            const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h * dy.stride);
+            const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
+            float fw = 0.0f, fb = 0.0f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float xh = (v[j] - mean[j]) * rstd[j], c = g[j] * w;
+                s[j] += c;
+                s[V + j] = fmaf(c, xh, s[V + j]);
+                fw = j >= skip ? fmaf(g[j], xh, fw) : fw;
+                fb = j >= skip ? fb + g[j] : fb;
+            }
+            if constexpr (N) {
+                sw[i] += fw;
+                sb[i] += fb;
+            } else {
+                // the lanes of a feature are all here, or none
+                fw = across(fw);
+                fb = across(fb);
+                if (tx == 0) {
+                    const bool first = tile == blockIdx.x;
+                    if (dw) dw[h] = first ? fw : dw[h] + fw;
+                    if (db) db[h] = first ? fb : db[h] + fb;
+                }
+            }
+        });
         if (!a.y.p) continue;
-        block_sum(s, scratch);
-        const float m0 = s[0] / float(a.H), m1 = s[1] / float(a.H);
-        for (int64_t h = threadIdx.x; h < a.H; h += kAnyThreads) {
-            const float g = float(dy[h * a.dy.feature]);
-            const float xh = (float(x[h * a.x.feature]) - mean) * rstd;
-            const float v = a.w ? g * weight_at<T>(a, a.w, h) : g;
-            dx[h * a.y.feature] = T(rstd * (v - m0 - xh * m1));
+        tile_sum(s, lanes, scratch);
+        x.forget();
+        dy.forget();
+#pragma unroll
+        for (int j = 0; j < 2 * V; ++j) s[j] /= float(a.H);
+        x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
+            const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h * dy.stride);
+            const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
+            float out[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float xh = (v[j] - mean[j]) * rstd[j];
+                out[j] = rstd[j] * (g[j] * w - s[j] - xh * s[V + j]);
+            }
+            store_own<T, V>(dx + h * a.y.feature, skip, out);
+        });
+    }
+    if constexpr (N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float w = across(sw[i]), c = across(sb[i]);
+            const int64_t h = ty + int64_t(i) * rows;
+            if (tx != 0 || h >= a.H) continue;
+            if (dw) dw[h] = w;
+            if (db) db[h] = c;
         }
-        __syncthreads();
     }
 }
 
@@ -159,6 +488,64 @@ constexpr int kMaxBlocks = 256;         // rows of partial sums
 
 int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A token-major call: threads that hold a row, N vectors each (0: the row is too long).
+struct RowShape {
+    int threads, n;
+};
+
+RowShape row_shape(int64_t H, int vec, int most) {
+    if (H < vec) return {kWave, 1};                  // an element a thread
+    const int64_t vectors = up(H, vec);
+    for (int threads = 256; threads <= most; threads *= 2)
+        for (int n = 1; n <= 4; ++n)
+            if (up(up(vectors, n), kWave) * kWave <= threads)
+                return {int(up(up(vectors, n), kWave) * kWave), n};
+    return {most, 0};
+}
+
+template <typename F> hipError_t with_row(const RowShape &r, F &&f) {
+    switch (r.n) {
+        case 1: return f(std::integral_constant<int, 1>{});
+        case 2: return f(std::integral_constant<int, 2>{});
+        case 3: return f(std::integral_constant<int, 3>{});
+        case 4: return f(std::integral_constant<int, 4>{});
+        default: return f(std::integral_constant<int, 0>{});
+    }
+}
+
+// A feature-major call: a tile of `lanes` vectors of tokens, the widest that leaves
+// about a workgroup a CU, whose threads hold N features each.
+struct TileShape {
+    int lanes, threads, n, vec;
+};
+
+TileShape tile_shape(int64_t H, int64_t B, int vec, int threads, int most) {
+    TileShape t;
+    t.vec = B < vec ? 1 : vec;
+    t.lanes = kMaxLanes;
+    while (t.lanes > 1 && up(B, int64_t(t.lanes) * t.vec) < 200) t.lanes /= 2;
+    const int64_t want = H * t.lanes;
+    t.threads = threads;
+    t.n = 2;
+    while (t.n <= most && want > int64_t(threads) * t.n) t.n *= 2;
+    if (t.n > most) t.n = 0;
+    return t;
+}
+
+template <int MOST, typename F> hipError_t with_tile(const TileShape &t, F &&f) {
+    if constexpr (MOST >= 16) if (t.n == 16) return f(std::integral_constant<int, 16>{});
+    switch (t.n) {
+        case 2: return f(std::integral_constant<int, 2>{});
+        case 4: return f(std::integral_constant<int, 4>{});
+        case 8: return f(std::integral_constant<int, 8>{});
+        default: return f(std::integral_constant<int, 0>{});
+    }
+}
+
+bool rows_of(int64_t H, int64_t feature) { return H == 1 || feature == 1; }
+
 }  // namespace
 
 int64_t layer_norm_workspace_bytes(int64_t H, int64_t B) {
@@ -174,9 +561,29 @@ hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const
                  bias, wdtype == DARB_F32, H, B, eps, mean, rstd, nullptr, nullptr};
     return with_type(xdtype, [&](auto type) {
         using T = decltype(type);
-        const int64_t blocks = B < 65536 ? B : 65536;
-        hipLaunchKernelGGL((any_norm_kernel<T>), dim3(unsigned(blocks)), dim3(kAnyThreads), 0, s, a);
-        return hipGetLastError();
+        if (rows_of(H, x_feature)) {
+            const RowShape r = row_shape(H, kVec<T>, kMaxThreads);
+            return with_row(r, [&](auto n) {
+                if (H < kVec<T>)
+                    hipLaunchKernelGGL((norm_rows_kernel<T, 1, 1>), dim3(unsigned(B)),
+                                       dim3(r.threads), 0, s, a);
+                else
+                    hipLaunchKernelGGL((norm_rows_kernel<T, kVec<T>, decltype(n)::value>),
+                                       dim3(unsigned(B)), dim3(r.threads), 0, s, a);
+                return hipGetLastError();
+            });
+        }
+        const TileShape t = tile_shape(H, B, kVec<T>, kMaxThreads, 8);
+        return with_tile<8>(t, [&](auto n) {
+            const dim3 grid(unsigned(up(B, int64_t(t.lanes) * t.vec)));
+            if (t.vec == 1)
+                hipLaunchKernelGGL((norm_columns_kernel<T, 1, decltype(n)::value>), grid,
+                                   dim3(t.threads), 0, s, a, t.lanes);
+            else
+                hipLaunchKernelGGL((norm_columns_kernel<T, kVec<T>, decltype(n)::value>), grid,
+                                   dim3(t.threads), 0, s, a, t.lanes);
+            return hipGetLastError();
+        });
     });
 }
 
@@ -191,14 +598,37 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
            H, B, 0.0f, const_cast<float *>(mean), const_cast<float *>(rstd), nullptr, nullptr};
     return with_type(xdtype, [&](auto type) {
         using T = decltype(type);
-        const int blocks = B < kMaxBlocks ? int(B) : kMaxBlocks;
+        const bool rows = rows_of(H, x_feature);
+        const TileShape t = tile_shape(H, B, kVec<T>, kGradThreads, 16);
+        const int64_t tasks = rows ? B : up(B, int64_t(t.lanes) * t.vec);
+        const int blocks = tasks < kMaxBlocks ? int(tasks) : kMaxBlocks;
         if (dweight) a.dw = static_cast<float *>(workspace);
         if (dbias) a.db = reinterpret_cast<float *>(static_cast<char *>(workspace) + padded(blocks * H * 4));
-        hipLaunchKernelGGL((any_norm_grad_kernel<T>), dim3(unsigned(blocks)), dim3(kAnyThreads), 0, s, a);
-        const hipError_t e = hipGetLastError();
+        hipError_t e;
+        if (rows) {
+            const RowShape r = row_shape(H, kVec<T>, kGradThreads);
+            e = with_row(r, [&](auto n) {
+                if (H < kVec<T>)
+                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, 1, 1>), dim3(unsigned(blocks)),
+                                       dim3(r.threads), 0, s, a);
+                else
+                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, kVec<T>, decltype(n)::value>),
+                                       dim3(unsigned(blocks)), dim3(r.threads), 0, s, a);
+                return hipGetLastError();
+            });
+        } else {
+            e = with_tile<16>(t, [&](auto n) {
+                if (t.vec == 1)
+                    hipLaunchKernelGGL((norm_grad_columns_kernel<T, 1, decltype(n)::value>),
+                                       dim3(unsigned(blocks)), dim3(t.threads), 0, s, a, t.lanes);
+                else
+                    hipLaunchKernelGGL((norm_grad_columns_kernel<T, kVec<T>, decltype(n)::value>),
+                                       dim3(unsigned(blocks)), dim3(t.threads), 0, s, a, t.lanes);
+                return hipGetLastError();
+            });
+        }
         if (e != hipSuccess || (!dweight && !dbias)) return e;
-        hipLaunchKernelGGL(sum_partials_kernel,
-                           dim3(unsigned((H + kSumFeatures - 1) / kSumFeatures)),
+        hipLaunchKernelGGL(sum_partials_kernel, dim3(unsigned(up(H, kSumFeatures))),
                            dim3(kSumFeatures * kSumSlices), 0, s, a.dw, a.db, H, blocks, dweight, dbias);
         return hipGetLastError();
     });

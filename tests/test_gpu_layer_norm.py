@@ -74,6 +74,8 @@ def test_layer_norm_orders(darb, H, B, dtype, wdtype):  # noqa: F811
     for order in ORDERS:
         rng = np.random.default_rng(H + B)
         seen.append(run(darb, x, dtype, wdtype, order, rng, f"norm {H}x{B} {dtype} {order}")[3:])
+    if H == 1 or B == 1:                     # a contiguous vector has both orders, a strided one
+        return
     for a, b in ((0, 2), (1, 3)):            # bits do not depend on leading dimension or alignment
         for p, q in zip(seen[a], seen[b]):
             assert all(torch.equal(s, t) for s, t in zip(p, q)), (H, B, a)

@@ -137,6 +137,8 @@ def test_logprobs_orders(darb, V, B, top, dtype):  # noqa: F811
         zd, z64, td, r, _ = run(darb, z, t, top, dtype, order, label)
         check_grad(darb, rng, zd, z64, td, r, dtype, label, entropy=order != "tokens")
         seen.append(r)
+    if V == 1 or B == 1:                     # a contiguous vector has both orders, a strided one
+        return
     # an order's bits do not depend on the leading dimension or the alignment
     for a, b in ((0, 2), (1, 3)):
         for x, y in zip(seen[a], seen[b]):
