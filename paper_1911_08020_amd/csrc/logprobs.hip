@@ -22,10 +22,10 @@ constexpr float kInf = __builtin_inff();
 // e^(z - m) is zero long before this distance; it keeps 0 * -inf out of U.
 constexpr float kFar = -1e4f;
 constexpr int kMaxTop = 64;
-constexpr int kRowThreads = 256;        // token-major: a workgroup per part of a row
 constexpr int kColThreads = 256;        // feature-major: a workgroup per (64 tokens, part)
 constexpr int kColRun = 16;             // feature-major: classes of a segment, of one thread
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256;       // to find alternatives; without, a wave
+constexpr int kHeldMaxima = 2048;       // segments of a row that is finished where it is read
 
 struct Stat {
     float m, s, u;                      // s = 0 and u = 0 where every logit is -inf
@@ -45,23 +45,31 @@ __device__ __forceinline__ Stat shuffle_xor(Stat a, int d) {
     return {__shfl_xor(a.m, d, kWave), __shfl_xor(a.s, d, kWave), __shfl_xor(a.u, d, kWave)};
 }
 
-// Adds n values to a running Stat; m is their maximum and the old maximum's (an infinite or
-// NaN logit makes s NaN: z - m is, or e^(z - m) is).
-template <int N> __device__ __forceinline__ void add_values(Stat &t, const float (&z)[N], float m) {
-    if (m == -kInf) return;
-    if (m != t.m) {
-        const float d = fmaxf(t.m - m, kFar), e = exp_fast(t.m - m);
-        t.u = e * (t.u + t.s * d);
-        t.s *= e;
-        t.m = m;
+// The same sums while values come in.  The greatest value's term is 1 exactly, so that a sum is
+// never below it and a log probability never above 0.
+struct Sums {
+    float m = -kInf, s = 0.0f, u = 0.0f;
+
+    // to: the greater of m and the new values' maximum
+    __device__ __forceinline__ void raise(float to) {
+        if (to == m) return;
+        const float d = fmaxf(m - to, kFar), e = exp_fast(m - to);
+        u = e * (u + s * d);
+        s *= e;
+        m = to;
     }
+    // values not above m, -inf among them; a NaN or +inf makes s NaN unless m is -inf
+    template <int N> __device__ __forceinline__ void add(const float (&z)[N]) {
+        if (m == -kInf) return;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float d = z[i] - m, e = exp_fast(d);
-        t.s += e;
-        t.u = fmaf(e, fmaxf(d, kFar), t.u);
+        for (int i = 0; i < N; ++i) {
+            const float d = z[i] - m, e = exp_fast(d);
+            s += e;
+            u = fmaf(e, fmaxf(d, kFar), u);
+        }
     }
-}
+    __device__ __forceinline__ Stat stat() const { return {m, s, u}; }
+};
 
 struct Args {
     const void *z;
@@ -85,70 +93,142 @@ __device__ __forceinline__ uint32_t order_of(float z) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
+__device__ __forceinline__ uint64_t key_at(uint64_t x, int lane) {
+    return uint64_t(uint32_t(__builtin_amdgcn_readlane(int(x >> 32), lane))) << 32 |
+           uint32_t(__builtin_amdgcn_readlane(int(x), lane));
+}
+__device__ __forceinline__ uint64_t from_lane_below(uint64_t x) {
+    constexpr int kWaveShr1 = 0x138;
+    const uint32_t hi = uint32_t(x >> 32), lo = uint32_t(x);
+    return uint64_t(dpp<kWaveShr1>(hi, hi)) << 32 | dpp<kWaveShr1>(lo, lo);
+}
+
 // The k greatest 64-bit keys seen so far, one per lane in descending order (0 = none).
 struct TopList {
     uint64_t key = 0;
-    __device__ __forceinline__ uint64_t least(int k) const {
-        return uint64_t(__shfl(static_cast<unsigned long long>(key), k - 1, kWave));
-    }
     // every lane offers a key (0 = none); all lanes take part
     __device__ __forceinline__ void offer(uint64_t mine, int k, int lane) {
-        uint64_t floor = least(k);
-        uint64_t who = __ballot(mine > floor);
+        uint64_t who = __ballot(mine > key_at(key, k - 1));
         while (who) {
             const int src = __ffsll(static_cast<unsigned long long>(who)) - 1;
-            const uint64_t c = __shfl(static_cast<unsigned long long>(mine), src, kWave);
-            const uint64_t up = __shfl_up(static_cast<unsigned long long>(key), 1, kWave);
+            const uint64_t c = key_at(mine, src);
             const int at = __popcll(__ballot(key > c));          // keys are distinct
+            const uint64_t up = from_lane_below(key);
             key = lane < at ? key : lane == at ? c : up;
-            floor = least(k);
-            if (lane == src) mine = 0;
-            who = __ballot(mine > floor);
+            who &= who - 1;
+            who &= __ballot(mine > key_at(key, k - 1));
         }
     }
 };
 
-// One wave: the alternatives of token b, given the segments' maxima.
-template <typename T>
-__device__ __forceinline__ void write_top(const Args &a, int64_t b, const float *maxima, float lse,
-                                          int lane) {
-    const int k = int(a.top);
-    TopList segs;
-    for (int64_t i = 0; i < a.nseg; i += kWave) {
-        const int64_t s = i + lane;
-        const uint64_t key = s < a.nseg ? uint64_t(order_of(maxima[s])) << 32 | (UINT32_MAX - uint32_t(s)) : 0;
-        segs.offer(key, k, lane);
-    }
-    const T *col = static_cast<const T *>(a.z) + b * a.token_stride;
-    TopList best;
-    for (int i = 0; i < k; ++i) {
-        const uint64_t key = __shfl(static_cast<unsigned long long>(segs.key), i, kWave);
-        if (key == 0) break;
-        const int64_t first = int64_t(UINT32_MAX - uint32_t(key)) * a.seg_len;
-        int64_t last = first + a.seg_len;
-        if (last > a.V) last = a.V;
-        for (int64_t v0 = first; v0 < last; v0 += kWave) {
-            const int64_t v = v0 + lane;
-            uint64_t mine = 0;
-            if (v < last)
-                mine = uint64_t(order_of(float(col[v * a.class_stride]))) << 32 | (UINT32_MAX - uint32_t(v));
-            best.offer(mine, k, lane);
-        }
-    }
-    if (lane < k) {
-        const int64_t v = UINT32_MAX - uint32_t(best.key);
-        const float z = float(col[v * a.class_stride]);
-        a.top_index[b * a.top + lane] = v;
-        a.top_logprob[b * a.top + lane] = lse == -kInf ? -kInf : z - lse;
+__device__ __forceinline__ uint64_t key_of(float z, uint32_t index) {
+    return uint64_t(order_of(z)) << 32 | (UINT32_MAX - index);
+}
+
+// What a workgroup needs to find a token's alternatives.
+constexpr int kKeys = 1024;
+struct TopRoom {
+    uint64_t keys[kKeys];
+    uint64_t segs[kMaxTop];
+    uint32_t count;
+};
+
+// f(key, rank) for those of keys[0 .. n) that have fewer than k greater ones (the keys are
+// distinct): every thread counts for its own.
+template <int THREADS, typename F>
+__device__ __forceinline__ void ranked(const uint64_t *keys, int n, int k, F &&f) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const uint64_t mine = keys[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += keys[j] > mine;
+        if (rank < k) f(mine, rank);
     }
 }
 
-// One wave: a token's results from its whole Stat.
+// A wave's part of a segment's keys that can be among the k greatest: f(key of this lane, or 0).
+template <typename T, int kEach, typename F>
+__device__ __forceinline__ void segment_keys(const Args &a, const T *col, int64_t seg, int lane,
+                                             uint32_t least, F &&f) {
+    int64_t end = (seg + 1) * a.seg_len;
+    if (end > a.V) end = a.V;
+    const int64_t own = seg * a.seg_len + int64_t(lane) * kEach;
+    if constexpr (kEach == 1) {
+        const uint64_t key = own < end ? key_of(float(col[own * a.class_stride]), uint32_t(own)) : 0;
+        f(uint32_t(key >> 32) >= least ? key : 0);
+    } else {
+        const bool whole = own + kEach <= end;
+        Loaded<T, kEach> x;
+        if (whole) x = load_vec<T, kEach>(col + own);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            uint64_t key = 0;
+            if (whole) key = key_of(x[j], uint32_t(own + j));
+            else if (own + j < end) key = key_of(float(col[own + j]), uint32_t(own + j));
+            f(uint32_t(key >> 32) >= least ? key : 0);
+        }
+    }
+}
+
+// The alternatives of token b by a whole workgroup, given the segments' maxima.  An element can
+// be among the k greatest only if it is not below the k-th greatest maximum, and only in a
+// segment with one of the k greatest: those few are collected and ranked.  (Long columns: each
+// wave keeps the k greatest of its share of the maxima first.  More equal elements than there
+// is room for: one wave goes through the segments.)
+template <typename T, int kEach, int THREADS>
+__device__ __forceinline__ void write_top(const Args &a, int64_t b, const float *maxima, float lse,
+                                          TopRoom &room) {
+    constexpr int kWaves = THREADS / kWave;
+    const int w = threadIdx.x / kWave, lane = lane_id(), k = int(a.top);
+    const int found = a.nseg < k ? int(a.nseg) : k;
+    int n = int(a.nseg);
+    if (a.nseg <= kKeys) {
+        for (int i = threadIdx.x; i < n; i += THREADS) room.keys[i] = key_of(maxima[i], uint32_t(i));
+    } else {
+        TopList mine;
+        for (int64_t i = int64_t(w) * kWave; i < a.nseg; i += THREADS) {
+            const int64_t seg = i + lane;
+            mine.offer(seg < a.nseg ? key_of(maxima[seg], uint32_t(seg)) : 0, k, lane);
+        }
+        n = kWaves * k;                              // at most 16 x 64; zeros where a wave has fewer
+        if (lane < k) room.keys[w * k + lane] = mine.key ? mine.key : uint64_t(w * k + lane);
+    }
+    if (threadIdx.x == 0) room.count = 0;
+    __syncthreads();
+    ranked<THREADS>(room.keys, n, found, [&](uint64_t key, int rank) { room.segs[rank] = key; });
+    __syncthreads();
+    const uint32_t least = a.nseg < k ? 1 : uint32_t(room.segs[found - 1] >> 32);
+    const T *col = static_cast<const T *>(a.z) + b * a.token_stride;
+    for (int i = w; i < found; i += kWaves)
+        segment_keys<T, kEach>(a, col, UINT32_MAX - uint32_t(room.segs[i]), lane, least, [&](uint64_t key) {
+            if (key) {
+                const uint32_t at = atomicAdd(&room.count, 1u);
+                if (at < kKeys) room.keys[at] = key;
+            }
+        });
+    __syncthreads();
+    auto write = [&](uint64_t key, int rank) {
+        const int64_t v = UINT32_MAX - uint32_t(key);
+        const float z = float(col[v * a.class_stride]);
+        a.top_index[b * a.top + rank] = v;
+        a.top_logprob[b * a.top + rank] = lse == -kInf ? -kInf : z - lse;
+    };
+    if (room.count <= kKeys) {
+        ranked<THREADS>(room.keys, int(room.count), k, write);
+    } else if (w == 0) {
+        TopList best;
+        for (int i = 0; i < found; ++i)
+            segment_keys<T, kEach>(a, col, UINT32_MAX - uint32_t(room.segs[i]), lane, least,
+                                   [&](uint64_t key) { best.offer(key, k, lane); });
+        if (lane < k) write(best.key, lane);
+    }
+}
+
+// A token's results from its whole Stat, which every thread holds; its lse.
 template <typename T>
-__device__ __forceinline__ float write_token(const Args &a, int64_t b, Stat t, int lane) {
+__device__ __forceinline__ float write_token(const Args &a, int64_t b, Stat t) {
     const bool empty = t.m == -kInf && t.s == 0.0f;         // nothing but -inf
     const float logs = logf(t.s), lse = empty ? -kInf : t.m + logs;
-    if (lane == 0) {
+    if (threadIdx.x == 0) {
         const int64_t y = a.targets ? a.targets[b] : -1;
         float lp = 0.0f;
         if (y >= a.V) {
@@ -166,50 +246,94 @@ __device__ __forceinline__ float write_token(const Args &a, int64_t b, Stat t, i
 
 // ---- token-major: a row's classes are contiguous --------------------------------------
 
-// grid (parts, B); each wave takes every kWaves-th run of 64 vectors of its part, which is a
-// segment: its maximum is also what the wave's sums run from.
-template <typename T>
-__global__ __launch_bounds__(kRowThreads) void rows_kernel(Args a) {
-    constexpr int V = kVec<T>, kWaves = kRowThreads / kWave, kRun = V * kWave;
+// grid (parts, B); each wave takes every kWaves-th run of 64 vectors of its part, four runs
+// together.  A run is a segment; the four's maximum is what the wave's sums run from.  A row
+// that is one part is finished here, its maxima kept in LDS.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void rows_kernel(Args a) {
+    constexpr int V = kVec<T>, kWaves = THREADS / kWave, kRun = V * kWave, kAtOnce = 4;
     __shared__ Stat stats[kWaves];
+    __shared__ float held[kHeldMaxima];
+    __shared__ TopRoom room;
     const int w = threadIdx.x / kWave, lane = lane_id();
     const int64_t b = a.first + blockIdx.y, part = blockIdx.x;
     const T *row = static_cast<const T *>(a.z) + b * a.token_stride;
     const int64_t begin = part * a.part_len;
     int64_t end = begin + a.part_len;
     if (end > a.V) end = a.V;
-    Stat t{-kInf, 0.0f, 0.0f};
-    for (int64_t v0 = begin + w * kRun; v0 < end; v0 += kWaves * kRun) {
-        const int64_t v = v0 + lane * V;
-        float z[V];
-        if (v + V <= end) {
-            const Loaded<T, V> x = load_vec<T, V>(row + v);
+    float *maxima = a.nparts == 1 ? held : a.maxima + b * a.nseg;
+    Sums t;
+    for (int64_t v0 = begin + w * kRun; v0 < end; v0 += kAtOnce * kWaves * kRun) {
+        float z[kAtOnce][V], m[kAtOnce];
+        if (v0 + ((kAtOnce - 1) * kWaves + 1) * kRun <= end) {
+            Loaded<T, V> x[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < V; ++i) z[i] = x[i];
+            for (int q = 0; q < kAtOnce; ++q) x[q] = load_vec<T, V>(row + v0 + q * (kWaves * kRun) + lane * V);
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q)
+#pragma unroll
+                for (int i = 0; i < V; ++i) z[q][i] = x[q][i];
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) z[i] = v + i < end ? float(row[v + i]) : -kInf;
-        }
-        float m = z[0];
-        bool nan = z[0] != z[0];
+            for (int q = 0; q < kAtOnce; ++q) {
+                const int64_t v = v0 + q * (kWaves * kRun) + lane * V;
+                if (v + V <= end) {
+                    const Loaded<T, V> x = load_vec<T, V>(row + v);
 #pragma unroll
-        for (int i = 1; i < V; ++i) {
-            m = fmaxf(m, z[i]);
-            nan |= z[i] != z[i];
+                    for (int i = 0; i < V; ++i) z[q][i] = x[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) z[q][i] = v + i < end ? float(row[v + i]) : -kInf;
+                }
+            }
         }
-        nan = __any(nan);
-        m = wave_max(m);
-        if (a.top && lane == 0) a.maxima[b * a.nseg + v0 / kRun] = nan ? __builtin_nanf("") : m;
-        add_values(t, z, fmaxf(m, t.m));
-        if (nan) t.s = __builtin_nanf("");
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            m[q] = z[q][0];
+#pragma unroll
+            for (int i = 1; i < V; ++i) m[q] = fmaxf(m[q], z[q][i]);
+        }
+        if (a.top) {
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) m[q] = wave_max(m[q]);
+            t.raise(fmaxf(t.m, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))));
+        } else {
+            const float all = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            if (__any(all > t.m)) t.raise(fmaxf(t.m, wave_max(all)));
+        }
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) t.add(z[q]);
+        // a NaN shows in s, or leaves no maximum: rare enough to look again
+        if (__any(t.s != t.s) || t.m == -kInf) {
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) {
+                bool nan = false;
+#pragma unroll
+                for (int i = 0; i < V; ++i) nan |= z[q][i] != z[q][i];
+                if (nan) t.s = __builtin_nanf("");
+                if (__any(nan)) m[q] = __builtin_nanf("");
+            }
+        }
+        if (a.top && lane == 0) {
+#pragma unroll
+            for (int q = 0; q < kAtOnce; ++q) {
+                const int64_t at = v0 + q * (kWaves * kRun);
+                if (at < end) maxima[at / kRun] = m[q];
+            }
+        }
     }
-    for (int d = 1; d < kWave; d <<= 1) t = join(t, shuffle_xor(t, d));
-    if (lane == 0) stats[w] = t;
+    Stat all = t.stat();
+    for (int d = 1; d < kWave; d <<= 1) all = join(all, shuffle_xor(all, d));
+    if (lane == 0) stats[w] = all;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < kWaves; ++i) t = join(t, stats[i]);
-        a.parts[b * a.nparts + part] = make_float4(t.m, t.s, t.u, 0.0f);
+    all = stats[0];
+    for (int i = 1; i < kWaves; ++i) all = join(all, stats[i]);
+    if (a.nparts > 1) {
+        if (threadIdx.x == 0) a.parts[b * a.nparts + part] = make_float4(all.m, all.s, all.u, 0.0f);
+        return;
     }
+    const float lse = write_token<T>(a, b, all);
+    if (a.top) write_top<T, V, THREADS>(a, b, held, lse, room);
 }
 
 // ---- feature-major: a class's tokens are contiguous -----------------------------------
@@ -230,17 +354,11 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
     const int64_t begin = part * a.part_len;
     int64_t end = begin + a.part_len;
     if (end > a.V) end = a.V;
-    Stat t[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) t[j] = {-kInf, 0.0f, 0.0f};
+    Sums t[V];
     for (int64_t v0 = begin + ty * kColRun; v0 < end; v0 += kRows * kColRun) {
         float m[V];
-        bool nan[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            m[j] = -kInf;
-            nan[j] = false;
-        }
+        for (int j = 0; j < V; ++j) m[j] = -kInf;
         constexpr int kAtOnce = 8;
 #pragma unroll 1
         for (int r0 = 0; r0 < kColRun; r0 += kAtOnce) {
@@ -257,23 +375,30 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
                 for (int r = 0; r < kAtOnce; ++r) {
                     y[r] = v0 + r0 + r < end ? x[r][j] : -kInf;
                     top = fmaxf(top, y[r]);
-                    nan[j] |= y[r] != y[r];
+                }
+                t[j].raise(fmaxf(top, t[j].m));
+                t[j].add(y);
+                // a NaN shows in s, or leaves no maximum: rare enough to look again
+                if (t[j].s != t[j].s || top == -kInf) {
+                    bool nan = m[j] != m[j];
+#pragma unroll
+                    for (int r = 0; r < kAtOnce; ++r) nan |= y[r] != y[r];
+                    if (nan) t[j].s = top = __builtin_nanf("");
                 }
                 m[j] = top;
-                add_values(t[j], y, fmaxf(top, t[j].m));
             }
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if (nan[j]) t[j].s = __builtin_nanf("");
-            if (a.top && live) a.maxima[(b + j) * a.nseg + v0 / kColRun] = nan[j] ? __builtin_nanf("") : m[j];
+            if (a.top && live) a.maxima[(b + j) * a.nseg + v0 / kColRun] = m[j];
         }
     }
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        sm[ty][tx * V + j] = t[j].m;
-        ss[ty][tx * V + j] = t[j].s;
-        su[ty][tx * V + j] = t[j].u;
+        const Stat mine = t[j].stat();
+        sm[ty][tx * V + j] = mine.m;
+        ss[ty][tx * V + j] = mine.s;
+        su[ty][tx * V + j] = mine.u;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kLanes * V; i += kColThreads) {
@@ -287,20 +412,20 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
     }
 }
 
-// A wave per token: its parts joined, the results written, the alternatives found.
-template <typename T>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(Args a) {
-    const int lane = lane_id();
-    const int64_t b = int64_t(blockIdx.x) * (kJoinThreads / kWave) + threadIdx.x / kWave;
-    if (b >= a.B) return;
+// A workgroup per token: its parts joined, the results written, the alternatives found.
+template <typename T, int kEach, int THREADS>
+__global__ __launch_bounds__(THREADS) void join_kernel(Args a) {
+    __shared__ TopRoom room;
+    const int64_t b = blockIdx.x;
     Stat t{-kInf, 0.0f, 0.0f};
-    for (int64_t i = lane; i < a.nparts; i += kWave) {
+    for (int64_t i = lane_id(); i < a.nparts; i += kWave) {       // in every wave
         const float4 p = a.parts[b * a.nparts + i];
         t = join(t, {p.x, p.y, p.z});
     }
     for (int d = 1; d < kWave; d <<= 1) t = join(t, shuffle_xor(t, d));
-    const float lse = write_token<T>(a, b, t, lane);
-    if (a.top) write_top<T>(a, b, a.maxima + b * a.nseg, lse, lane);
+    t = {lane_of(t.m, 0), lane_of(t.s, 0), lane_of(t.u, 0)};     // lanes differ in the last bits
+    const float lse = write_token<T>(a, b, t);
+    if (THREADS > kWave) write_top<T, kEach, THREADS>(a, b, a.maxima + b * a.nseg, lse, room);
 }
 
 // ---- the gradient ---------------------------------------------------------------------
@@ -454,6 +579,7 @@ template <int V, typename F> hipError_t with_lanes(int lanes, F &&f) {
 struct Cut {
     bool rows;                          // token-major
     int vec, lanes;                     // feature-major
+    int threads;                        // token-major
     int64_t part_len, nparts, seg_len, nseg;
 };
 
@@ -464,11 +590,16 @@ Cut cut_of(int dtype, int64_t V, int64_t B, bool rows) {
     if (rows) {
         c.lanes = 0;
         c.seg_len = c.vec * kWave;
-        const int64_t step = c.seg_len * (kRowThreads / kWave);     // one round of a workgroup
+        // a wave has at least four runs, or one where rows are few; a long row several parts
+        const int64_t runs = (V + c.seg_len - 1) / c.seg_len, each = B < 256 ? 1 : 4;
+        c.threads = 256;
+        while (c.threads < 1024 && runs >= 2 * each * c.threads / kWave) c.threads *= 2;
+        const int64_t step = c.seg_len * (c.threads / kWave);       // one round of a workgroup
         const int64_t rounds = (V + step - 1) / step;
-        // about 1024 workgroups, each of at least 4 rounds
-        int64_t parts = (1024 + B - 1) / B;
+        int64_t parts = (512 + B - 1) / B;
         if (parts > rounds / 4) parts = rounds / 4;
+        const int64_t held = (V + c.seg_len * kHeldMaxima - 1) / (c.seg_len * kHeldMaxima);
+        if (parts < held) parts = held;
         if (parts < 1) parts = 1;
         c.part_len = (rounds + parts - 1) / parts * step;
     } else {
@@ -522,9 +653,15 @@ hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64
         hipError_t e;
         if (c.rows) {
             e = over_grid_y(a, B, [&](const Args &part, unsigned n) {
-                hipLaunchKernelGGL((rows_kernel<T>), dim3(unsigned(c.nparts), n),
-                                   dim3(kRowThreads), 0, s, part);
+                const dim3 grid(unsigned(c.nparts), n);
+                if (c.threads == 256)
+                    hipLaunchKernelGGL((rows_kernel<T, 256>), grid, dim3(256), 0, s, part);
+                else if (c.threads == 512)
+                    hipLaunchKernelGGL((rows_kernel<T, 512>), grid, dim3(512), 0, s, part);
+                else
+                    hipLaunchKernelGGL((rows_kernel<T, 1024>), grid, dim3(1024), 0, s, part);
             });
+            if (e != hipSuccess || c.nparts == 1) return e;
         } else {
             const int64_t tiles = (B + c.lanes * c.vec - 1) / (c.lanes * c.vec);
             auto columns = [&](auto vec) {
@@ -542,9 +679,14 @@ hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64
                            : columns(std::integral_constant<int, kVec<T>>{});
         }
         if (e != hipSuccess) return e;
-        const int64_t waves = kJoinThreads / kWave;
-        hipLaunchKernelGGL((join_kernel<T>), dim3(unsigned((B + waves - 1) / waves)),
-                           dim3(kJoinThreads), 0, s, a);
+        if (!top)
+            hipLaunchKernelGGL((join_kernel<T, 1, kWave>), dim3(unsigned(B)), dim3(kWave), 0, s, a);
+        else if (c.rows)
+            hipLaunchKernelGGL((join_kernel<T, kVec<T>, kJoinThreads>), dim3(unsigned(B)),
+                               dim3(kJoinThreads), 0, s, a);
+        else
+            hipLaunchKernelGGL((join_kernel<T, 1, kJoinThreads>), dim3(unsigned(B)),
+                               dim3(kJoinThreads), 0, s, a);
         return hipGetLastError();
     });
 }
