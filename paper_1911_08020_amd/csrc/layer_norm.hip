@@ -198,10 +198,16 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
     for (int i = 0; i < kHeld; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) sw[i][j] = sb[i][j] = 0.0f;
+    // the next token's rows are on their way while this one's sums cross the workgroup
+    Row<T, V, N> next_x, next_dy;
+    auto fetch = [&](int64_t b) {
+        next_x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H);
+        next_dy.open(static_cast<const T *>(a.dy.p) + b * a.dy.token, a.H);
+    };
+    fetch(blockIdx.x);
     for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
-        Row<T, V, N> x, dy;
-        x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H);
-        dy.open(static_cast<const T *>(a.dy.p) + b * a.dy.token, a.H);
+        Row<T, V, N> x = next_x, dy = next_dy;
+        if (b + gridDim.x < a.B) fetch(b + gridDim.x);
         T *dx = static_cast<T *>(a.y.p) + b * a.y.token;
         const float mean = a.mean[b], rstd = a.rstd[b];
         float s[2] = {0.0f, 0.0f};
@@ -265,8 +271,14 @@ template <typename T, int V, int N> struct Tile {
     Loaded<T, V> held[N ? N : 1];
     const T *p;
     int64_t H, stride;
+    uint32_t at;                        // the thread's first vector, in bytes from p
     int first, rows;
 
+    // a vector of feature i * rows + first: a base that the workgroup shares and 32 bits of a
+    // thread's own (tile_shape sees to it that they suffice where N is not 0)
+    __device__ __forceinline__ const T *row(int64_t i) const {
+        return reinterpret_cast<const T *>(reinterpret_cast<const char *>(p + i * rows * stride) + at);
+    }
     // f(feature's place in the thread, feature, vector)
     template <typename F> __device__ __forceinline__ void each(F &&f) const {
         if constexpr (N) {
@@ -276,8 +288,11 @@ template <typename T, int V, int N> struct Tile {
                 if (h < H) f(i, h, held[i]);
             }
         } else {
-            for (int64_t h = first; h < H; h += rows) f(0, h, load_vec<T, V>(p + h * stride));
+            for (int64_t h = first; h < H; h += rows) f(0, h, get(h));
         }
+    }
+    __device__ __forceinline__ Loaded<T, V> get(int64_t h) const {
+        return load_vec<T, V>(p + b + h * stride);
     }
     __device__ __forceinline__ void forget() {
         if constexpr (N) {
@@ -285,21 +300,38 @@ template <typename T, int V, int N> struct Tile {
             for (int i = 0; i < N; ++i) forget_uses(held[i]);
         }
     }
-    __device__ __forceinline__ void open(const T *at, int64_t H_, int64_t stride_, int first_, int rows_) {
-        p = at;
+    int64_t b;
+    __device__ __forceinline__ void open(const void *p_, int64_t b_, int64_t H_, int64_t stride_, int first_, int rows_) {
+        p = static_cast<const T *>(p_);
+        b = b_;
         H = H_;
         stride = stride_;
         first = first_;
         rows = rows_;
         if constexpr (N) {
+            // past the last feature: the thread's tokens of the round's first one
+            const uint32_t token = uint32_t(b) * uint32_t(sizeof(T));
+            const uint32_t own = token + uint32_t(first) * uint32_t(stride) * uint32_t(sizeof(T));
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int64_t h = first + int64_t(i) * rows;
-                held[i] = load_vec<T, V>(p + (h < H ? h : H - 1) * stride);
+                if (int64_t(i) * rows >= H) break;
+                at = first + int64_t(i) * rows < H ? own : token;
+                held[i] = load_vec<T, V>(row(i));
             }
+            at = own;
         }
     }
 };
+
+template <typename T, int V, int N>
+__device__ __forceinline__ T *out_row(const Matrix &m, int64_t i, int64_t h, int first, int rows, int64_t b) {
+    if constexpr (N) {
+        const uint32_t at = (uint32_t(first) * uint32_t(m.feature) + uint32_t(b)) * uint32_t(sizeof(T));
+        return reinterpret_cast<T *>(reinterpret_cast<char *>(static_cast<T *>(m.p) + i * rows * m.feature) + at);
+    } else {
+        return static_cast<T *>(m.p) + b + h * m.feature;
+    }
+}
 
 // s summed over the threads with the same tokens (lanes of them side by side), in each of them;
 // scratch: kMaxWaves * lanes * K floats.
@@ -323,15 +355,21 @@ template <int K> __device__ __forceinline__ void tile_sum(float (&s)[K], int lan
 
 constexpr int kMaxLanes = 8;
 
+// The tile of task i: tasks go to the 8 XCDs in turn, each with an L2 of its own, and tiles that
+// lie side by side (parts of the same cache lines, where a tile is narrow) go to one XCD.
+__device__ __forceinline__ int64_t tile_of(int64_t i, int64_t tiles) {
+    const int64_t xcd = i % 8, whole = tiles / 8, more = tiles % 8;
+    return xcd * whole + (xcd < more ? xcd : more) + i / 8;
+}
+
 template <typename T, int V, int N>
 __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int lanes) {
     __shared__ float scratch[kMaxWaves * kMaxLanes * V];
     const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes, rows = blockDim.x / lanes;
     int skip;
-    const int64_t b = back_from_end<V>((int64_t(blockIdx.x) * lanes + tx) * V, a.B, skip);
+    const int64_t b = back_from_end<V>((tile_of(blockIdx.x, gridDim.x) * lanes + tx) * V, a.B, skip);
     Tile<T, V, N> x;
-    x.open(static_cast<const T *>(a.x.p) + b, a.H, a.x.feature, ty, rows);
-    T *y = static_cast<T *>(a.y.p) + b;
+    x.open(a.x.p, b, a.H, a.x.feature, ty, rows);
     float mean[V], rstd[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) mean[j] = rstd[j] = 0.0f;
@@ -354,12 +392,12 @@ __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int l
     x.forget();
 #pragma unroll
     for (int j = 0; j < V; ++j) rstd[j] = 1.0f / sqrtf(rstd[j] / float(a.H) + a.eps);
-    x.each([&](int, int64_t h, const Loaded<T, V> &v) {
+    x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
         const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f, c = a.b ? weight_at<T>(a, a.b, h) : 0.0f;
         float out[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) out[j] = fmaf((v[j] - mean[j]) * rstd[j], w, c);
-        store_own<T, V>(y + h * a.y.feature, skip, out);
+        store_own<T, V>(out_row<T, V, N>(a.y, i, h, ty, rows, b), skip, out);
     });
     if (ty == 0) {
 #pragma unroll
@@ -388,11 +426,10 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a,
     };
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         int skip;
-        const int64_t b = back_from_end<V>((tile * lanes + tx) * V, a.B, skip);
+        const int64_t b = back_from_end<V>((tile_of(tile, tiles) * lanes + tx) * V, a.B, skip);
         Tile<T, V, N> x, dy;
-        x.open(static_cast<const T *>(a.x.p) + b, a.H, a.x.feature, ty, rows);
-        dy.open(static_cast<const T *>(a.dy.p) + b, a.H, a.dy.feature, ty, rows);
-        T *dx = static_cast<T *>(a.y.p) + b;
+        x.open(a.x.p, b, a.H, a.x.feature, ty, rows);
+        dy.open(a.dy.p, b, a.H, a.dy.feature, ty, rows);
         float mean[V], rstd[V], s[2 * V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -401,7 +438,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a,
             s[j] = s[V + j] = 0.0f;
         }
         x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
-            const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h * dy.stride);
+            const Loaded<T, V> g = N ? dy.held[i] : dy.get(h);
             const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
             float fw = 0.0f, fb = 0.0f;
 #pragma unroll
@@ -433,7 +470,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a,
 #pragma unroll
         for (int j = 0; j < 2 * V; ++j) s[j] /= float(a.H);
         x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
-            const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h * dy.stride);
+            const Loaded<T, V> g = N ? dy.held[i] : dy.get(h);
             const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
             float out[V];
 #pragma unroll
@@ -441,7 +478,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a,
                 const float xh = (v[j] - mean[j]) * rstd[j];
                 out[j] = rstd[j] * (g[j] * w - s[j] - xh * s[V + j]);
             }
-            store_own<T, V>(dx + h * a.y.feature, skip, out);
+            store_own<T, V>(out_row<T, V, N>(a.y, i, h, ty, rows, b), skip, out);
         });
     }
     if constexpr (N) {
@@ -458,7 +495,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a,
 
 // ---- the partial sums of dw and db -----------------------------------------------------
 
-constexpr int kSumFeatures = 64, kSumSlices = 16;
+constexpr int kSumFeatures = 16, kSumSlices = 64;    // 64 bytes a row; many workgroups
 
 __global__ __launch_bounds__(kSumFeatures * kSumSlices) void sum_partials_kernel(
     const float *__restrict__ dw_parts, const float *__restrict__ db_parts, int64_t H, int blocks,
@@ -521,7 +558,7 @@ struct TileShape {
     int lanes, threads, n, vec;
 };
 
-TileShape tile_shape(int64_t H, int64_t B, int vec, int threads, int most) {
+TileShape tile_shape(int64_t H, int64_t B, int64_t stride, int vec, int threads, int most) {
     TileShape t;
     t.vec = B < vec ? 1 : vec;
     t.lanes = kMaxLanes;
@@ -530,7 +567,8 @@ TileShape tile_shape(int64_t H, int64_t B, int vec, int threads, int most) {
     t.threads = threads;
     t.n = 2;
     while (t.n <= most && want > int64_t(threads) * t.n) t.n *= 2;
-    if (t.n > most) t.n = 0;
+    // a thread's vectors lie within 32 bits of bytes of their round's first
+    if (t.n > most || (int64_t(threads) * stride + B) * 4 >= int64_t(1) << 32) t.n = 0;
     return t;
 }
 
@@ -573,7 +611,7 @@ hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const
                 return hipGetLastError();
             });
         }
-        const TileShape t = tile_shape(H, B, kVec<T>, kMaxThreads, 8);
+        const TileShape t = tile_shape(H, B, x_feature > y_feature ? x_feature : y_feature, kVec<T>, kMaxThreads, 8);
         return with_tile<8>(t, [&](auto n) {
             const dim3 grid(unsigned(up(B, int64_t(t.lanes) * t.vec)));
             if (t.vec == 1)
@@ -599,7 +637,9 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
     return with_type(xdtype, [&](auto type) {
         using T = decltype(type);
         const bool rows = rows_of(H, x_feature);
-        const TileShape t = tile_shape(H, B, kVec<T>, kGradThreads, 16);
+        int64_t stride = x_feature > dy_feature ? x_feature : dy_feature;
+        if (dx && dx_feature > stride) stride = dx_feature;
+        const TileShape t = tile_shape(H, B, stride, kVec<T>, kGradThreads, 16);
         const int64_t tasks = rows ? B : up(B, int64_t(t.lanes) * t.vec);
         const int blocks = tasks < kMaxBlocks ? int(tasks) : kMaxBlocks;
         if (dweight) a.dw = static_cast<float *>(workspace);

@@ -41,8 +41,16 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
     return {m, a.s * ea + b.s * eb, ea * (a.u + a.s * da) + eb * (b.u + b.s * db)};
 }
 
-__device__ __forceinline__ Stat shuffle_xor(Stat a, int d) {
-    return {__shfl_xor(a.m, d, kWave), __shfl_xor(a.s, d, kWave), __shfl_xor(a.u, d, kWave)};
+// The Stat of a wave's first LANES lanes, the same bits in every lane (a lane's own sum may be
+// off in the last: its first addition can fuse with a product).
+template <int LANES> __device__ __forceinline__ Stat join_lanes(Stat a) {
+    auto over = [](float x, auto op) {
+        return lane_of(group_reduce<LANES, decltype(op)>(x), LANES - 1);
+    };
+    const float m = over(a.m, MaxOp{});
+    if (m == -kInf) return {m, over(a.s, AddOp{}), 0.0f};
+    const float e = exp_fast(a.m - m), d = fmaxf(a.m - m, kFar);
+    return {m, over(a.s * e, AddOp{}), over(e * (a.u + a.s * d), AddOp{})};
 }
 
 // The same sums while values come in.  The greatest value's term is 1 exactly, so that a sum is
@@ -58,9 +66,8 @@ struct Sums {
         s *= e;
         m = to;
     }
-    // values not above m, -inf among them; a NaN or +inf makes s NaN unless m is -inf
+    // values not above m (which is not -inf), -inf among them; a NaN or +inf makes s NaN
     template <int N> __device__ __forceinline__ void add(const float (&z)[N]) {
-        if (m == -kInf) return;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float d = z[i] - m, e = exp_fast(d);
@@ -69,6 +76,18 @@ struct Sums {
         }
     }
     __device__ __forceinline__ Stat stat() const { return {m, s, u}; }
+};
+
+// The lane's V consecutive logits of a row from v on, those before `end`.  A vector that would
+// pass it starts V before it instead (a row holds V at least) and leaves out its first `skip`.
+template <typename T, int V> struct Run {
+    Loaded<T, V> x;
+    int skip;
+    __device__ __forceinline__ void load(const T *row, int64_t v, int64_t end) {
+        const int64_t own = v + V <= end ? v : end - V;
+        skip = v - own < V ? int(v - own) : V;
+        x = load_vec<T, V>(row + own);
+    }
 };
 
 struct Args {
@@ -91,6 +110,11 @@ __device__ __forceinline__ uint32_t order_of(float z) {
     if (z != z) return ~0u;
     const uint32_t b = __float_as_uint(z + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// The value with that order (NaN for all NaN).
+__device__ __forceinline__ float value_of(uint32_t order) {
+    return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order);
 }
 
 __device__ __forceinline__ uint64_t key_at(uint64_t x, int lane) {
@@ -126,11 +150,12 @@ __device__ __forceinline__ uint64_t key_of(float z, uint32_t index) {
 }
 
 // What a workgroup needs to find a token's alternatives.
-constexpr int kKeys = 1024;
+constexpr int kKeys = 1024, kSegs = 1024;
 struct TopRoom {
     uint64_t keys[kKeys];
-    uint64_t segs[kMaxTop];
-    uint32_t count;
+    uint32_t segs[kSegs];
+    uint32_t least;                     // no alternative's order is below
+    uint32_t found, count;              // entries of segs, of keys
 };
 
 // f(key, rank) for those of keys[0 .. n) that have fewer than k greater ones (the keys are
@@ -145,61 +170,132 @@ __device__ __forceinline__ void ranked(const uint64_t *keys, int n, int k, F &&f
     }
 }
 
-// A wave's part of a segment's keys that can be among the k greatest: f(key of this lane, or 0).
+// The greatest x that k or more values reach, given how many reach any: by halving from lo,
+// which k reach, to hi, which none passes.
+template <typename F>
+__device__ __forceinline__ uint32_t kth_greatest(uint32_t lo, uint32_t hi, int k, F &&reach) {
+    while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        const int r = reach(mid);
+        if (r >= k) lo = mid;
+        else hi = mid - 1;
+        if (r == k) break;
+    }
+    return lo;
+}
+
+// One wave: a bound that k or more logits reach, from n maxima of segments.  They are taken as
+// 256 groups (every 256th of them): the k-th greatest of the groups' maxima is such a bound, and
+// little more than k segments reach it.  Fewer than k maxima: 1, which every logit reaches.
+constexpr int kGroups = 4;              // a lane
+__device__ __forceinline__ uint32_t bound_of(const float *maxima, int64_t n, int k, int lane) {
+    if (n < k) return 1;
+    uint32_t o[kGroups] = {};
+    for (int64_t i = lane; i < n; i += kGroups * kWave)
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) {
+            const int64_t at = i + q * kWave;
+            const uint32_t x = at < n ? order_of(maxima[at]) : 0;
+            o[q] = x > o[q] ? x : o[q];
+        }
+    uint32_t hi = 0;
+#pragma unroll
+    for (int q = 0; q < kGroups; ++q) hi = o[q] > hi ? o[q] : hi;
+    return kth_greatest(1, wave_max_u32(hi), k, [&](uint32_t x) {
+        int r = 0;
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) r += __popcll(__ballot(o[q] >= x));
+        return r;
+    });
+}
+
+// One wave: the segments with the k greatest of n maxima exactly, of equal ones the first; for
+// columns so full of equal values that too many segments reach the bound.
+__device__ __forceinline__ void pick_segments(const float *maxima, int64_t n, int k, int lane, TopRoom &room) {
+    auto reach = [&](uint32_t x) {
+        int r = 0;
+        for (int64_t i = 0; i < n; i += kWave)
+            r += __popcll(__ballot(i + lane < n && order_of(maxima[i + lane]) >= x));
+        return r;
+    };
+    const uint32_t lo = kth_greatest(room.least, ~0u, k, reach);
+    int equal = k - (lo == ~0u ? 0 : reach(lo + 1)), at = 0;     // how many of those at lo to take
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+    for (int64_t i = 0; i < n && at < k; i += kWave) {
+        const uint32_t o = i + lane < n ? order_of(maxima[i + lane]) : 0;
+        const uint64_t same = __ballot(o == lo);
+        const bool take = o > lo || (o == lo && __popcll(same & below) < equal);
+        const uint64_t all = __ballot(take);
+        if (take) room.segs[at + __popcll(all & below)] = uint32_t(i + lane);
+        at += __popcll(all);
+        equal -= __popcll(same);
+        equal = equal < 0 ? 0 : equal;
+    }
+    if (lane == 0) {
+        room.least = lo;
+        room.found = uint32_t(k);
+    }
+}
+
+// A lane's keys of segments first ... last of the list that can be among the k greatest: f(key
+// of this lane, or 0).  A wave takes as many segments at once as it has lanes for.
 template <typename T, int kEach, typename F>
-__device__ __forceinline__ void segment_keys(const Args &a, const T *col, int64_t seg, int lane,
-                                             uint32_t least, F &&f) {
+__device__ __forceinline__ void segment_keys(const Args &a, const T *col, const TopRoom &room, int first,
+                                             int found, int lane, F &&f) {
+    constexpr int kLanes = kEach == 1 ? kColRun : kWave;
+    const int i = first + lane / kLanes;
+    const int64_t seg = room.segs[i < found ? i : found - 1];
     int64_t end = (seg + 1) * a.seg_len;
     if (end > a.V) end = a.V;
-    const int64_t own = seg * a.seg_len + int64_t(lane) * kEach;
+    const uint32_t least = room.least;
+    int64_t own = seg * a.seg_len + int64_t(lane % kLanes) * kEach;
+    if (i >= found) own = end;                       // nothing
     if constexpr (kEach == 1) {
         const uint64_t key = own < end ? key_of(float(col[own * a.class_stride]), uint32_t(own)) : 0;
         f(uint32_t(key >> 32) >= least ? key : 0);
     } else {
-        const bool whole = own + kEach <= end;
-        Loaded<T, kEach> x;
-        if (whole) x = load_vec<T, kEach>(col + own);
+        Run<T, kEach> x;
+        x.load(col, own, end);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            uint64_t key = 0;
-            if (whole) key = key_of(x[j], uint32_t(own + j));
-            else if (own + j < end) key = key_of(float(col[own + j]), uint32_t(own + j));
+            const uint64_t key = j >= x.skip ? key_of(x.x[j], uint32_t(own + j - x.skip)) : 0;
             f(uint32_t(key >> 32) >= least ? key : 0);
         }
     }
 }
 
-// The alternatives of token b by a whole workgroup, given the segments' maxima.  An element can
-// be among the k greatest only if it is not below the k-th greatest maximum, and only in a
-// segment with one of the k greatest: those few are collected and ranked.  (Long columns: each
-// wave keeps the k greatest of its share of the maxima first.  More equal elements than there
-// is room for: one wave goes through the segments.)
+// The alternatives of token b by a whole workgroup, given the segments' maxima: the elements
+// not below the bound, which only segments whose maximum reaches it hold, are collected and
+// ranked.  (More equal elements than there is room for: one wave goes through the segments.)
 template <typename T, int kEach, int THREADS>
 __device__ __forceinline__ void write_top(const Args &a, int64_t b, const float *maxima, float lse,
                                           TopRoom &room) {
-    constexpr int kWaves = THREADS / kWave;
+    constexpr int kWaves = THREADS / kWave, kAtOnce = kEach == 1 ? kWave / kColRun : 1;
     const int w = threadIdx.x / kWave, lane = lane_id(), k = int(a.top);
-    const int found = a.nseg < k ? int(a.nseg) : k;
-    int n = int(a.nseg);
-    if (a.nseg <= kKeys) {
-        for (int i = threadIdx.x; i < n; i += THREADS) room.keys[i] = key_of(maxima[i], uint32_t(i));
-    } else {
-        TopList mine;
-        for (int64_t i = int64_t(w) * kWave; i < a.nseg; i += THREADS) {
-            const int64_t seg = i + lane;
-            mine.offer(seg < a.nseg ? key_of(maxima[seg], uint32_t(seg)) : 0, k, lane);
+    if (w == 0) {
+        const uint32_t bound = bound_of(maxima, a.nseg, k, lane);
+        if (lane == 0) {
+            room.least = bound;
+            room.found = room.count = 0;
         }
-        n = kWaves * k;                              // at most 16 x 64; zeros where a wave has fewer
-        if (lane < k) room.keys[w * k + lane] = mine.key ? mine.key : uint64_t(w * k + lane);
     }
-    if (threadIdx.x == 0) room.count = 0;
     __syncthreads();
-    ranked<THREADS>(room.keys, n, found, [&](uint64_t key, int rank) { room.segs[rank] = key; });
+    const uint32_t bound = room.least;
+    for (int64_t i = threadIdx.x; i < a.nseg; i += THREADS)
+        if (order_of(maxima[i]) >= bound) {
+            const uint32_t at = atomicAdd(&room.found, 1u);
+            if (at < kSegs) room.segs[at] = uint32_t(i);
+        }
     __syncthreads();
-    const uint32_t least = a.nseg < k ? 1 : uint32_t(room.segs[found - 1] >> 32);
+    if (room.found > kSegs) {                        // then there are more than k
+        __syncthreads();
+        if (w == 0) pick_segments(maxima, a.nseg, k, lane, room);
+        __syncthreads();
+    }
+    const int found = int(room.found);
     const T *col = static_cast<const T *>(a.z) + b * a.token_stride;
-    for (int i = w; i < found; i += kWaves)
-        segment_keys<T, kEach>(a, col, UINT32_MAX - uint32_t(room.segs[i]), lane, least, [&](uint64_t key) {
+    for (int i = w * kAtOnce; i < found; i += kWaves * kAtOnce)
+        segment_keys<T, kEach>(a, col, room, i, found, lane, [&](uint64_t key) {
             if (key) {
                 const uint32_t at = atomicAdd(&room.count, 1u);
                 if (at < kKeys) room.keys[at] = key;
@@ -207,36 +303,39 @@ __device__ __forceinline__ void write_top(const Args &a, int64_t b, const float 
         });
     __syncthreads();
     auto write = [&](uint64_t key, int rank) {
-        const int64_t v = UINT32_MAX - uint32_t(key);
-        const float z = float(col[v * a.class_stride]);
-        a.top_index[b * a.top + rank] = v;
-        a.top_logprob[b * a.top + rank] = lse == -kInf ? -kInf : z - lse;
+        a.top_index[b * a.top + rank] = UINT32_MAX - uint32_t(key);
+        a.top_logprob[b * a.top + rank] = lse == -kInf ? -kInf : value_of(uint32_t(key >> 32)) - lse;
     };
     if (room.count <= kKeys) {
         ranked<THREADS>(room.keys, int(room.count), k, write);
     } else if (w == 0) {
         TopList best;
-        for (int i = 0; i < found; ++i)
-            segment_keys<T, kEach>(a, col, UINT32_MAX - uint32_t(room.segs[i]), lane, least,
+        for (int i = 0; i < found; i += kAtOnce)
+            segment_keys<T, kEach>(a, col, room, i, found, lane,
                                    [&](uint64_t key) { best.offer(key, k, lane); });
         if (lane < k) write(best.key, lane);
     }
 }
 
+// A token's target and its logit, read ahead.
+struct Given {
+    int64_t target;
+    float z;
+};
+template <typename T> __device__ __forceinline__ Given given_of(const Args &a, int64_t b) {
+    const int64_t y = a.targets ? a.targets[b] : -1;
+    const int64_t at = y < 0 || y >= a.V ? 0 : y;
+    return {y, float(static_cast<const T *>(a.z)[b * a.token_stride + at * a.class_stride])};
+}
+
 // A token's results from its whole Stat, which every thread holds; its lse.
-template <typename T>
-__device__ __forceinline__ float write_token(const Args &a, int64_t b, Stat t) {
+__device__ __forceinline__ float write_token(const Args &a, int64_t b, Stat t, Given y) {
     const bool empty = t.m == -kInf && t.s == 0.0f;         // nothing but -inf
     const float logs = logf(t.s), lse = empty ? -kInf : t.m + logs;
     if (threadIdx.x == 0) {
-        const int64_t y = a.targets ? a.targets[b] : -1;
-        float lp = 0.0f;
-        if (y >= a.V) {
-            lp = __builtin_nanf("");
-        } else if (y >= 0) {
-            const float z = float(static_cast<const T *>(a.z)[b * a.token_stride + y * a.class_stride]);
-            lp = empty ? -kInf : z - lse;
-        }
+        float lp = empty ? -kInf : y.z - lse;
+        if (y.target < 0) lp = 0.0f;
+        if (y.target >= a.V) lp = __builtin_nanf("");
         a.logprob[b] = lp;
         a.entropy[b] = empty ? 0.0f : logs - t.u / t.s;
         a.lse[b] = lse;
@@ -246,12 +345,13 @@ __device__ __forceinline__ float write_token(const Args &a, int64_t b, Stat t) {
 
 // ---- token-major: a row's classes are contiguous --------------------------------------
 
-// grid (parts, B); each wave takes every kWaves-th run of 64 vectors of its part, four runs
-// together.  A run is a segment; the four's maximum is what the wave's sums run from.  A row
+// grid (parts, B); each wave takes every kWaves-th run of 64 vectors of its part, 16
+// values a lane together.  A run is a segment; the greatest value is what the wave's sums run
+// from.  A row
 // that is one part is finished here, its maxima kept in LDS.
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void rows_kernel(Args a) {
-    constexpr int V = kVec<T>, kWaves = THREADS / kWave, kRun = V * kWave, kAtOnce = 4;
+__global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 7) void rows_kernel(Args a) {
+    constexpr int V = kVec<T>, kWaves = THREADS / kWave, kRun = V * kWave, kAtOnce = 16 / V;
     __shared__ Stat stats[kWaves];
     __shared__ float held[kHeldMaxima];
     __shared__ TopRoom room;
@@ -262,29 +362,23 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(Args a) {
     int64_t end = begin + a.part_len;
     if (end > a.V) end = a.V;
     float *maxima = a.nparts == 1 ? held : a.maxima + b * a.nseg;
+    const Given given = a.nparts == 1 ? given_of<T>(a, b) : Given{};
     Sums t;
     for (int64_t v0 = begin + w * kRun; v0 < end; v0 += kAtOnce * kWaves * kRun) {
         float z[kAtOnce][V], m[kAtOnce];
-        if (v0 + ((kAtOnce - 1) * kWaves + 1) * kRun <= end) {
-            Loaded<T, V> x[kAtOnce];
+        {
+            Run<T, V> x[kAtOnce];
 #pragma unroll
-            for (int q = 0; q < kAtOnce; ++q) x[q] = load_vec<T, V>(row + v0 + q * (kWaves * kRun) + lane * V);
+            for (int q = 0; q < kAtOnce; ++q) x[q].load(row, v0 + q * (kWaves * kRun) + lane * V, end);
 #pragma unroll
             for (int q = 0; q < kAtOnce; ++q)
 #pragma unroll
-                for (int i = 0; i < V; ++i) z[q][i] = x[q][i];
-        } else {
+                for (int i = 0; i < V; ++i) z[q][i] = x[q].x[i];
+            if (v0 + ((kAtOnce - 1) * kWaves + 1) * kRun > end) {
 #pragma unroll
-            for (int q = 0; q < kAtOnce; ++q) {
-                const int64_t v = v0 + q * (kWaves * kRun) + lane * V;
-                if (v + V <= end) {
-                    const Loaded<T, V> x = load_vec<T, V>(row + v);
+                for (int q = 0; q < kAtOnce; ++q)
 #pragma unroll
-                    for (int i = 0; i < V; ++i) z[q][i] = x[i];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) z[q][i] = v + i < end ? float(row[v + i]) : -kInf;
-                }
+                    for (int i = 0; i < V; ++i) z[q][i] = i >= x[q].skip ? z[q][i] : -kInf;
             }
         }
 #pragma unroll
@@ -296,13 +390,20 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(Args a) {
         if (a.top) {
 #pragma unroll
             for (int q = 0; q < kAtOnce; ++q) m[q] = wave_max(m[q]);
-            t.raise(fmaxf(t.m, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))));
+            float all = m[0];
+#pragma unroll
+            for (int q = 1; q < kAtOnce; ++q) all = fmaxf(all, m[q]);
+            t.raise(fmaxf(t.m, all));
         } else {
-            const float all = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+            float all = m[0];
+#pragma unroll
+            for (int q = 1; q < kAtOnce; ++q) all = fmaxf(all, m[q]);
             if (__any(all > t.m)) t.raise(fmaxf(t.m, wave_max(all)));
         }
+        if (t.m != -kInf) {
 #pragma unroll
-        for (int q = 0; q < kAtOnce; ++q) t.add(z[q]);
+            for (int q = 0; q < kAtOnce; ++q) t.add(z[q]);
+        }
         // a NaN shows in s, or leaves no maximum: rare enough to look again
         if (__any(t.s != t.s) || t.m == -kInf) {
 #pragma unroll
@@ -322,25 +423,29 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(Args a) {
             }
         }
     }
-    Stat all = t.stat();
-    for (int d = 1; d < kWave; d <<= 1) all = join(all, shuffle_xor(all, d));
-    if (lane == 0) stats[w] = all;
+    // the wave's lanes share their maximum
+    if (lane == 0) stats[w].m = t.m;
+    const float sum = wave_sum(t.s), weighted = wave_sum(t.u);
+    if (lane == 0) {
+        stats[w].s = sum;
+        stats[w].u = weighted;
+    }
     __syncthreads();
-    all = stats[0];
-    for (int i = 1; i < kWaves; ++i) all = join(all, stats[i]);
+    const Stat none{-kInf, 0.0f, 0.0f};
+    const Stat all = join_lanes<16>(lane % 16 < kWaves ? stats[lane % 16] : none);
     if (a.nparts > 1) {
         if (threadIdx.x == 0) a.parts[b * a.nparts + part] = make_float4(all.m, all.s, all.u, 0.0f);
         return;
     }
-    const float lse = write_token<T>(a, b, all);
+    const float lse = write_token(a, b, all, given);
     if (a.top) write_top<T, V, THREADS>(a, b, held, lse, room);
 }
 
 // ---- feature-major: a class's tokens are contiguous -----------------------------------
 
 // grid (parts, token tiles of kLanes * V): a lane takes V tokens, kLanes of them a row of the
-// tile; a thread takes runs of kColRun classes, each a segment.  Tokens past the end: the last
-// V again (the same values are written twice).
+// tile; a thread takes runs of kColRun classes, each a segment.  A lane whose
+// tokens would pass the end reads the last V and leaves out what the lane before it has.
 template <typename T, int V, int kLanes>
 __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
     constexpr int kRows = kColThreads / kLanes;
@@ -348,9 +453,12 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
     const int tx = threadIdx.x % kLanes, ty = threadIdx.x / kLanes;
     const int64_t part = blockIdx.x, tile = a.first + blockIdx.y;
     int64_t b = (tile * kLanes + tx) * V;
-    const bool live = b < a.B;
-    if (b > a.B - V) b = a.B - V;
-    const T *z = static_cast<const T *>(a.z) + b;
+    int skip = 0;                                    // tokens that the lane before has
+    if (b > a.B - V) {
+        skip = b - (a.B - V) < V ? int(b - (a.B - V)) : V;
+        b = a.B - V;
+    }
+    const T *z = static_cast<const T *>(a.z) + (V == 1 ? b * a.token_stride : b);
     const int64_t begin = part * a.part_len;
     int64_t end = begin + a.part_len;
     if (end > a.V) end = a.V;
@@ -377,7 +485,7 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
                     top = fmaxf(top, y[r]);
                 }
                 t[j].raise(fmaxf(top, t[j].m));
-                t[j].add(y);
+                if (t[j].m != -kInf) t[j].add(y);
                 // a NaN shows in s, or leaves no maximum: rare enough to look again
                 if (t[j].s != t[j].s || top == -kInf) {
                     bool nan = m[j] != m[j];
@@ -390,7 +498,7 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if (a.top && live) a.maxima[(b + j) * a.nseg + v0 / kColRun] = m[j];
+            if (a.top && j >= skip) a.maxima[(b + j) * a.nseg + v0 / kColRun] = m[j];
         }
     }
 #pragma unroll
@@ -405,10 +513,9 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
         Stat all{sm[0][i], ss[0][i], su[0][i]};
         for (int r = 1; r < kRows; ++r) all = join(all, {sm[r][i], ss[r][i], su[r][i]});
         // where lane i / V has its tokens
-        const int64_t own = (tile * kLanes + i / V) * V;
-        if (own < a.B)
-            a.parts[((own > a.B - V ? a.B - V : own) + i % V) * a.nparts + part] =
-                make_float4(all.m, all.s, all.u, 0.0f);
+        const int64_t own = (tile * kLanes + i / V) * V, at = own > a.B - V ? a.B - V : own;
+        if (at + i % V >= own)
+            a.parts[(at + i % V) * a.nparts + part] = make_float4(all.m, all.s, all.u, 0.0f);
     }
 }
 
@@ -417,14 +524,13 @@ template <typename T, int kEach, int THREADS>
 __global__ __launch_bounds__(THREADS) void join_kernel(Args a) {
     __shared__ TopRoom room;
     const int64_t b = blockIdx.x;
+    const Given given = given_of<T>(a, b);
     Stat t{-kInf, 0.0f, 0.0f};
     for (int64_t i = lane_id(); i < a.nparts; i += kWave) {       // in every wave
         const float4 p = a.parts[b * a.nparts + i];
         t = join(t, {p.x, p.y, p.z});
     }
-    for (int d = 1; d < kWave; d <<= 1) t = join(t, shuffle_xor(t, d));
-    t = {lane_of(t.m, 0), lane_of(t.s, 0), lane_of(t.u, 0)};     // lanes differ in the last bits
-    const float lse = write_token<T>(a, b, t);
+    const float lse = write_token(a, b, join_lanes<kWave>(t), given);
     if (THREADS > kWave) write_top<T, kEach, THREADS>(a, b, a.maxima + b * a.nseg, lse, room);
 }
 
@@ -583,11 +689,12 @@ struct Cut {
     int64_t part_len, nparts, seg_len, nseg;
 };
 
-Cut cut_of(int dtype, int64_t V, int64_t B, bool rows) {
+Cut cut_of(int dtype, int64_t V, int64_t B, bool contiguous) {
     Cut c;
-    c.rows = rows;
     c.vec = dtype == DARB_F32 ? 4 : 8;
-    if (rows) {
+    // rows shorter than a vector go by columns, an element a lane
+    c.rows = contiguous && V >= c.vec;
+    if (c.rows) {
         c.lanes = 0;
         c.seg_len = c.vec * kWave;
         // a wave has at least four runs, or one where rows are few; a long row several parts
@@ -603,7 +710,7 @@ Cut cut_of(int dtype, int64_t V, int64_t B, bool rows) {
         if (parts < 1) parts = 1;
         c.part_len = (rounds + parts - 1) / parts * step;
     } else {
-        if (B < c.vec) c.vec = 1;
+        if (B < c.vec || contiguous) c.vec = 1;
         c.lanes = lanes_of(B, c.vec);
         c.seg_len = kColRun;
         const int64_t step = kColThreads / c.lanes * kColRun;       // one round of a workgroup
@@ -632,8 +739,8 @@ int64_t logprobs_max_top() { return kMaxTop; }
 int64_t logprobs_workspace_bytes(int64_t V, int64_t B, int64_t top) {
     int64_t parts = 0;
     for (int dtype : {int(DARB_F32), int(DARB_F16)})
-        for (bool rows : {false, true}) {
-            const Cut c = cut_of(dtype, V, B, rows);
+        for (bool contiguous : {false, true}) {
+            const Cut c = cut_of(dtype, V, B, contiguous);
             if (c.nparts > parts) parts = c.nparts;
         }
     return padded(parts * B * 16) + (top ? padded((V + kColRun - 1) / kColRun * B * 4) : 0);

@@ -31,7 +31,8 @@ struct MaxOp {  // a NaN is left out
 };
 
 // Over each aligned group of LANES (1 ... 64, a power of two) lanes; every lane of a group of
-// up to 16 gets the result, lane 63 that of 64, lanes 16 ... 31 and 48 ... 63 that of 32.
+// up to 16 gets the result (where x is a product its first addition may be fused, and lanes
+// differ in the last bit: take one lane's), lane 63 that of 64.
 template <int LANES, typename Op> __device__ __forceinline__ float group_reduce(float x) {
     if (LANES >= 2) x = Op::of(x, dpp<kDppXor1>(x, x));
     if (LANES >= 4) x = Op::of(x, dpp<kDppXor2>(x, x));
