@@ -198,23 +198,41 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
     for (int i = 0; i < kHeld; ++i)
 #pragma unroll
         for (int j = 0; j < V; ++j) sw[i][j] = sb[i][j] = 0.0f;
-    // the next token's rows are on their way while this one's sums cross the workgroup
+    // The next token's rows are on their way while this one's sums cross the workgroup.  Loads
+    // return in order: nothing that is needed sooner may be issued after them.
+    float held_w[kHeld][V];
+    if constexpr (N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            int skip;
+            const int64_t at = (int64_t(i) * blockDim.x + threadIdx.x) * V;
+            weights<T, V>(a, a.w, back_from_end<V>(at, a.H, skip), 1.0f, held_w[i]);
+        }
+    }
     Row<T, V, N> next_x, next_dy;
+    float next_mean, next_rstd;
     auto fetch = [&](int64_t b) {
+        next_mean = a.mean[b];
+        next_rstd = a.rstd[b];
         next_x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H);
         next_dy.open(static_cast<const T *>(a.dy.p) + b * a.dy.token, a.H);
     };
     fetch(blockIdx.x);
     for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
         Row<T, V, N> x = next_x, dy = next_dy;
+        const float mean = next_mean, rstd = next_rstd;
         if (b + gridDim.x < a.B) fetch(b + gridDim.x);
         T *dx = static_cast<T *>(a.y.p) + b * a.y.token;
-        const float mean = a.mean[b], rstd = a.rstd[b];
         float s[2] = {0.0f, 0.0f};
         x.each([&](int i, int64_t h, int skip, const Loaded<T, V> &v) {
             const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h);
             float w[V];
-            weights<T, V>(a, a.w, h, 1.0f, w);
+            if constexpr (N) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) w[j] = held_w[i][j];
+            } else {
+                weights<T, V>(a, a.w, h, 1.0f, w);
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const bool own = j >= skip;
@@ -240,7 +258,12 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
         x.each([&](int i, int64_t h, int skip, const Loaded<T, V> &v) {
             const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h);
             float w[V], out[V];
-            weights<T, V>(a, a.w, h, 1.0f, w);
+            if constexpr (N) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) w[j] = held_w[i][j];
+            } else {
+                weights<T, V>(a, a.w, h, 1.0f, w);
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float xh = (v[j] - mean) * rstd;
@@ -333,14 +356,26 @@ __device__ __forceinline__ T *out_row(const Matrix &m, int64_t i, int64_t h, int
     }
 }
 
+// x summed over the lanes of a wave that are equal modulo `lanes` (1, 2, 4 or 8): rotations
+// inside rows of 16, then rows and halves swapped and added.  (Lanes add in different orders.)
+__device__ __forceinline__ float sum_equal_lanes(float x, int lanes) {
+    constexpr int kRor8 = 0x128, kRor4 = 0x124;
+    if (lanes <= 1) x += dpp<kDppXor1>(x, x);
+    if (lanes <= 2) x += dpp<kDppXor2>(x, x);
+    if (lanes <= 4) x += dpp<kRor4>(x, x);
+    x += dpp<kRor8>(x, x);
+    auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
+    auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+}
+
 // s summed over the threads with the same tokens (lanes of them side by side), in each of them;
 // scratch: kMaxWaves * lanes * K floats.
 template <int K> __device__ __forceinline__ void tile_sum(float (&s)[K], int lanes, float *scratch) {
     const int waves = blockDim.x / kWave, w = threadIdx.x / kWave, lane = lane_id();
 #pragma unroll
-    for (int j = 0; j < K; ++j)
-        for (int d = lanes; d < kWave; d <<= 1) s[j] += __shfl_xor(s[j], d, kWave);
-    if (waves == 1) return;
+    for (int j = 0; j < K; ++j) s[j] = sum_equal_lanes(s[j], lanes);
     __syncthreads();                                 // the scratch's last use
     if (lane < lanes)
 #pragma unroll
@@ -364,10 +399,20 @@ __device__ __forceinline__ int64_t tile_of(int64_t i, int64_t tiles) {
 
 template <typename T, int V, int N>
 __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int lanes) {
+    constexpr int kHeld = N ? N : 1;
     __shared__ float scratch[kMaxWaves * kMaxLanes * V];
     const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes, rows = blockDim.x / lanes;
     int skip;
     const int64_t b = back_from_end<V>((tile_of(blockIdx.x, gridDim.x) * lanes + tx) * V, a.B, skip);
+    float w[kHeld], c[kHeld];
+    if constexpr (N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int64_t h = ty + int64_t(i) * rows < a.H ? ty + int64_t(i) * rows : 0;
+            w[i] = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
+            c[i] = a.b ? weight_at<T>(a, a.b, h) : 0.0f;
+        }
+    }
     Tile<T, V, N> x;
     x.open(a.x.p, b, a.H, a.x.feature, ty, rows);
     float mean[V], rstd[V];
@@ -393,10 +438,13 @@ __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int l
 #pragma unroll
     for (int j = 0; j < V; ++j) rstd[j] = 1.0f / sqrtf(rstd[j] / float(a.H) + a.eps);
     x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
-        const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f, c = a.b ? weight_at<T>(a, a.b, h) : 0.0f;
+        if constexpr (!N) {
+            w[i] = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
+            c[i] = a.b ? weight_at<T>(a, a.b, h) : 0.0f;
+        }
         float out[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = fmaf((v[j] - mean[j]) * rstd[j], w, c);
+        for (int j = 0; j < V; ++j) out[j] = fmaf((v[j] - mean[j]) * rstd[j], w[i], c[i]);
         store_own<T, V>(out_row<T, V, N>(a.y, i, h, ty, rows, b), skip, out);
     });
     if (ty == 0) {
@@ -424,6 +472,14 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a,
         for (int d = 1; d < lanes; d <<= 1) s += __shfl_xor(s, d, kWave);
         return s;
     };
+    float w[kHeld];
+    if constexpr (N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int64_t h = ty + int64_t(i) * rows < a.H ? ty + int64_t(i) * rows : 0;
+            w[i] = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
+        }
+    }
     for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         int skip;
         const int64_t b = back_from_end<V>((tile_of(tile, tiles) * lanes + tx) * V, a.B, skip);
@@ -439,11 +495,11 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a,
         }
         x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
             const Loaded<T, V> g = N ? dy.held[i] : dy.get(h);
-            const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
+            if constexpr (!N) w[i] = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
             float fw = 0.0f, fb = 0.0f;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float xh = (v[j] - mean[j]) * rstd[j], c = g[j] * w;
+                const float xh = (v[j] - mean[j]) * rstd[j], c = g[j] * w[i];
                 s[j] += c;
                 s[V + j] = fmaf(c, xh, s[V + j]);
                 fw = j >= skip ? fmaf(g[j], xh, fw) : fw;
@@ -471,12 +527,12 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a,
         for (int j = 0; j < 2 * V; ++j) s[j] /= float(a.H);
         x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
             const Loaded<T, V> g = N ? dy.held[i] : dy.get(h);
-            const float w = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
+            if constexpr (!N) w[i] = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
             float out[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const float xh = (v[j] - mean[j]) * rstd[j];
-                out[j] = rstd[j] * (g[j] * w - s[j] - xh * s[V + j]);
+                out[j] = rstd[j] * (g[j] * w[i] - s[j] - xh * s[V + j]);
             }
             store_own<T, V>(out_row<T, V, N>(a.y, i, h, ty, rows, b), skip, out);
         });
@@ -521,7 +577,8 @@ __global__ __launch_bounds__(kSumFeatures * kSumSlices) void sum_partials_kernel
     if (db) db[h] = b;
 }
 
-constexpr int kMaxBlocks = 256;         // rows of partial sums
+// Rows of partial sums, at most: token-major a workgroup a CU, feature-major as many as tiles.
+constexpr int kMaxRowBlocks = 256, kMaxTileBlocks = 512;
 
 int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -558,11 +615,11 @@ struct TileShape {
     int lanes, threads, n, vec;
 };
 
-TileShape tile_shape(int64_t H, int64_t B, int64_t stride, int vec, int threads, int most) {
+TileShape tile_shape(int64_t H, int64_t B, int64_t stride, int vec, int threads, int most, int tiles) {
     TileShape t;
     t.vec = B < vec ? 1 : vec;
     t.lanes = kMaxLanes;
-    while (t.lanes > 1 && up(B, int64_t(t.lanes) * t.vec) < 200) t.lanes /= 2;
+    while (t.lanes > 1 && up(B, int64_t(t.lanes) * t.vec) < tiles) t.lanes /= 2;
     const int64_t want = H * t.lanes;
     t.threads = threads;
     t.n = 2;
@@ -587,7 +644,7 @@ bool rows_of(int64_t H, int64_t feature) { return H == 1 || feature == 1; }
 }  // namespace
 
 int64_t layer_norm_workspace_bytes(int64_t H, int64_t B) {
-    const int64_t blocks = B < kMaxBlocks ? B : kMaxBlocks;
+    const int64_t blocks = B < kMaxTileBlocks ? B : kMaxTileBlocks;
     return 2 * padded(blocks * H * 4);
 }
 
@@ -611,7 +668,7 @@ hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const
                 return hipGetLastError();
             });
         }
-        const TileShape t = tile_shape(H, B, x_feature > y_feature ? x_feature : y_feature, kVec<T>, kMaxThreads, 8);
+        const TileShape t = tile_shape(H, B, x_feature > y_feature ? x_feature : y_feature, kVec<T>, kMaxThreads, 8, 200);
         return with_tile<8>(t, [&](auto n) {
             const dim3 grid(unsigned(up(B, int64_t(t.lanes) * t.vec)));
             if (t.vec == 1)
@@ -639,9 +696,10 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
         const bool rows = rows_of(H, x_feature);
         int64_t stride = x_feature > dy_feature ? x_feature : dy_feature;
         if (dx && dx_feature > stride) stride = dx_feature;
-        const TileShape t = tile_shape(H, B, stride, kVec<T>, kGradThreads, 16);
+        const TileShape t = tile_shape(H, B, stride, kVec<T>, kGradThreads, 16, 384);
         const int64_t tasks = rows ? B : up(B, int64_t(t.lanes) * t.vec);
-        const int blocks = tasks < kMaxBlocks ? int(tasks) : kMaxBlocks;
+        const int most = rows ? kMaxRowBlocks : kMaxTileBlocks;
+        const int blocks = tasks < most ? int(tasks) : most;
         if (dweight) a.dw = static_cast<float *>(workspace);
         if (dbias) a.db = reinterpret_cast<float *>(static_cast<char *>(workspace) + padded(blocks * H * 4));
         hipError_t e;
