@@ -106,6 +106,7 @@ template <typename T, int V, int N> struct Row {
     Loaded<T, V> held[N ? N : 1];
     const T *p;
     int64_t H;
+    int tid, threads;                   // the thread's place among a row's
 
     // f(vector's place in the thread, its first feature, elements to leave out, vector)
     template <typename F> __device__ __forceinline__ void each(F &&f) const {
@@ -113,13 +114,13 @@ template <typename T, int V, int N> struct Row {
         if constexpr (N) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int64_t at = (int64_t(i) * blockDim.x + threadIdx.x) * V;
+                const int64_t at = (int64_t(i) * threads + tid) * V;
                 if (at >= H) break;
                 const int64_t h = back_from_end<V>(at, H, skip);
                 f(i, h, skip, held[i]);
             }
         } else {
-            for (int64_t at = int64_t(threadIdx.x) * V; at < H; at += int64_t(blockDim.x) * V) {
+            for (int64_t at = int64_t(tid) * V; at < H; at += int64_t(threads) * V) {
                 const int64_t h = back_from_end<V>(at, H, skip);
                 f(0, h, skip, load_vec<T, V>(p + h));
             }
@@ -131,14 +132,16 @@ template <typename T, int V, int N> struct Row {
             for (int i = 0; i < N; ++i) forget_uses(held[i]);
         }
     }
-    __device__ __forceinline__ void open(const T *row, int64_t len) {
+    __device__ __forceinline__ void open(const T *row, int64_t len, int tid_, int threads_) {
         p = row;
         H = len;
+        tid = tid_;
+        threads = threads_;
         if constexpr (N) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 int skip;
-                const int64_t at = (int64_t(i) * blockDim.x + threadIdx.x) * V;
+                const int64_t at = (int64_t(i) * threads + tid) * V;
                 held[i] = load_vec<T, V>(p + back_from_end<V>(at, H, skip));
             }
         }
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_rows_kernel(Args a) {
     __shared__ float scratch[kMaxWaves];
     const int64_t b = blockIdx.x;
     Row<T, V, N> x;
-    x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H);
+    x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H, threadIdx.x, blockDim.x);
     T *y = static_cast<T *>(a.y.p) + b * a.y.token;
     float s[1] = {0.0f};
     x.each([&](int, int64_t, int skip, const Loaded<T, V> &v) {
@@ -185,12 +188,17 @@ __global__ __launch_bounds__(kMaxThreads) void norm_rows_kernel(Args a) {
     }
 }
 
-// The workgroup takes every gridDim.x-th token.  Held rows: dw and db sum in registers; longer
-// ones: in the workgroup's row of the workspace.
-template <typename T, int V, int N>
+// The workgroup takes every gridDim.x-th token, or, where a row is one wave's (TEAMS), each of
+// its waves a token of its own and no barrier.  Held rows: dw and db sum in registers (the teams'
+// then in LDS); longer ones: in the workgroup's row of the workspace.
+template <typename T, int V, int N, bool TEAMS>
 __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
     constexpr int kHeld = N ? N : 1;
     __shared__ float scratch[2 * kMaxWaves];
+    const int threads = TEAMS ? kWave : int(blockDim.x);           // of a row
+    const int tid = TEAMS ? threadIdx.x % kWave : threadIdx.x;
+    const int64_t team = TEAMS ? threadIdx.x / kWave : 0, teams = TEAMS ? blockDim.x / kWave : 1;
+    const int64_t first_b = blockIdx.x * teams + team, step = gridDim.x * teams;
     float *dw = a.dw ? a.dw + blockIdx.x * a.H : nullptr;
     float *db = a.db ? a.db + blockIdx.x * a.H : nullptr;
     float sw[kHeld][V], sb[kHeld][V];
@@ -205,7 +213,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             int skip;
-            const int64_t at = (int64_t(i) * blockDim.x + threadIdx.x) * V;
+            const int64_t at = (int64_t(i) * threads + tid) * V;
             weights<T, V>(a, a.w, back_from_end<V>(at, a.H, skip), 1.0f, held_w[i]);
         }
     }
@@ -214,14 +222,14 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
     auto fetch = [&](int64_t b) {
         next_mean = a.mean[b];
         next_rstd = a.rstd[b];
-        next_x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H);
-        next_dy.open(static_cast<const T *>(a.dy.p) + b * a.dy.token, a.H);
+        next_x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H, tid, threads);
+        next_dy.open(static_cast<const T *>(a.dy.p) + b * a.dy.token, a.H, tid, threads);
     };
-    fetch(blockIdx.x);
-    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
+    if (first_b < a.B) fetch(first_b);
+    for (int64_t b = first_b; b < a.B; b += step) {
         Row<T, V, N> x = next_x, dy = next_dy;
         const float mean = next_mean, rstd = next_rstd;
-        if (b + gridDim.x < a.B) fetch(b + gridDim.x);
+        if (b + step < a.B) fetch(b + step);
         T *dx = static_cast<T *>(a.y.p) + b * a.y.token;
         float s[2] = {0.0f, 0.0f};
         x.each([&](int i, int64_t h, int skip, const Loaded<T, V> &v) {
@@ -251,7 +259,12 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
             }
         });
         if (!a.y.p) continue;
-        block_sum(s, scratch);
+        if constexpr (TEAMS) {
+            s[0] = wave_sum(s[0]);
+            s[1] = wave_sum(s[1]);
+        } else {
+            block_sum(s, scratch);
+        }
         x.forget();
         dy.forget();
         const float m0 = s[0] / float(a.H), m1 = s[1] / float(a.H);
@@ -273,14 +286,34 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
         });
     }
     if constexpr (N) {
+        // team by team, in LDS; the last one's sums are the workgroup's
+        __shared__ float together[TEAMS ? 2 : 1][TEAMS ? N * V * kWave : 1];
+        for (int64_t turn = 0; turn < teams; ++turn) {
+            if (team == turn) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int64_t at = (int64_t(i) * blockDim.x + threadIdx.x) * V;
-            if (at >= a.H) break;
-            int skip;
-            const int64_t h = back_from_end<V>(at, a.H, skip);
-            if (dw) store_own<float, V>(dw + h, skip, sw[i]);
-            if (db) store_own<float, V>(db + h, skip, sb[i]);
+                for (int i = 0; i < N; ++i) {
+                    const int64_t at = (int64_t(i) * threads + tid) * V;
+                    if (at >= a.H) break;
+                    int skip;
+                    const int64_t h = back_from_end<V>(at, a.H, skip);
+                    if (TEAMS) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) {
+                            float &w = together[0][(i * V + j) * kWave + tid], &c = together[1][(i * V + j) * kWave + tid];
+                            if (turn > 0) {
+                                sw[i][j] += w;
+                                sb[i][j] += c;
+                            }
+                            w = sw[i][j];
+                            c = sb[i][j];
+                        }
+                    }
+                    if (turn + 1 < teams) continue;
+                    if (dw) store_own<float, V>(dw + h, skip, sw[i]);
+                    if (db) store_own<float, V>(db + h, skip, sb[i]);
+                }
+            }
+            if (TEAMS) __syncthreads();
         }
     }
 }
@@ -456,8 +489,9 @@ __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int l
     }
 }
 
+// Two workgroups share a CU where the registers suffice.
 template <typename T, int V, int N>
-__global__ __launch_bounds__(kGradThreads) void norm_grad_columns_kernel(Args a, int lanes) {
+__global__ __launch_bounds__(kGradThreads, N * V <= 32 ? 4 : 2) void norm_grad_columns_kernel(Args a, int lanes) {
     constexpr int kHeld = N ? N : 1;
     __shared__ float scratch[kMaxWaves * kMaxLanes * 2 * V];
     const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes, rows = blockDim.x / lanes;
@@ -584,14 +618,19 @@ int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// A token-major call: threads that hold a row, N vectors each (0: the row is too long).
+// Features of a thread up to which a wave takes a row of the gradient by itself.
+constexpr int kTeamFeatures = 16;
+
+// A token-major call: threads that hold a row, N vectors each (0: the row is too long); one wave
+// where it needs at most one_wave vectors a lane.
 struct RowShape {
     int threads, n;
 };
 
-RowShape row_shape(int64_t H, int vec, int most) {
+RowShape row_shape(int64_t H, int vec, int most, int one_wave) {
     if (H < vec) return {kWave, 1};                  // an element a thread
     const int64_t vectors = up(H, vec);
+    if (vectors <= kWave * one_wave) return {kWave, int(up(vectors, kWave))};
     for (int threads = 256; threads <= most; threads *= 2)
         for (int n = 1; n <= 4; ++n)
             if (up(up(vectors, n), kWave) * kWave <= threads)
@@ -657,7 +696,7 @@ hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const
     return with_type(xdtype, [&](auto type) {
         using T = decltype(type);
         if (rows_of(H, x_feature)) {
-            const RowShape r = row_shape(H, kVec<T>, kMaxThreads);
+            const RowShape r = row_shape(H, kVec<T>, kMaxThreads, 1);
             return with_row(r, [&](auto n) {
                 if (H < kVec<T>)
                     hipLaunchKernelGGL((norm_rows_kernel<T, 1, 1>), dim3(unsigned(B)),
@@ -697,21 +736,24 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
         int64_t stride = x_feature > dy_feature ? x_feature : dy_feature;
         if (dx && dx_feature > stride) stride = dx_feature;
         const TileShape t = tile_shape(H, B, stride, kVec<T>, kGradThreads, 16, 384);
-        const int64_t tasks = rows ? B : up(B, int64_t(t.lanes) * t.vec);
-        const int most = rows ? kMaxRowBlocks : kMaxTileBlocks;
+        const RowShape r = row_shape(H, kVec<T>, kGradThreads, kTeamFeatures / kVec<T>);
+        const bool teams = r.threads == kWave;
+        const int64_t tasks = rows ? teams ? up(B, kGradThreads / kWave) : B : up(B, int64_t(t.lanes) * t.vec);
+        const int most = rows && !teams ? kMaxRowBlocks : kMaxTileBlocks;
         const int blocks = tasks < most ? int(tasks) : most;
         if (dweight) a.dw = static_cast<float *>(workspace);
         if (dbias) a.db = reinterpret_cast<float *>(static_cast<char *>(workspace) + padded(blocks * H * 4));
         hipError_t e;
         if (rows) {
-            const RowShape r = row_shape(H, kVec<T>, kGradThreads);
+            const dim3 grid{unsigned(blocks)}, threads{unsigned(teams ? kGradThreads : r.threads)};
             e = with_row(r, [&](auto n) {
-                if (H < kVec<T>)
-                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, 1, 1>), dim3(unsigned(blocks)),
-                                       dim3(r.threads), 0, s, a);
+                constexpr int N = decltype(n)::value, VT = kVec<T>;
+                if (H < VT)
+                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, 1, 1, true>), grid, threads, 0, s, a);
+                else if (teams && N > 0 && N * VT <= kTeamFeatures)
+                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, VT, N && N * VT <= kTeamFeatures ? N : 1, true>), grid, threads, 0, s, a);
                 else
-                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, kVec<T>, decltype(n)::value>),
-                                       dim3(unsigned(blocks)), dim3(r.threads), 0, s, a);
+                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, VT, N, false>), grid, threads, 0, s, a);
                 return hipGetLastError();
             });
         } else {
