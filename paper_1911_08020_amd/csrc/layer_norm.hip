@@ -390,17 +390,14 @@ __device__ __forceinline__ T *out_row(const Matrix &m, int64_t i, int64_t h, int
 }
 
 // x summed over the lanes of a wave that are equal modulo `lanes` (1, 2, 4 or 8): rotations
-// inside rows of 16, then rows and halves swapped and added.  (Lanes add in different orders.)
+// inside rows of 16, then across the rows.  (Lanes add in different orders.)
 __device__ __forceinline__ float sum_equal_lanes(float x, int lanes) {
     constexpr int kRor8 = 0x128, kRor4 = 0x124;
     if (lanes <= 1) x += dpp<kDppXor1>(x, x);
     if (lanes <= 2) x += dpp<kDppXor2>(x, x);
     if (lanes <= 4) x += dpp<kRor4>(x, x);
     x += dpp<kRor8>(x, x);
-    auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
-    auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+    return sum_rows(x);
 }
 
 // s summed over the threads with the same tokens (lanes of them side by side), in each of them;
@@ -590,20 +587,39 @@ constexpr int kSumFeatures = 16, kSumSlices = 64;    // 64 bytes a row; many wor
 __global__ __launch_bounds__(kSumFeatures * kSumSlices) void sum_partials_kernel(
     const float *__restrict__ dw_parts, const float *__restrict__ db_parts, int64_t H, int blocks,
     float *__restrict__ dw, float *__restrict__ db) {
-    __shared__ float s[2][kSumSlices][kSumFeatures];
+    constexpr int kSumWaves = kSumFeatures * kSumSlices / kWave, kAtOnce = 4;
+    __shared__ float s[2][kSumWaves][kSumFeatures];
     const int f = threadIdx.x % kSumFeatures, slice = threadIdx.x / kSumFeatures;
-    const int64_t h = int64_t(blockIdx.x) * kSumFeatures + f;
+    const int64_t h = int64_t(blockIdx.x) * kSumFeatures + f, at = h < H ? h : H - 1;
     float w = 0.0f, b = 0.0f;
-    if (h < H)
-        for (int k = slice; k < blocks; k += kSumSlices) {
-            if (dw) w += dw_parts[k * H + h];
-            if (db) b += db_parts[k * H + h];
+    for (int k = slice; k < blocks; k += kSumSlices * kAtOnce) {
+        float x[kAtOnce], y[kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            const int row = k + q * kSumSlices, in = row < blocks ? row : blocks - 1;
+            x[q] = dw ? dw_parts[in * H + at] : 0.0f;
+            y[q] = db ? db_parts[in * H + at] : 0.0f;
         }
-    s[0][slice][f] = w;
-    s[1][slice][f] = b;
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            const bool live = k + q * kSumSlices < blocks;
+            w += live ? x[q] : 0.0f;
+            b += live ? y[q] : 0.0f;
+        }
+    }
+    // the wave's four slices, then the waves
+    w = sum_rows(w);
+    b = sum_rows(b);
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    if (lane < kSumFeatures) {
+        s[0][wave][lane] = w;
+        s[1][wave][lane] = b;
+    }
     __syncthreads();
-    if (slice != 0 || h >= H) return;
-    for (int k = 1; k < kSumSlices; ++k) {
+    if (threadIdx.x >= kSumFeatures || h >= H) return;
+    w = b = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kSumWaves; ++k) {
         w += s[0][k][f];
         b += s[1][k][f];
     }

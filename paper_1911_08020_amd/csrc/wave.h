@@ -51,6 +51,14 @@ __device__ __forceinline__ float lane_of(float x, int lane) {
 __device__ __forceinline__ float wave_sum(float x) { return lane_of(group_reduce<64, AddOp>(x), 63); }
 __device__ __forceinline__ float wave_max(float x) { return lane_of(group_reduce<64, MaxOp>(x), 63); }
 
+// x summed over the lanes that hold the same place in their rows of 16, in each of them.
+__device__ __forceinline__ float sum_rows(float x) {
+    const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+}
+
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) {
     auto of = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
     x = of(x, dpp<kDppXor1>(x, x));
