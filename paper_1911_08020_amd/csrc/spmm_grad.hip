@@ -9,6 +9,8 @@
 // index lists them by column: for every weight its row and slot, columns in ascending order,
 // a column's weights in storage order.  The index depends on the offsets alone; a program
 // that retrains the retained values keeps it as long as the mask.
+#include <type_traits>
+
 #include "darb_internal.h"
 #include "float_io.h"
 #include "wave.h"
@@ -173,45 +175,70 @@ struct GradArgs {
     int wdtype, xdtype;
 };
 
-__device__ __forceinline__ float value_at(const GradArgs &a, int64_t s) {
-    return a.wdtype == DARB_F32 ? static_cast<const float *>(a.values)[s]
-                                : float(static_cast<const half_t *>(a.values)[s]);
-}
+// The weight's row of dY from one of the lane's columns on, and its value.  32 bits of offset
+// (WIDE: 64) from bases that all lanes share.
+template <bool WIDE> struct Gather {
+    const GradArgs &a;
+    uint32_t ld;                        // bytes of a row of dY, below 2^24 as rows are
+    __device__ __forceinline__ const float *row(const Entry &e, int64_t col) const {
+        if (WIDE) return a.dY + int64_t(e.row) * a.ldy + col;
+        const uint32_t at = __umul24(e.row, ld) + uint32_t(col) * 4u;
+        return reinterpret_cast<const float *>(reinterpret_cast<const char *>(a.dY) + at);
+    }
+    __device__ __forceinline__ float value(const Entry &e) const {
+        const uint32_t s = e.slot;
+        if (a.wdtype == DARB_F32) return WIDE ? static_cast<const float *>(a.values)[s] : at32<float>(a.values, s);
+        return float(WIDE ? static_cast<const half_t *>(a.values)[s] : at32<half_t>(a.values, s));
+    }
+    template <typename T> __device__ __forceinline__ static T at32(const void *p, uint32_t i) {
+        return *reinterpret_cast<const T *>(static_cast<const char *>(p) + i * uint32_t(sizeof(T)));
+    }
+};
 
 // A workgroup takes kWaves / KS columns; KS waves share a column's weights.  LPE lanes take one
 // weight, V batch columns each, U times: a wave handles 64 / LPE weights at once and
 // LPE * V * U batch columns; a wider batch goes over the column's weights again for each such
-// tile, adding to dvalues.  A lane whose columns would pass the batch's end (RAGGED) takes the
-// last V instead and leaves those that the lane before has out of its part of the dot product.
-template <int LPE, int V, int U, int KS, bool RAGGED>
+// tile, adding to dvalues.  In the last tile a lane whose columns would pass the batch's end
+// takes the last V instead and leaves those that the lane before has out of its dot product.
+template <int LPE, int V, int U, int KS, bool WIDE>
 __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
     constexpr int kGroups = kWave / LPE;      // weights at once
-    constexpr int kAhead = U > 1 ? 2 : 4;     // steps whose gathers are in flight together
+    constexpr int kAhead = V * U >= 16 ? 2 : 4;     // steps whose gathers are in flight together
     constexpr int kCols = LPE * V;            // batch columns of one of the U parts
+    constexpr uint32_t kTurn = kGroups * kAhead;
     __shared__ float part[KS > 1 ? (KS - 1) * (kWaves / KS) : 1][KS > 1 ? kCols * U : 1];
     const int w = threadIdx.x / kWave, lane = lane_id();
     const int group = lane / LPE, in = lane % LPE;
-    const int64_t c = int64_t(blockIdx.x) * (kWaves / KS) + w / KS;
+    // Workgroups go to the 8 XCDs in turn, each with an L2 of its own, and a row's neighbouring
+    // slots lie in neighbouring columns: an XCD takes columns side by side, so that a cache line
+    // of values or of dvalues is its alone.
+    const int64_t xcd = blockIdx.x % 8, whole = gridDim.x / 8, more = gridDim.x % 8;
+    const int64_t block = xcd * whole + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const int64_t c = block * (kWaves / KS) + w / KS;
     const int share = w % KS;
     const bool has = c < a.N;
     uint32_t begin = 0, end = 0;
     if (has) {
-        begin = a.starts[c];
-        end = a.starts[c + 1];
+        begin = __builtin_amdgcn_readfirstlane(a.starts[c]);
+        end = __builtin_amdgcn_readfirstlane(a.starts[c + 1]);
     }
-    // the wave's share of the weights: whole steps of kGroups
-    const uint32_t steps = (end - begin + kGroups - 1) / kGroups;
-    const uint32_t from = begin + steps * share / KS * kGroups;
-    uint32_t to = begin + steps * (share + 1) / KS * kGroups;
-    if (to > end) to = end;
+    const Gather<WIDE> gather{a, uint32_t(a.ldy) * 4u};
+    // The waves take turns of kAhead steps, so that the waves of all columns, which hold rows in
+    // one order, go through the same part of dY at about the same time.
+    const uint32_t from = begin + share * kTurn;
+    auto entry_at = [&](uint32_t i0, int q) {
+        const uint32_t i = i0 + q * kGroups + group;
+        return a.entries[i < end ? i : end - 1];
+    };
     for (int64_t tile = 0; tile < a.B; tile += int64_t(kCols) * U) {
         float x[U][V], acc[U][V];
         int64_t col[U];
         int skip[U];
+        const bool ragged = tile + kCols * U > a.B;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t own = tile + u * kCols + in * V;
-            col[u] = !RAGGED || own + V <= a.B ? own : a.B - V;
+            col[u] = own + V <= a.B ? own : a.B - V;
             skip[u] = own - col[u] < V ? int(own - col[u]) : V;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -224,39 +251,56 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
                 }
             }
         }
-        for (uint32_t i0 = from; i0 < to; i0 += kGroups * kAhead) {
-            Entry e[kAhead];
-            bool live[kAhead];
+        // one turn; RAGGED: the batch may end in it, LAST: the weights may
+        auto turn = [&](uint32_t i0, const Entry (&e)[kAhead], auto is_ragged, auto is_last) {
+            constexpr bool RAGGED = decltype(is_ragged)::value, LAST = decltype(is_last)::value;
             float v[kAhead];
             Loaded<float, V> dy[kAhead][U];
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) {
-                const uint32_t i = i0 + q * kGroups + group;
-                live[q] = i < to;
-                e[q] = a.entries[live[q] ? i : to - 1];
-            }
-#pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
-                v[q] = a.dX && live[q] ? value_at(a, e[q].slot) : 0.0f;
+                v[q] = a.dX ? gather.value(e[q]) : 0.0f;
+                const float *row = gather.row(e[q], col[0]);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    dy[q][u] = load_vec<float, V>(a.dY + int64_t(e[q].row) * a.ldy + col[u]);
+                    dy[q][u] = load_vec<float, V>(RAGGED ? gather.row(e[q], col[u]) : row + u * kCols);
             }
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) {
+                const bool live = !LAST || i0 + q * kGroups + group < end;
                 float dot = 0.0f;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        if (live[q]) acc[u][i] = fmaf(v[q], dy[q][u][i], acc[u][i]);
+                        const float to = fmaf(v[q], dy[q][u][i], acc[u][i]);
+                        acc[u][i] = live ? to : acc[u][i];
                         if (!RAGGED || i >= skip[u]) dot = fmaf(x[u][i], dy[q][u][i], dot);
                     }
                 dot = group_reduce<LPE, AddOp>(dot);
-                if (a.dvalues && live[q] && in == 0)
-                    a.dvalues[e[q].slot] = tile == 0 ? dot : a.dvalues[e[q].slot] + dot;
+                if (a.dvalues && live && in == 0) {
+                    float *to = WIDE ? a.dvalues + e[q].slot
+                                     : reinterpret_cast<float *>(reinterpret_cast<char *>(a.dvalues) + e[q].slot * 4u);
+                    *to = tile == 0 ? dot : *to + dot;
+                }
             }
-        }
+        };
+        auto weights = [&](auto is_ragged) {
+            if (from >= end) return;
+            Entry next[kAhead], e[kAhead];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) next[q] = entry_at(from, q);
+            for (uint32_t i0 = from; i0 < end; i0 += kTurn * KS) {
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q) e[q] = next[q];
+                if (i0 + kTurn * KS < end)
+#pragma unroll
+                    for (int q = 0; q < kAhead; ++q) next[q] = entry_at(i0 + kTurn * KS, q);
+                if (i0 + kTurn <= end) turn(i0, e, is_ragged, std::false_type{});
+                else turn(i0, e, is_ragged, std::true_type{});
+            }
+        };
+        if (ragged) weights(std::true_type{});
+        else weights(std::false_type{});
         if (!a.dX) continue;
         // the groups' sums, then the waves', in a fixed order
 #pragma unroll
@@ -293,17 +337,25 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
     }
 }
 
-template <int LPE, int V, int U> hipError_t launch_grad_t(const GradArgs &a, hipStream_t s) {
-    constexpr int KS = 4;
-    const int64_t blocks = (a.N + kWaves / KS - 1) / (kWaves / KS);
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    if (a.B % (LPE * V) == 0)
-        hipLaunchKernelGGL((spmm_grad_kernel<LPE, V, U, KS, false>), dim3(unsigned(blocks)),
-                           dim3(kThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((spmm_grad_kernel<LPE, V, U, KS, true>), dim3(unsigned(blocks)),
-                           dim3(kThreads), 0, s, a);
-    return hipGetLastError();
+// Waves to a column: enough to fill the card, but no more than have a few turns each.
+template <int LPE, int V, int U> hipError_t launch_grad_t(const GradArgs &a, int64_t M, int64_t nnz, hipStream_t s) {
+    const int64_t turn = kWave / LPE * (V * U >= 16 ? 2 : 4);
+    int ks = 4;
+    while (ks > 1 && (a.N * ks / 2 >= 8192 || nnz / a.N < 2 * ks * turn)) ks /= 2;
+    // offsets of 32 bits, and a product of 24 bits each
+    const bool wide = M >= 1 << 24 || a.ldy >= 1 << 22 || M * a.ldy >= int64_t(1) << 30 || nnz >= 1 << 30;
+    auto launch = [&](auto share, auto is_wide) {
+        constexpr int KS = decltype(share)::value;
+        const int64_t blocks = (a.N + kWaves / KS - 1) / (kWaves / KS);
+        if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+        hipLaunchKernelGGL((spmm_grad_kernel<LPE, V, U, KS, decltype(is_wide)::value>),
+                           dim3(unsigned(blocks)), dim3(kThreads), 0, s, a);
+        return hipGetLastError();
+    };
+    if (wide) return launch(std::integral_constant<int, 1>{}, std::true_type{});
+    if (ks == 1) return launch(std::integral_constant<int, 1>{}, std::false_type{});
+    if (ks == 2) return launch(std::integral_constant<int, 2>{}, std::false_type{});
+    return launch(std::integral_constant<int, 4>{}, std::false_type{});
 }
 
 struct IndexParts {
@@ -350,16 +402,16 @@ hipError_t launch_spmm_grad(const darb_plan &p, const void *index, int wdtype, c
     const IndexParts x = parts_of(p, const_cast<void *>(index));
     const GradArgs a{x.starts, x.entries, values, X, dY, dvalues, dX,
                      p.N, B, ldx, ldy, lddx, wdtype, xdtype};
-    if (B == 1) return launch_grad_t<1, 1, 1>(a, s);
-    if (B < 4) return launch_grad_t<4, 1, 1>(a, s);
-    if (B == 4) return launch_grad_t<1, 4, 1>(a, s);
-    if (B <= 8) return launch_grad_t<2, 4, 1>(a, s);
-    if (B <= 16) return launch_grad_t<4, 4, 1>(a, s);
-    if (B <= 32) return launch_grad_t<8, 4, 1>(a, s);
-    if (B <= 64) return launch_grad_t<16, 4, 1>(a, s);
-    if (B <= 128) return launch_grad_t<16, 4, 2>(a, s);
-    if (B <= 192) return launch_grad_t<16, 4, 3>(a, s);
-    return launch_grad_t<16, 4, 4>(a, s);
+    if (B == 1) return launch_grad_t<1, 1, 1>(a, p.M, p.nnz, s);
+    if (B < 4) return launch_grad_t<4, 1, 1>(a, p.M, p.nnz, s);
+    if (B == 4) return launch_grad_t<1, 4, 1>(a, p.M, p.nnz, s);
+    if (B <= 8) return launch_grad_t<2, 4, 1>(a, p.M, p.nnz, s);
+    if (B <= 16) return launch_grad_t<4, 4, 1>(a, p.M, p.nnz, s);
+    if (B <= 32) return launch_grad_t<4, 4, 2>(a, p.M, p.nnz, s);
+    if (B <= 64) return launch_grad_t<8, 4, 2>(a, p.M, p.nnz, s);
+    if (B <= 128) return launch_grad_t<8, 4, 4>(a, p.M, p.nnz, s);
+    if (B <= 192) return launch_grad_t<16, 4, 3>(a, p.M, p.nnz, s);
+    return launch_grad_t<16, 4, 4>(a, p.M, p.nnz, s);
 }
 
 }  // namespace darb
