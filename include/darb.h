@@ -466,15 +466,19 @@ int darb_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, const voi
  *   dvalues   device fp32 [nnz], overwritten, or NULL
  *   dX        device fp32 [N x B], leading dimension lddx >= B, overwritten (a column that no
  *             row keeps: zeros), or NULL; not both NULL
+ *   workspace device, 256-byte aligned, >= darb_spmm_grad_workspace's bytes: none for a small
+ *             dY (then it may be NULL), at most 72 bytes a weight and 4 KiB a row
  * values may be NULL if dX is, X if dvalues is.
  * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_NOT_UPLOADED, DARB_E_WORKSPACE, DARB_E_HIP.
  */
 int darb_transpose_bytes(const darb_plan *plan, int64_t *bytes);
 int darb_transpose(const darb_plan *plan, const uint8_t *offsets, void *index,
                    int64_t index_bytes, void *stream);
+int darb_spmm_grad_workspace(const darb_plan *plan, int64_t B, int64_t *bytes);
 int darb_spmm_grad(const darb_plan *plan, const void *index, int wdtype, const void *values,
                    int xdtype, int64_t B, const void *X, int64_t ldx, const float *dY,
-                   int64_t ldy, float *dvalues, float *dX, int64_t lddx, void *stream);
+                   int64_t ldy, float *dvalues, float *dX, int64_t lddx, void *workspace,
+                   int64_t workspace_bytes, void *stream);
 
 /*
  * AdamW with decoupled weight decay over many tensors at once.  Step t >= 1:

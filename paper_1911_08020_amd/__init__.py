@@ -129,7 +129,8 @@ def _load_library():
                                   P, P, P, I64, P], I),
         "darb_transpose_bytes": ([P, ctypes.POINTER(I64)], I),
         "darb_transpose": ([P, P, P, I64, P], I),
-        "darb_spmm_grad": ([P, P, I, P, I, I64, P, I64, P, I64, P, P, I64, P], I),
+        "darb_spmm_grad_workspace": ([P, I64, ctypes.POINTER(I64)], I),
+        "darb_spmm_grad": ([P, P, I, P, I, I64, P, I64, P, I64, P, P, I64, P, I64, P], I),
         "darb_adamw_workspace": ([P, I64, ctypes.POINTER(I64)], I),
         "darb_adamw_create": ([P, I64, I, P, I64, P, ctypes.POINTER(P)], I),
         "darb_adamw_step": ([P, P, P, I64] + [ctypes.c_double] * 4 + [I64, P, ctypes.c_uint32, P], I),
@@ -157,7 +158,8 @@ EXPORTED = ("darb_plan_create", "darb_plan_create_counts", "darb_plan_device_wor
             "darb_quantize_i8", "darb_spmv_i8", "darb_spmm_i8", "darb_lstm_layer",
             "darb_lstm_workspace", "darb_token_logprobs_workspace", "darb_token_logprobs",
             "darb_token_logprobs_grad", "darb_layer_norm", "darb_layer_norm_workspace",
-            "darb_layer_norm_grad", "darb_transpose_bytes", "darb_transpose", "darb_spmm_grad",
+            "darb_layer_norm_grad", "darb_transpose_bytes", "darb_transpose",
+            "darb_spmm_grad_workspace", "darb_spmm_grad",
             "darb_adamw_workspace", "darb_adamw_create", "darb_adamw_step", "darb_adamw_moments",
             "darb_adamw_destroy", "darb_stream_read", "darb_stream_read_shape", "darb_stream_copy", "darb_strerror",
             "darb_last_error", "darb_version")
@@ -537,7 +539,7 @@ class Plan:
         return index
 
     def spmm_grad(self, index, values, X, dY, dvalues=None, dX=None, need_values=True,
-                  need_X=True, stream=None):
+                  need_X=True, workspace=None, stream=None):
         """(dvalues fp32 [nnz], dX fp32 [N, B]) of Y = W_darb X for dY fp32 [M, B]; None in the
         place of a gradient that is not needed (``values`` may then be None for dX, ``X`` for
         dvalues).  ``index``: ``transpose``'s of the format's offsets."""
@@ -574,11 +576,20 @@ class Plan:
                 dvalues = torch.empty(self.nnz, dtype=torch.float32, device=dY.device)
             _require_cuda(dvalues)
             _check_format(dvalues, self.nnz, "dvalues", (torch.float32,))
+        _check(_lib.darb_spmm_grad_workspace(self._h, B, ctypes.byref(need)),
+               "darb_spmm_grad_workspace")
+        if need.value:
+            if workspace is None:
+                workspace = torch.empty(need.value, dtype=torch.uint8, device=dY.device)
+            _require_cuda(workspace)
+            _check_format(workspace, need.value, "workspace", (torch.uint8,))
         _check(_lib.darb_spmm_grad(self._h, _ptr(index), wcode, _ptr(values) if need_X else None,
                                    xcode, B, _ptr(X) if need_values else None, ldx, _ptr(dY), ldy,
                                    _ptr(dvalues) if need_values else None,
-                                   _ptr(dX) if need_X else None, lddx, _stream_ptr(stream)),
-               "darb_spmm_grad")
+                                   _ptr(dX) if need_X else None, lddx,
+                                   None if workspace is None else _ptr(workspace),
+                                   0 if workspace is None else workspace.numel(),
+                                   _stream_ptr(stream)), "darb_spmm_grad")
         return (dvalues if need_values else None), (dX if need_X else None)
 
     # -- argument checks --------------------------------------------------------------

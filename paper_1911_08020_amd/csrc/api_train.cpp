@@ -289,9 +289,20 @@ int darb_transpose(const darb_plan *p, const uint8_t *offsets, void *index, int6
                     "transpose launch");
 }
 
+int darb_spmm_grad_workspace(const darb_plan *p, int64_t B, int64_t *bytes) {
+    clear_error();
+    if (!p || !bytes) return fail(DARB_E_INVALID, "NULL pointer");
+    if (B < 1 || B >= kMax) return fail(DARB_E_INVALID, "B must be in [1, 2^31)");
+    int rc = check_index(p);
+    if (rc) return rc;
+    *bytes = spmm_grad_workspace_bytes(*p, B);
+    return DARB_OK;
+}
+
 int darb_spmm_grad(const darb_plan *p, const void *index, int wdtype, const void *values,
                    int xdtype, int64_t B, const void *X, int64_t ldx, const float *dY,
-                   int64_t ldy, float *dvalues, float *dX, int64_t lddx, void *stream) {
+                   int64_t ldy, float *dvalues, float *dX, int64_t lddx, void *workspace,
+                   int64_t workspace_bytes, void *stream) {
     clear_error();
     int rc = check_uploaded(p);
     if (rc) return rc;
@@ -308,8 +319,10 @@ int darb_spmm_grad(const darb_plan *p, const void *index, int wdtype, const void
     if (B < 1 || B >= kMax) return fail(DARB_E_INVALID, "B must be in [1, 2^31)");
     if (ldy < B || (dvalues && ldx < B) || (dX && lddx < B))
         return fail(DARB_E_INVALID, "a leading dimension is below B");
+    const int64_t need = spmm_grad_workspace_bytes(*p, B);
+    if (need > 0 && (rc = check_workspace(workspace, workspace_bytes, need))) return rc;
     return launched(launch_spmm_grad(*p, index, wdtype, values, xdtype, B, X, ldx, dY, ldy,
-                                     dvalues, dX, lddx, static_cast<hipStream_t>(stream)),
+                                     dvalues, dX, lddx, workspace, static_cast<hipStream_t>(stream)),
                     "spmm gradient launch");
 }
 

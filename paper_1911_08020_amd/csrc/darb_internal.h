@@ -195,7 +195,9 @@ int64_t transpose_bytes(const darb_plan &p);
 hipError_t launch_transpose(const darb_plan &p, const uint8_t *offsets, void *index, hipStream_t s);
 hipError_t launch_spmm_grad(const darb_plan &p, const void *index, int wdtype, const void *values,
                             int xdtype, int64_t B, const void *X, int64_t ldx, const float *dY,
-                            int64_t ldy, float *dvalues, float *dX, int64_t lddx, hipStream_t s);
+                            int64_t ldy, float *dvalues, float *dX, int64_t lddx, void *workspace,
+                            hipStream_t s);
+int64_t spmm_grad_workspace_bytes(const darb_plan &p, int64_t B);
 // AdamW: the tensors' table and, for every tile of adam_tile_elements() elements, whose it is;
 // both in the caller's workspace.  A launch takes `count` (at most kAdamGrads, or half of it
 // for the moments) consecutive tensors, whose gradients' addresses travel with it.

@@ -22,6 +22,8 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kRange = 128;      // columns of one wave while the index is built: whole blocks
 constexpr int kScanThreads = 1024;
+// Elements of dY from which it is cut into tiles of the batch.
+constexpr int64_t kSplitFrom = (3 << 20) / 4;
 
 struct Entry {
     uint32_t row, slot;
@@ -164,6 +166,14 @@ __global__ __launch_bounds__(kThreads) void place_columns_kernel(
 
 // ---- the gradients --------------------------------------------------------------------
 
+// Workgroups go to the 8 XCDs in turn, each with an L2 of its own: the task of workgroup i of n
+// such that an XCD's tasks lie side by side.  A row's neighbouring slots lie in neighbouring
+// columns, so that a cache line of values or of dvalues belongs to one XCD.
+__device__ __forceinline__ int64_t side_by_side(uint32_t i, uint32_t n) {
+    const uint32_t xcd = i % 8, whole = n / 8, more = n % 8;
+    return int64_t(xcd) * whole + (xcd < more ? xcd : more) + i / 8;
+}
+
 struct GradArgs {
     const uint32_t *starts;
     const Entry *entries;
@@ -209,11 +219,7 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
     __shared__ float part[KS > 1 ? (KS - 1) * (kWaves / KS) : 1][KS > 1 ? kCols * U : 1];
     const int w = threadIdx.x / kWave, lane = lane_id();
     const int group = lane / LPE, in = lane % LPE;
-    // Workgroups go to the 8 XCDs in turn, each with an L2 of its own, and a row's neighbouring
-    // slots lie in neighbouring columns: an XCD takes columns side by side, so that a cache line
-    // of values or of dvalues is its alone.
-    const int64_t xcd = blockIdx.x % 8, whole = gridDim.x / 8, more = gridDim.x % 8;
-    const int64_t block = xcd * whole + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const int64_t block = side_by_side(blockIdx.x, gridDim.x);
     const int64_t c = block * (kWaves / KS) + w / KS;
     const int share = w % KS;
     const bool has = c < a.N;
@@ -338,10 +344,14 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
 }
 
 // Waves to a column: enough to fill the card, but no more than have a few turns each.
-template <int LPE, int V, int U> hipError_t launch_grad_t(const GradArgs &a, int64_t M, int64_t nnz, hipStream_t s) {
-    const int64_t turn = kWave / LPE * (V * U >= 16 ? 2 : 4);
+int waves_of(int64_t N, int64_t nnz, int64_t turn) {
     int ks = 4;
-    while (ks > 1 && (a.N * ks / 2 >= 8192 || nnz / a.N < 2 * ks * turn)) ks /= 2;
+    while (ks > 1 && (N * ks / 2 >= 8192 || nnz / N < 2 * ks * turn)) ks /= 2;
+    return ks;
+}
+
+template <int LPE, int V, int U> hipError_t launch_grad_t(const GradArgs &a, int64_t M, int64_t nnz, hipStream_t s) {
+    const int ks = waves_of(a.N, nnz, kWave / LPE * (V * U >= 16 ? 2 : 4));
     // offsets of 32 bits, and a product of 24 bits each
     const bool wide = M >= 1 << 24 || a.ldy >= 1 << 22 || M * a.ldy >= int64_t(1) << 30 || nnz >= 1 << 30;
     auto launch = [&](auto share, auto is_wide) {
@@ -356,6 +366,233 @@ template <int LPE, int V, int U> hipError_t launch_grad_t(const GradArgs &a, int
     if (ks == 1) return launch(std::integral_constant<int, 1>{}, std::false_type{});
     if (ks == 2) return launch(std::integral_constant<int, 2>{}, std::false_type{});
     return launch(std::integral_constant<int, 4>{}, std::false_type{});
+}
+
+// ---- a dY too large for the L2s --------------------------------------------------------
+//
+// Gathers of dY's rows run at the L2's rate only while what they gather from stays in an XCD's
+// 4 MB.  A larger dY is copied into tiles of 64 batch columns, [tile][M][64] (a row 256 aligned
+// bytes, zeros past the batch), the weights' values into the index' order beside their rows, and
+// each XCD goes through tile after tile.  A tile's part of dvalues lies in the index' order too;
+// the parts are added, slot by slot, at the end.
+
+constexpr int kSplitCols = 64;
+constexpr int kSplitTiles = 16;         // tiles of a launch, at most: what bounds the workspace
+
+struct Pair {
+    uint32_t row;
+    float value;
+};
+
+struct SplitArgs {
+    GradArgs g;
+    Pair *pairs;
+    float *tiles;                       // [tiles][M][kSplitCols]
+    float *parts;                       // [tiles][nnz]
+    int64_t M, nnz, first_tile;
+    uint32_t blocks;                    // workgroups of a tile
+};
+
+__global__ __launch_bounds__(kThreads) void pair_values_kernel(GradArgs a, int64_t nnz, Pair *__restrict__ pairs) {
+    const int64_t i = side_by_side(blockIdx.x, gridDim.x) * kThreads + threadIdx.x;
+    if (i >= nnz) return;
+    const Entry e = a.entries[i];
+    float v = 0.0f;
+    if (a.dX) v = a.wdtype == DARB_F32 ? static_cast<const float *>(a.values)[e.slot]
+                                       : float(static_cast<const half_t *>(a.values)[e.slot]);
+    pairs[i] = {e.row, v};
+}
+
+// grid.y: tiles; a thread copies four columns of a row.
+__global__ __launch_bounds__(kThreads) void tile_rows_kernel(SplitArgs a) {
+    constexpr int kPerRow = kSplitCols / 4;
+    const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x, r = i / kPerRow;
+    if (r >= a.M) return;
+    const int64_t c = (a.first_tile + blockIdx.y) * kSplitCols + i % kPerRow * 4;
+    const float *from = a.g.dY + r * a.g.ldy + c;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (c + 4 <= a.g.B) {
+        const Loaded<float, 4> v = load_vec<float, 4>(from);
+        x = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+        if (c < a.g.B) x.x = from[0];
+        if (c + 1 < a.g.B) x.y = from[1];
+        if (c + 2 < a.g.B) x.z = from[2];
+    }
+    reinterpret_cast<float4 *>(a.tiles)[(blockIdx.y * a.M + r) * kPerRow + i % kPerRow] = x;
+}
+
+// As spmm_grad_kernel with 8 lanes to a weight, 8 batch columns each.
+template <int KS>
+__global__ __launch_bounds__(kThreads) void split_grad_kernel(SplitArgs a) {
+    constexpr int LPE = 8, U = 2, V = 4, kGroups = kWave / LPE, kAhead = 4;
+    constexpr uint32_t kTurn = kGroups * kAhead;
+    __shared__ float part[KS > 1 ? (KS - 1) * (kWaves / KS) : 1][kSplitCols];
+    const int w = threadIdx.x / kWave, lane = lane_id(), group = lane / LPE, in = lane % LPE;
+    const int64_t task = side_by_side(blockIdx.x, gridDim.x);
+    const int64_t t = task / a.blocks, c = (task - t * a.blocks) * (kWaves / KS) + w / KS;
+    const int share = w % KS;
+    const bool has = c < a.g.N;
+    uint32_t begin = 0, end = 0;
+    if (has) {
+        begin = __builtin_amdgcn_readfirstlane(a.g.starts[c]);
+        end = __builtin_amdgcn_readfirstlane(a.g.starts[c + 1]);
+    }
+    const int64_t col0 = (a.first_tile + t) * kSplitCols + in * V;
+    float x[U][V], acc[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int64_t col = col0 + u * (LPE * V) + i;
+            acc[u][i] = x[u][i] = 0.0f;
+            if (has && a.parts && col < a.g.B)
+                x[u][i] = a.g.xdtype == DARB_F32 ? static_cast<const float *>(a.g.X)[c * a.g.ldx + col]
+                                                 : float(static_cast<const half_t *>(a.g.X)[c * a.g.ldx + col]);
+        }
+    const char *tile = reinterpret_cast<const char *>(a.tiles + t * a.M * kSplitCols);
+    float *parts = a.parts ? a.parts + t * a.nnz : nullptr;
+    const uint32_t from = begin + share * kTurn;
+    auto pair_at = [&](uint32_t i0, int q) {
+        const uint32_t i = i0 + q * kGroups + group;
+        return a.pairs[i < end ? i : end - 1];
+    };
+    auto turn = [&](uint32_t i0, const Pair (&e)[kAhead], auto is_last) {
+        constexpr bool LAST = decltype(is_last)::value;
+        Loaded<float, V> dy[kAhead][U];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const uint32_t at = (e[q].row << 8) + uint32_t(in) * 16u;       // rows below 2^24
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                dy[q][u] = load_vec<float, V>(reinterpret_cast<const float *>(tile + at) + u * (LPE * V));
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const uint32_t i = i0 + q * kGroups + group;
+            const bool live = !LAST || i < end;
+            float dot = 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float to = fmaf(e[q].value, dy[q][u][j], acc[u][j]);
+                    acc[u][j] = live ? to : acc[u][j];
+                    dot = fmaf(x[u][j], dy[q][u][j], dot);
+                }
+            dot = group_reduce<LPE, AddOp>(dot);
+            if (parts && live && in == 0) parts[i] = dot;
+        }
+    };
+    if (from < end) {
+        Pair next[kAhead], e[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) next[q] = pair_at(from, q);
+        for (uint32_t i0 = from; i0 < end; i0 += kTurn * KS) {
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) e[q] = next[q];
+            if (i0 + kTurn * KS < end)
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q) next[q] = pair_at(i0 + kTurn * KS, q);
+            if (i0 + kTurn <= end) turn(i0, e, std::false_type{});
+            else turn(i0, e, std::true_type{});
+        }
+    }
+    if (!a.g.dX) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float s = acc[u][j];
+            for (int d = LPE; d < kWave; d <<= 1) s += __shfl_xor(s, d, kWave);
+            acc[u][j] = s;
+        }
+    if constexpr (KS > 1) {
+        if (share > 0 && group == 0)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    part[(w / KS) * (KS - 1) + share - 1][u * (LPE * V) + in * V + j] = acc[u][j];
+        __syncthreads();
+        if (share == 0 && group == 0)
+            for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < V; ++j)
+                        acc[u][j] += part[(w / KS) * (KS - 1) + k][u * (LPE * V) + in * V + j];
+    }
+    if (has && share == 0 && group == 0)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t col = col0 + u * (LPE * V);
+            float *to = a.g.dX + c * a.g.lddx + col;
+            if (col + V <= a.g.B) {
+                store_vec<float, V>(to, acc[u]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (col + j < a.g.B) to[j] = acc[u][j];
+            }
+        }
+}
+
+// dvalues from the tiles' parts, added to what earlier tiles left where there were any.
+__global__ __launch_bounds__(kThreads) void sum_parts_kernel(const float *__restrict__ parts, int64_t nnz, int tiles,
+                                                             const Entry *__restrict__ entries, bool add,
+                                                             float *__restrict__ dvalues) {
+    const int64_t i = side_by_side(blockIdx.x, gridDim.x) * kThreads + threadIdx.x;
+    if (i >= nnz) return;
+    const uint32_t slot = entries[i].slot;
+    float s = add ? dvalues[slot] : 0.0f;
+#pragma unroll 4
+    for (int t = 0; t < tiles; ++t) s += parts[t * nnz + i];
+    dvalues[slot] = s;
+}
+
+bool is_split(int64_t M, int64_t B) { return B > kSplitCols && M < 1 << 24 && M * B > kSplitFrom; }
+
+struct SplitRoom {
+    int64_t tiles, pairs_at, tiles_at, parts_at, bytes;
+};
+
+SplitRoom split_room(const darb_plan &p, int64_t B) {
+    SplitRoom r;
+    r.tiles = (B + kSplitCols - 1) / kSplitCols;
+    const int64_t at_once = r.tiles < kSplitTiles ? r.tiles : kSplitTiles;
+    r.pairs_at = 0;
+    r.tiles_at = padded(p.nnz * int64_t(sizeof(Pair)));
+    r.parts_at = r.tiles_at + padded(at_once * p.M * kSplitCols * 4);
+    r.bytes = r.parts_at + padded(at_once * p.nnz * 4);
+    return r;
+}
+
+hipError_t launch_split(const darb_plan &p, const GradArgs &g, void *workspace, hipStream_t s) {
+    const SplitRoom r = split_room(p, g.B);
+    char *w = static_cast<char *>(workspace);
+    SplitArgs a{g, reinterpret_cast<Pair *>(w + r.pairs_at), reinterpret_cast<float *>(w + r.tiles_at),
+                g.dvalues ? reinterpret_cast<float *>(w + r.parts_at) : nullptr, p.M, p.nnz, 0, 0};
+    const dim3 each(unsigned((p.nnz + kThreads - 1) / kThreads));
+    hipLaunchKernelGGL(pair_values_kernel, each, dim3(kThreads), 0, s, g, p.nnz, a.pairs);
+    hipError_t e = hipGetLastError();
+    const int ks = waves_of(p.N, p.nnz, 32);
+    a.blocks = uint32_t((p.N + kWaves / ks - 1) / (kWaves / ks));
+    for (a.first_tile = 0; e == hipSuccess && a.first_tile < r.tiles; a.first_tile += kSplitTiles) {
+        const int64_t n = r.tiles - a.first_tile < kSplitTiles ? r.tiles - a.first_tile : kSplitTiles;
+        if (a.blocks * n > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+        const dim3 rows(unsigned((p.M * (kSplitCols / 4) + kThreads - 1) / kThreads), unsigned(n));
+        hipLaunchKernelGGL(tile_rows_kernel, rows, dim3(kThreads), 0, s, a);
+        const dim3 grid(unsigned(a.blocks * n));
+        if (ks == 1) hipLaunchKernelGGL((split_grad_kernel<1>), grid, dim3(kThreads), 0, s, a);
+        else if (ks == 2) hipLaunchKernelGGL((split_grad_kernel<2>), grid, dim3(kThreads), 0, s, a);
+        else hipLaunchKernelGGL((split_grad_kernel<4>), grid, dim3(kThreads), 0, s, a);
+        if (g.dvalues)
+            hipLaunchKernelGGL(sum_parts_kernel, each, dim3(kThreads), 0, s, a.parts, p.nnz, int(n),
+                               g.entries, a.first_tile > 0, g.dvalues);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 struct IndexParts {
@@ -396,12 +633,17 @@ hipError_t launch_transpose(const darb_plan &p, const uint8_t *offsets, void *in
     return hipGetLastError();
 }
 
+int64_t spmm_grad_workspace_bytes(const darb_plan &p, int64_t B) {
+    return is_split(p.M, B) ? split_room(p, B).bytes : 0;
+}
+
 hipError_t launch_spmm_grad(const darb_plan &p, const void *index, int wdtype, const void *values,
                             int xdtype, int64_t B, const void *X, int64_t ldx, const float *dY,
-                            int64_t ldy, float *dvalues, float *dX, int64_t lddx, hipStream_t s) {
+                            int64_t ldy, float *dvalues, float *dX, int64_t lddx, void *workspace,
+                            hipStream_t s) {
     const IndexParts x = parts_of(p, const_cast<void *>(index));
-    const GradArgs a{x.starts, x.entries, values, X, dY, dvalues, dX,
-                     p.N, B, ldx, ldy, lddx, wdtype, xdtype};
+    const GradArgs a{x.starts, x.entries, values, X, dY, dvalues, dX, p.N, B, ldx, ldy, lddx, wdtype, xdtype};
+    if (is_split(p.M, B)) return launch_split(p, a, workspace, s);
     if (B == 1) return launch_grad_t<1, 1, 1>(a, p.M, p.nnz, s);
     if (B < 4) return launch_grad_t<4, 1, 1>(a, p.M, p.nnz, s);
     if (B == 4) return launch_grad_t<1, 4, 1>(a, p.M, p.nnz, s);

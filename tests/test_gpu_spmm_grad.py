@@ -99,6 +99,28 @@ def test_spmm_grad_shapes_and_types(darb, M, N, bs, B, types):  # noqa: F811
     assert (host(dX)[empty] == 0).all()
 
 
+@pytest.mark.parametrize("M,N,bs,B", [(9000, 70, [16, 64], 97), (2100, 130, [4, 32], 1100), (12300, 40, [8], 65)])
+def test_spmm_grad_by_batch_tiles(darb, M, N, bs, B):  # noqa: F811
+    # a dY past the L2: tiles of 64 batch columns, whose dvalues are added up afterwards, more
+    # than 16 of them in several launches; a workspace whose contents do not matter
+    rng = np.random.default_rng(M)
+    plan, v, o, rows, cols = make(darb, rng, M, N, bs)
+    X, dY = rng.standard_normal((N, B)).astype(np.float32), rng.standard_normal((M, B)).astype(np.float32)
+    index = plan.transpose(o)
+    say(f"spmm_grad tiles {M}x{N} B={B}")
+    ws = torch.full((plan.nnz * 72 + plan.M * 4096 + 768,), 255, dtype=torch.uint8, device="cuda")
+    dv, dX = plan.spmm_grad(index, v, dev(X), dev(dY), workspace=ws)
+    wv, sv, wX, sX = want(rows, cols, host(v), X, dY, N)
+    compare(host(dv), wv, sv, 1e-5, "tiles dvalues")
+    compare(host(dX), wX, sX, 1e-5, "tiles dX")
+    dv2, none = plan.spmm_grad(index, None, dev(X), dev(dY), need_X=False)
+    assert torch.equal(dv, dv2)
+    none, dX2 = plan.spmm_grad(index, v, None, dev(dY), need_values=False)
+    assert torch.equal(dX, dX2)
+    with pytest.raises(ValueError):
+        plan.spmm_grad(index, v, dev(X), dev(dY), workspace=ws[:100])
+
+
 def test_spmm_grad_one_heavy_column(darb):  # noqa: F811
     # every row keeps the same column of each block: lists of M weights, and empty ones
     rng = np.random.default_rng(1)

@@ -83,8 +83,12 @@ def test_transpose_and_grad_refuse():
     assert L.darb_transpose_bytes(p.handle, ctypes.byref(n)) == 0 and n.value > 8 * p.nnz
     assert L.darb_transpose_bytes(None, ctypes.byref(n)) == darb.E_INVALID
     assert L.darb_transpose(p.handle, BUF, WS, BIG, None) == darb.E_NOT_UPLOADED
-    assert L.darb_spmm_grad(p.handle, WS, 0, BUF, 0, 4, BUF, 4, BUF, 4, BUF, BUF, 4, None) == darb.E_NOT_UPLOADED
-    assert L.darb_spmm_grad(None, WS, 0, BUF, 0, 4, BUF, 4, BUF, 4, BUF, BUF, 4, None) == darb.E_INVALID
+    assert L.darb_spmm_grad(p.handle, WS, 0, BUF, 0, 4, BUF, 4, BUF, 4, BUF, BUF, 4, WS, BIG,
+                            None) == darb.E_NOT_UPLOADED
+    assert L.darb_spmm_grad(None, WS, 0, BUF, 0, 4, BUF, 4, BUF, 4, BUF, BUF, 4, WS, BIG, None) == darb.E_INVALID
+    assert L.darb_spmm_grad_workspace(p.handle, 4, ctypes.byref(n)) == 0 and n.value == 0
+    assert L.darb_spmm_grad_workspace(p.handle, 1 << 20, ctypes.byref(n)) == 0 and 0 < n.value <= 72 * p.nnz + 4096 * p.M + 768
+    assert L.darb_spmm_grad_workspace(p.handle, 0, ctypes.byref(n)) == darb.E_INVALID
     # fewer than 2^31 weights: 2^25 rows of 64
     big = darb.Plan(1 << 25, 64, np.full(1 << 25, 1.0), 1.0, 0, 1, 1)
     assert L.darb_transpose_bytes(big.handle, ctypes.byref(n)) == darb.E_INVALID
