@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamTensor *__res
     const int gtype = (grads.type[local / 16] >> (local % 16 * 2)) & 3;
     const float gs = k.grad_scale ? *k.grad_scale : 1.0f;
     const float keep = float(1.0 - k.lr * t.decay);
-    const int w = threadIdx.x / kWave, lane = lane_id();
+    const int w = wave_id(), lane = lane_id();
     const int64_t first = int64_t(tile.index) * kTile;
     const uint32_t key = tile.tensor * 0xBB67AE85u + k.seed;
 #pragma unroll
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const AdamTensor *__r
     const AdamTile tile = tiles[blockIdx.x];
     const AdamTensor t = tensors[tile.tensor];
     float *om = out.m[tile.tensor - first_tensor], *ov = out.v[tile.tensor - first_tensor];
-    const int w = threadIdx.x / kWave, lane = lane_id();
+    const int w = wave_id(), lane = lane_id();
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
         const int64_t block = int64_t(tile.index) * (kTile / kAdamBlock) + r * (kThreads / kWave) + w;

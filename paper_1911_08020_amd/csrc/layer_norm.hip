@@ -62,7 +62,7 @@ __device__ __forceinline__ void weights(const Args &a, const void *w, int64_t h,
 
 // The workgroup's sum of s[0 .. N), each in every thread; scratch: N * kMaxWaves floats.
 template <int N> __device__ __forceinline__ void block_sum(float (&s)[N], float *scratch) {
-    const int waves = blockDim.x / kWave, w = threadIdx.x / kWave;
+    const int waves = blockDim.x / kWave, w = wave_id();
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
     if (waves == 1) return;
@@ -393,17 +393,17 @@ __device__ __forceinline__ T *out_row(const Matrix &m, int64_t i, int64_t h, int
 // inside rows of 16, then across the rows.  (Lanes add in different orders.)
 __device__ __forceinline__ float sum_equal_lanes(float x, int lanes) {
     constexpr int kRor8 = 0x128, kRor4 = 0x124;
-    if (lanes <= 1) x += dpp<kDppXor1>(x, x);
-    if (lanes <= 2) x += dpp<kDppXor2>(x, x);
-    if (lanes <= 4) x += dpp<kRor4>(x, x);
-    x += dpp<kRor8>(x, x);
+    if (lanes <= 1) x += dpp_all<kDppXor1>(x);
+    if (lanes <= 2) x += dpp_all<kDppXor2>(x);
+    if (lanes <= 4) x += dpp_all<kRor4>(x);
+    x += dpp_all<kRor8>(x);
     return sum_rows(x);
 }
 
 // s summed over the threads with the same tokens (lanes of them side by side), in each of them;
 // scratch: kMaxWaves * lanes * K floats.
 template <int K> __device__ __forceinline__ void tile_sum(float (&s)[K], int lanes, float *scratch) {
-    const int waves = blockDim.x / kWave, w = threadIdx.x / kWave, lane = lane_id();
+    const int waves = blockDim.x / kWave, w = wave_id(), lane = lane_id();
 #pragma unroll
     for (int j = 0; j < K; ++j) s[j] = sum_equal_lanes(s[j], lanes);
     __syncthreads();                                 // the scratch's last use

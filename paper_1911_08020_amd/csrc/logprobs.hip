@@ -271,7 +271,7 @@ template <typename T, int kEach, int THREADS>
 __device__ __forceinline__ void write_top(const Args &a, int64_t b, const float *maxima, float lse,
                                           TopRoom &room) {
     constexpr int kWaves = THREADS / kWave, kAtOnce = kEach == 1 ? kWave / kColRun : 1;
-    const int w = threadIdx.x / kWave, lane = lane_id(), k = int(a.top);
+    const int w = wave_id(), lane = lane_id(), k = int(a.top);
     if (w == 0) {
         const uint32_t bound = bound_of(maxima, a.nseg, k, lane);
         if (lane == 0) {
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 7) void rows_kernel(Ar
     __shared__ Stat stats[kWaves];
     __shared__ float held[kHeldMaxima];
     __shared__ TopRoom room;
-    const int w = threadIdx.x / kWave, lane = lane_id();
+    const int w = wave_id(), lane = lane_id();
     const int64_t b = a.first + blockIdx.y, part = blockIdx.x;
     const T *row = static_cast<const T *>(a.z) + b * a.token_stride;
     const int64_t begin = part * a.part_len;

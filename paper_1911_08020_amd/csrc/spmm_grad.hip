@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kThreads) void count_columns_kernel(
     const uint8_t *__restrict__ offsets, const int32_t *__restrict__ perm, BinTable bins,
     int64_t M, int64_t N, int64_t segments, int64_t tasks, uint32_t *__restrict__ counts) {
     __shared__ uint32_t cnt[kWaves][kRange];
-    const int w = threadIdx.x / kWave, lane = lane_id();
+    const int w = wave_id(), lane = lane_id();
     const int64_t task = int64_t(blockIdx.x) * kWaves + w;
     if (task >= tasks) return;                       // no barrier below
     const int64_t range = task / segments, seg = task - range * segments;
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(kThreads) void place_columns_kernel(
     int64_t M, int64_t N, int64_t segments, int64_t tasks, const uint32_t *__restrict__ counts,
     Entry *__restrict__ entries) {
     __shared__ uint32_t pos[kWaves][kRange];
-    const int w = threadIdx.x / kWave, lane = lane_id();
+    const int w = wave_id(), lane = lane_id();
     const int64_t task = int64_t(blockIdx.x) * kWaves + w;
     if (task >= tasks) return;                       // no barrier below
     const int64_t range = task / segments, seg = task - range * segments;
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
     constexpr int kCols = LPE * V;            // batch columns of one of the U parts
     constexpr uint32_t kTurn = kGroups * kAhead;
     __shared__ float part[KS > 1 ? (KS - 1) * (kWaves / KS) : 1][KS > 1 ? kCols * U : 1];
-    const int w = threadIdx.x / kWave, lane = lane_id();
+    const int w = wave_id(), lane = lane_id();
     const int group = lane / LPE, in = lane % LPE;
     const int64_t block = side_by_side(blockIdx.x, gridDim.x);
     const int64_t c = block * (kWaves / KS) + w / KS;
@@ -232,9 +232,18 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
     // The waves take turns of kAhead steps, so that the waves of all columns, which hold rows in
     // one order, go through the same part of dY at about the same time.
     const uint32_t from = begin + share * kTurn;
-    auto entry_at = [&](uint32_t i0, int q) {
-        const uint32_t i = i0 + q * kGroups + group;
-        return a.entries[i < end ? i : end - 1];
+    // a turn's entries; past the end the last one again
+    auto load_entries = [&](uint32_t i0, Entry (&e)[kAhead]) {
+        if (i0 + kTurn <= end) {
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) e[q] = (a.entries + i0)[q * kGroups + group];
+        } else {
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                const uint32_t i = i0 + q * kGroups + group;
+                e[q] = a.entries[i < end ? i : end - 1];
+            }
+        }
     };
     for (int64_t tile = 0; tile < a.B; tile += int64_t(kCols) * U) {
         float x[U][V], acc[U][V];
@@ -293,14 +302,11 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
         auto weights = [&](auto is_ragged) {
             if (from >= end) return;
             Entry next[kAhead], e[kAhead];
-#pragma unroll
-            for (int q = 0; q < kAhead; ++q) next[q] = entry_at(from, q);
+            load_entries(from, next);
             for (uint32_t i0 = from; i0 < end; i0 += kTurn * KS) {
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q) e[q] = next[q];
-                if (i0 + kTurn * KS < end)
-#pragma unroll
-                    for (int q = 0; q < kAhead; ++q) next[q] = entry_at(i0 + kTurn * KS, q);
+                if (i0 + kTurn * KS < end) load_entries(i0 + kTurn * KS, next);
                 if (i0 + kTurn <= end) turn(i0, e, is_ragged, std::false_type{});
                 else turn(i0, e, is_ragged, std::true_type{});
             }
@@ -428,7 +434,7 @@ __global__ __launch_bounds__(kThreads) void split_grad_kernel(SplitArgs a) {
     constexpr int LPE = 8, U = 2, V = 4, kGroups = kWave / LPE, kAhead = 4;
     constexpr uint32_t kTurn = kGroups * kAhead;
     __shared__ float part[KS > 1 ? (KS - 1) * (kWaves / KS) : 1][kSplitCols];
-    const int w = threadIdx.x / kWave, lane = lane_id(), group = lane / LPE, in = lane % LPE;
+    const int w = wave_id(), lane = lane_id(), group = lane / LPE, in = lane % LPE;
     const int64_t task = side_by_side(blockIdx.x, gridDim.x);
     const int64_t t = task / a.blocks, c = (task - t * a.blocks) * (kWaves / KS) + w / KS;
     const int share = w % KS;
@@ -453,9 +459,17 @@ __global__ __launch_bounds__(kThreads) void split_grad_kernel(SplitArgs a) {
     const char *tile = reinterpret_cast<const char *>(a.tiles + t * a.M * kSplitCols);
     float *parts = a.parts ? a.parts + t * a.nnz : nullptr;
     const uint32_t from = begin + share * kTurn;
-    auto pair_at = [&](uint32_t i0, int q) {
-        const uint32_t i = i0 + q * kGroups + group;
-        return a.pairs[i < end ? i : end - 1];
+    auto load_pairs = [&](uint32_t i0, Pair (&e)[kAhead]) {
+        if (i0 + kTurn <= end) {
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) e[q] = (a.pairs + i0)[q * kGroups + group];
+        } else {
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                const uint32_t i = i0 + q * kGroups + group;
+                e[q] = a.pairs[i < end ? i : end - 1];
+            }
+        }
     };
     auto turn = [&](uint32_t i0, const Pair (&e)[kAhead], auto is_last) {
         constexpr bool LAST = decltype(is_last)::value;
@@ -469,8 +483,7 @@ __global__ __launch_bounds__(kThreads) void split_grad_kernel(SplitArgs a) {
         }
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-            const uint32_t i = i0 + q * kGroups + group;
-            const bool live = !LAST || i < end;
+            const bool live = !LAST || i0 + q * kGroups + group < end;
             float dot = 0.0f;
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -481,19 +494,16 @@ __global__ __launch_bounds__(kThreads) void split_grad_kernel(SplitArgs a) {
                     dot = fmaf(x[u][j], dy[q][u][j], dot);
                 }
             dot = group_reduce<LPE, AddOp>(dot);
-            if (parts && live && in == 0) parts[i] = dot;
+            if (parts && live && in == 0) (parts + i0)[q * kGroups + group] = dot;
         }
     };
     if (from < end) {
         Pair next[kAhead], e[kAhead];
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q) next[q] = pair_at(from, q);
+        load_pairs(from, next);
         for (uint32_t i0 = from; i0 < end; i0 += kTurn * KS) {
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) e[q] = next[q];
-            if (i0 + kTurn * KS < end)
-#pragma unroll
-                for (int q = 0; q < kAhead; ++q) next[q] = pair_at(i0 + kTurn * KS, q);
+            if (i0 + kTurn * KS < end) load_pairs(i0 + kTurn * KS, next);
             if (i0 + kTurn <= end) turn(i0, e, std::false_type{});
             else turn(i0, e, std::true_type{});
         }

@@ -18,6 +18,14 @@ __device__ __forceinline__ uint32_t dpp(uint32_t x, uint32_t other) {
     return uint32_t(__builtin_amdgcn_update_dpp(int(other), int(x), CTRL, ROWS, 0xf, false));
 }
 
+// Patterns in which every lane has a source: the move folds into the operation that uses it.
+template <int CTRL> __device__ __forceinline__ float dpp_all(float x) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_all(uint32_t x) {
+    return uint32_t(__builtin_amdgcn_mov_dpp(int(x), CTRL, 0xf, 0xf, true));
+}
+
 constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140;
 constexpr int kDppBcast15 = 0x142, kDppBcast31 = 0x143;
 
@@ -34,10 +42,10 @@ struct MaxOp {  // a NaN is left out
 // up to 16 gets the result (where x is a product its first addition may be fused, and lanes
 // differ in the last bit: take one lane's), lane 63 that of 64.
 template <int LANES, typename Op> __device__ __forceinline__ float group_reduce(float x) {
-    if (LANES >= 2) x = Op::of(x, dpp<kDppXor1>(x, x));
-    if (LANES >= 4) x = Op::of(x, dpp<kDppXor2>(x, x));
-    if (LANES >= 8) x = Op::of(x, dpp<kDppHalfMirror>(x, x));
-    if (LANES >= 16) x = Op::of(x, dpp<kDppMirror>(x, x));
+    if (LANES >= 2) x = Op::of(x, dpp_all<kDppXor1>(x));
+    if (LANES >= 4) x = Op::of(x, dpp_all<kDppXor2>(x));
+    if (LANES >= 8) x = Op::of(x, dpp_all<kDppHalfMirror>(x));
+    if (LANES >= 16) x = Op::of(x, dpp_all<kDppMirror>(x));
     if (LANES >= 32) x = Op::of(x, dpp<kDppBcast15, 0xa>(x, Op::none()));
     if (LANES >= 64) x = Op::of(x, dpp<kDppBcast31, 0xc>(x, Op::none()));
     return x;
@@ -61,13 +69,18 @@ __device__ __forceinline__ float sum_rows(float x) {
 
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) {
     auto of = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-    x = of(x, dpp<kDppXor1>(x, x));
-    x = of(x, dpp<kDppXor2>(x, x));
-    x = of(x, dpp<kDppHalfMirror>(x, x));
-    x = of(x, dpp<kDppMirror>(x, x));
+    x = of(x, dpp_all<kDppXor1>(x));
+    x = of(x, dpp_all<kDppXor2>(x));
+    x = of(x, dpp_all<kDppHalfMirror>(x));
+    x = of(x, dpp_all<kDppMirror>(x));
     x = of(x, dpp<kDppBcast15, 0xa>(x, 0u));
     x = of(x, dpp<kDppBcast31, 0xc>(x, 0u));
     return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
+}
+
+// The wave's place in its workgroup, known to be the same in all lanes.
+__device__ __forceinline__ int wave_id() {
+    return __builtin_amdgcn_readfirstlane(int(threadIdx.x) / 64);
 }
 
 __device__ __forceinline__ int lane_id() {
