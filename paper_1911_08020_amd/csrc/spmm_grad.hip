@@ -459,16 +459,19 @@ __global__ __launch_bounds__(kThreads) void split_grad_kernel(SplitArgs a) {
     const char *tile = reinterpret_cast<const char *>(a.tiles + t * a.M * kSplitCols);
     float *parts = a.parts ? a.parts + t * a.nnz : nullptr;
     const uint32_t from = begin + share * kTurn;
-    auto load_pairs = [&](uint32_t i0, Pair (&e)[kAhead]) {
-        if (i0 + kTurn <= end) {
+    // A turn's weights, a lane each (past the end the last one again), which their groups then
+    // fetch through LDS: read from memory by all lanes of a group they would cost the L1 as much
+    // as the rows of dY.
+    static_assert(kTurn <= kWave, "a lane per weight");
+    auto load_pair = [&](uint32_t i0) {
+        const uint32_t i = i0 + lane % kTurn;
+        return a.pairs[i < end ? i : end - 1];
+    };
+    auto spread = [&](const Pair &mine, Pair (&e)[kAhead]) {
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) e[q] = (a.pairs + i0)[q * kGroups + group];
-        } else {
-#pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
-                const uint32_t i = i0 + q * kGroups + group;
-                e[q] = a.pairs[i < end ? i : end - 1];
-            }
+        for (int q = 0; q < kAhead; ++q) {
+            e[q].row = __shfl(mine.row, q * kGroups + group, kWave);
+            e[q].value = __shfl(mine.value, q * kGroups + group, kWave);
         }
     };
     auto turn = [&](uint32_t i0, const Pair (&e)[kAhead], auto is_last) {
@@ -498,12 +501,10 @@ __global__ __launch_bounds__(kThreads) void split_grad_kernel(SplitArgs a) {
         }
     };
     if (from < end) {
-        Pair next[kAhead], e[kAhead];
-        load_pairs(from, next);
+        Pair next = load_pair(from), e[kAhead];
         for (uint32_t i0 = from; i0 < end; i0 += kTurn * KS) {
-#pragma unroll
-            for (int q = 0; q < kAhead; ++q) e[q] = next[q];
-            if (i0 + kTurn * KS < end) load_pairs(i0 + kTurn * KS, next);
+            spread(next, e);
+            if (i0 + kTurn * KS < end) next = load_pair(i0 + kTurn * KS);
             if (i0 + kTurn <= end) turn(i0, e, std::false_type{});
             else turn(i0, e, std::true_type{});
         }
