@@ -232,16 +232,35 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
     // The waves take turns of kAhead steps, so that the waves of all columns, which hold rows in
     // one order, go through the same part of dY at about the same time.
     const uint32_t from = begin + share * kTurn;
-    // a turn's entries; past the end the last one again
-    auto load_entries = [&](uint32_t i0, Entry (&e)[kAhead]) {
-        if (i0 + kTurn <= end) {
+    // A turn's weights, past the end the last one again.  Where it has no more than a wave has
+    // lanes, each lane reads one and its value, and the groups fetch theirs through LDS: read from
+    // memory by all lanes of a group they would cost the L1 as much as the rows of dY.
+    constexpr bool kSpread = LPE > 1 && kTurn <= kWave;
+    struct Weights {
+        Entry e[kSpread ? 1 : kAhead];
+        float v[kSpread ? 1 : kAhead];
+    };
+    auto load_weights = [&](uint32_t i0, Weights &t) {
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) e[q] = (a.entries + i0)[q * kGroups + group];
-        } else {
+        for (int q = 0; q < (kSpread ? 1 : kAhead); ++q) {
+            const uint32_t i = kSpread ? i0 + lane % kTurn : i0 + q * kGroups + group;
+            t.e[q] = a.entries[i < end ? i : end - 1];
+        }
+    };
+    auto load_values = [&](Weights &t) {
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
-                const uint32_t i = i0 + q * kGroups + group;
-                e[q] = a.entries[i < end ? i : end - 1];
+        for (int q = 0; q < (kSpread ? 1 : kAhead); ++q) t.v[q] = a.dX ? gather.value(t.e[q]) : 0.0f;
+    };
+    auto spread = [&](const Weights &t, Entry (&e)[kAhead], float (&v)[kAhead]) {
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            if constexpr (kSpread) {
+                const int from_lane = q * kGroups + group;
+                e[q] = {__shfl(t.e[0].row, from_lane, kWave), __shfl(t.e[0].slot, from_lane, kWave)};
+                v[q] = __shfl(t.v[0], from_lane, kWave);
+            } else {
+                e[q] = t.e[q];
+                v[q] = t.v[q];
             }
         }
     };
@@ -267,13 +286,11 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
             }
         }
         // one turn; RAGGED: the batch may end in it, LAST: the weights may
-        auto turn = [&](uint32_t i0, const Entry (&e)[kAhead], auto is_ragged, auto is_last) {
+        auto turn = [&](uint32_t i0, const Entry (&e)[kAhead], const float (&v)[kAhead], auto is_ragged, auto is_last) {
             constexpr bool RAGGED = decltype(is_ragged)::value, LAST = decltype(is_last)::value;
-            float v[kAhead];
             Loaded<float, V> dy[kAhead][U];
 #pragma unroll
             for (int q = 0; q < kAhead; ++q) {
-                v[q] = a.dX ? gather.value(e[q]) : 0.0f;
                 const float *row = gather.row(e[q], col[0]);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -301,14 +318,17 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
         };
         auto weights = [&](auto is_ragged) {
             if (from >= end) return;
-            Entry next[kAhead], e[kAhead];
-            load_entries(from, next);
+            Entry e[kAhead];
+            float v[kAhead];
+            Weights next;
+            load_weights(from, next);
+            load_values(next);
             for (uint32_t i0 = from; i0 < end; i0 += kTurn * KS) {
-#pragma unroll
-                for (int q = 0; q < kAhead; ++q) e[q] = next[q];
-                if (i0 + kTurn * KS < end) load_entries(i0 + kTurn * KS, next);
-                if (i0 + kTurn <= end) turn(i0, e, is_ragged, std::false_type{});
-                else turn(i0, e, is_ragged, std::true_type{});
+                spread(next, e, v);
+                if (i0 + kTurn * KS < end) load_weights(i0 + kTurn * KS, next);
+                if (i0 + kTurn <= end) turn(i0, e, v, is_ragged, std::false_type{});
+                else turn(i0, e, v, is_ragged, std::true_type{});
+                if (i0 + kTurn * KS < end) load_values(next);
             }
         };
         if (ragged) weights(std::true_type{});
