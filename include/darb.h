@@ -386,10 +386,12 @@ int darb_lstm_workspace(int64_t H, int64_t T, int64_t batch, int64_t *floats);
  *   top          0 ... 64, at most V
  *   logprob, entropy, lse      device fp32 [B]
  *   top_logprob  device fp32 [B x top]; top_index device int64 [B x top] (NULL if top is 0)
- *   workspace    device, 256-byte aligned, >= darb_token_logprobs_workspace's bytes
+ *   workspace    device, 256-byte aligned, >= darb_token_logprobs_workspace's bytes; NULL
+ *                where those are 0 (rows that one workgroup reads)
  * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_WORKSPACE, DARB_E_HIP.
  */
-int darb_token_logprobs_workspace(int64_t V, int64_t B, int64_t top, int64_t *bytes);
+int darb_token_logprobs_workspace(int zdtype, int64_t V, int64_t B, int64_t z_feature_stride,
+                                  int64_t z_batch_stride, int64_t top, int64_t *bytes);
 int darb_token_logprobs(int zdtype, int64_t V, int64_t B, const void *z, int64_t z_feature_stride,
                         int64_t z_batch_stride, const int64_t *targets, int64_t top,
                         float *logprob, float *entropy, float *lse, float *top_logprob,

@@ -119,7 +119,7 @@ def _load_library():
         "darb_spmm_i8": ([P, P, P, P, P, I, I64, P, I64, P, I64, P], I),
         "darb_lstm_layer": ([P, P, P, P, P, P, I, I64, I64, I64, P, P, P, P, P, I64, P], I),
         "darb_lstm_workspace": ([I64, I64, I64, ctypes.POINTER(I64)], I),
-        "darb_token_logprobs_workspace": ([I64, I64, I64, ctypes.POINTER(I64)], I),
+        "darb_token_logprobs_workspace": ([I, I64, I64, I64, I64, I64, ctypes.POINTER(I64)], I),
         "darb_token_logprobs": ([I, I64, I64, P, I64, I64, P, I64, P, P, P, P, P, P, I64, P], I),
         "darb_token_logprobs_grad": ([I, I64, I64, P, I64, I64, P, P, P, P, P, P, I64, I64, P], I),
         "darb_layer_norm": ([I, I, I64, I64, P, I64, I64, P, P, ctypes.c_double, P, I64, I64, P,
@@ -543,6 +543,10 @@ class Plan:
         """(dvalues fp32 [nnz], dX fp32 [N, B]) of Y = W_darb X for dY fp32 [M, B]; None in the
         place of a gradient that is not needed (``values`` may then be None for dX, ``X`` for
         dvalues).  ``index``: ``transpose``'s of the format's offsets."""
+        if need_values and need_X and dvalues is None and dX is None and workspace is None:
+            done = _native.spmm_grad(self._ref, index, values, X, dY, stream)
+            if done is not None:
+                return done
         torch = _torch()
         _require_cuda(index, dY)
         need = ctypes.c_int64()

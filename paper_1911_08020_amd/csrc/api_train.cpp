@@ -131,14 +131,23 @@ using namespace darb;
 
 extern "C" {
 
-int darb_token_logprobs_workspace(int64_t V, int64_t B, int64_t top, int64_t *bytes) {
-    clear_error();
-    if (!bytes) return fail(DARB_E_INVALID, "bytes is NULL");
+static int check_logits(int zdtype, int64_t V, int64_t B, int64_t top, Strides *s) {
     int rc = check_sizes(V, B, "V");
     if (rc) return rc;
+    if (!float_dtype(zdtype)) return fail(DARB_E_DTYPE, "unknown logit dtype");
     if (top < 0 || top > logprobs_max_top() || top > V)
         return fail(DARB_E_INVALID, "top must be in [0, 64] and at most V");
-    *bytes = logprobs_workspace_bytes(V, B, top);
+    return common_order(s, 1, V, B, "z");
+}
+
+int darb_token_logprobs_workspace(int zdtype, int64_t V, int64_t B, int64_t z_feature_stride,
+                                  int64_t z_batch_stride, int64_t top, int64_t *bytes) {
+    clear_error();
+    if (!bytes) return fail(DARB_E_INVALID, "bytes is NULL");
+    Strides s[1] = {{z_feature_stride, z_batch_stride}};
+    int rc = check_logits(zdtype, V, B, top, s);
+    if (rc) return rc;
+    *bytes = logprobs_workspace_bytes(zdtype, V, B, s[0].feature, top);
     return DARB_OK;
 }
 
@@ -148,20 +157,15 @@ int darb_token_logprobs(int zdtype, int64_t V, int64_t B, const void *z, int64_t
                         int64_t *top_index, void *workspace, int64_t workspace_bytes,
                         void *stream) {
     clear_error();
-    int rc = check_sizes(V, B, "V");
+    Strides s[1] = {{z_feature_stride, z_batch_stride}};
+    int rc = check_logits(zdtype, V, B, top, s);
     if (rc) return rc;
-    if (!float_dtype(zdtype)) return fail(DARB_E_DTYPE, "unknown logit dtype");
-    if (top < 0 || top > logprobs_max_top() || top > V)
-        return fail(DARB_E_INVALID, "top must be in [0, 64] and at most V");
     if (!z || !logprob || !entropy || !lse || (top && (!top_logprob || !top_index)))
         return fail(DARB_E_INVALID, "NULL buffer");
     if (!aligned(z, size_of(zdtype)) || !aligned(targets, 8) || !aligned(top_index, 8))
         return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
-    Strides s[1] = {{z_feature_stride, z_batch_stride}};
-    rc = common_order(s, 1, V, B, "z");
-    if (rc) return rc;
-    rc = check_workspace(workspace, workspace_bytes, logprobs_workspace_bytes(V, B, top));
-    if (rc) return rc;
+    const int64_t need = logprobs_workspace_bytes(zdtype, V, B, s[0].feature, top);
+    if (need > 0 && (rc = check_workspace(workspace, workspace_bytes, need))) return rc;
     return launched(launch_logprobs(zdtype, V, B, z, s[0].feature, s[0].batch, targets, top,
                                     logprob, entropy, lse, top_logprob, top_index, workspace,
                                     static_cast<hipStream_t>(stream)), "token logprobs launch");

@@ -168,7 +168,7 @@ hipError_t launch_plan_device(int64_t M, int64_t N, const int64_t *counts, int64
 // Log probabilities and their gradient.  One of the strides of z is 1 (the class stride, or
 // else the token stride), and dz's is the same one; V = 1 and B = 1 go either way.
 int64_t logprobs_max_top();
-int64_t logprobs_workspace_bytes(int64_t V, int64_t B, int64_t top);
+int64_t logprobs_workspace_bytes(int dtype, int64_t V, int64_t B, int64_t class_stride, int64_t top);
 hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64_t class_stride,
                            int64_t token_stride, const int64_t *targets, int64_t top,
                            float *logprob, float *entropy, float *lse, float *top_logprob,

@@ -735,15 +735,11 @@ int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 int64_t logprobs_max_top() { return kMaxTop; }
 
-// Enough for either order and every type.
-int64_t logprobs_workspace_bytes(int64_t V, int64_t B, int64_t top) {
-    int64_t parts = 0;
-    for (int dtype : {int(DARB_F32), int(DARB_F16)})
-        for (bool contiguous : {false, true}) {
-            const Cut c = cut_of(dtype, V, B, contiguous);
-            if (c.nparts > parts) parts = c.nparts;
-        }
-    return padded(parts * B * 16) + (top ? padded((V + kColRun - 1) / kColRun * B * 4) : 0);
+// The parts of every token, and the segments' maxima; nothing where a workgroup finishes a row.
+int64_t logprobs_workspace_bytes(int dtype, int64_t V, int64_t B, int64_t class_stride, int64_t top) {
+    const Cut c = cut_of(dtype, V, B, rows_of(V, class_stride));
+    if (c.rows && c.nparts == 1) return 0;
+    return padded(c.nparts * B * 16) + (top ? padded(c.nseg * B * 4) : 0);
 }
 
 hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64_t class_stride,

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple, Optional
 
-from . import (BF16, F16, F32, _AdamTensor, _check, _check_format, _lib, _ptr, _require_cuda,
+from . import (BF16, F16, F32, _AdamTensor, _check, _check_format, _lib, _native, _ptr,
                _stream_ptr, _torch)
 
 
@@ -20,6 +20,16 @@ class TokenLogprobs(NamedTuple):
     lse: object                         # fp32 [B]
     top_logprob: Optional[object]       # fp32 [B, top], greatest first
     top_index: Optional[object]         # int64 [B, top]
+
+
+def _require_cuda(*ts):
+    torch = _torch()
+    for t in ts:
+        if not t.is_cuda:
+            raise ValueError("device tensors required (torch cuda tensors)")
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor is on {t.device}, the current device is "
+                             f"cuda:{torch.cuda.current_device()}")
 
 
 def _float_code(t, name: str) -> int:
@@ -73,6 +83,8 @@ def _workspace(fn, where: str, device, workspace, *sizes):
     need = ctypes.c_int64()
     _check(fn(*sizes, ctypes.byref(need)), where)
     if workspace is None:
+        if need.value == 0:
+            return None
         workspace = torch.empty(need.value, dtype=torch.uint8, device=device)
     _require_cuda(workspace)
     _check_format(workspace, need.value, "workspace", (torch.uint8,))
@@ -87,6 +99,10 @@ def token_logprobs(logits, targets=None, top: int = 0, workspace=None, stream=No
     ``targets``: int64 [B]; a negative one means that the column has none (logprob 0).  See
     darb_token_logprobs in include/darb.h for masked logits (-inf), NaN and refused values.
     """
+    if workspace is None:
+        done = _native.token_logprobs(logits, targets, top, stream)
+        if done is not None:
+            return TokenLogprobs(*done)
     torch = _torch()
     _require_cuda(logits)
     code = _float_code(logits, "logits")
@@ -96,7 +112,7 @@ def token_logprobs(logits, targets=None, top: int = 0, workspace=None, stream=No
     dev = logits.device
     tp = _optional(targets, B, "targets", torch.int64)
     workspace = _workspace(_lib.darb_token_logprobs_workspace, "darb_token_logprobs_workspace",
-                           dev, workspace, V, B, top)
+                           dev, workspace, code, V, B, fs, bs, top)
     out = torch.empty((3, B), dtype=torch.float32, device=dev)
     tl = torch.empty((B, top), dtype=torch.float32, device=dev) if top else None
     ti = torch.empty((B, top), dtype=torch.int64, device=dev) if top else None
@@ -104,8 +120,10 @@ def token_logprobs(logits, targets=None, top: int = 0, workspace=None, stream=No
     _check(_lib.darb_token_logprobs(code, V, B, _ptr(logits), fs, bs, tp, top,
                                     ctypes.c_void_p(base), ctypes.c_void_p(base + 4 * B),
                                     ctypes.c_void_p(base + 8 * B), _ptr(tl) if top else None,
-                                    _ptr(ti) if top else None, _ptr(workspace),
-                                    workspace.numel(), _stream_ptr(stream)),
+                                    _ptr(ti) if top else None,
+                                    None if workspace is None else _ptr(workspace),
+                                    0 if workspace is None else workspace.numel(),
+                                    _stream_ptr(stream)),
            "darb_token_logprobs")
     return TokenLogprobs(out[0], out[1], out[2], tl, ti)
 
@@ -114,6 +132,10 @@ def token_logprobs_grad(logits, targets, lse, grad_logprob=None, entropy=None, g
                         out=None, stream=None):
     """The gradient by the logits of sum(grad_logprob * logprob + grad_entropy * entropy), from
     ``token_logprobs``' lse (and entropy).  ``out`` may be ``logits`` itself."""
+    done = _native.token_logprobs_grad(logits, targets, lse, grad_logprob, entropy, grad_entropy,
+                                       out, stream)
+    if done is not None:
+        return done
     torch = _torch()
     _require_cuda(logits)
     code = _float_code(logits, "logits")
@@ -144,6 +166,9 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=None, 
                stream=None):
     """(y, mean, rstd): layer norm over the features of x [H, B] (fp32, fp16 or bf16), with
     weight and bias [H] in fp32 or x's type; mean and rstd fp32 [B].  ``y`` may be x."""
+    done = _native.layer_norm(x, weight, bias, eps, y, mean, rstd, stream)
+    if done is not None:
+        return done
     torch = _torch()
     _require_cuda(x)
     code = _float_code(x, "x")
@@ -173,6 +198,10 @@ def layer_norm_grad(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias
                     need_x: bool = True, need_params: bool = True, workspace=None, stream=None):
     """(dx, dweight, dbias) of ``layer_norm`` from dy and x [H, B] and its mean and rstd; dweight
     and dbias are fp32 [H].  None in the place of what is not needed.  ``dx`` may be dy or x."""
+    if need_x and need_params and dx is dweight is dbias is workspace is None:
+        done = _native.layer_norm_grad(dy, x, mean, rstd, weight, stream)
+        if done is not None:
+            return done
     torch = _torch()
     _require_cuda(dy, x)
     code = _float_code(x, "x")
@@ -304,6 +333,13 @@ class AdamW:
         """One step with the gradients (contiguous, fp32, fp16 or bf16, each of its parameter's
         size; None leaves a tensor as it is).  ``grad_scale``: a device fp32 tensor whose first
         element multiplies every gradient (a clipping or loss scale computed on the device)."""
+        t = self.steps + 1
+        seed = (self.seed + t * 0x6A09E667) & 0xFFFFFFFF
+        lr = self.lr if lr is None else float(lr)
+        if _native.adamw_step(self._h.value, self.params, grads, lr, *self.betas, self.eps, t,
+                              grad_scale, seed, stream):
+            self.steps = t
+            return
         count = len(self.params)
         if len(grads) != count:
             raise ValueError(f"one gradient per tensor ({count}), got {len(grads)}")
@@ -316,10 +352,7 @@ class AdamW:
             if not g.is_contiguous() or g.numel() != p.numel():
                 raise ValueError(f"gradient {i} must be contiguous with {p.numel()} elements")
             ptrs[i] = g.data_ptr() or None
-        t = self.steps + 1
-        seed = (self.seed + t * 0x6A09E667) & 0xFFFFFFFF
-        _check(_lib.darb_adamw_step(self._h, ptrs, types, count,
-                                    self.lr if lr is None else float(lr), *self.betas, self.eps, t,
+        _check(_lib.darb_adamw_step(self._h, ptrs, types, count, lr, *self.betas, self.eps, t,
                                     _optional(grad_scale, 1, "grad_scale"), seed,
                                     _stream_ptr(stream)), "darb_adamw_step")
         self.steps = t
@@ -330,6 +363,8 @@ class AdamW:
         if out is None:
             out = tuple([torch.empty(p.numel(), dtype=torch.float32, device=p.device)
                          for p in self.params] for _ in range(2))
+        if _native.adamw_moments(self._h.value, self.params, out[0], out[1], stream):
+            return out
         count = len(self.params)
         arrays = []
         for name, ts in zip("mv", out):

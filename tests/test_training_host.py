@@ -33,13 +33,17 @@ def test_logprobs_refuses(kw, code):
 
 
 def test_logprobs_workspace():
-    n = ctypes.c_int64()
-    W = L.darb_token_logprobs_workspace
-    assert W(10000, 700, 20, ctypes.byref(n)) == 0 and n.value % 256 == 0 and n.value > 0
-    plain = ctypes.c_int64()
-    assert W(10000, 700, 0, ctypes.byref(plain)) == 0 and plain.value < n.value
-    assert W(10, 5, 0, None) == darb.E_INVALID and W(0, 5, 0, ctypes.byref(n)) == darb.E_INVALID
-    assert W(10, 5, 11, ctypes.byref(n)) == darb.E_INVALID
+    n, plain = ctypes.c_int64(), ctypes.c_int64()
+
+    def ws(out, zdtype=0, V=10000, B=700, fs=700, bs=1, top=20):
+        return L.darb_token_logprobs_workspace(zdtype, V, B, fs, bs, top, out)
+    assert ws(ctypes.byref(n)) == 0 and n.value % 256 == 0 and n.value > 0
+    assert ws(ctypes.byref(plain), top=0) == 0 and 0 < plain.value < n.value
+    assert ws(ctypes.byref(n), fs=1, bs=10000) == 0 and n.value == 0         # rows finished where they are read
+    assert ws(ctypes.byref(n), V=1 << 24, B=1, fs=1, bs=1) == 0 and n.value > 0
+    assert ws(None) == darb.E_INVALID and ws(ctypes.byref(n), V=0) == darb.E_INVALID
+    assert ws(ctypes.byref(n), V=10, top=11) == darb.E_INVALID and ws(ctypes.byref(n), zdtype=5) == darb.E_DTYPE
+    assert ws(ctypes.byref(n), fs=3, bs=3) == darb.E_INVALID
 
 
 def test_logprobs_grad_refuses():
