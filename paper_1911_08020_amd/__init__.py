@@ -536,6 +536,8 @@ class Plan:
         _check_format(index, need.value, "index", (torch.uint8,))
         _check(_lib.darb_transpose(self._h, _ptr(offsets), _ptr(index), index.numel(),
                                    _stream_ptr(stream)), "darb_transpose")
+        if stream is not None:
+            index.record_stream(stream)
         return index
 
     def spmm_grad(self, index, values, X, dY, dvalues=None, dX=None, need_values=True,
@@ -594,6 +596,10 @@ class Plan:
                                    None if workspace is None else _ptr(workspace),
                                    0 if workspace is None else workspace.numel(),
                                    _stream_ptr(stream)), "darb_spmm_grad")
+        if stream is not None:              # allocated on the current stream, used on this one
+            for t in (workspace, dvalues if need_values else None, dX if need_X else None):
+                if t is not None:
+                    t.record_stream(stream)
         return (dvalues if need_values else None), (dX if need_X else None)
 
     # -- argument checks --------------------------------------------------------------

@@ -111,15 +111,21 @@ int check_device(const darb_adamw &a) {
     return DARB_OK;
 }
 
-// The launches of a call over all tensors: at most `most` tensors and 2^24 tiles each.
+// The launches of a call over all tensors: f(first tensor, tensors, first tile, tiles) for at most
+// `most` tensors and 2^22 tiles each (a launch has below 2^32 threads); a larger tensor takes
+// several.
 template <typename F> int over_tensors(const darb_adamw &a, int64_t most, F &&f) {
-    const int64_t count = int64_t(a.tensors.size());
-    for (int64_t i = 0; i < count;) {
-        int64_t j = i + 1;
-        while (j < count && j - i < most && a.first_tile[j + 1] - a.first_tile[i] < (1 << 24)) ++j;
-        const int rc = f(i, j - i, a.first_tile[i], a.first_tile[j] - a.first_tile[i]);
+    constexpr int64_t kMostTiles = int64_t(1) << 22;
+    const int64_t count = int64_t(a.tensors.size()), all = a.first_tile[count];
+    int64_t i = 0;
+    for (int64_t tile = 0; tile < all;) {
+        while (a.first_tile[i + 1] <= tile) ++i;         // the tensor of this tile
+        int64_t end = tile + kMostTiles < all ? tile + kMostTiles : all, j = i + 1;
+        while (j < count && j - i < most && a.first_tile[j] < end) ++j;
+        if (end > a.first_tile[j]) end = a.first_tile[j];
+        const int rc = f(i, j - i, tile, end - tile);
         if (rc) return rc;
-        i = j;
+        tile = end;
     }
     return DARB_OK;
 }

@@ -327,6 +327,12 @@ PyObject *encode(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 // ---- evaluating and retraining a layer -------------------------------------------------
+//
+// These allocate outputs and workspaces, which belong to the current stream: a call on a given
+// stream is left to the Python code, which tells the allocator so.
+
+// The current stream's handle, for None.
+bool current(PyObject *o, void **s) { return o == Py_None && stream_of(o, s); }
 
 bool any_float_code(const at::Tensor &t, int *code) {
     if (t.scalar_type() != at::kBFloat16) return float_code(t, code);
@@ -359,9 +365,9 @@ template <typename T> bool optional(PyObject *o, int64_t n, at::ScalarType type,
     return true;
 }
 
-// A new dense tensor in x's memory order.
+// A new dense tensor in x's memory order (contiguous where one token or feature leaves it open).
 at::Tensor dense_like(const at::Tensor &x) {
-    if (x.stride(0) == 1 && x.size(0) > 1)
+    if (x.stride(0) == 1 && x.size(0) > 1 && x.size(1) > 1)
         return at::empty_strided(x.sizes(), {1, x.size(0)}, x.options());
     return at::empty(x.sizes(), x.options());
 }
@@ -405,7 +411,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (n != 4) return none();
         const at::Tensor *z = matrix(a[0]);
         if (!z || !any_float_code(*z, &code) || !optional(a[1], z->size(1), at::kLong, &t) ||
-            !PyLong_CheckExact(a[2]) || !stream_of(a[3], &s))
+            !PyLong_CheckExact(a[2]) || !current(a[3], &s))
             return none();
         const int64_t V = z->size(0), B = z->size(1), fs = z->stride(0), bs = z->stride(1);
         const long long top = PyLong_AsLongLong(a[2]);
@@ -450,7 +456,7 @@ PyObject *token_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int64_t V = z->size(0), B = z->size(1);
         if (!optional(a[1], B, at::kLong, &t) || !optional(a[2], B, at::kFloat, &lse) || !lse ||
             !optional(a[3], B, at::kFloat, &g) || !optional(a[4], B, at::kFloat, &h) ||
-            !optional(a[5], B, at::kFloat, &gh) || !stream_of(a[7], &s))
+            !optional(a[5], B, at::kFloat, &gh) || !current(a[7], &s))
             return none();
         at::Tensor dz;
         PyObject *res = given_or(a[6], &dz, [&](PyObject *o) { return matrix_like(o, *z); },
@@ -489,7 +495,7 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!x || !any_float_code(*x, &code)) return none();
         const int64_t H = x->size(0), B = x->size(1);
         if (!norm_weight(a[1], *x, H, code, &wcode, &w) || !norm_weight(a[2], *x, H, code, &wcode, &b) ||
-            !PyFloat_CheckExact(a[3]) || !stream_of(a[7], &s))
+            !PyFloat_CheckExact(a[3]) || !current(a[7], &s))
             return none();
         const double eps = PyFloat_AS_DOUBLE(a[3]);
         const auto f32 = x->options().dtype(at::kFloat);
@@ -529,7 +535,7 @@ PyObject *layer_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int64_t H = x->size(0), B = x->size(1);
         int64_t bytes;
         if (!dy || !optional(a[2], B, at::kFloat, &mean) || !mean || !optional(a[3], B, at::kFloat, &rstd) ||
-            !rstd || !norm_weight(a[4], *x, H, code, &wcode, &w) || !stream_of(a[5], &s) ||
+            !rstd || !norm_weight(a[4], *x, H, code, &wcode, &w) || !current(a[5], &s) ||
             darb_layer_norm_workspace(H, B, &bytes) != DARB_OK)
             return none();
         const auto f32 = x->options().dtype(at::kFloat);
@@ -563,7 +569,7 @@ PyObject *spmm_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const at::Tensor *index = buffer(a[1], need, at::kByte), *values = values_of(a[2], p->nnz, &wcode);
         const at::Tensor *X = tensor(a[3]), *dY = tensor(a[4]);
         if (!index || !values || !X || !dY || !float_code(*X, &xcode) || dY->scalar_type() != at::kFloat ||
-            dY->dim() != 2 || !stream_of(a[5], &s))
+            dY->dim() != 2 || !current(a[5], &s))
             return none();
         const int64_t B = dY->size(1), ldy = leading(*dY, p->M, B), ldx = leading(*X, p->N, B);
         if (ldy < 0 || ldx < 0 || darb_spmm_grad_workspace(p->plan, B, &bytes) != DARB_OK) return none();

@@ -35,6 +35,7 @@ struct Args {
     float eps;
     float *mean, *rstd;
     float *dw, *db;                     // partial sums [blocks][H], or null
+    int64_t first;                      // the launch's first token or tile
 };
 
 template <typename T>
@@ -151,7 +152,7 @@ template <typename T, int V, int N> struct Row {
 template <typename T, int V, int N>
 __global__ __launch_bounds__(kMaxThreads) void norm_rows_kernel(Args a) {
     __shared__ float scratch[kMaxWaves];
-    const int64_t b = blockIdx.x;
+    const int64_t b = a.first + blockIdx.x;
     Row<T, V, N> x;
     x.open(static_cast<const T *>(a.x.p) + b * a.x.token, a.H, threadIdx.x, blockDim.x);
     T *y = static_cast<T *>(a.y.p) + b * a.y.token;
@@ -433,7 +434,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int l
     __shared__ float scratch[kMaxWaves * kMaxLanes * V];
     const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes, rows = blockDim.x / lanes;
     int skip;
-    const int64_t b = back_from_end<V>((tile_of(blockIdx.x, gridDim.x) * lanes + tx) * V, a.B, skip);
+    const int64_t b = back_from_end<V>(((a.first + tile_of(blockIdx.x, gridDim.x)) * lanes + tx) * V, a.B, skip);
     float w[kHeld], c[kHeld];
     if constexpr (N) {
 #pragma unroll
@@ -694,6 +695,17 @@ template <int MOST, typename F> hipError_t with_tile(const TileShape &t, F &&f) 
     }
 }
 
+// One launch per 2^20 workgroups (a launch has below 2^32 threads).
+template <typename F> hipError_t over_grid(Args a, int64_t n, F &&launch) {
+    constexpr int64_t kMost = 1 << 20;
+    for (a.first = 0; a.first < n; a.first += kMost) {
+        launch(a, dim3(unsigned(n - a.first < kMost ? n - a.first : kMost)));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 bool rows_of(int64_t H, int64_t feature) { return H == 1 || feature == 1; }
 
 }  // namespace
@@ -708,31 +720,31 @@ hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const
                              const void *bias, float eps, void *y, int64_t y_feature,
                              int64_t y_token, float *mean, float *rstd, hipStream_t s) {
     const Args a{{const_cast<void *>(x), x_feature, x_token}, {y, y_feature, y_token}, {}, weight,
-                 bias, wdtype == DARB_F32, H, B, eps, mean, rstd, nullptr, nullptr};
+                 bias, wdtype == DARB_F32, H, B, eps, mean, rstd, nullptr, nullptr, 0};
     return with_type(xdtype, [&](auto type) {
         using T = decltype(type);
         if (rows_of(H, x_feature)) {
             const RowShape r = row_shape(H, kVec<T>, kMaxThreads, 1);
             return with_row(r, [&](auto n) {
-                if (H < kVec<T>)
-                    hipLaunchKernelGGL((norm_rows_kernel<T, 1, 1>), dim3(unsigned(B)),
-                                       dim3(r.threads), 0, s, a);
-                else
-                    hipLaunchKernelGGL((norm_rows_kernel<T, kVec<T>, decltype(n)::value>),
-                                       dim3(unsigned(B)), dim3(r.threads), 0, s, a);
-                return hipGetLastError();
+                return over_grid(a, B, [&](const Args &part, dim3 grid) {
+                    if (H < kVec<T>)
+                        hipLaunchKernelGGL((norm_rows_kernel<T, 1, 1>), grid, dim3(r.threads), 0, s, part);
+                    else
+                        hipLaunchKernelGGL((norm_rows_kernel<T, kVec<T>, decltype(n)::value>), grid,
+                                           dim3(r.threads), 0, s, part);
+                });
             });
         }
         const TileShape t = tile_shape(H, B, x_feature > y_feature ? x_feature : y_feature, kVec<T>, kMaxThreads, 8, 200);
         return with_tile<8>(t, [&](auto n) {
-            const dim3 grid(unsigned(up(B, int64_t(t.lanes) * t.vec)));
-            if (t.vec == 1)
-                hipLaunchKernelGGL((norm_columns_kernel<T, 1, decltype(n)::value>), grid,
-                                   dim3(t.threads), 0, s, a, t.lanes);
-            else
-                hipLaunchKernelGGL((norm_columns_kernel<T, kVec<T>, decltype(n)::value>), grid,
-                                   dim3(t.threads), 0, s, a, t.lanes);
-            return hipGetLastError();
+            return over_grid(a, up(B, int64_t(t.lanes) * t.vec), [&](const Args &part, dim3 grid) {
+                if (t.vec == 1)
+                    hipLaunchKernelGGL((norm_columns_kernel<T, 1, decltype(n)::value>), grid,
+                                       dim3(t.threads), 0, s, part, t.lanes);
+                else
+                    hipLaunchKernelGGL((norm_columns_kernel<T, kVec<T>, decltype(n)::value>), grid,
+                                       dim3(t.threads), 0, s, part, t.lanes);
+            });
         });
     });
 }
@@ -745,7 +757,7 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
                                   float *dbias, void *workspace, hipStream_t s) {
     Args a{{const_cast<void *>(x), x_feature, x_token}, {dx, dx_feature, dx_token},
            {const_cast<void *>(dy), dy_feature, dy_token}, weight, nullptr, wdtype == DARB_F32,
-           H, B, 0.0f, const_cast<float *>(mean), const_cast<float *>(rstd), nullptr, nullptr};
+           H, B, 0.0f, const_cast<float *>(mean), const_cast<float *>(rstd), nullptr, nullptr, 0};
     return with_type(xdtype, [&](auto type) {
         using T = decltype(type);
         const bool rows = rows_of(H, x_feature);

@@ -523,7 +523,7 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
 template <typename T, int kEach, int THREADS>
 __global__ __launch_bounds__(THREADS) void join_kernel(Args a) {
     __shared__ TopRoom room;
-    const int64_t b = blockIdx.x;
+    const int64_t b = a.first + blockIdx.x;
     const Given given = given_of<T>(a, b);
     Stat t{-kInf, 0.0f, 0.0f};
     for (int64_t i = lane_id(); i < a.nparts; i += kWave) {       // in every wave
@@ -652,9 +652,9 @@ __global__ __launch_bounds__(kGradThreads) void grad_columns_kernel(GradArgs a) 
     }
 }
 
-constexpr int64_t kMaxGridY = 65535;
+constexpr int64_t kMaxGridY = 32768;             // and a launch has below 2^32 threads
 
-// One launch per 65535 rows or tiles.
+// One launch per kMaxGridY rows or tiles.
 template <typename A, typename F> hipError_t over_grid_y(A a, int64_t n, F &&launch) {
     for (a.first = 0; a.first < n; a.first += kMaxGridY) {
         launch(a, unsigned(n - a.first < kMaxGridY ? n - a.first : kMaxGridY));
@@ -782,14 +782,17 @@ hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64
                            : columns(std::integral_constant<int, kVec<T>>{});
         }
         if (e != hipSuccess) return e;
-        if (!top)
-            hipLaunchKernelGGL((join_kernel<T, 1, kWave>), dim3(unsigned(B)), dim3(kWave), 0, s, a);
-        else if (c.rows)
-            hipLaunchKernelGGL((join_kernel<T, kVec<T>, kJoinThreads>), dim3(unsigned(B)),
-                               dim3(kJoinThreads), 0, s, a);
-        else
-            hipLaunchKernelGGL((join_kernel<T, 1, kJoinThreads>), dim3(unsigned(B)),
-                               dim3(kJoinThreads), 0, s, a);
+        constexpr int64_t kMost = 1 << 20;               // a launch has below 2^32 threads
+        Args part = a;
+        for (part.first = 0; part.first < B; part.first += kMost) {
+            const dim3 grid(unsigned(B - part.first < kMost ? B - part.first : kMost));
+            if (!top)
+                hipLaunchKernelGGL((join_kernel<T, 1, kWave>), grid, dim3(kWave), 0, s, part);
+            else if (c.rows)
+                hipLaunchKernelGGL((join_kernel<T, kVec<T>, kJoinThreads>), grid, dim3(kJoinThreads), 0, s, part);
+            else
+                hipLaunchKernelGGL((join_kernel<T, 1, kJoinThreads>), grid, dim3(kJoinThreads), 0, s, part);
+        }
         return hipGetLastError();
     });
 }

@@ -383,7 +383,7 @@ template <int LPE, int V, int U> hipError_t launch_grad_t(const GradArgs &a, int
     auto launch = [&](auto share, auto is_wide) {
         constexpr int KS = decltype(share)::value;
         const int64_t blocks = (a.N + kWaves / KS - 1) / (kWaves / KS);
-        if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+        if (blocks >= 1 << 24) return hipErrorInvalidConfiguration;      // 2^32 threads
         hipLaunchKernelGGL((spmm_grad_kernel<LPE, V, U, KS, decltype(is_wide)::value>),
                            dim3(unsigned(blocks)), dim3(kThreads), 0, s, a);
         return hipGetLastError();
@@ -609,9 +609,11 @@ hipError_t launch_split(const darb_plan &p, const GradArgs &g, void *workspace, 
     hipError_t e = hipGetLastError();
     const int ks = waves_of(p.N, p.nnz, 32);
     a.blocks = uint32_t((p.N + kWaves / ks - 1) / (kWaves / ks));
-    for (a.first_tile = 0; e == hipSuccess && a.first_tile < r.tiles; a.first_tile += kSplitTiles) {
-        const int64_t n = r.tiles - a.first_tile < kSplitTiles ? r.tiles - a.first_tile : kSplitTiles;
-        if (a.blocks * n > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    int64_t most = ((int64_t(1) << 24) - 1) / a.blocks;          // a launch has below 2^32 threads
+    if (most < 1) return hipErrorInvalidConfiguration;
+    if (most > kSplitTiles) most = kSplitTiles;
+    for (a.first_tile = 0; e == hipSuccess && a.first_tile < r.tiles; a.first_tile += most) {
+        const int64_t n = r.tiles - a.first_tile < most ? r.tiles - a.first_tile : most;
         const dim3 rows(unsigned((p.M * (kSplitCols / 4) + kThreads - 1) / kThreads), unsigned(n));
         hipLaunchKernelGGL(tile_rows_kernel, rows, dim3(kThreads), 0, s, a);
         const dim3 grid(unsigned(a.blocks * n));
@@ -650,7 +652,7 @@ hipError_t launch_transpose(const darb_plan &p, const uint8_t *offsets, void *in
     const IndexParts x = parts_of(p, index);
     const int64_t segments = segments_of(p.M, p.N), tasks = segments * ranges_of(p.N);
     const int64_t blocks = (tasks + kWaves - 1) / kWaves;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    if (blocks >= 1 << 24) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(count_columns_kernel, dim3(unsigned(blocks)), dim3(kThreads), 0, s, offsets,
                        p.d_perm, p.bins, p.M, p.N, segments, tasks, x.counts);
     hipError_t e = hipGetLastError();

@@ -59,12 +59,21 @@ def _matrix(t, name: str, like=None):
 
 
 def _empty_like(t):
-    """A dense tensor in t's memory order."""
+    """A dense tensor in t's memory order (contiguous where one token or feature leaves it open)."""
     torch = _torch()
     F, B = t.shape
-    if t.stride(0) == 1 and F > 1:
+    if t.stride(0) == 1 and F > 1 and B > 1:
         return torch.empty((B, F), dtype=t.dtype, device=t.device).t()
     return torch.empty((F, B), dtype=t.dtype, device=t.device)
+
+
+def _used_on(stream, *ts):
+    """Tensors allocated on the current stream and used on a given one: their memory is not
+    handed out again before that stream's work is done."""
+    if stream is not None:
+        for t in ts:
+            if t is not None:
+                t.record_stream(stream)
 
 
 def _vector(t, n: int, name: str, dtype=None):
@@ -125,6 +134,7 @@ def token_logprobs(logits, targets=None, top: int = 0, workspace=None, stream=No
                                     0 if workspace is None else workspace.numel(),
                                     _stream_ptr(stream)),
            "darb_token_logprobs")
+    _used_on(stream, out, tl, ti, workspace)
     return TokenLogprobs(out[0], out[1], out[2], tl, ti)
 
 
@@ -150,6 +160,7 @@ def token_logprobs_grad(logits, targets, lse, grad_logprob=None, entropy=None, g
         _vector(lse, B, "lse"), _optional(grad_logprob, B, "grad_logprob"),
         _optional(entropy, B, "entropy"), _optional(grad_entropy, B, "grad_entropy"), _ptr(out),
         ofs, obs, _stream_ptr(stream)), "darb_token_logprobs_grad")
+    _used_on(stream, out)
     return out
 
 
@@ -191,6 +202,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=None, 
                                 bs, wp, bp, float(eps), _ptr(y), yfs, ybs,
                                 _vector(mean, B, "mean"), _vector(rstd, B, "rstd"),
                                 _stream_ptr(stream)), "darb_layer_norm")
+    _used_on(stream, y, mean, rstd)
     return y, mean, rstd
 
 
@@ -228,6 +240,7 @@ def layer_norm_grad(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias
         dfs, dbs, _vector(dweight, H, "dweight") if need_params else None,
         _vector(dbias, H, "dbias") if need_params else None, _ptr(workspace), workspace.numel(),
         _stream_ptr(stream)), "darb_layer_norm_grad")
+    _used_on(stream, workspace, *([dx] if need_x else []), *([dweight, dbias] if need_params else []))
     return (dx if need_x else None, dweight if need_params else None,
             dbias if need_params else None)
 
@@ -364,6 +377,7 @@ class AdamW:
             out = tuple([torch.empty(p.numel(), dtype=torch.float32, device=p.device)
                          for p in self.params] for _ in range(2))
         if _native.adamw_moments(self._h.value, self.params, out[0], out[1], stream):
+            _used_on(stream, *out[0], *out[1])
             return out
         count = len(self.params)
         arrays = []
@@ -376,4 +390,5 @@ class AdamW:
             arrays.append(a)
         _check(_lib.darb_adamw_moments(self._h, *arrays, count, _stream_ptr(stream)),
                "darb_adamw_moments")
+        _used_on(stream, *out[0], *out[1])
         return out

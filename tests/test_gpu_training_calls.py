@@ -28,7 +28,7 @@ def f(darb):  # noqa: F811
     b = rng.choice([4, 16], size=M)
     plan = darb.Plan(M, N, 1.0 / b, 0.1, 0, 4, 16).upload()
     v, o = plan.encode(dev(rng.standard_normal((M, N)).astype(np.float32)))
-    d = dict(plan=plan, v=v, index=plan.transpose(o), X=dev(rng.standard_normal((N, B)).astype(np.float32)),
+    d = dict(plan=plan, v=v, o=o, index=plan.transpose(o), X=dev(rng.standard_normal((N, B)).astype(np.float32)),
              dY=dev(rng.standard_normal((M, B)).astype(np.float32)), t=torch.from_numpy(rng.integers(0, M, B)).cuda(),
              g=dev(rng.standard_normal(B).astype(np.float32)), w=dev(rng.standard_normal(M).astype(np.float32)))
     for order in ("features", "tokens"):
@@ -92,3 +92,17 @@ def test_native_adamw_equals_python_path(darb):  # noqa: F811
     m, n = a.moments(), b.moments(out=tuple([plain(torch.empty_like(t)) for t in q] for _ in range(2)))
     for x, y in zip(p + m[0] + m[1], q + n[0] + n[1]):
         assert torch.equal(x, y.as_subclass(torch.Tensor))
+
+
+def test_one_token_goes_on_into_a_product(darb, f):  # noqa: F811
+    """A single token leaves the memory order open: the norm's output and the gradients' are
+    contiguous, as the products take them."""
+    for wrap in (plain, lambda t: t):
+        h = f["X"][:, :1].contiguous()
+        y, mean, rstd = darb.layer_norm(wrap(h))
+        f["plan"].spmm(f["v"], f["o"], y)
+        r = darb.token_logprobs(y)
+        dz = darb.token_logprobs_grad(wrap(y), None, r.lse, r.logprob)
+        dx = darb.layer_norm_grad(wrap(y), h, mean, rstd)[0]
+        for t in (y, dz, dx):
+            assert t.is_contiguous() and t.stride(1) == 1
