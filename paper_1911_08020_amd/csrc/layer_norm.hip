@@ -21,6 +21,10 @@ namespace {
 constexpr int kMaxThreads = 1024;
 constexpr int kMaxWaves = kMaxThreads / kWave;
 constexpr int kGradThreads = 512;       // twice the registers a thread: x, dy and the sums
+// Feature-major gradients: fp32 tiles of whole cache lines in workgroups of 1024 threads; the
+// sums of 8 tokens a lane need the registers of 512.
+template <typename T> constexpr int kTileThreads = sizeof(T) == 4 ? 1024 : kGradThreads;
+template <typename T> constexpr int kMostHeld = sizeof(T) == 4 ? 8 : 16;
 
 struct Matrix {                         // element (h, b) at h * feature + b * token
     void *p;
@@ -72,11 +76,11 @@ template <int N> __device__ __forceinline__ void block_sum(float (&s)[N], float 
 #pragma unroll
         for (int i = 0; i < N; ++i) scratch[i * kMaxWaves + w] = s[i];
     __syncthreads();
+    // a lane reads one wave's sum: one latency for all of them
+    const int k = lane_id() % kMaxWaves;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        s[i] = 0.0f;
-        for (int k = 0; k < waves; ++k) s[i] += scratch[i * kMaxWaves + k];
-    }
+    for (int i = 0; i < N; ++i)
+        s[i] = lane_of(group_reduce<kMaxWaves, AddOp>(k < waves ? scratch[i * kMaxWaves + k] : 0.0f), kMaxWaves - 1);
 }
 
 // A vector that would pass the end of its axis starts V before it instead, and leaves out its
@@ -401,25 +405,35 @@ __device__ __forceinline__ float sum_equal_lanes(float x, int lanes) {
     return sum_rows(x);
 }
 
-// s summed over the threads with the same tokens (lanes of them side by side), in each of them;
-// scratch: kMaxWaves * lanes * K floats.
-template <int K> __device__ __forceinline__ void tile_sum(float (&s)[K], int lanes, float *scratch) {
+constexpr int kMaxLanes = 8;
+
+// What tile_sum needs for K sums of up to kMaxLanes lanes.
+template <int K> struct TileRoom {
+    float waves[K * kMaxLanes * kMaxWaves], sums[K * kMaxLanes];
+};
+
+// s summed over the threads with the same tokens (lanes of them side by side), in each of them.
+// The waves' sums are added by a row of 16 lanes each, one wave's sum a lane: read by every
+// thread, one after the other, they took a fifth of a small call.
+template <int K> __device__ __forceinline__ void tile_sum(float (&s)[K], int lanes, TileRoom<K> &room) {
     const int waves = blockDim.x / kWave, w = wave_id(), lane = lane_id();
 #pragma unroll
     for (int j = 0; j < K; ++j) s[j] = sum_equal_lanes(s[j], lanes);
-    __syncthreads();                                 // the scratch's last use
-    if (lane < lanes)
+    if (lane < lanes)                                // the room's last use is two barriers ago
 #pragma unroll
-        for (int j = 0; j < K; ++j) scratch[(w * K + j) * lanes + lane] = s[j];
+        for (int j = 0; j < K; ++j) room.waves[(j * lanes + lane) * kMaxWaves + w] = s[j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < K * lanes * kMaxWaves; i += blockDim.x) {      // whole rows
+        const int k = i % kMaxWaves;
+        const float sum = group_reduce<kMaxWaves, AddOp>(k < waves ? room.waves[i] : 0.0f);
+        if (k == kMaxWaves - 1) room.sums[i / kMaxWaves] = sum;
+    }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-        s[j] = 0.0f;
-        for (int k = 0; k < waves; ++k) s[j] += scratch[(k * K + j) * lanes + lane % lanes];
-    }
+    for (int j = 0; j < K; ++j) s[j] = room.sums[j * lanes + (lane & (lanes - 1))];
 }
 
-constexpr int kMaxLanes = 8;
+__device__ __forceinline__ int log2_of(int power) { return __ffs(power) - 1; }
 
 // The tile of task i: tasks go to the 8 XCDs in turn, each with an L2 of its own, and tiles that
 // lie side by side (parts of the same cache lines, where a tile is narrow) go to one XCD.
@@ -431,8 +445,8 @@ __device__ __forceinline__ int64_t tile_of(int64_t i, int64_t tiles) {
 template <typename T, int V, int N>
 __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int lanes) {
     constexpr int kHeld = N ? N : 1;
-    __shared__ float scratch[kMaxWaves * kMaxLanes * V];
-    const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes, rows = blockDim.x / lanes;
+    __shared__ TileRoom<V> room;
+    const int tx = threadIdx.x & (lanes - 1), ty = threadIdx.x >> log2_of(lanes), rows = blockDim.x >> log2_of(lanes);
     int skip;
     const int64_t b = back_from_end<V>(((a.first + tile_of(blockIdx.x, gridDim.x)) * lanes + tx) * V, a.B, skip);
     float w[kHeld], c[kHeld];
@@ -453,7 +467,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int l
 #pragma unroll
         for (int j = 0; j < V; ++j) mean[j] += v[j];
     });
-    tile_sum(mean, lanes, scratch);
+    tile_sum(mean, lanes, room);
     x.forget();
 #pragma unroll
     for (int j = 0; j < V; ++j) mean[j] /= float(a.H);
@@ -464,7 +478,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int l
             rstd[j] = fmaf(d, d, rstd[j]);
         }
     });
-    tile_sum(rstd, lanes, scratch);
+    tile_sum(rstd, lanes, room);
     x.forget();
 #pragma unroll
     for (int j = 0; j < V; ++j) rstd[j] = 1.0f / sqrtf(rstd[j] / float(a.H) + a.eps);
@@ -487,12 +501,11 @@ __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int l
     }
 }
 
-// Two workgroups share a CU where the registers suffice.
 template <typename T, int V, int N>
-__global__ __launch_bounds__(kGradThreads, N * V <= 32 ? 4 : 2) void norm_grad_columns_kernel(Args a, int lanes) {
+__global__ __launch_bounds__(kTileThreads<T>) void norm_grad_columns_kernel(Args a, int lanes) {
     constexpr int kHeld = N ? N : 1;
-    __shared__ float scratch[kMaxWaves * kMaxLanes * 2 * V];
-    const int tx = threadIdx.x % lanes, ty = threadIdx.x / lanes, rows = blockDim.x / lanes;
+    __shared__ TileRoom<2 * V> room;
+    const int tx = threadIdx.x & (lanes - 1), ty = threadIdx.x >> log2_of(lanes), rows = blockDim.x >> log2_of(lanes);
     const int64_t tiles = (a.B + lanes * V - 1) / (lanes * V);
     float *dw = a.dw ? a.dw + blockIdx.x * a.H : nullptr;
     float *db = a.db ? a.db + blockIdx.x * a.H : nullptr;
@@ -552,7 +565,7 @@ __global__ __launch_bounds__(kGradThreads, N * V <= 32 ? 4 : 2) void norm_grad_c
             }
         });
         if (!a.y.p) continue;
-        tile_sum(s, lanes, scratch);
+        tile_sum(s, lanes, room);
         x.forget();
         dy.forget();
 #pragma unroll
@@ -583,7 +596,7 @@ __global__ __launch_bounds__(kGradThreads, N * V <= 32 ? 4 : 2) void norm_grad_c
 
 // ---- the partial sums of dw and db -----------------------------------------------------
 
-constexpr int kSumFeatures = 16, kSumSlices = 64;    // 64 bytes a row; many workgroups
+constexpr int kSumFeatures = 32, kSumSlices = 32;    // a cache line a row
 
 __global__ __launch_bounds__(kSumFeatures * kSumSlices) void sum_partials_kernel(
     const float *__restrict__ dw_parts, const float *__restrict__ db_parts, int64_t H, int blocks,
@@ -608,9 +621,9 @@ __global__ __launch_bounds__(kSumFeatures * kSumSlices) void sum_partials_kernel
             b += live ? y[q] : 0.0f;
         }
     }
-    // the wave's four slices, then the waves
-    w = sum_rows(w);
-    b = sum_rows(b);
+    // the wave's two slices, then the waves
+    w += __shfl_xor(w, kSumFeatures, kWave);
+    b += __shfl_xor(b, kSumFeatures, kWave);
     const int wave = threadIdx.x / kWave, lane = lane_id();
     if (lane < kSumFeatures) {
         s[0][wave][lane] = w;
@@ -763,7 +776,7 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
         const bool rows = rows_of(H, x_feature);
         int64_t stride = x_feature > dy_feature ? x_feature : dy_feature;
         if (dx && dx_feature > stride) stride = dx_feature;
-        const TileShape t = tile_shape(H, B, stride, kVec<T>, kGradThreads, 16, 384);
+        const TileShape t = tile_shape(H, B, stride, kVec<T>, kTileThreads<T>, kMostHeld<T>, sizeof(T) == 4 ? 200 : 384);
         const RowShape r = row_shape(H, kVec<T>, kGradThreads, kTeamFeatures / kVec<T>);
         const bool teams = r.threads == kWave;
         const int64_t tasks = rows ? teams ? up(B, kGradThreads / kWave) : B : up(B, int64_t(t.lanes) * t.vec);
@@ -785,7 +798,7 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
                 return hipGetLastError();
             });
         } else {
-            e = with_tile<16>(t, [&](auto n) {
+            e = with_tile<kMostHeld<T>>(t, [&](auto n) {
                 if (t.vec == 1)
                     hipLaunchKernelGGL((norm_grad_columns_kernel<T, 1, decltype(n)::value>),
                                        dim3(unsigned(blocks)), dim3(t.threads), 0, s, a, t.lanes);
