@@ -57,9 +57,9 @@ template <typename T> __device__ __forceinline__ void load_some(const T *p, int 
     }
 }
 
-template <typename T> __device__ __forceinline__ void store_some(T *p, int n, const float (&f)[kV]) {
+template <bool STREAM = false, typename T> __device__ __forceinline__ void store_some(T *p, int n, const float (&f)[kV]) {
     if (n == kV) {
-        store_vec<T, kV>(p, f);
+        store_vec<T, kV, STREAM>(p, f);
     } else {
 #pragma unroll
         for (int i = 0; i < kV; ++i)
@@ -258,8 +258,8 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const AdamTensor *__r
                 v[i] = value_v((cv >> (8 * i)) & 255, sv);
             }
         }
-        if (om) store_some(om + at, n, m);
-        if (ov) store_some(ov + at, n, v);
+        if (om) store_some<true>(om + at, n, m);
+        if (ov) store_some<true>(ov + at, n, v);
     }
 }
 

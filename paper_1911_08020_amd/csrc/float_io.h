@@ -47,7 +47,8 @@ template <typename T, int V> __device__ __forceinline__ void forget_uses(Loaded<
     }
 }
 
-template <typename T, int V> __device__ __forceinline__ void store_vec(T *p, const float (&f)[V]) {
+// STREAM: to memory that nothing reads while it could stay in a cache.
+template <typename T, int V, bool STREAM = false> __device__ __forceinline__ void store_vec(T *p, const float (&f)[V]) {
     typename VecOf<T, V>::Type t;
     if constexpr (V == 1) {
         t = T(f[0]);
@@ -55,7 +56,9 @@ template <typename T, int V> __device__ __forceinline__ void store_vec(T *p, con
 #pragma unroll
         for (int i = 0; i < V; ++i) t[i] = T(f[i]);
     }
-    *reinterpret_cast<typename VecOf<T, V>::Type *>(p) = t;
+    typename VecOf<T, V>::Type *to = reinterpret_cast<typename VecOf<T, V>::Type *>(p);
+    if constexpr (STREAM) __builtin_nontemporal_store(t, to);
+    else *to = t;
 }
 
 // F with the C++ type of a darb_dtype (which the caller has checked).
