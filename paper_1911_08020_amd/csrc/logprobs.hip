@@ -5,9 +5,9 @@
 // U = sum e^(z - m) (z - m), rescaled when m grows; parts of a column join the same way.  Then
 // lse = m + log S, log p_t = z_t - lse, entropy = log S - U / S.
 //
-// The alternatives come from the same pass: it keeps the maximum of every segment (a run of
-// consecutive classes), the k greatest logits lie in the k segments with the greatest maxima
-// (of equal ones the earlier segments), and only those segments are read again.
+// The alternatives come from the same pass: it keeps the maximum of every segment (what a thread
+// reads), the k-th greatest of 256 groups of maxima is a bound that k logits reach, and only the
+// segments whose maximum reaches it are read again.
 #include <type_traits>
 
 #include "darb_internal.h"
@@ -25,7 +25,8 @@ constexpr int kMaxTop = 64;
 constexpr int kColThreads = 256;        // feature-major: a workgroup per (64 tokens, part)
 constexpr int kColRun = 16;             // feature-major: classes of a segment, of one thread
 constexpr int kJoinThreads = 256;       // to find alternatives; without, a wave
-constexpr int kHeldMaxima = 2048;       // segments of a row that is finished where it is read
+constexpr int kPartRounds = 64;         // vectors of a thread in a part, at most, to find alternatives
+constexpr int kSegLanes = kColRun;      // lanes that read a segment again
 
 struct Stat {
     float m, s, u;                      // s = 0 and u = 0 where every logit is -inf
@@ -114,7 +115,10 @@ struct Args {
     int64_t *top_index;
     float4 *parts;                      // [B][nparts] Stat of each part
     uint32_t *maxima;                   // [B][nseg] orders, kept if top > 0
-    int64_t nparts, nseg, part_len, seg_len;
+    int64_t nparts, nseg, part_len;
+    // Token-major: the threads of a part, the vectors that each reads, the threads that share a
+    // segment.  (Feature-major segments are kColRun classes.)
+    int part_threads, rounds, seg_threads;
     int64_t first;                      // the launch's first row or tile
 };
 
@@ -133,31 +137,6 @@ __device__ __forceinline__ uint32_t order_of(float z) { return z != z ? kNanOrde
 // The value with that order (NaN for all NaN).
 __device__ __forceinline__ float value_of(uint32_t order) {
     return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order);
-}
-
-// The wave's maximum of each of two or four numbers, as orders (a NaN may be left out).  All go
-// through the lanes together: folded into a half or a quarter of the wave each, then by rows.
-template <int N> __device__ __forceinline__ void wave_orders(const float (&m)[N], uint32_t (&order)[N]) {
-    static_assert(N == 2 || N == 4, "two or four");
-    auto of = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-    auto halves = [&](float a, float b) {            // lanes 0 ... 31: of a; the others: of b
-        const auto r = __builtin_amdgcn_permlane32_swap(number_order(a), number_order(b), false, false);
-        return of(r[0], r[1]);
-    };
-    const uint32_t ab = halves(m[0], m[1]), cd = N == 4 ? halves(m[N - 2], m[N - 1]) : ab;
-    const auto r = __builtin_amdgcn_permlane16_swap(ab, cd, false, false);       // rows: a c b d
-    uint32_t x = of(r[0], r[1]);
-    x = of(x, dpp_all<kDppXor1>(x));
-    x = of(x, dpp_all<kDppXor2>(x));
-    x = of(x, dpp_all<kDppHalfMirror>(x));
-    x = of(x, dpp_all<kDppMirror>(x));
-    auto lane = [&](int i) { return uint32_t(__builtin_amdgcn_readlane(int(x), i)); };
-    order[0] = lane(0);
-    order[1] = lane(32);
-    if constexpr (N == 4) {
-        order[2] = lane(16);
-        order[3] = lane(48);
-    }
 }
 
 __device__ __forceinline__ uint64_t key_at(uint64_t x, int lane) {
@@ -258,71 +237,59 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t *maxima, int64_t n, 
     });
 }
 
-// One wave: the segments with the k greatest of n maxima exactly, of equal ones the first; for
-// columns so full of equal values that too many segments reach the bound.
-__device__ __forceinline__ void pick_segments(const uint32_t *maxima, int64_t n, int k, int lane, TopRoom &room) {
-    auto reach = [&](uint32_t x) {
-        int r = 0;
-        for (int64_t i = 0; i < n; i += kWave)
-            r += __popcll(__ballot(i + lane < n && maxima[i + lane] >= x));
-        return r;
-    };
-    const uint32_t lo = kth_greatest(room.least, ~0u, k, reach);
-    int equal = k - (lo == ~0u ? 0 : reach(lo + 1)), at = 0;     // how many of those at lo to take
-    const uint64_t below = (uint64_t(1) << lane) - 1;
-    for (int64_t i = 0; i < n && at < k; i += kWave) {
-        const uint32_t o = i + lane < n ? maxima[i + lane] : 0;
-        const uint64_t same = __ballot(o == lo);
-        const bool take = o > lo || (o == lo && __popcll(same & below) < equal);
-        const uint64_t all = __ballot(take);
-        if (take) room.segs[at + __popcll(all & below)] = uint32_t(i + lane);
-        at += __popcll(all);
-        equal -= __popcll(same);
-        equal = equal < 0 ? 0 : equal;
-    }
-    if (lane == 0) {
-        room.least = lo;
-        room.found = uint32_t(k);
-    }
-}
-
-// A lane's keys of segments first ... last of the list that can be among the k greatest: f(key
-// of this lane, or 0).  A wave takes as many segments at once as it has lanes for.
+// The keys of a segment (-1: none) whose order is `least` at least, kSegLanes lanes together:
+// f(key, or 0), with all lanes of the wave.
 template <typename T, int kEach, typename F>
-__device__ __forceinline__ void segment_keys(const Args &a, const T *col, const TopRoom &room, int first,
-                                             int found, int lane, F &&f) {
-    constexpr int kLanes = kEach == 1 ? kColRun : kWave;
-    const int i = first + lane / kLanes;
-    const int64_t seg = room.segs[i < found ? i : found - 1];
-    int64_t end = (seg + 1) * a.seg_len;
-    if (end > a.V) end = a.V;
-    const uint32_t least = room.least;
-    int64_t own = seg * a.seg_len + int64_t(lane % kLanes) * kEach;
-    if (i >= found) own = end;                       // nothing
+__device__ __forceinline__ void segment_keys(const Args &a, const T *col, int64_t seg, uint32_t least, int lane, F &&f) {
+    const int in = lane % kSegLanes;
     if constexpr (kEach == 1) {
-        const uint64_t key = own < end ? key_of(float(col[own * a.class_stride]), uint32_t(own)) : 0;
+        const int64_t v = seg * kColRun + in;
+        const uint64_t key = seg >= 0 && v < a.V ? key_of(float(col[v * a.class_stride]), uint32_t(v)) : 0;
         f(uint32_t(key >> 32) >= least ? key : 0);
     } else {
-        Run<T, kEach> x;
-        x.load(col, own, end);
+        const uint32_t s = seg < 0 ? 0 : uint32_t(seg), of_part = uint32_t(a.part_threads / a.seg_threads);
+        const uint32_t part = s / of_part, thread = (s - part * of_part) * a.seg_threads;
+        const int64_t begin = part * a.part_len;
+        int64_t end = begin + a.part_len;
+        if (end > a.V) end = a.V;
+        const int vectors = a.rounds * a.seg_threads;
+        for (int first = 0; first < vectors; first += kSegLanes) {
+            const int i = first + in, round = i / a.seg_threads, t = i - round * a.seg_threads;
+            int64_t v = begin + (int64_t(round) * a.part_threads + thread + t) * kEach;
+            if (seg < 0 || i >= vectors) v = end;                    // nothing
+            Run<T, kEach> x;
+            x.load(col, v, end);
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            const uint64_t key = j >= x.skip ? key_of(x.x[j], uint32_t(own + j - x.skip)) : 0;
-            f(uint32_t(key >> 32) >= least ? key : 0);
+            for (int j = 0; j < kEach; ++j) {
+                const uint64_t key = j >= x.skip ? key_of(x.x[j], uint32_t(v + j - x.skip)) : 0;
+                f(uint32_t(key >> 32) >= least ? key : 0);
+            }
         }
     }
 }
 
-// The alternatives of token b by a whole workgroup, given the segments' maxima: the elements
-// not below the bound, which only segments whose maximum reaches it hold, are collected and
-// ranked.  (More equal elements than there is room for: one wave goes through the segments.)
-template <typename T, int kEach, int THREADS>
+// The alternatives of token b by a whole workgroup, given the segments' maxima (HELD: at most a
+// thread's each, in LDS): the elements not below the bound, which only segments whose maximum
+// reaches it hold, are collected and ranked.  Where so many are equal that there is no room for
+// them, each wave goes through a share of the segments with a list of its k greatest.
+template <typename T, int kEach, int THREADS, bool HELD>
 __device__ __forceinline__ void write_top(const Args &a, int64_t b, const uint32_t *maxima, float lse,
                                           TopRoom &room) {
-    constexpr int kWaves = THREADS / kWave, kAtOnce = kEach == 1 ? kWave / kColRun : 1;
+    constexpr int kWaves = THREADS / kWave, kAtOnce = kWave / kSegLanes;
+    static_assert(kWaves * kMaxTop <= kKeys && THREADS % 256 == 0 && sizeof(room.keys) >= THREADS * 4, "rooms");
     const int w = wave_id(), lane = lane_id(), k = int(a.top);
+    const uint32_t *groups = maxima;
+    if constexpr (!HELD) {
+        uint32_t most = 0;
+#pragma unroll 8
+        for (int64_t i = threadIdx.x; i < a.nseg; i += THREADS) most = maxima[i] > most ? maxima[i] : most;
+        uint32_t *mine = reinterpret_cast<uint32_t *>(room.keys);    // not in use yet
+        mine[threadIdx.x] = most;
+        groups = mine;
+        __syncthreads();
+    }
     if (w == 0) {
-        const uint32_t bound = bound_of(maxima, a.nseg, k, lane);
+        const uint32_t bound = bound_of(groups, a.nseg < THREADS ? a.nseg : THREADS, k, lane);
         if (lane == 0) {
             room.least = bound;
             room.found = room.count = 0;
@@ -336,34 +303,38 @@ __device__ __forceinline__ void write_top(const Args &a, int64_t b, const uint32
             if (at < kSegs) room.segs[at] = uint32_t(i);
         }
     __syncthreads();
-    if (room.found > kSegs) {                        // then there are more than k
-        __syncthreads();
-        if (w == 0) pick_segments(maxima, a.nseg, k, lane, room);
-        __syncthreads();
-    }
     const int found = int(room.found);
     const T *col = static_cast<const T *>(a.z) + b * a.token_stride;
-    for (int i = w * kAtOnce; i < found; i += kWaves * kAtOnce)
-        segment_keys<T, kEach>(a, col, room, i, found, lane, [&](uint64_t key) {
-            if (key) {
-                const uint32_t at = atomicAdd(&room.count, 1u);
-                if (at < kKeys) room.keys[at] = key;
-            }
-        });
+    if (found <= kSegs)
+        for (int first = w * kAtOnce; first < found; first += kWaves * kAtOnce) {
+            const int i = first + lane / kSegLanes;
+            segment_keys<T, kEach>(a, col, i < found ? int64_t(room.segs[i]) : -1, bound, lane, [&](uint64_t key) {
+                if (key) {
+                    const uint32_t at = atomicAdd(&room.count, 1u);
+                    if (at < kKeys) room.keys[at] = key;
+                }
+            });
+        }
     __syncthreads();
-    auto write = [&](uint64_t key, int rank) {
+    int n = int(room.count);
+    if (found > kSegs || n > kKeys) {
+        TopList best;
+        for (int64_t first = w * kAtOnce; first < a.nseg; first += kWaves * kAtOnce) {
+            const int64_t i = first + lane / kSegLanes;
+            const uint32_t last = uint32_t(key_at(best.key, k - 1) >> 32), least = last > bound ? last : bound;
+            const bool reaches = i < a.nseg && maxima[i] >= least;
+            if (__any(reaches))
+                segment_keys<T, kEach>(a, col, reaches ? i : -1, least, lane,
+                                       [&](uint64_t key) { best.offer(key, k, lane); });
+        }
+        if (lane < k) room.keys[w * k + lane] = best.key;            // 0, which none keeps, for none
+        __syncthreads();
+        n = kWaves * k;
+    }
+    ranked<THREADS>(room.keys, n, k, [&](uint64_t key, int rank) {
         a.top_index[b * a.top + rank] = UINT32_MAX - uint32_t(key);
         a.top_logprob[b * a.top + rank] = lse == -kInf ? -kInf : value_of(uint32_t(key >> 32)) - lse;
-    };
-    if (room.count <= kKeys) {
-        ranked<THREADS>(room.keys, int(room.count), k, write);
-    } else if (w == 0) {
-        TopList best;
-        for (int i = 0; i < found; i += kAtOnce)
-            segment_keys<T, kEach>(a, col, room, i, found, lane,
-                                   [&](uint64_t key) { best.offer(key, k, lane); });
-        if (lane < k) write(best.key, lane);
-    }
+    });
 }
 
 // A token's target and its logit, read ahead.
@@ -395,14 +366,17 @@ __device__ __forceinline__ float write_token(const Args &a, int64_t b, Stat t, G
 // ---- token-major: a row's classes are contiguous --------------------------------------
 
 // grid (parts, B); each wave takes every kWaves-th run of 64 vectors of its part, 16
-// values a lane together.  A run is a segment; the greatest value is what the wave's sums run
-// from.  A row
-// that is one part is finished here, its maxima kept in LDS.
+// values a lane together; the greatest value is what the wave's sums run from.  A segment is what
+// a thread reads, or four neighbours where a row has several parts: no maximum crosses the wave in
+// the loop, which cost a seventh of it (131 072 x 512 bf16).  A row that is one part is finished
+// here, its maxima kept in LDS.
+constexpr int kPartSegThreads = 4;      // of rows of several parts
+
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 7) void rows_kernel(Args a) {
     constexpr int V = kVec<T>, kWaves = THREADS / kWave, kRun = V * kWave, kAtOnce = 16 / V;
     __shared__ Stat stats[kWaves];
-    __shared__ uint32_t held[kHeldMaxima];
+    __shared__ uint32_t held[THREADS];
     __shared__ TopRoom room;
     const int w = wave_id(), lane = lane_id();
     const int64_t b = a.first + blockIdx.y, part = blockIdx.x;
@@ -412,6 +386,8 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 7) void rows_kernel(Ar
     if (end > a.V) end = a.V;
     const Given given = a.nparts == 1 ? given_of<T>(a, b) : Given{};
     Sums t;
+    float most = -kInf;                              // of the thread's elements
+    bool any_nan = false;
     // the next runs are on their way while these are summed
     Loaded<T, V> x[kAtOnce];
     auto load = [&](int64_t v0) {
@@ -448,19 +424,11 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 7) void rows_kernel(Ar
 #pragma unroll
             for (int i = 1; i < V; ++i) m[q] = fmaxf(m[q], z[q][i]);
         }
-        uint32_t order[kAtOnce] = {};
-        if (a.top) {
-            wave_orders(m, order);
-            uint32_t all = order[0];
+        float all = m[0];
 #pragma unroll
-            for (int q = 1; q < kAtOnce; ++q) all = order[q] > all ? order[q] : all;
-            t.raise(fmaxf(t.m, value_of(all)));
-        } else {
-            float all = m[0];
-#pragma unroll
-            for (int q = 1; q < kAtOnce; ++q) all = fmaxf(all, m[q]);
-            if (__any(all > t.m)) t.raise(fmaxf(t.m, wave_max(all)));
-        }
+        for (int q = 1; q < kAtOnce; ++q) all = fmaxf(all, m[q]);
+        most = fmaxf(most, all);
+        if (__any(all > t.m)) t.raise(fmaxf(t.m, wave_max(all)));
         if (t.m != -kInf) {
 #pragma unroll
             for (int q = 0; q < kAtOnce; ++q) t.add(z[q]);
@@ -473,17 +441,20 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 7) void rows_kernel(Ar
 #pragma unroll
                 for (int i = 0; i < V; ++i) nan |= z[q][i] != z[q][i];
                 if (nan) t.s = __builtin_nanf("");
-                if (__any(nan)) order[q] = kNanOrder;
+                any_nan |= nan;
             }
         }
-        if (a.top && lane == 0) {
-#pragma unroll
-            for (int q = 0; q < kAtOnce; ++q) {
-                const int64_t v = v0 + q * (kWaves * kRun);
-                const uint32_t at = uint32_t(v) / kRun;
-                if (v < end && a.nparts == 1) held[at] = order[q];
-                else if (v < end) a.maxima[b * a.nseg + at] = order[q];
-            }
+    }
+    if (a.top) {                                     // a thread without elements: that of -inf
+        uint32_t order = any_nan ? kNanOrder : number_order(most);
+        if (a.nparts == 1) {
+            held[threadIdx.x] = order;
+        } else {
+            auto of = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
+            order = of(order, dpp_all<kDppXor1>(order));
+            order = of(order, dpp_all<kDppXor2>(order));
+            if (lane % kPartSegThreads == 0)
+                a.maxima[b * a.nseg + (part * THREADS + threadIdx.x) / kPartSegThreads] = order;
         }
     }
     // the wave's lanes share their maximum
@@ -501,7 +472,7 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 8 : 7) void rows_kernel(Ar
         return;
     }
     const float lse = write_token(a, b, all, given);
-    if (a.top) write_top<T, V, THREADS>(a, b, held, lse, room);
+    if (a.top) write_top<T, V, THREADS, true>(a, b, held, lse, room);
 }
 
 // ---- feature-major: a class's tokens are contiguous -----------------------------------
@@ -536,14 +507,13 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
     int64_t end = begin + a.part_len;
     if (end > a.V) end = a.V;
     Sums t[V];
-    const int run = int(a.seg_len);
-    for (int64_t v0 = begin + ty * run; v0 < end; v0 += kRows * run) {
+    for (int64_t v0 = begin + ty * kColRun; v0 < end; v0 += kRows * kColRun) {
         float m[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) m[j] = -kInf;
         constexpr int kAtOnce = kColRun / 2;
 #pragma unroll 1
-        for (int r0 = 0; r0 < run; r0 += kAtOnce) {
+        for (int r0 = 0; r0 < kColRun; r0 += kAtOnce) {
             Loaded<T, V> x[kAtOnce];
 #pragma unroll
             for (int r = 0; r < kAtOnce; ++r) {
@@ -605,7 +575,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(Args a) {
         t = join(t, {p.x, p.y, p.z});
     }
     const float lse = write_token(a, b, join_lanes<kWave>(t), given);
-    if (THREADS > kWave) write_top<T, kEach, THREADS>(a, b, a.maxima + b * a.nseg, lse, room);
+    if constexpr (THREADS > kWave) write_top<T, kEach, THREADS, false>(a, b, a.maxima + b * a.nseg, lse, room);
 }
 
 // ---- the gradient ---------------------------------------------------------------------
@@ -782,7 +752,8 @@ struct Cut {
     bool rows;                          // token-major
     int vec, lanes;                     // feature-major
     int threads;                        // token-major
-    int64_t part_len, nparts, seg_len, nseg;
+    int64_t part_len, nparts, nseg;
+    int rounds, seg_threads;            // token-major
 };
 
 Cut cut_of(int dtype, int64_t V, int64_t B, bool contiguous, int64_t top) {
@@ -792,34 +763,34 @@ Cut cut_of(int dtype, int64_t V, int64_t B, bool contiguous, int64_t top) {
     c.rows = contiguous && V >= c.vec;
     if (c.rows) {
         c.lanes = 0;
-        c.seg_len = c.vec * kWave;
         // a wave has at least four runs, or one where rows are few; a long row several parts
-        const int64_t runs = (V + c.seg_len - 1) / c.seg_len, each = B < 256 ? 1 : 4;
+        const int64_t run = c.vec * kWave, runs = (V + run - 1) / run, each = B < 256 ? 1 : 4;
         c.threads = 256;
         while (c.threads < 1024 && runs >= 2 * each * c.threads / kWave) c.threads *= 2;
-        const int64_t step = c.seg_len * (c.threads / kWave);       // one round of a workgroup
+        const int64_t step = int64_t(c.vec) * c.threads;            // one round of a workgroup
         const int64_t rounds = (V + step - 1) / step;
         int64_t parts = (512 + B - 1) / B;
         if (parts > rounds / 4) parts = rounds / 4;
-        const int64_t held = (V + c.seg_len * kHeldMaxima - 1) / (c.seg_len * kHeldMaxima);
-        if (parts < held) parts = held;
-        if (parts < 1) parts = 1;
-        c.part_len = (rounds + parts - 1) / parts * step;
+        const int64_t least = top ? (rounds + kPartRounds - 1) / kPartRounds : 1;
+        if (parts < least) parts = least;
+        c.rounds = int((rounds + parts - 1) / parts);
+        c.part_len = c.rounds * step;
+        c.nparts = (V + c.part_len - 1) / c.part_len;
+        c.seg_threads = c.nparts == 1 ? 1 : kPartSegThreads;
+        c.nseg = c.nparts * c.threads / c.seg_threads;
     } else {
         if (B < c.vec || contiguous) c.vec = 1;
         c.lanes = lanes_of(B, c.vec);
-        // without alternatives the segments say only how long a thread's runs are: half as long,
-        // twice as many workgroups
-        c.seg_len = kColRun;
-        const int64_t step = kColThreads / c.lanes * c.seg_len;     // one round of a workgroup
+        const int64_t step = kColThreads / c.lanes * kColRun;     // one round of a workgroup
         const int64_t rounds = (V + step - 1) / step;
         const int64_t tiles = (B + c.lanes * c.vec - 1) / (c.lanes * c.vec);
         int64_t parts = (1024 + tiles - 1) / tiles;
         if (parts > rounds) parts = rounds;
         c.part_len = (rounds + parts - 1) / parts * step;
+        c.nparts = (V + c.part_len - 1) / c.part_len;
+        c.nseg = (V + kColRun - 1) / kColRun;
+        c.threads = c.rounds = c.seg_threads = 0;
     }
-    c.nparts = (V + c.part_len - 1) / c.part_len;
-    c.nseg = (V + c.seg_len - 1) / c.seg_len;
     return c;
 }
 
@@ -848,7 +819,7 @@ hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64
     uint32_t *maxima = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + padded(c.nparts * B * 16));
     const Args a{z, class_stride, token_stride, V, B, targets, top, logprob, entropy, lse,
                  top_logprob, top_index, static_cast<float4 *>(workspace), maxima, c.nparts,
-                 c.nseg, c.part_len, c.seg_len, 0};
+                 c.nseg, c.part_len, c.threads, c.rounds, c.seg_threads, 0};
     return with_type(dtype, [&](auto type) {
         using T = decltype(type);
         hipError_t e;
