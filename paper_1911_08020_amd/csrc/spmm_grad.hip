@@ -419,22 +419,28 @@ struct SplitArgs {
     uint32_t blocks;                    // workgroups of a tile
 };
 
-__global__ __launch_bounds__(kThreads) void pair_values_kernel(GradArgs a, int64_t nnz, Pair *__restrict__ pairs) {
-    const int64_t i = side_by_side(blockIdx.x, gridDim.x) * kThreads + threadIdx.x;
-    if (i >= nnz) return;
-    const Entry e = a.entries[i];
+__device__ __forceinline__ void pair_values(const SplitArgs &a, uint32_t block, uint32_t blocks) {
+    const int64_t i = side_by_side(block, blocks) * kThreads + threadIdx.x;
+    if (i >= a.nnz) return;
+    const Entry e = a.g.entries[i];
     float v = 0.0f;
-    if (a.dX) v = a.wdtype == DARB_F32 ? static_cast<const float *>(a.values)[e.slot]
-                                       : float(static_cast<const half_t *>(a.values)[e.slot]);
-    pairs[i] = {e.row, v};
+    if (a.g.dX) v = a.g.wdtype == DARB_F32 ? static_cast<const float *>(a.g.values)[e.slot]
+                                           : float(static_cast<const half_t *>(a.g.values)[e.slot]);
+    a.pairs[i] = {e.row, v};
 }
 
-// grid.y: tiles; a thread copies four columns of a row.
-__global__ __launch_bounds__(kThreads) void tile_rows_kernel(SplitArgs a) {
+// The first pair_blocks workgroups gather the weights' values while the others copy the tiles, a
+// thread four columns of a row: one waits for latency, the other for bandwidth.
+__global__ __launch_bounds__(kThreads) void tile_rows_kernel(SplitArgs a, uint32_t pair_blocks, uint32_t row_blocks) {
     constexpr int kPerRow = kSplitCols / 4;
-    const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x, r = i / kPerRow;
+    if (blockIdx.x < pair_blocks) {
+        pair_values(a, blockIdx.x, pair_blocks);
+        return;
+    }
+    const uint32_t block = blockIdx.x - pair_blocks, tile = block / row_blocks;
+    const int64_t i = int64_t(block - tile * row_blocks) * kThreads + threadIdx.x, r = i / kPerRow;
     if (r >= a.M) return;
-    const int64_t c = (a.first_tile + blockIdx.y) * kSplitCols + i % kPerRow * 4;
+    const int64_t c = (a.first_tile + tile) * kSplitCols + i % kPerRow * 4;
     const float *from = a.g.dY + r * a.g.ldy + c;
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (c + 4 <= a.g.B) {
@@ -445,7 +451,7 @@ __global__ __launch_bounds__(kThreads) void tile_rows_kernel(SplitArgs a) {
         if (c + 1 < a.g.B) x.y = from[1];
         if (c + 2 < a.g.B) x.z = from[2];
     }
-    reinterpret_cast<float4 *>(a.tiles)[(blockIdx.y * a.M + r) * kPerRow + i % kPerRow] = x;
+    reinterpret_cast<float4 *>(a.tiles)[(tile * a.M + r) * kPerRow + i % kPerRow] = x;
 }
 
 // As spmm_grad_kernel with 8 lanes to a weight, 8 batch columns each.
@@ -577,8 +583,16 @@ __global__ __launch_bounds__(kThreads) void sum_parts_kernel(const float *__rest
     if (i >= nnz) return;
     const uint32_t slot = entries[i].slot;
     float s = add ? dvalues[slot] : 0.0f;
+    int t = 0;
+    for (; t + 8 <= tiles; t += 8) {                 // loads side by side
+        float x[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = parts[(t + q) * nnz + i];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s += x[q];
+    }
 #pragma unroll 4
-    for (int t = 0; t < tiles; ++t) s += parts[t * nnz + i];
+    for (; t < tiles; ++t) s += parts[t * nnz + i];
     dvalues[slot] = s;
 }
 
@@ -605,17 +619,21 @@ hipError_t launch_split(const darb_plan &p, const GradArgs &g, void *workspace, 
     SplitArgs a{g, reinterpret_cast<Pair *>(w + r.pairs_at), reinterpret_cast<float *>(w + r.tiles_at),
                 g.dvalues ? reinterpret_cast<float *>(w + r.parts_at) : nullptr, p.M, p.nnz, 0, 0};
     const dim3 each(unsigned((p.nnz + kThreads - 1) / kThreads));
-    hipLaunchKernelGGL(pair_values_kernel, each, dim3(kThreads), 0, s, g, p.nnz, a.pairs);
-    hipError_t e = hipGetLastError();
+    hipError_t e = hipSuccess;
     const int ks = waves_of(p.N, p.nnz, 32);
     a.blocks = uint32_t((p.N + kWaves / ks - 1) / (kWaves / ks));
-    int64_t most = ((int64_t(1) << 24) - 1) / a.blocks;          // a launch has below 2^32 threads
+    // a launch has below 2^32 threads
+    const uint32_t row_blocks = uint32_t((p.M * (kSplitCols / 4) + kThreads - 1) / kThreads);
+    int64_t most = ((int64_t(1) << 24) - 1) / a.blocks;
+    const int64_t most_rows = ((int64_t(1) << 24) - 1 - each.x) / row_blocks;
+    if (most > most_rows) most = most_rows;
     if (most < 1) return hipErrorInvalidConfiguration;
     if (most > kSplitTiles) most = kSplitTiles;
     for (a.first_tile = 0; e == hipSuccess && a.first_tile < r.tiles; a.first_tile += most) {
         const int64_t n = r.tiles - a.first_tile < most ? r.tiles - a.first_tile : most;
-        const dim3 rows(unsigned((p.M * (kSplitCols / 4) + kThreads - 1) / kThreads), unsigned(n));
-        hipLaunchKernelGGL(tile_rows_kernel, rows, dim3(kThreads), 0, s, a);
+        const uint32_t pair_blocks = a.first_tile == 0 ? each.x : 0;
+        hipLaunchKernelGGL(tile_rows_kernel, dim3(pair_blocks + row_blocks * uint32_t(n)), dim3(kThreads), 0, s, a,
+                           pair_blocks, row_blocks);
         const dim3 grid(unsigned(a.blocks * n));
         if (ks == 1) hipLaunchKernelGGL((split_grad_kernel<1>), grid, dim3(kThreads), 0, s, a);
         else if (ks == 2) hipLaunchKernelGGL((split_grad_kernel<2>), grid, dim3(kThreads), 0, s, a);
