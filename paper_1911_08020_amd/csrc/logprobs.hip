@@ -511,7 +511,9 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
         float m[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) m[j] = -kInf;
-        constexpr int kAtOnce = kColRun / 2;
+        // fp32: all loads of a run under way at once (10 000 x 700: 11.5 -> 10.4 us); eight tokens
+        // of 16 bits a lane would take the registers of other waves (32 000 x 2048: 35 -> 42 us)
+        constexpr int kAtOnce = sizeof(T) == 4 ? kColRun : kColRun / 2;
 #pragma unroll 1
         for (int r0 = 0; r0 < kColRun; r0 += kAtOnce) {
             Loaded<T, V> x[kAtOnce];
