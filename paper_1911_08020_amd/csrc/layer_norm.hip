@@ -65,12 +65,14 @@ __device__ __forceinline__ void weights(const Args &a, const void *w, int64_t h,
     }
 }
 
-// The workgroup's sum of s[0 .. N), each in every thread; scratch: N * kMaxWaves floats.
-template <int N> __device__ __forceinline__ void block_sum(float (&s)[N], float *scratch) {
-    const int waves = blockDim.x / kWave, w = wave_id();
+// The sum of s[0 .. N) over `waves` waves of the workgroup from `first` on, each in every thread;
+// scratch: N * kMaxWaves floats.
+template <int N>
+__device__ __forceinline__ void block_sum(float (&s)[N], float *scratch, int first, int waves) {
+    const int w = wave_id();
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
-    if (waves == 1) return;
+    if (blockDim.x == kWave) return;
     __syncthreads();                                 // the scratch's last use
     if (lane_id() == 0)
 #pragma unroll
@@ -80,7 +82,7 @@ template <int N> __device__ __forceinline__ void block_sum(float (&s)[N], float 
     const int k = lane_id() % kMaxWaves;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        s[i] = lane_of(group_reduce<kMaxWaves, AddOp>(k < waves ? scratch[i * kMaxWaves + k] : 0.0f), kMaxWaves - 1);
+        s[i] = lane_of(group_reduce<kMaxWaves, AddOp>(k < waves ? scratch[i * kMaxWaves + first + k] : 0.0f), kMaxWaves - 1);
 }
 
 // A vector that would pass the end of its axis starts V before it instead, and leaves out its
@@ -165,7 +167,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_rows_kernel(Args a) {
 #pragma unroll
         for (int j = 0; j < V; ++j) s[0] += j >= skip ? v[j] : 0.0f;
     });
-    block_sum(s, scratch);
+    block_sum(s, scratch, 0, blockDim.x / kWave);
     x.forget();
     const float mean = s[0] / float(a.H);
     s[0] = 0.0f;
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_rows_kernel(Args a) {
             s[0] = fmaf(d, d, s[0]);
         }
     });
-    block_sum(s, scratch);
+    block_sum(s, scratch, 0, blockDim.x / kWave);
     x.forget();
     const float rstd = 1.0f / sqrtf(s[0] / float(a.H) + a.eps);
     x.each([&](int, int64_t h, int skip, const Loaded<T, V> &v) {
@@ -193,17 +195,26 @@ __global__ __launch_bounds__(kMaxThreads) void norm_rows_kernel(Args a) {
     }
 }
 
-// The workgroup takes every gridDim.x-th token, or, where a row is one wave's (TEAMS), each of
-// its waves a token of its own and no barrier.  Held rows: dw and db sum in registers (the teams'
-// then in LDS); longer ones: in the workgroup's row of the workspace.
-template <typename T, int V, int N, bool TEAMS>
-__global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
+// Threads of a workgroup whose registers (128 or 256 a thread) hold n vectors of two rows, this
+// one and the next, and their sums without spilling.
+constexpr int row_threads(int vec, int n) { return n > 0 && n * (vec + 4) <= 24 ? kMaxThreads : kGradThreads; }
+
+// A workgroup is one or several teams of `threads` threads, each of which takes a token at a
+// time: teams of one wave (WAVES) without a barrier, larger ones in step.  (One row of 1500 at a
+// time left a CU's SIMDs waiting: 8192 of them in bf16 took 47 us, four together 26.)  Held rows:
+// dw and db sum in registers, the teams' then in LDS; longer ones: in the workgroup's row of the
+// workspace.
+template <typename T, int V, int N, bool WAVES>
+__global__ __launch_bounds__(WAVES ? kGradThreads : row_threads(V, N)) void norm_grad_rows_kernel(
+    Args a, int threads) {
     constexpr int kHeld = N ? N : 1;
+    constexpr bool kSeveral = WAVES || row_threads(V, N) > kGradThreads;
     __shared__ float scratch[2 * kMaxWaves];
-    const int threads = TEAMS ? kWave : int(blockDim.x);           // of a row
-    const int tid = TEAMS ? threadIdx.x % kWave : threadIdx.x;
-    const int64_t team = TEAMS ? threadIdx.x / kWave : 0, teams = TEAMS ? blockDim.x / kWave : 1;
-    const int64_t first_b = blockIdx.x * teams + team, step = gridDim.x * teams;
+    if (WAVES) threads = kWave;
+    const int waves = threads / kWave;                             // of a row
+    const int team = kSeveral ? wave_id() / waves : 0, teams = kSeveral ? int(blockDim.x) / threads : 1;
+    const int tid = threadIdx.x - team * threads;
+    const int64_t step = int64_t(gridDim.x) * teams, first_b = int64_t(blockIdx.x) * teams + team;
     float *dw = a.dw ? a.dw + blockIdx.x * a.H : nullptr;
     float *db = a.db ? a.db + blockIdx.x * a.H : nullptr;
     float sw[kHeld][V], sb[kHeld][V];
@@ -231,13 +242,14 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
         next_dy.open(static_cast<const T *>(a.dy.p) + b * a.dy.token, a.H, tid, threads);
     };
     if (first_b < a.B) fetch(first_b);
-    for (int64_t b = first_b; b < a.B; b += step) {
+    for (int64_t b = first_b; b - team < a.B; b += step) {          // as often in every team
+        const bool live = !kSeveral || b < a.B;
         Row<T, V, N> x = next_x, dy = next_dy;
         const float mean = next_mean, rstd = next_rstd;
         if (b + step < a.B) fetch(b + step);
         T *dx = static_cast<T *>(a.y.p) + b * a.y.token;
         float s[2] = {0.0f, 0.0f};
-        x.each([&](int i, int64_t h, int skip, const Loaded<T, V> &v) {
+        if (live) x.each([&](int i, int64_t h, int skip, const Loaded<T, V> &v) {
             const Loaded<T, V> g = N ? dy.held[i] : load_vec<T, V>(dy.p + h);
             float w[V];
             if constexpr (N) {
@@ -264,12 +276,13 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
             }
         });
         if (!a.y.p) continue;
-        if constexpr (TEAMS) {
+        if constexpr (WAVES) {
             s[0] = wave_sum(s[0]);
             s[1] = wave_sum(s[1]);
         } else {
-            block_sum(s, scratch);
+            block_sum(s, scratch, team * waves, waves);
         }
+        if (!live) continue;                         // the last round
         x.forget();
         dy.forget();
         const float m0 = s[0] / float(a.H), m1 = s[1] / float(a.H);
@@ -292,33 +305,35 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(Args a) {
     }
     if constexpr (N) {
         // team by team, in LDS; the last one's sums are the workgroup's
-        __shared__ float together[TEAMS ? 2 : 1][TEAMS ? N * V * kWave : 1];
-        for (int64_t turn = 0; turn < teams; ++turn) {
-            if (team == turn) {
+        __shared__ float together[kSeveral ? N * V * (WAVES ? kWave : kGradThreads) : 1];
+        auto add = [&](float (&sum)[kHeld][V]) {
+            for (int turn = 0; turn < teams && teams > 1; ++turn) {
+                if (team == turn) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int64_t at = (int64_t(i) * threads + tid) * V;
-                    if (at >= a.H) break;
-                    int skip;
-                    const int64_t h = back_from_end<V>(at, a.H, skip);
-                    if (TEAMS) {
+                    for (int i = 0; i < N; ++i)
 #pragma unroll
                         for (int j = 0; j < V; ++j) {
-                            float &w = together[0][(i * V + j) * kWave + tid], &c = together[1][(i * V + j) * kWave + tid];
-                            if (turn > 0) {
-                                sw[i][j] += w;
-                                sb[i][j] += c;
-                            }
-                            w = sw[i][j];
-                            c = sb[i][j];
+                            float &t = together[(i * V + j) * threads + tid];
+                            if (turn > 0) sum[i][j] += t;
+                            t = sum[i][j];
                         }
-                    }
-                    if (turn + 1 < teams) continue;
-                    if (dw) store_own<float, V>(dw + h, skip, sw[i]);
-                    if (db) store_own<float, V>(db + h, skip, sb[i]);
                 }
+                __syncthreads();
             }
-            if (TEAMS) __syncthreads();
+        };
+        if constexpr (kSeveral) {
+            add(sw);
+            add(sb);
+        }
+        if (team + 1 < teams) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int64_t at = (int64_t(i) * threads + tid) * V;
+            if (at >= a.H) break;
+            int skip;
+            const int64_t h = back_from_end<V>(at, a.H, skip);
+            if (dw) store_own<float, V>(dw + h, skip, sw[i]);
+            if (db) store_own<float, V>(db + h, skip, sb[i]);
         }
     }
 }
@@ -657,15 +672,15 @@ struct RowShape {
     int threads, n;
 };
 
-RowShape row_shape(int64_t H, int vec, int most, int one_wave) {
+RowShape row_shape(int64_t H, int vec, int most, int one_wave, bool gradient = false) {
     if (H < vec) return {kWave, 1};                  // an element a thread
     const int64_t vectors = up(H, vec);
     if (vectors <= kWave * one_wave) return {kWave, int(up(vectors, kWave))};
     for (int threads = 256; threads <= most; threads *= 2)
         for (int n = 1; n <= 4; ++n)
-            if (up(up(vectors, n), kWave) * kWave <= threads)
+            if (up(up(vectors, n), kWave) * kWave <= threads && (!gradient || threads <= row_threads(vec, n)))
                 return {int(up(up(vectors, n), kWave) * kWave), n};
-    return {most, 0};
+    return {gradient ? kGradThreads : most, 0};
 }
 
 template <typename F> hipError_t with_row(const RowShape &r, F &&f) {
@@ -777,24 +792,29 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
         int64_t stride = x_feature > dy_feature ? x_feature : dy_feature;
         if (dx && dx_feature > stride) stride = dx_feature;
         const TileShape t = tile_shape(H, B, stride, kVec<T>, kTileThreads<T>, kMostHeld<T>, sizeof(T) == 4 ? 200 : 384);
-        const RowShape r = row_shape(H, kVec<T>, kGradThreads, kTeamFeatures / kVec<T>);
-        const bool teams = r.threads == kWave;
-        const int64_t tasks = rows ? teams ? up(B, kGradThreads / kWave) : B : up(B, int64_t(t.lanes) * t.vec);
-        const int most = rows && !teams ? kMaxRowBlocks : kMaxTileBlocks;
+        const RowShape r = row_shape(H, kVec<T>, kMaxThreads, kTeamFeatures / kVec<T>, true);
+        const bool waves = r.threads == kWave;
+        // Teams of a workgroup: of one wave each, or up to four of 256 threads at most where each
+        // has two rows or more.  (Two of 512, or rows that then spill, are slower by a tenth or more.)
+        int teams = waves ? kGradThreads / kWave : 1;
+        if (!waves && r.threads <= 256 && row_threads(kVec<T>, r.n) == kMaxThreads)
+            while (teams < 4 && B >= int64_t(2 * kMaxRowBlocks) * (teams + 1)) ++teams;
+        const int64_t tasks = rows ? up(B, teams) : up(B, int64_t(t.lanes) * t.vec);
+        const int most = rows && !waves ? kMaxRowBlocks : kMaxTileBlocks;
         const int blocks = tasks < most ? int(tasks) : most;
         if (dweight) a.dw = static_cast<float *>(workspace);
         if (dbias) a.db = reinterpret_cast<float *>(static_cast<char *>(workspace) + padded(blocks * H * 4));
         hipError_t e;
         if (rows) {
-            const dim3 grid{unsigned(blocks)}, threads{unsigned(teams ? kGradThreads : r.threads)};
+            const dim3 grid{unsigned(blocks)}, threads{unsigned(r.threads * teams)};
             e = with_row(r, [&](auto n) {
                 constexpr int N = decltype(n)::value, VT = kVec<T>;
                 if (H < VT)
-                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, 1, 1, true>), grid, threads, 0, s, a);
-                else if (teams && N > 0 && N * VT <= kTeamFeatures)
-                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, VT, N && N * VT <= kTeamFeatures ? N : 1, true>), grid, threads, 0, s, a);
+                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, 1, 1, true>), grid, threads, 0, s, a, r.threads);
+                else if (waves && N > 0 && N * VT <= kTeamFeatures)
+                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, VT, N && N * VT <= kTeamFeatures ? N : 1, true>), grid, threads, 0, s, a, r.threads);
                 else
-                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, VT, N, false>), grid, threads, 0, s, a);
+                    hipLaunchKernelGGL((norm_grad_rows_kernel<T, VT, N, false>), grid, threads, 0, s, a, r.threads);
                 return hipGetLastError();
             });
         } else {
