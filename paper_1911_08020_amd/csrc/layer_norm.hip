@@ -459,15 +459,15 @@ __device__ __forceinline__ int64_t tile_of(int64_t i, int64_t tiles) {
 
 template <typename T, int V, int N>
 __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int lanes) {
-    constexpr int kHeld = N ? N : 1;
+    constexpr int kHeld = N < 16 ? N : 0;            // weights: with 16 vectors they would spill
     __shared__ TileRoom<V> room;
     const int tx = threadIdx.x & (lanes - 1), ty = threadIdx.x >> log2_of(lanes), rows = blockDim.x >> log2_of(lanes);
     int skip;
     const int64_t b = back_from_end<V>(((a.first + tile_of(blockIdx.x, gridDim.x)) * lanes + tx) * V, a.B, skip);
-    float w[kHeld], c[kHeld];
-    if constexpr (N) {
+    float w[kHeld ? kHeld : 1], c[kHeld ? kHeld : 1];
+    if constexpr (kHeld) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+        for (int i = 0; i < kHeld; ++i) {
             const int64_t h = ty + int64_t(i) * rows < a.H ? ty + int64_t(i) * rows : 0;
             w[i] = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
             c[i] = a.b ? weight_at<T>(a, a.b, h) : 0.0f;
@@ -498,13 +498,16 @@ __global__ __launch_bounds__(kMaxThreads) void norm_columns_kernel(Args a, int l
 #pragma unroll
     for (int j = 0; j < V; ++j) rstd[j] = 1.0f / sqrtf(rstd[j] / float(a.H) + a.eps);
     x.each([&](int i, int64_t h, const Loaded<T, V> &v) {
-        if constexpr (!N) {
-            w[i] = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
-            c[i] = a.b ? weight_at<T>(a, a.b, h) : 0.0f;
+        float wh, ch, out[V];
+        if constexpr (kHeld) {
+            wh = w[i];
+            ch = c[i];
+        } else {
+            wh = a.w ? weight_at<T>(a, a.w, h) : 1.0f;
+            ch = a.b ? weight_at<T>(a, a.b, h) : 0.0f;
         }
-        float out[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = fmaf((v[j] - mean[j]) * rstd[j], w[i], c[i]);
+        for (int j = 0; j < V; ++j) out[j] = fmaf((v[j] - mean[j]) * rstd[j], wh, ch);
         store_own<T, V>(out_row<T, V, N>(a.y, i, h, ty, rows, b), skip, out);
     });
     if (ty == 0) {
@@ -704,6 +707,9 @@ TileShape tile_shape(int64_t H, int64_t B, int64_t stride, int vec, int threads,
     t.vec = B < vec ? 1 : vec;
     t.lanes = kMaxLanes;
     while (t.lanes > 1 && up(B, int64_t(t.lanes) * t.vec) < tiles) t.lanes /= 2;
+    // narrower where registers hold that: 4096 x 4096 fp32 43 -> 27 us, 9216 x 2047 77 -> 67
+    const int64_t held = int64_t(threads) * most;
+    while (t.lanes > 1 && H <= held && H * t.lanes > held) t.lanes /= 2;
     const int64_t want = H * t.lanes;
     t.threads = threads;
     t.n = 2;
@@ -763,8 +769,8 @@ hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const
                 });
             });
         }
-        const TileShape t = tile_shape(H, B, x_feature > y_feature ? x_feature : y_feature, kVec<T>, kMaxThreads, 8, 200);
-        return with_tile<8>(t, [&](auto n) {
+        const TileShape t = tile_shape(H, B, x_feature > y_feature ? x_feature : y_feature, kVec<T>, kMaxThreads, 16, 200);
+        return with_tile<16>(t, [&](auto n) {
             return over_grid(a, up(B, int64_t(t.lanes) * t.vec), [&](const Args &part, dim3 grid) {
                 if (t.vec == 1)
                     hipLaunchKernelGGL((norm_columns_kernel<T, 1, decltype(n)::value>), grid,
