@@ -612,6 +612,152 @@ __global__ __launch_bounds__(kTileThreads<T>) void norm_grad_columns_kernel(Args
     }
 }
 
+// ---- feature-major, many features of few tokens: the features cut too ------------------
+//
+// Where whole columns fit a workgroup only in tiles of a vector or two, 16 bytes of every cache
+// line, the features are cut into chunks: a first launch sums a chunk of kSplitTokens tokens (the
+// columns' two sums into `parts`, dw and db into partial rows of the token tile), a second one
+// adds the columns' sums and writes dx, reading x and dy again (from a cache, mostly).
+
+constexpr int kSplitTokens = 64, kSplitThreads = 256;
+
+struct SplitArgs {
+    Args n;                             // n.dw, n.db: partial sums [tiles][H]
+    float *parts;                       // [chunks][2][B]
+    int tiles, chunk;                   // chunk: features, a multiple of the rows of a workgroup
+};
+
+// f(round, feature, x, dy) for the thread's vectors of its chunk, kAtOnce loads of each together.
+template <typename T, int V, typename F>
+__device__ __forceinline__ void each_of_chunk(const SplitArgs &a, int64_t first, int ty, int64_t b, F &&f) {
+    constexpr int kRows = kSplitThreads / (kSplitTokens / V), kAtOnce = V > 4 ? 2 : 4;
+    const T *x = static_cast<const T *>(a.n.x.p) + b, *dy = static_cast<const T *>(a.n.dy.p) + b;
+    for (int r0 = 0; r0 < a.chunk; r0 += kRows * kAtOnce) {
+        Loaded<T, V> v[kAtOnce], g[kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            int64_t h = first + r0 + q * kRows + ty;
+            if (h >= a.n.H) h = a.n.H - 1;
+            v[q] = load_vec<T, V>(x + h * a.n.x.feature);
+            g[q] = load_vec<T, V>(dy + h * a.n.dy.feature);
+        }
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+            const int r = r0 + q * kRows + ty;
+            f(r, first + r, r < a.chunk && first + r < a.n.H, v[q], g[q]);
+        }
+    }
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kSplitThreads) void split_sums_kernel(SplitArgs a) {
+    constexpr int kLanes = kSplitTokens / V, kWaves = kSplitThreads / kWave, kMaxChunk = 256;
+    __shared__ float sums[2][kWaves][kSplitTokens], params[2][kMaxChunk];
+    const int tx = threadIdx.x % kLanes, ty = threadIdx.x / kLanes;
+    const int64_t task = tile_of(blockIdx.x, gridDim.x), c = task / a.tiles, tile = task - c * a.tiles;
+    int skip;
+    const int64_t b = back_from_end<V>(tile * kSplitTokens + tx * V, a.n.B, skip);
+    float mean[V], rstd[V], s[2][V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        mean[j] = a.n.mean[b + j];
+        rstd[j] = a.n.rstd[b + j];
+        s[0][j] = s[1][j] = 0.0f;
+    }
+    each_of_chunk<T, V>(a, c * a.chunk, ty, b, [&](int r, int64_t h, bool in, const Loaded<T, V> &v, const Loaded<T, V> &g) {
+        const float w = in ? a.n.w ? weight_at<T>(a.n, a.n.w, h) : 1.0f : 0.0f;
+        float fw = 0.0f, fb = 0.0f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float xh = (v[j] - mean[j]) * rstd[j], t = g[j] * w;
+            s[0][j] = in ? s[0][j] + t : s[0][j];
+            s[1][j] = in ? fmaf(t, xh, s[1][j]) : s[1][j];
+            fw = j >= skip ? fmaf(g[j], xh, fw) : fw;
+            fb = j >= skip ? fb + g[j] : fb;
+        }
+        fw = group_reduce<kLanes, AddOp>(fw);
+        fb = group_reduce<kLanes, AddOp>(fb);
+        if (tx == 0 && in) {
+            params[0][r] = fw;
+            params[1][r] = fb;
+        }
+    });
+    // over the lanes and waves that have the same tokens
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float t = kLanes == 16 ? sum_rows(s[k][j]) : sum_equal_lanes(s[k][j], kLanes);
+            if (lane_id() < kLanes) sums[k][wave_id()][tx * V + j] = t;
+        }
+    __syncthreads();
+    const int i = threadIdx.x % kSplitTokens, k = threadIdx.x / kSplitTokens;
+    if (k < 2) {
+        float t = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) t += sums[k][w][i];
+        // where lane i / V has its tokens
+        const int64_t own = tile * kSplitTokens + i / V * V, at = (own > a.n.B - V ? a.n.B - V : own) + i % V;
+        if (at >= own) a.parts[(c * 2 + k) * a.n.B + at] = t;
+    }
+    const int64_t h = c * a.chunk + threadIdx.x;
+    if (int(threadIdx.x) < a.chunk && h < a.n.H) {
+        if (a.n.dw) a.n.dw[tile * a.n.H + h] = params[0][threadIdx.x];
+        if (a.n.db) a.n.db[tile * a.n.H + h] = params[1][threadIdx.x];
+    }
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kSplitThreads) void split_dx_kernel(SplitArgs a, int chunks) {
+    constexpr int kLanes = kSplitTokens / V, kWaves = kSplitThreads / kWave;
+    __shared__ float sums[2][kWaves][kSplitTokens];
+    const int tx = threadIdx.x % kLanes, ty = threadIdx.x / kLanes;
+    const int64_t task = tile_of(blockIdx.x, gridDim.x), c = task / a.tiles, tile = task - c * a.tiles;
+    {
+        const int64_t token = tile * kSplitTokens + lane_id(), at = token < a.n.B ? token : a.n.B - 1;
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll 4
+        for (int k = wave_id(); k < chunks; k += kWaves) {
+            s0 += a.parts[int64_t(k) * 2 * a.n.B + at];
+            s1 += a.parts[(int64_t(k) * 2 + 1) * a.n.B + at];
+        }
+        sums[0][wave_id()][lane_id()] = s0;
+        sums[1][wave_id()][lane_id()] = s1;
+    }
+    int skip;
+    const int64_t b = back_from_end<V>(tile * kSplitTokens + tx * V, a.n.B, skip);
+    float mean[V], rstd[V], m0[V], m1[V];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        mean[j] = a.n.mean[b + j];
+        rstd[j] = a.n.rstd[b + j];
+        // what the lane leaves out may lie before the tile
+        const int64_t token = b + j - tile * kSplitTokens;
+        const int i = token < 0 ? 0 : int(token);
+        m0[j] = m1[j] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            m0[j] += sums[0][w][i];
+            m1[j] += sums[1][w][i];
+        }
+        m0[j] /= float(a.n.H);
+        m1[j] /= float(a.n.H);
+    }
+    T *dx = static_cast<T *>(a.n.y.p) + b;
+    each_of_chunk<T, V>(a, c * a.chunk, ty, b, [&](int, int64_t h, bool in, const Loaded<T, V> &v, const Loaded<T, V> &g) {
+        if (!in) return;
+        const float w = a.n.w ? weight_at<T>(a.n, a.n.w, h) : 1.0f;
+        float out[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float xh = (v[j] - mean[j]) * rstd[j];
+            out[j] = rstd[j] * (g[j] * w - m0[j] - xh * m1[j]);
+        }
+        store_own<T, V>(dx + h * a.n.y.feature, skip, out);
+    });
+}
+
 // ---- the partial sums of dw and db -----------------------------------------------------
 
 constexpr int kSumFeatures = 32, kSumSlices = 32;    // a cache line a row
@@ -742,6 +888,15 @@ template <typename F> hipError_t over_grid(Args a, int64_t n, F &&launch) {
 
 bool rows_of(int64_t H, int64_t feature) { return H == 1 || feature == 1; }
 
+// A feature-major gradient whose features are cut: 9216 x 64 fp32 35 -> 13 us, 9216 x 700 66 ->
+// 31 (bf16 78 -> 22), 4096 x 700 23 -> 16; from here on no size measured is slower by more than a
+// twentieth, below (1024 x 700 fp32 11.8 -> 12.5) the third launch costs more.  The workspace, 8
+// bytes a feature and token of up to 512, holds the parts (chunks of 64 features at least) and a
+// partial row per 64 tokens.
+bool is_split(int64_t H, int64_t B, int vec) {
+    return B >= 8 && B <= 8192 && (H > 2048 || (vec > 4 && H > 1024 && B >= 128));
+}
+
 }  // namespace
 
 int64_t layer_norm_workspace_bytes(int64_t H, int64_t B) {
@@ -811,6 +966,28 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
         if (dweight) a.dw = static_cast<float *>(workspace);
         if (dbias) a.db = reinterpret_cast<float *>(static_cast<char *>(workspace) + padded(blocks * H * 4));
         hipError_t e;
+        if (!rows && is_split(H, B, kVec<T>)) {
+            SplitArgs p{a, nullptr, int(up(B, kSplitTokens)), 256};
+            while (p.chunk > 64 && up(H, p.chunk) * p.tiles < 512) p.chunk /= 2;
+            const int64_t chunks = up(H, p.chunk);
+            float *next = static_cast<float *>(workspace);
+            p.parts = next;
+            next += padded(chunks * 2 * B * 4) / 4;
+            p.n.dw = dweight ? next : nullptr;
+            next += padded(p.tiles * H * 4) / 4;
+            p.n.db = dbias ? next : nullptr;
+            const dim3 grid{unsigned(chunks * p.tiles)};
+            hipLaunchKernelGGL((split_sums_kernel<T, kVec<T>>), grid, dim3(kSplitThreads), 0, s, p);
+            e = hipGetLastError();
+            if (e == hipSuccess && dx) {
+                hipLaunchKernelGGL((split_dx_kernel<T, kVec<T>>), grid, dim3(kSplitThreads), 0, s, p, int(chunks));
+                e = hipGetLastError();
+            }
+            if (e != hipSuccess || (!dweight && !dbias)) return e;
+            hipLaunchKernelGGL(sum_partials_kernel, dim3(unsigned(up(H, kSumFeatures))),
+                               dim3(kSumFeatures * kSumSlices), 0, s, p.n.dw, p.n.db, H, p.tiles, dweight, dbias);
+            return hipGetLastError();
+        }
         if (rows) {
             const dim3 grid{unsigned(blocks)}, threads{unsigned(r.threads * teams)};
             e = with_row(r, [&](auto n) {
