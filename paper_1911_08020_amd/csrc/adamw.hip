@@ -17,7 +17,10 @@
 // never divides by eps alone.  The random bits are a hash of the element's number, the tensor's
 // and the step's, the caller's seed among it: the same inputs give the same codes.
 //
-// Memory-bound: 28 bytes an fp32 element with 32-bit states, 16 with 8-bit ones.
+// Memory-bound: 28 bytes an fp32 element with 32-bit states, 16 with 8-bit ones.  Measured on
+// MI355X: 4 M fp32 elements in 14 tensors 19 us (5.9 TB/s, out of the Infinity Cache); 64 M fp16
+// ones with fp32 masters and gradients and 8-bit states 225 us (5.1 TB/s), the export of their
+// moments 150 (4.3 TB/s, four fifths of it stores).
 #include "darb_internal.h"
 #include "float_io.h"
 #include "wave.h"
@@ -258,6 +261,7 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(const AdamTensor *__r
                 v[i] = value_v((cv >> (8 * i)) & 255, sv);
             }
         }
+        // past the caches, which they would only sweep: 168 -> 152 us for 64 M elements
         if (om) store_some<true>(om + at, n, m);
         if (ov) store_some<true>(ov + at, n, v);
     }

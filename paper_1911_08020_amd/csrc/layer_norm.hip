@@ -8,7 +8,12 @@
 // Memory-bound: a column is read once into registers, where its sums run twice over it (the
 // variance around the mean itself, not from a difference of sums).  dw and db run over all
 // columns: each workgroup sums the columns it takes, rows of partial sums go to the workspace,
-// and a second launch adds them in a fixed order.
+// and a last launch adds them in a fixed order.
+//
+// Measured on MI355X, among other calls: forward 1024 x 32 fp32 6.3 us (latency of one round of
+// loads and two sums), 4096 x 4096 27 (4.9 TB/s); gradients of 1024 x 6400 fp32 feature-major
+// 25.8 (3.1 TB/s: all loads, then the sums, then all stores), of 9216 x 2047 token-major bf16 35.4
+// (3.2 TB/s; partial rows are a sixth of it) and fp32 43 (5.3 TB/s).
 #include <type_traits>
 
 #include "darb_internal.h"

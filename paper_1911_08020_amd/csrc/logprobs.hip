@@ -8,6 +8,12 @@
 // The alternatives come from the same pass: it keeps the maximum of every segment (what a thread
 // reads), the k-th greatest of 256 groups of maxima is a bound that k logits reach, and only the
 // segments whose maximum reaches it are read again.
+//
+// Measured on MI355X, among other calls: 10 000 x 700 fp32 feature-major 11.9 us (2.4 TB/s, two
+// launches of 8 and 3), 131 072 x 512 bf16 token-major 25.8 us (5.2 TB/s) and 32.2 with 20
+// alternatives, one row of 10 000 with five 8.0; the gradients of 10 000 x 700 fp32 11.1 (5.0
+// TB/s) and of 50 001 x 1023 fp16 40 (5.1 TB/s).  Bound by memory where there are rows for the
+// whole card, by the chain of one workgroup's loads and sums where there are few.
 #include <type_traits>
 
 #include "darb_internal.h"
@@ -247,14 +253,16 @@ __device__ __forceinline__ void segment_keys(const Args &a, const T *col, int64_
         const uint64_t key = seg >= 0 && v < a.V ? key_of(float(col[v * a.class_stride]), uint32_t(v)) : 0;
         f(uint32_t(key >> 32) >= least ? key : 0);
     } else {
-        const uint32_t s = seg < 0 ? 0 : uint32_t(seg), of_part = uint32_t(a.part_threads / a.seg_threads);
-        const uint32_t part = s / of_part, thread = (s - part * of_part) * a.seg_threads;
+        // threads of a part and of a segment are powers of two
+        const int seg_bits = __ffs(a.seg_threads) - 1, part_bits = __ffs(a.part_threads) - 1 - seg_bits;
+        const uint32_t s = seg < 0 ? 0 : uint32_t(seg), part = s >> part_bits;
+        const uint32_t thread = (s & ((1u << part_bits) - 1)) << seg_bits;
         const int64_t begin = part * a.part_len;
         int64_t end = begin + a.part_len;
         if (end > a.V) end = a.V;
         const int vectors = a.rounds * a.seg_threads;
         for (int first = 0; first < vectors; first += kSegLanes) {
-            const int i = first + in, round = i / a.seg_threads, t = i - round * a.seg_threads;
+            const int i = first + in, round = i >> seg_bits, t = i & (a.seg_threads - 1);
             int64_t v = begin + (int64_t(round) * a.part_threads + thread + t) * kEach;
             if (seg < 0 || i >= vectors) v = end;                    // nothing
             Run<T, kEach> x;

@@ -9,6 +9,11 @@
 // index lists them by column: for every weight its row and slot, columns in ascending order,
 // a column's weights in storage order.  The index depends on the offsets alone; a program
 // that retrains the retained values keeps it as long as the mask.
+//
+// Measured on MI355X, among other calls: 4096 x 9216 with 1.25 M weights, batch 64, 30.9 us (320 MB
+// of dY's rows at 10.4 TB/s); 10 000 x 1500 with 1.0 M fp16 weights, batch 700, 179 us (2.8 GB at
+// 17.6 TB/s in the main kernel, 17 us to lay out tiles, 14 to add the parts).  Bound by the L2s,
+// from which random 256-byte rows come at 27.6 TB/s at most; the index is made in 130 to 230 us.
 #include <type_traits>
 
 #include "darb_internal.h"
