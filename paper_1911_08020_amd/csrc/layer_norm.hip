@@ -899,7 +899,8 @@ bool rows_of(int64_t H, int64_t feature) { return H == 1 || feature == 1; }
 // bytes a feature and token of up to 512, holds the parts (chunks of 64 features at least) and a
 // partial row per 64 tokens.
 bool is_split(int64_t H, int64_t B, int vec) {
-    return B >= 8 && B <= 8192 && (H > 2048 || (vec > 4 && H > 1024 && B >= 128));
+    const bool fits = up(H, 256) * up(B, kSplitTokens) < 1 << 24;    // a launch has below 2^32 threads
+    return fits && B >= 8 && B <= 8192 && (H > 2048 || (vec > 4 && H > 1024 && B >= 128));
 }
 
 }  // namespace
