@@ -28,6 +28,7 @@ The library must have been built (``python paper_1911_08020_amd/build.py`` or
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Tuple
@@ -208,6 +209,32 @@ def _stream_ptr(stream=None):
             return ctypes.c_void_p(p)
         stream = _torch().cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _memory_of(stream):
+    """The context in which a call on a given stream allocates: that stream's own memory.  Blocks
+    of the current stream may still be in use by work that is queued there, which the given stream
+    does not wait for."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return _torch().cuda.stream(_as_stream(stream))
+
+
+def _as_stream(stream):
+    cuda = _torch().cuda
+    return stream if isinstance(stream, cuda.Stream) else cuda.ExternalStream(stream.cuda_stream)
+
+
+def _used_on(stream, *ts):
+    """What a call on a given stream leaves with its caller, given or new: the memory is not handed
+    out again before that stream is done with it, nor before the current one is, on which the caller
+    may go on with it."""
+    if stream is not None:
+        streams = _as_stream(stream), _torch().cuda.current_stream()
+        for t in ts:
+            if t is not None:
+                for s in streams:
+                    t.record_stream(s)
 
 
 def _dtype_code(t) -> int:
@@ -531,13 +558,13 @@ class Plan:
         need = ctypes.c_int64()
         _check(_lib.darb_transpose_bytes(self._h, ctypes.byref(need)), "darb_transpose_bytes")
         if index is None:
-            index = torch.empty(need.value, dtype=torch.uint8, device=offsets.device)
+            with _memory_of(stream):
+                index = torch.empty(need.value, dtype=torch.uint8, device=offsets.device)
         _require_cuda(index)
         _check_format(index, need.value, "index", (torch.uint8,))
         _check(_lib.darb_transpose(self._h, _ptr(offsets), _ptr(index), index.numel(),
                                    _stream_ptr(stream)), "darb_transpose")
-        if stream is not None:
-            index.record_stream(stream)
+        _used_on(stream, index)
         return index
 
     def spmm_grad(self, index, values, X, dY, dvalues=None, dX=None, need_values=True,
@@ -567,7 +594,8 @@ class Plan:
             self._check_values(values)
             wcode = _dtype_code(values)
             if dX is None:
-                dX = torch.empty((self.N, B), dtype=torch.float32, device=dY.device)
+                with _memory_of(stream):
+                    dX = torch.empty((self.N, B), dtype=torch.float32, device=dY.device)
             _require_cuda(dX)
             if dX.dtype != torch.float32:
                 raise TypeError("dX must be fp32")
@@ -579,14 +607,16 @@ class Plan:
             if not need_X and xcode == F16:
                 wcode = F16                 # the values' type does not matter
             if dvalues is None:
-                dvalues = torch.empty(self.nnz, dtype=torch.float32, device=dY.device)
+                with _memory_of(stream):
+                    dvalues = torch.empty(self.nnz, dtype=torch.float32, device=dY.device)
             _require_cuda(dvalues)
             _check_format(dvalues, self.nnz, "dvalues", (torch.float32,))
         _check(_lib.darb_spmm_grad_workspace(self._h, B, ctypes.byref(need)),
                "darb_spmm_grad_workspace")
         if need.value:
             if workspace is None:
-                workspace = torch.empty(need.value, dtype=torch.uint8, device=dY.device)
+                with _memory_of(stream):
+                    workspace = torch.empty(need.value, dtype=torch.uint8, device=dY.device)
             _require_cuda(workspace)
             _check_format(workspace, need.value, "workspace", (torch.uint8,))
         _check(_lib.darb_spmm_grad(self._h, _ptr(index), wcode, _ptr(values) if need_X else None,
@@ -596,10 +626,7 @@ class Plan:
                                    None if workspace is None else _ptr(workspace),
                                    0 if workspace is None else workspace.numel(),
                                    _stream_ptr(stream)), "darb_spmm_grad")
-        if stream is not None:              # allocated on the current stream, used on this one
-            for t in (workspace, dvalues if need_values else None, dX if need_X else None):
-                if t is not None:
-                    t.record_stream(stream)
+        _used_on(stream, workspace, dvalues if need_values else None, dX if need_X else None)
         return (dvalues if need_values else None), (dX if need_X else None)
 
     # -- argument checks --------------------------------------------------------------

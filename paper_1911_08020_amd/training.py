@@ -4,14 +4,17 @@ Argument marshalling for the calls of include/darb.h.  Activations are [features
 either memory order: contiguous along the batch, as the products' X and Y are, or along the
 features, as the transposed view of a [batch, features] tensor is.  Results that have the
 shape of an input come in its order.
+
+A call on a given stream takes its results and workspace from that stream's memory.  Its inputs
+are the caller's to have ready for that stream, and to keep until it is done with them.
 """
 from __future__ import annotations
 
 import ctypes
 from typing import NamedTuple, Optional
 
-from . import (BF16, F16, F32, _AdamTensor, _check, _check_format, _lib, _native, _ptr,
-               _stream_ptr, _torch)
+from . import (BF16, F16, F32, _AdamTensor, _check, _check_format, _lib, _memory_of, _native,
+               _ptr, _stream_ptr, _torch, _used_on)
 
 
 class TokenLogprobs(NamedTuple):
@@ -67,15 +70,6 @@ def _empty_like(t):
     return torch.empty((F, B), dtype=t.dtype, device=t.device)
 
 
-def _used_on(stream, *ts):
-    """Tensors allocated on the current stream and used on a given one: their memory is not
-    handed out again before that stream's work is done."""
-    if stream is not None:
-        for t in ts:
-            if t is not None:
-                t.record_stream(stream)
-
-
 def _vector(t, n: int, name: str, dtype=None):
     torch = _torch()
     _require_cuda(t)
@@ -120,11 +114,12 @@ def token_logprobs(logits, targets=None, top: int = 0, workspace=None, stream=No
     top = int(top)
     dev = logits.device
     tp = _optional(targets, B, "targets", torch.int64)
-    workspace = _workspace(_lib.darb_token_logprobs_workspace, "darb_token_logprobs_workspace",
-                           dev, workspace, code, V, B, fs, bs, top)
-    out = torch.empty((3, B), dtype=torch.float32, device=dev)
-    tl = torch.empty((B, top), dtype=torch.float32, device=dev) if top else None
-    ti = torch.empty((B, top), dtype=torch.int64, device=dev) if top else None
+    with _memory_of(stream):
+        workspace = _workspace(_lib.darb_token_logprobs_workspace, "darb_token_logprobs_workspace",
+                               dev, workspace, code, V, B, fs, bs, top)
+        out = torch.empty((3, B), dtype=torch.float32, device=dev)
+        tl = torch.empty((B, top), dtype=torch.float32, device=dev) if top else None
+        ti = torch.empty((B, top), dtype=torch.int64, device=dev) if top else None
     base = out.data_ptr()
     _check(_lib.darb_token_logprobs(code, V, B, _ptr(logits), fs, bs, tp, top,
                                     ctypes.c_void_p(base), ctypes.c_void_p(base + 4 * B),
@@ -152,7 +147,8 @@ def token_logprobs_grad(logits, targets, lse, grad_logprob=None, entropy=None, g
     fs, bs = _matrix(logits, "logits")
     V, B = logits.shape
     if out is None:
-        out = _empty_like(logits)
+        with _memory_of(stream):
+            out = _empty_like(logits)
     _require_cuda(out)
     ofs, obs = _matrix(out, "out", logits)
     _check(_lib.darb_token_logprobs_grad(
@@ -190,14 +186,15 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, y=None, mean=None, 
     if wt is not None and bt is not None and wt != bt:
         raise TypeError("weight and bias must have one dtype")
     wdtype = wt or bt or torch.float32
-    if y is None:
-        y = _empty_like(x)
+    with _memory_of(stream):
+        if y is None:
+            y = _empty_like(x)
+        if mean is None:
+            mean = torch.empty(B, dtype=torch.float32, device=x.device)
+        if rstd is None:
+            rstd = torch.empty(B, dtype=torch.float32, device=x.device)
     _require_cuda(y)
     yfs, ybs = _matrix(y, "y", x)
-    if mean is None:
-        mean = torch.empty(B, dtype=torch.float32, device=x.device)
-    if rstd is None:
-        rstd = torch.empty(B, dtype=torch.float32, device=x.device)
     _check(_lib.darb_layer_norm(code, F32 if wdtype == torch.float32 else code, H, B, _ptr(x), fs,
                                 bs, wp, bp, float(eps), _ptr(y), yfs, ybs,
                                 _vector(mean, B, "mean"), _vector(rstd, B, "rstd"),
@@ -222,18 +219,18 @@ def layer_norm_grad(dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias
     H, B = x.shape
     wp, wt = _norm_weight(weight, x, H, "weight")
     dfs = dbs = 0
-    if need_x:
-        if dx is None:
+    with _memory_of(stream):
+        if need_x and dx is None:
             dx = _empty_like(x)
+        if need_params and dweight is None:
+            dweight = torch.empty(H, dtype=torch.float32, device=x.device)
+        if need_params and dbias is None:
+            dbias = torch.empty(H, dtype=torch.float32, device=x.device)
+        workspace = _workspace(_lib.darb_layer_norm_workspace, "darb_layer_norm_workspace",
+                               x.device, workspace, H, B)
+    if need_x:
         _require_cuda(dx)
         dfs, dbs = _matrix(dx, "dx", x)
-    if need_params:
-        if dweight is None:
-            dweight = torch.empty(H, dtype=torch.float32, device=x.device)
-        if dbias is None:
-            dbias = torch.empty(H, dtype=torch.float32, device=x.device)
-    workspace = _workspace(_lib.darb_layer_norm_workspace, "darb_layer_norm_workspace", x.device,
-                           workspace, H, B)
     _check(_lib.darb_layer_norm_grad(
         code, F32 if wt in (None, torch.float32) else code, H, B, _ptr(dy), gfs, gbs, _ptr(x), fs,
         bs, _vector(mean, B, "mean"), _vector(rstd, B, "rstd"), wp, _ptr(dx) if need_x else None,
@@ -374,8 +371,9 @@ class AdamW:
         """(list of m, list of v): the values that the states stand for, fp32, flat."""
         torch = _torch()
         if out is None:
-            out = tuple([torch.empty(p.numel(), dtype=torch.float32, device=p.device)
-                         for p in self.params] for _ in range(2))
+            with _memory_of(stream):
+                out = tuple([torch.empty(p.numel(), dtype=torch.float32, device=p.device)
+                             for p in self.params] for _ in range(2))
         if _native.adamw_moments(self._h.value, self.params, out[0], out[1], stream):
             _used_on(stream, *out[0], *out[1])
             return out
