@@ -97,3 +97,30 @@ def test_a_stream_that_torch_does_not_know(darb, pair):  # noqa: F811
         got = CALLS[name](darb, pair[0], stream=Handle(st))
         torch.cuda.synchronize()
         assert same(flat(got), want), name
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_made_for_a_given_stream(darb, busy, bits):  # noqa: F811
+    """The masters and the first states are there when the given stream's first step reads them."""
+    say(f"adamw made for a given stream: {bits} bits")
+    sizes = [70000, 257, 1]
+    start = [torch.randn(n, device="cuda").half() for n in sizes]
+    grads = [torch.randn(n, device="cuda") for n in sizes]
+    p = [t.clone() for t in start]
+    want = darb.AdamW(p, masters=True, state_bits=bits)
+    want.step(grads)
+    want = copies([p, want.masters, want.moments()])
+    p = [t.clone() for t in start]
+    st = torch.cuda.Stream()
+    # memory that is handed out again holds no zeros
+    for n in sizes:
+        for kind in (torch.float32, torch.uint8):
+            junk = [torch.full((n,), 77, dtype=kind, device="cuda") for _ in range(4)]
+            del junk
+    torch.cuda.synchronize()
+    busy.queue()
+    opt = darb.AdamW(p, masters=True, state_bits=bits, stream=st)
+    opt.step(grads, stream=st)
+    got = flat([p, opt.masters, opt.moments(stream=st)])
+    torch.cuda.synchronize()
+    assert same(got, want)
