@@ -310,6 +310,20 @@ class AdamW:
                                           self.workspace.numel(), _stream_ptr(stream),
                                           ctypes.byref(h)), "darb_adamw_create")
         self._h = h
+        self._streams = set()               # that _hold_on was told of
+
+    def _hold_on(self, stream):
+        """The table, states, masters and parameters are in use on this stream (None: the current
+        one): dropping the optimizer does not hand them out before its work there is done."""
+        at = _native.current_stream() if stream is None else stream.cuda_stream
+        if at not in self._streams:
+            torch = _torch()
+            s = torch.cuda.current_stream() if stream is None else _as_stream(stream)
+            for t in [self.workspace, *self.params, *self.masters,
+                      *(t for state in self.state_tensors for t in state)]:
+                if t is not None:
+                    t.record_stream(s)
+            self._streams.add(at)
 
     def __del__(self, _destroy=_lib.darb_adamw_destroy):
         h = getattr(self, "_h", None)
@@ -350,6 +364,7 @@ class AdamW:
         t = self.steps + 1
         seed = (self.seed + t * 0x6A09E667) & 0xFFFFFFFF
         lr = self.lr if lr is None else float(lr)
+        self._hold_on(stream)
         if _native.adamw_step(self._h.value, self.params, grads, lr, *self.betas, self.eps, t,
                               grad_scale, seed, stream):
             self.steps = t
@@ -374,6 +389,7 @@ class AdamW:
     def moments(self, out=None, stream=None):
         """(list of m, list of v): the values that the states stand for, fp32, flat."""
         torch = _torch()
+        self._hold_on(stream)
         if out is None:
             with _memory_of(stream):
                 out = tuple([torch.empty(p.numel(), dtype=torch.float32, device=p.device)

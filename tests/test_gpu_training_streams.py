@@ -124,3 +124,36 @@ def test_adamw_made_for_a_given_stream(darb, busy, bits):  # noqa: F811
     got = flat([p, opt.masters, opt.moments(stream=st)])
     torch.cuda.synchronize()
     assert same(got, want)
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_adamw_dropped_before_its_step_is_done(darb, busy, given):  # noqa: F811
+    """The step's table, states and masters are not handed out while its stream still needs them."""
+    say(f"adamw dropped: stream {'given' if given else 'current'}")
+    sizes = [70000, 257]
+    start = [torch.randn(n, device="cuda").half() for n in sizes]
+    grads = [torch.randn(n, device="cuda") for n in sizes]
+    p = [t.clone() for t in start]
+    darb.AdamW(p, masters=True, lr=0.1).step(grads)
+    want = copies(p)
+    p = [t.clone() for t in start]
+    opt = darb.AdamW(p, masters=True, lr=0.1)
+    held = [opt.workspace, *opt.masters, *flat(opt.state_tensors)]
+    ranges = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in held]
+    like = [(t.shape, t.dtype) for t in held]
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        busy.queue()
+        if not given:
+            opt.step(grads)
+    if given:
+        opt.step(grads, stream=st)
+    del opt, held
+    new = [torch.empty(shape, dtype=dtype, device="cuda") for shape, dtype in like * 3]
+    for t in new:
+        begin, end = t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()
+        assert all(end <= a or b <= begin for a, b in ranges)
+        t.fill_(85)
+    torch.cuda.synchronize()
+    assert same(p, want)
