@@ -512,7 +512,7 @@ int darb_spmm_grad(const darb_plan *plan, const void *index, int wdtype, const v
  *   decay       the tensor's weight decay, >= 0
  * darb_adamw_step:
  *   grads       host array of `count` device pointers, [n] of the type in gdtypes; NULL: the
- *               tensor is left as it is
+ *               tensor is left as it is (and its entry of gdtypes is not read)
  *   grad_scale  device fp32 [1] or NULL (1)
  *   lr >= 0, 0 <= beta1, beta2 < 1, eps >= 0, step >= 1
  * darb_adamw_moments writes the values that the states stand for: host arrays of `count`

@@ -282,6 +282,7 @@ hipError_t launch_adamw(int bits, const AdamTensor *tensors, const AdamTile *til
                     c.grad_scale, c.seed};
     Grads g{};
     for (int i = 0; i < count; ++i) {
+        if (!grads[i]) continue;                     // its type may be anything
         g.p[i] = grads[i];
         g.type[i / 16] |= uint32_t(types[i]) << (i % 16 * 2);
     }
