@@ -42,13 +42,15 @@ struct Strides {
 bool as_rows(const Strides &s, int64_t F, int64_t B) { return F == 1 || (s.feature == 1 && (B == 1 || s.batch >= F)); }
 bool as_columns(const Strides &s, int64_t F, int64_t B) { return B == 1 || (s.batch == 1 && (F == 1 || s.feature >= B)); }
 
-// All operands in one order, or an error.  Sets the unused strides of that order.
-int common_order(Strides *s, int count, int64_t F, int64_t B, const char *where) {
+// All operands in one order, or an error.  Sets the unused strides of that order.  (One token's
+// operands may each have their own feature stride: where one is not 1, all go by columns.)
+int common_order(Strides *s, int count, int64_t F, int64_t B, const char *where, bool *by_rows) {
     bool rows = true, columns = true;
     for (int i = 0; i < count; ++i) {
         rows = rows && as_rows(s[i], F, B);
         columns = columns && as_columns(s[i], F, B);
     }
+    *by_rows = rows;
     if (!rows && !columns)
         return fail(DARB_E_INVALID, std::string(where) + ": one stride must be 1, along the same "
                                     "axis in every operand, and the other at least that axis' length");
@@ -137,13 +139,13 @@ using namespace darb;
 
 extern "C" {
 
-static int check_logits(int zdtype, int64_t V, int64_t B, int64_t top, Strides *s) {
+static int check_logits(int zdtype, int64_t V, int64_t B, int64_t top, Strides *s, bool *rows) {
     int rc = check_sizes(V, B, "V");
     if (rc) return rc;
     if (!float_dtype(zdtype)) return fail(DARB_E_DTYPE, "unknown logit dtype");
     if (top < 0 || top > logprobs_max_top() || top > V)
         return fail(DARB_E_INVALID, "top must be in [0, 64] and at most V");
-    return common_order(s, 1, V, B, "z");
+    return common_order(s, 1, V, B, "z", rows);
 }
 
 int darb_token_logprobs_workspace(int zdtype, int64_t V, int64_t B, int64_t z_feature_stride,
@@ -151,9 +153,10 @@ int darb_token_logprobs_workspace(int zdtype, int64_t V, int64_t B, int64_t z_fe
     clear_error();
     if (!bytes) return fail(DARB_E_INVALID, "bytes is NULL");
     Strides s[1] = {{z_feature_stride, z_batch_stride}};
-    int rc = check_logits(zdtype, V, B, top, s);
+    bool rows;
+    int rc = check_logits(zdtype, V, B, top, s, &rows);
     if (rc) return rc;
-    *bytes = logprobs_workspace_bytes(zdtype, V, B, s[0].feature, top);
+    *bytes = logprobs_workspace_bytes(zdtype, V, B, rows, top);
     return DARB_OK;
 }
 
@@ -164,15 +167,16 @@ int darb_token_logprobs(int zdtype, int64_t V, int64_t B, const void *z, int64_t
                         void *stream) {
     clear_error();
     Strides s[1] = {{z_feature_stride, z_batch_stride}};
-    int rc = check_logits(zdtype, V, B, top, s);
+    bool rows;
+    int rc = check_logits(zdtype, V, B, top, s, &rows);
     if (rc) return rc;
     if (!z || !logprob || !entropy || !lse || (top && (!top_logprob || !top_index)))
         return fail(DARB_E_INVALID, "NULL buffer");
     if (!aligned(z, size_of(zdtype)) || !aligned(targets, 8) || !aligned(top_index, 8))
         return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
-    const int64_t need = logprobs_workspace_bytes(zdtype, V, B, s[0].feature, top);
+    const int64_t need = logprobs_workspace_bytes(zdtype, V, B, rows, top);
     if (need > 0 && (rc = check_workspace(workspace, workspace_bytes, need))) return rc;
-    return launched(launch_logprobs(zdtype, V, B, z, s[0].feature, s[0].batch, targets, top,
+    return launched(launch_logprobs(zdtype, V, B, rows, z, s[0].feature, s[0].batch, targets, top,
                                     logprob, entropy, lse, top_logprob, top_index, workspace,
                                     static_cast<hipStream_t>(stream)), "token logprobs launch");
 }
@@ -194,9 +198,10 @@ int darb_token_logprobs_grad(int zdtype, int64_t V, int64_t B, const void *z,
     if (!aligned(z, size_of(zdtype)) || !aligned(dz, size_of(zdtype)) || !aligned(targets, 8))
         return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
     Strides s[2] = {{z_feature_stride, z_batch_stride}, {dz_feature_stride, dz_batch_stride}};
-    rc = common_order(s, 2, V, B, "z, dz");
+    bool rows;
+    rc = common_order(s, 2, V, B, "z, dz", &rows);
     if (rc) return rc;
-    return launched(launch_logprobs_grad(zdtype, V, B, z, s[0].feature, s[0].batch, targets, lse,
+    return launched(launch_logprobs_grad(zdtype, V, B, rows, z, s[0].feature, s[0].batch, targets, lse,
                                          grad_logprob, entropy, grad_entropy, dz, s[1].feature,
                                          s[1].batch, static_cast<hipStream_t>(stream)),
                     "token logprobs gradient launch");
@@ -228,9 +233,10 @@ int darb_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const void *x,
         return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
     if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(DARB_E_INVALID, "eps must be finite and >= 0");
     Strides s[2] = {{x_feature_stride, x_batch_stride}, {y_feature_stride, y_batch_stride}};
-    rc = common_order(s, 2, H, B, "x, y");
+    bool rows;
+    rc = common_order(s, 2, H, B, "x, y", &rows);
     if (rc) return rc;
-    return launched(launch_layer_norm(xdtype, wdtype, H, B, x, s[0].feature, s[0].batch, weight,
+    return launched(launch_layer_norm(xdtype, wdtype, H, B, rows, x, s[0].feature, s[0].batch, weight,
                                       bias, float(eps), y, s[1].feature, s[1].batch, mean, rstd,
                                       static_cast<hipStream_t>(stream)), "layer norm launch");
 }
@@ -260,11 +266,12 @@ int darb_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, const voi
         return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
     Strides s[3] = {{x_feature_stride, x_batch_stride}, {dy_feature_stride, dy_batch_stride},
                     {dx_feature_stride, dx_batch_stride}};
-    rc = common_order(s, dx ? 3 : 2, H, B, "x, dy, dx");
+    bool rows;
+    rc = common_order(s, dx ? 3 : 2, H, B, "x, dy, dx", &rows);
     if (rc) return rc;
     rc = check_workspace(workspace, workspace_bytes, layer_norm_workspace_bytes(H, B));
     if (rc) return rc;
-    return launched(launch_layer_norm_grad(xdtype, wdtype, H, B, dy, s[1].feature, s[1].batch, x,
+    return launched(launch_layer_norm_grad(xdtype, wdtype, H, B, rows, dy, s[1].feature, s[1].batch, x,
                                            s[0].feature, s[0].batch, mean, rstd, weight, dx,
                                            s[2].feature, s[2].batch, dweight, dbias, workspace,
                                            static_cast<hipStream_t>(stream)),

@@ -165,27 +165,28 @@ hipError_t launch_plan_device(int64_t M, int64_t N, const int64_t *counts, int64
                               int lmin, int lmax, int32_t *perm, int64_t *rowinfo, void *scratch,
                               hipStream_t s);
 // ---- evaluating and retraining a layer ----
-// Log probabilities and their gradient.  One of the strides of z is 1 (the class stride, or
-// else the token stride), and dz's is the same one; V = 1 and B = 1 go either way.
+// `rows`: a token's elements are contiguous in every operand (class or feature strides of 1), or
+// else a class's tokens are (token strides of 1, or one token).
+// Log probabilities and their gradient.
 int64_t logprobs_max_top();
-int64_t logprobs_workspace_bytes(int dtype, int64_t V, int64_t B, int64_t class_stride, int64_t top);
-hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64_t class_stride,
-                           int64_t token_stride, const int64_t *targets, int64_t top,
-                           float *logprob, float *entropy, float *lse, float *top_logprob,
+int64_t logprobs_workspace_bytes(int dtype, int64_t V, int64_t B, bool rows, int64_t top);
+hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, bool rows, const void *z,
+                           int64_t class_stride, int64_t token_stride, const int64_t *targets,
+                           int64_t top, float *logprob, float *entropy, float *lse, float *top_logprob,
                            int64_t *top_index, void *workspace, hipStream_t s);
-hipError_t launch_logprobs_grad(int dtype, int64_t V, int64_t B, const void *z,
+hipError_t launch_logprobs_grad(int dtype, int64_t V, int64_t B, bool rows, const void *z,
                                 int64_t class_stride, int64_t token_stride,
                                 const int64_t *targets, const float *lse,
                                 const float *grad_logprob, const float *entropy,
                                 const float *grad_entropy, void *dz, int64_t out_class_stride,
                                 int64_t out_token_stride, hipStream_t s);
 int64_t layer_norm_workspace_bytes(int64_t H, int64_t B);
-hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const void *x,
-                             int64_t x_feature, int64_t x_token, const void *weight,
+hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, bool rows,
+                             const void *x, int64_t x_feature, int64_t x_token, const void *weight,
                              const void *bias, float eps, void *y, int64_t y_feature,
                              int64_t y_token, float *mean, float *rstd, hipStream_t s);
-hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, const void *dy,
-                                  int64_t dy_feature, int64_t dy_token, const void *x,
+hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, bool rows,
+                                  const void *dy, int64_t dy_feature, int64_t dy_token, const void *x,
                                   int64_t x_feature, int64_t x_token, const float *mean,
                                   const float *rstd, const void *weight, void *dx,
                                   int64_t dx_feature, int64_t dx_token, float *dweight,

@@ -891,8 +891,6 @@ template <typename F> hipError_t over_grid(Args a, int64_t n, F &&launch) {
     return hipSuccess;
 }
 
-bool rows_of(int64_t H, int64_t feature) { return H == 1 || feature == 1; }
-
 // A feature-major gradient whose features are cut: 9216 x 64 fp32 35 -> 13 us, 9216 x 700 66 ->
 // 31 (bf16 78 -> 22), 4096 x 700 23 -> 16; from here on no size measured is slower by more than a
 // twentieth, below (1024 x 700 fp32 11.8 -> 12.5) the third launch costs more.  The workspace, 8
@@ -910,15 +908,15 @@ int64_t layer_norm_workspace_bytes(int64_t H, int64_t B) {
     return 2 * padded(blocks * H * 4);
 }
 
-hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const void *x,
-                             int64_t x_feature, int64_t x_token, const void *weight,
+hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, bool rows,
+                             const void *x, int64_t x_feature, int64_t x_token, const void *weight,
                              const void *bias, float eps, void *y, int64_t y_feature,
                              int64_t y_token, float *mean, float *rstd, hipStream_t s) {
     const Args a{{const_cast<void *>(x), x_feature, x_token}, {y, y_feature, y_token}, {}, weight,
                  bias, wdtype == DARB_F32, H, B, eps, mean, rstd, nullptr, nullptr, 0};
     return with_type(xdtype, [&](auto type) {
         using T = decltype(type);
-        if (rows_of(H, x_feature)) {
+        if (rows) {
             const RowShape r = row_shape(H, kVec<T>, kMaxThreads, 1);
             return with_row(r, [&](auto n) {
                 return over_grid(a, B, [&](const Args &part, dim3 grid) {
@@ -944,8 +942,8 @@ hipError_t launch_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const
     });
 }
 
-hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, const void *dy,
-                                  int64_t dy_feature, int64_t dy_token, const void *x,
+hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, bool rows,
+                                  const void *dy, int64_t dy_feature, int64_t dy_token, const void *x,
                                   int64_t x_feature, int64_t x_token, const float *mean,
                                   const float *rstd, const void *weight, void *dx,
                                   int64_t dx_feature, int64_t dx_token, float *dweight,
@@ -955,7 +953,6 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
            H, B, 0.0f, const_cast<float *>(mean), const_cast<float *>(rstd), nullptr, nullptr, 0};
     return with_type(xdtype, [&](auto type) {
         using T = decltype(type);
-        const bool rows = rows_of(H, x_feature);
         int64_t stride = x_feature > dy_feature ? x_feature : dy_feature;
         if (dx && dx_feature > stride) stride = dx_feature;
         const TileShape t = tile_shape(H, B, stride, kVec<T>, kTileThreads<T>, kMostHeld<T>, sizeof(T) == 4 ? 200 : 384);

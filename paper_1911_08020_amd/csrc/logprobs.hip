@@ -804,10 +804,6 @@ Cut cut_of(int dtype, int64_t V, int64_t B, bool contiguous, int64_t top) {
     return c;
 }
 
-// Either order of the logits has its class or its token stride 1 (with one class or one token
-// the other stride is never used).
-bool rows_of(int64_t V, int64_t class_stride) { return V == 1 || class_stride == 1; }
-
 int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 }  // namespace
@@ -815,17 +811,17 @@ int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 int64_t logprobs_max_top() { return kMaxTop; }
 
 // The parts of every token, and the segments' maxima; nothing where a workgroup finishes a row.
-int64_t logprobs_workspace_bytes(int dtype, int64_t V, int64_t B, int64_t class_stride, int64_t top) {
-    const Cut c = cut_of(dtype, V, B, rows_of(V, class_stride), top);
+int64_t logprobs_workspace_bytes(int dtype, int64_t V, int64_t B, bool rows, int64_t top) {
+    const Cut c = cut_of(dtype, V, B, rows, top);
     if (c.rows && c.nparts == 1) return 0;
     return padded(c.nparts * B * 16) + (top ? padded(c.nseg * B * 4) : 0);
 }
 
-hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64_t class_stride,
-                           int64_t token_stride, const int64_t *targets, int64_t top,
-                           float *logprob, float *entropy, float *lse, float *top_logprob,
+hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, bool rows, const void *z,
+                           int64_t class_stride, int64_t token_stride, const int64_t *targets,
+                           int64_t top, float *logprob, float *entropy, float *lse, float *top_logprob,
                            int64_t *top_index, void *workspace, hipStream_t s) {
-    const Cut c = cut_of(dtype, V, B, rows_of(V, class_stride), top);
+    const Cut c = cut_of(dtype, V, B, rows, top);
     uint32_t *maxima = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + padded(c.nparts * B * 16));
     const Args a{z, class_stride, token_stride, V, B, targets, top, logprob, entropy, lse,
                  top_logprob, top_index, static_cast<float4 *>(workspace), maxima, c.nparts,
@@ -876,7 +872,7 @@ hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, const void *z, int64
     });
 }
 
-hipError_t launch_logprobs_grad(int dtype, int64_t V, int64_t B, const void *z,
+hipError_t launch_logprobs_grad(int dtype, int64_t V, int64_t B, bool rows, const void *z,
                                 int64_t class_stride, int64_t token_stride,
                                 const int64_t *targets, const float *lse,
                                 const float *grad_logprob, const float *entropy,
@@ -889,7 +885,7 @@ hipError_t launch_logprobs_grad(int dtype, int64_t V, int64_t B, const void *z,
         constexpr int VT = kVec<T>;
         auto launch = [&](auto with_entropy) {
             constexpr bool E = decltype(with_entropy)::value;
-            if (rows_of(V, class_stride)) {
+            if (rows) {
                 const int64_t each = kGradThreads * 4 * VT;
                 return over_grid_y(a, B, [&](const GradArgs &part, unsigned n) {
                     hipLaunchKernelGGL((grad_rows_kernel<T, E>),
