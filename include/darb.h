@@ -367,8 +367,9 @@ int darb_lstm_workspace(int64_t H, int64_t T, int64_t batch, int64_t *floats);
  * order: element (f, b) lies at f * feature_stride + b * batch_stride (elements), and one of
  * the two strides is 1 (batch_stride: the order of the products' X and Y; feature_stride: a
  * batch of rows).  Along an axis of size 1 the stride is not used and may be anything.  The
- * other stride is at least the unit axis' length.  Sums and statistics are fp32; results of
- * a 16-bit type are rounded once, to nearest even.  All calls are deterministic.
+ * other stride is at least the unit axis' length (one token or one feature that is only read
+ * may have 0: the same element everywhere).  Sums and statistics are fp32; results of a 16-bit
+ * type are rounded once, to nearest even.  All calls are deterministic.
  */
 
 /*

@@ -39,16 +39,24 @@ struct Strides {
     int64_t feature, batch;
 };
 
-bool as_rows(const Strides &s, int64_t F, int64_t B) { return F == 1 || (s.feature == 1 && (B == 1 || s.batch >= F)); }
-bool as_columns(const Strides &s, int64_t F, int64_t B) { return B == 1 || (s.batch == 1 && (F == 1 || s.feature >= B)); }
+// The other axis' stride reaches over the unit axis; where that has one element it is `least`.
+bool as_rows(const Strides &s, int64_t F, int64_t B, int64_t least) {
+    return (F == 1 || s.feature == 1) && (B == 1 || s.batch >= (F > 1 ? F : least));
+}
+bool as_columns(const Strides &s, int64_t F, int64_t B, int64_t least) {
+    return (B == 1 || s.batch == 1) && (F == 1 || s.feature >= (B > 1 ? B : least));
+}
 
 // All operands in one order, or an error.  Sets the unused strides of that order.  (One token's
-// operands may each have their own feature stride: where one is not 1, all go by columns.)
-int common_order(Strides *s, int count, int64_t F, int64_t B, const char *where, bool *by_rows) {
+// operands may each have their own feature stride: where one is not 1, all go by columns.)  The
+// first `reads` operands are only read, and may repeat one element (a stride of 0) where the unit
+// axis has one.
+int common_order(Strides *s, int count, int reads, int64_t F, int64_t B, const char *where, bool *by_rows) {
     bool rows = true, columns = true;
     for (int i = 0; i < count; ++i) {
-        rows = rows && as_rows(s[i], F, B);
-        columns = columns && as_columns(s[i], F, B);
+        const int64_t least = i < reads ? 0 : 1;
+        rows = rows && as_rows(s[i], F, B, least);
+        columns = columns && as_columns(s[i], F, B, least);
     }
     *by_rows = rows;
     if (!rows && !columns)
@@ -145,7 +153,7 @@ static int check_logits(int zdtype, int64_t V, int64_t B, int64_t top, Strides *
     if (!float_dtype(zdtype)) return fail(DARB_E_DTYPE, "unknown logit dtype");
     if (top < 0 || top > logprobs_max_top() || top > V)
         return fail(DARB_E_INVALID, "top must be in [0, 64] and at most V");
-    return common_order(s, 1, V, B, "z", rows);
+    return common_order(s, 1, 1, V, B, "z", rows);
 }
 
 int darb_token_logprobs_workspace(int zdtype, int64_t V, int64_t B, int64_t z_feature_stride,
@@ -199,7 +207,7 @@ int darb_token_logprobs_grad(int zdtype, int64_t V, int64_t B, const void *z,
         return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
     Strides s[2] = {{z_feature_stride, z_batch_stride}, {dz_feature_stride, dz_batch_stride}};
     bool rows;
-    rc = common_order(s, 2, V, B, "z, dz", &rows);
+    rc = common_order(s, 2, 1, V, B, "z, dz", &rows);
     if (rc) return rc;
     return launched(launch_logprobs_grad(zdtype, V, B, rows, z, s[0].feature, s[0].batch, targets, lse,
                                          grad_logprob, entropy, grad_entropy, dz, s[1].feature,
@@ -234,7 +242,7 @@ int darb_layer_norm(int xdtype, int wdtype, int64_t H, int64_t B, const void *x,
     if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(DARB_E_INVALID, "eps must be finite and >= 0");
     Strides s[2] = {{x_feature_stride, x_batch_stride}, {y_feature_stride, y_batch_stride}};
     bool rows;
-    rc = common_order(s, 2, H, B, "x, y", &rows);
+    rc = common_order(s, 2, 1, H, B, "x, y", &rows);
     if (rc) return rc;
     return launched(launch_layer_norm(xdtype, wdtype, H, B, rows, x, s[0].feature, s[0].batch, weight,
                                       bias, float(eps), y, s[1].feature, s[1].batch, mean, rstd,
@@ -267,7 +275,7 @@ int darb_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, const voi
     Strides s[3] = {{x_feature_stride, x_batch_stride}, {dy_feature_stride, dy_batch_stride},
                     {dx_feature_stride, dx_batch_stride}};
     bool rows;
-    rc = common_order(s, dx ? 3 : 2, H, B, "x, dy, dx", &rows);
+    rc = common_order(s, dx ? 3 : 2, 2, H, B, "x, dy, dx", &rows);
     if (rc) return rc;
     rc = check_workspace(workspace, workspace_bytes, layer_norm_workspace_bytes(H, B));
     if (rc) return rc;

@@ -74,3 +74,22 @@ def test_logprob_gradient_of_one_token(darb, V, dtype):  # noqa: F811
         got = darb.token_logprobs_grad(z, word, r.lse, g, out=dz)
         assert got is dz and untouched(dz) and untouched(z)
         check(wide(dz), want, 1e-5 * (hit + p) + rounding(want, dtype), "dz")
+
+
+def test_one_element_repeated(darb):  # noqa: F811
+    """One token or one feature that is only read may repeat an element; one that is written may not."""
+    for F, B in ((300, 1), (1, 300)):
+        say(f"one element repeated: {F} x {B}")
+        rng = np.random.default_rng(F)
+        x = torch.from_numpy(rng.standard_normal((F, B)).astype(np.float32)).cuda()
+        dy = torch.full((1, 1), 0.25, device="cuda").expand(F, B)
+        y, mean, rstd = darb.layer_norm(x)
+        got = darb.layer_norm_grad(dy, x, mean, rstd)
+        for a, b in zip(got, darb.layer_norm_grad(dy.contiguous(), x, mean, rstd)):
+            assert torch.allclose(a, b, rtol=1e-5, atol=1e-6)
+        r, want = darb.token_logprobs(dy), darb.token_logprobs(dy.contiguous())
+        assert torch.allclose(r.lse, want.lse, rtol=1e-6) and torch.allclose(r.entropy, want.entropy, rtol=1e-5)
+        with pytest.raises(darb.DarbError):
+            darb.layer_norm(x, y=torch.zeros(1, 1, device="cuda").expand(F, B))
+        with pytest.raises(darb.DarbError):
+            darb.token_logprobs_grad(x, None, r.lse, r.lse, out=torch.zeros(1, 1, device="cuda").expand(F, B))
