@@ -768,12 +768,12 @@ __global__ __launch_bounds__(kSplitThreads) void split_dx_kernel(SplitArgs a, in
 constexpr int kSumFeatures = 32, kSumSlices = 32;    // a cache line a row
 
 __global__ __launch_bounds__(kSumFeatures * kSumSlices) void sum_partials_kernel(
-    const float *__restrict__ dw_parts, const float *__restrict__ db_parts, int64_t H, int blocks,
-    float *__restrict__ dw, float *__restrict__ db) {
+    const float *__restrict__ dw_parts, const float *__restrict__ db_parts, int64_t first, int64_t H,
+    int blocks, float *__restrict__ dw, float *__restrict__ db) {
     constexpr int kSumWaves = kSumFeatures * kSumSlices / kWave, kAtOnce = 4;
     __shared__ float s[2][kSumWaves][kSumFeatures];
     const int f = threadIdx.x % kSumFeatures, slice = threadIdx.x / kSumFeatures;
-    const int64_t h = int64_t(blockIdx.x) * kSumFeatures + f, at = h < H ? h : H - 1;
+    const int64_t h = first + int64_t(blockIdx.x) * kSumFeatures + f, at = h < H ? h : H - 1;
     float w = 0.0f, b = 0.0f;
     for (int k = slice; k < blocks; k += kSumSlices * kAtOnce) {
         float x[kAtOnce], y[kAtOnce];
@@ -901,6 +901,20 @@ bool is_split(int64_t H, int64_t B, int vec) {
     return fits && B >= 8 && B <= 8192 && (H > 2048 || (vec > 4 && H > 1024 && B >= 128));
 }
 
+// A launch per 2^26 features (it has below 2^32 threads).
+hipError_t launch_sum_partials(const float *dw_parts, const float *db_parts, int64_t H, int blocks, float *dw,
+                               float *db, hipStream_t s) {
+    constexpr int64_t kMost = int64_t(1) << 26;
+    for (int64_t first = 0; first < H; first += kMost) {
+        const int64_t n = H - first < kMost ? H - first : kMost;
+        hipLaunchKernelGGL(sum_partials_kernel, dim3(unsigned(up(n, kSumFeatures))), dim3(kSumFeatures * kSumSlices),
+                           0, s, dw_parts, db_parts, first, H, blocks, dw, db);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 }  // namespace
 
 int64_t layer_norm_workspace_bytes(int64_t H, int64_t B) {
@@ -987,9 +1001,7 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
                 e = hipGetLastError();
             }
             if (e != hipSuccess || (!dweight && !dbias)) return e;
-            hipLaunchKernelGGL(sum_partials_kernel, dim3(unsigned(up(H, kSumFeatures))),
-                               dim3(kSumFeatures * kSumSlices), 0, s, p.n.dw, p.n.db, H, p.tiles, dweight, dbias);
-            return hipGetLastError();
+            return launch_sum_partials(p.n.dw, p.n.db, H, p.tiles, dweight, dbias, s);
         }
         if (rows) {
             const dim3 grid{unsigned(blocks)}, threads{unsigned(r.threads * teams)};
@@ -1015,9 +1027,7 @@ hipError_t launch_layer_norm_grad(int xdtype, int wdtype, int64_t H, int64_t B, 
             });
         }
         if (e != hipSuccess || (!dweight && !dbias)) return e;
-        hipLaunchKernelGGL(sum_partials_kernel, dim3(unsigned(up(H, kSumFeatures))),
-                           dim3(kSumFeatures * kSumSlices), 0, s, a.dw, a.db, H, blocks, dweight, dbias);
-        return hipGetLastError();
+        return launch_sum_partials(a.dw, a.db, H, blocks, dweight, dbias, s);
     });
 }
 
