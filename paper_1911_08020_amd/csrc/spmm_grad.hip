@@ -188,6 +188,7 @@ struct GradArgs {
     float *dvalues, *dX;
     int64_t N, B, ldx, ldy, lddx;
     int wdtype, xdtype;
+    int64_t first;                      // the launch's first column
 };
 
 // The weight's row of dY from one of the lane's columns on, and its value.  32 bits of offset
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void spmm_grad_kernel(GradArgs a) {
     const int w = wave_id(), lane = lane_id();
     const int group = lane / LPE, in = lane % LPE;
     const int64_t block = side_by_side(blockIdx.x, gridDim.x);
-    const int64_t c = block * (kWaves / KS) + w / KS;
+    const int64_t c = a.first + block * (kWaves / KS) + w / KS;
     const int share = w % KS;
     const bool has = c < a.N;
     uint32_t begin = 0, end = 0;
@@ -381,17 +382,31 @@ int waves_of(int64_t N, int64_t nnz, int64_t turn) {
     return ks;
 }
 
+// f(first column, workgroups) for every launch over the columns: below 2^32 threads, also where it
+// has kSplitTiles times as many workgroups.
+template <int KS, typename F> hipError_t over_columns(int64_t N, F &&f) {
+    constexpr int64_t kEach = kWaves / KS, kMost = (int64_t(1) << 19) * kEach;
+    for (int64_t first = 0; first < N; first += kMost) {
+        const int64_t n = N - first < kMost ? N - first : kMost;
+        const hipError_t e = f(first, uint32_t((n + kEach - 1) / kEach));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <int LPE, int V, int U> hipError_t launch_grad_t(const GradArgs &a, int64_t M, int64_t nnz, hipStream_t s) {
     const int ks = waves_of(a.N, nnz, kWave / LPE * (V * U >= 16 ? 2 : 4));
     // offsets of 32 bits, and a product of 24 bits each
     const bool wide = M >= 1 << 24 || a.ldy >= 1 << 22 || M * a.ldy >= int64_t(1) << 30 || nnz >= 1 << 30;
     auto launch = [&](auto share, auto is_wide) {
         constexpr int KS = decltype(share)::value;
-        const int64_t blocks = (a.N + kWaves / KS - 1) / (kWaves / KS);
-        if (blocks >= 1 << 24) return hipErrorInvalidConfiguration;      // 2^32 threads
-        hipLaunchKernelGGL((spmm_grad_kernel<LPE, V, U, KS, decltype(is_wide)::value>),
-                           dim3(unsigned(blocks)), dim3(kThreads), 0, s, a);
-        return hipGetLastError();
+        return over_columns<KS>(a.N, [&](int64_t first, uint32_t blocks) {
+            GradArgs part = a;
+            part.first = first;
+            hipLaunchKernelGGL((spmm_grad_kernel<LPE, V, U, KS, decltype(is_wide)::value>),
+                               dim3(blocks), dim3(kThreads), 0, s, part);
+            return hipGetLastError();
+        });
     };
     if (wide) return launch(std::integral_constant<int, 1>{}, std::true_type{});
     if (ks == 1) return launch(std::integral_constant<int, 1>{}, std::false_type{});
@@ -467,7 +482,7 @@ __global__ __launch_bounds__(kThreads) void split_grad_kernel(SplitArgs a) {
     __shared__ float part[KS > 1 ? (KS - 1) * (kWaves / KS) : 1][kSplitCols];
     const int w = wave_id(), lane = lane_id(), group = lane / LPE, in = lane % LPE;
     const int64_t task = side_by_side(blockIdx.x, gridDim.x);
-    const int64_t t = task / a.blocks, c = (task - t * a.blocks) * (kWaves / KS) + w / KS;
+    const int64_t t = task / a.blocks, c = a.g.first + (task - t * a.blocks) * (kWaves / KS) + w / KS;
     const int share = w % KS;
     const bool has = c < a.g.N;
     uint32_t begin = 0, end = 0;
@@ -624,31 +639,38 @@ hipError_t launch_split(const darb_plan &p, const GradArgs &g, void *workspace, 
     SplitArgs a{g, reinterpret_cast<Pair *>(w + r.pairs_at), reinterpret_cast<float *>(w + r.tiles_at),
                 g.dvalues ? reinterpret_cast<float *>(w + r.parts_at) : nullptr, p.M, p.nnz, 0, 0};
     const dim3 each(unsigned((p.nnz + kThreads - 1) / kThreads));
-    hipError_t e = hipSuccess;
     const int ks = waves_of(p.N, p.nnz, 32);
-    a.blocks = uint32_t((p.N + kWaves / ks - 1) / (kWaves / ks));
     // a launch has below 2^32 threads
     const uint32_t row_blocks = uint32_t((p.M * (kSplitCols / 4) + kThreads - 1) / kThreads);
-    int64_t most = ((int64_t(1) << 24) - 1) / a.blocks;
-    const int64_t most_rows = ((int64_t(1) << 24) - 1 - each.x) / row_blocks;
-    if (most > most_rows) most = most_rows;
-    if (most < 1) return hipErrorInvalidConfiguration;
+    int64_t most = ((int64_t(1) << 24) - 1 - each.x) / row_blocks;
     if (most > kSplitTiles) most = kSplitTiles;
-    for (a.first_tile = 0; e == hipSuccess && a.first_tile < r.tiles; a.first_tile += most) {
+    auto columns = [&](auto share, int64_t n) {
+        constexpr int KS = decltype(share)::value;
+        return over_columns<KS>(p.N, [&](int64_t first, uint32_t blocks) {
+            a.g.first = first;
+            a.blocks = blocks;
+            hipLaunchKernelGGL((split_grad_kernel<KS>), dim3(unsigned(blocks * n)), dim3(kThreads), 0, s, a);
+            return hipGetLastError();
+        });
+    };
+    for (a.first_tile = 0; a.first_tile < r.tiles; a.first_tile += most) {
         const int64_t n = r.tiles - a.first_tile < most ? r.tiles - a.first_tile : most;
         const uint32_t pair_blocks = a.first_tile == 0 ? each.x : 0;
         hipLaunchKernelGGL(tile_rows_kernel, dim3(pair_blocks + row_blocks * uint32_t(n)), dim3(kThreads), 0, s, a,
                            pair_blocks, row_blocks);
-        const dim3 grid(unsigned(a.blocks * n));
-        if (ks == 1) hipLaunchKernelGGL((split_grad_kernel<1>), grid, dim3(kThreads), 0, s, a);
-        else if (ks == 2) hipLaunchKernelGGL((split_grad_kernel<2>), grid, dim3(kThreads), 0, s, a);
-        else hipLaunchKernelGGL((split_grad_kernel<4>), grid, dim3(kThreads), 0, s, a);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (ks == 1) e = columns(std::integral_constant<int, 1>{}, n);
+        else if (ks == 2) e = columns(std::integral_constant<int, 2>{}, n);
+        else e = columns(std::integral_constant<int, 4>{}, n);
+        if (e != hipSuccess) return e;
         if (g.dvalues)
             hipLaunchKernelGGL(sum_parts_kernel, each, dim3(kThreads), 0, s, a.parts, p.nnz, int(n),
                                g.entries, a.first_tile > 0, g.dvalues);
         e = hipGetLastError();
+        if (e != hipSuccess) return e;
     }
-    return e;
+    return hipSuccess;
 }
 
 struct IndexParts {
@@ -698,7 +720,7 @@ hipError_t launch_spmm_grad(const darb_plan &p, const void *index, int wdtype, c
                             int64_t ldy, float *dvalues, float *dX, int64_t lddx, void *workspace,
                             hipStream_t s) {
     const IndexParts x = parts_of(p, const_cast<void *>(index));
-    const GradArgs a{x.starts, x.entries, values, X, dY, dvalues, dX, p.N, B, ldx, ldy, lddx, wdtype, xdtype};
+    const GradArgs a{x.starts, x.entries, values, X, dY, dvalues, dX, p.N, B, ldx, ldy, lddx, wdtype, xdtype, 0};
     if (is_split(p.M, B)) return launch_split(p, a, workspace, s);
     if (B == 1) return launch_grad_t<1, 1, 1>(a, p.M, p.nnz, s);
     if (B < 4) return launch_grad_t<4, 1, 1>(a, p.M, p.nnz, s);
