@@ -225,6 +225,13 @@ def _as_stream(stream):
     return stream if isinstance(stream, cuda.Stream) else cuda.ExternalStream(stream.cuda_stream)
 
 
+def _after_current(stream):
+    """A call that waits for its stream and keeps what it allocates takes memory of the current
+    stream: the given one first waits for the work queued there."""
+    if stream is not None:
+        _as_stream(stream).wait_stream(_torch().cuda.current_stream())
+
+
 def _used_on(stream, *ts):
     """What a call on a given stream leaves with its caller, given or new: the memory is not handed
     out again before that stream is done with it, nor before the current one is, on which the caller
@@ -273,7 +280,11 @@ def _row_major_ld(t, rows: int, cols: int, name: str) -> int:
 
 
 class Plan:
-    """A DARB plan: block sizes and grouped layout from row densities (section 3.2)."""
+    """A DARB plan: block sizes and grouped layout from row densities (section 3.2).
+
+    A call on a given stream takes its results and workspace from that stream's memory.  Its inputs
+    are the caller's to have ready for that stream, and to keep, with the plan, until it is done.
+    """
 
     def __init__(self, M: int, N: int, row_density, matrix_density: float,
                  mode: int = ROUND_FLOOR, b_min: int = 1, b_max: int = 128, *, _counts=None):
@@ -322,6 +333,7 @@ class Plan:
         ws = torch.empty(need.value, dtype=torch.uint8, device=row_count.device)
         h = ctypes.c_void_p()
         with torch.cuda.device(row_count.device):
+            _after_current(stream)
             _check(_lib.darb_plan_create_device(int(M), int(N), _ptr(row_count), int(kept),
                                                 int(mode), int(b_min), int(b_max), _ptr(ws),
                                                 ws.numel(), _stream_ptr(stream), ctypes.byref(h)),
@@ -368,6 +380,7 @@ class Plan:
         dev = torch.device("cuda") if device is None else torch.device(device)
         with torch.cuda.device(dev):
             ws = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+            _after_current(stream)
             _check(_lib.darb_plan_upload(self._h, _ptr(ws), self.workspace_bytes,
                                          _stream_ptr(stream)), "darb_plan_upload")
         self.workspace = ws
@@ -388,13 +401,15 @@ class Plan:
         _require_cuda(W)
         ldw = _row_major_ld(W, self.M, self.N, "W")
         if values is None or offsets is None:
-            values, offsets = self.empty_format(W.dtype, W.device)
+            with _memory_of(stream):
+                values, offsets = self.empty_format(W.dtype, W.device)
         _require_cuda(values, offsets)
         self._check_values_offsets(values, offsets)
         if values.dtype != W.dtype:
             raise TypeError("values must have W's dtype")
         _check(_lib.darb_encode(self._h, _dtype_code(W), _ptr(W), ldw, _ptr(values),
                                 _ptr(offsets), _stream_ptr(stream)), "darb_encode")
+        _used_on(stream, values, offsets)
         return values, offsets
 
     def decode(self, values, offsets, out=None, stream=None):
@@ -402,12 +417,14 @@ class Plan:
         _require_cuda(values, offsets)
         self._check_values_offsets(values, offsets)
         if out is None:
-            out = torch.empty((self.M, self.N), dtype=values.dtype, device=values.device)
+            with _memory_of(stream):
+                out = torch.empty((self.M, self.N), dtype=values.dtype, device=values.device)
         if out.dtype != values.dtype:
             raise TypeError("out must have the values' dtype")
         ldw = _row_major_ld(out, self.M, self.N, "out")
         _check(_lib.darb_decode(self._h, _dtype_code(values), _ptr(values), _ptr(offsets),
                                 _ptr(out), ldw, _stream_ptr(stream)), "darb_decode")
+        _used_on(stream, out)
         return out
 
     def spmv(self, values, offsets, x, y=None, stream=None):
@@ -417,10 +434,11 @@ class Plan:
         torch = _torch()
         _require_cuda(values, offsets, x)
         self._check_values_offsets(values, offsets)
-        y = self._vector_out(x, y)
+        y = self._vector_out(x, y, stream)
         _check(_lib.darb_spmv(self._h, _dtype_code(values), _ptr(values), _ptr(offsets),
                               _dtype_code(x), _ptr(x), _ptr(y), _stream_ptr(stream)),
                "darb_spmv")
+        _used_on(stream, y)
         return y
 
     def spmm(self, values, offsets, X, Y=None, stream=None):
@@ -430,10 +448,11 @@ class Plan:
         torch = _torch()
         _require_cuda(values, offsets, X)
         self._check_values_offsets(values, offsets)
-        B, ldx, Y, ldy = self._matrix_out(X, Y)
+        B, ldx, Y, ldy = self._matrix_out(X, Y, stream)
         _check(_lib.darb_spmm(self._h, _dtype_code(values), _ptr(values), _ptr(offsets),
                               _dtype_code(X), B, _ptr(X), ldx, _ptr(Y), ldy,
                               _stream_ptr(stream)), "darb_spmm")
+        _used_on(stream, Y)
         return Y
 
     # -- bit-packed offsets (section 4.2) ---------------------------------------------
@@ -448,10 +467,12 @@ class Plan:
         _require_cuda(offsets)
         _check_format(offsets, self.nnz, "offsets", (torch.uint8,))
         if packed is None:
-            packed = self.empty_packed(offsets.device)
+            with _memory_of(stream):
+                packed = self.empty_packed(offsets.device)
         self._check_packed(packed)
         _check(_lib.darb_pack_offsets(self._h, _ptr(offsets), _ptr(packed), _stream_ptr(stream)),
                "darb_pack_offsets")
+        _used_on(stream, packed)
         return packed
 
     def unpack_offsets(self, packed, offsets=None, stream=None):
@@ -459,10 +480,12 @@ class Plan:
         _require_cuda(packed)
         self._check_packed(packed)
         if offsets is None:
-            offsets = torch.empty(self.nnz, dtype=torch.uint8, device=packed.device)
+            with _memory_of(stream):
+                offsets = torch.empty(self.nnz, dtype=torch.uint8, device=packed.device)
         _check_format(offsets, self.nnz, "offsets", (torch.uint8,))
         _check(_lib.darb_unpack_offsets(self._h, _ptr(packed), _ptr(offsets),
                                         _stream_ptr(stream)), "darb_unpack_offsets")
+        _used_on(stream, offsets)
         return offsets
 
     def spmv_packed(self, values, packed, x, y=None, stream=None):
@@ -472,10 +495,11 @@ class Plan:
         _require_cuda(values, packed, x)
         self._check_values(values)
         self._check_packed(packed)
-        y = self._vector_out(x, y)
+        y = self._vector_out(x, y, stream)
         _check(_lib.darb_spmv_packed(self._h, _dtype_code(values), _ptr(values), _ptr(packed),
                                      _dtype_code(x), _ptr(x), _ptr(y), _stream_ptr(stream)),
                "darb_spmv_packed")
+        _used_on(stream, y)
         return y
 
     def spmm_packed(self, values, packed, X, Y=None, stream=None):
@@ -485,10 +509,11 @@ class Plan:
         _require_cuda(values, packed, X)
         self._check_values(values)
         self._check_packed(packed)
-        B, ldx, Y, ldy = self._matrix_out(X, Y)
+        B, ldx, Y, ldy = self._matrix_out(X, Y, stream)
         _check(_lib.darb_spmm_packed(self._h, _dtype_code(values), _ptr(values), _ptr(packed),
                                      _dtype_code(X), B, _ptr(X), ldx, _ptr(Y), ldy,
                                      _stream_ptr(stream)), "darb_spmm_packed")
+        _used_on(stream, Y)
         return Y
 
     # -- INT8 values ------------------------------------------------------------------
@@ -501,13 +526,15 @@ class Plan:
         torch = _torch()
         _require_cuda(values)
         self._check_values(values)
-        if codes is None:
-            codes = torch.empty(self.nnz, dtype=torch.int8, device=values.device)
-        if scales is None:
-            scales = torch.empty(self.M, dtype=torch.float32, device=values.device)
+        with _memory_of(stream):
+            if codes is None:
+                codes = torch.empty(self.nnz, dtype=torch.int8, device=values.device)
+            if scales is None:
+                scales = torch.empty(self.M, dtype=torch.float32, device=values.device)
         self._check_i8(codes, scales)
         _check(_lib.darb_quantize_i8(self._h, _dtype_code(values), _ptr(values), _ptr(codes),
                                      _ptr(scales), _stream_ptr(stream)), "darb_quantize_i8")
+        _used_on(stream, codes, scales)
         return codes, scales
 
     def _i8_offsets(self, offsets, packed):
@@ -529,9 +556,10 @@ class Plan:
         _require_cuda(codes, scales, x)
         self._check_i8(codes, scales)
         po, pp = self._i8_offsets(offsets, packed)
-        y = self._vector_out(x, y)
+        y = self._vector_out(x, y, stream)
         _check(_lib.darb_spmv_i8(self._h, _ptr(codes), _ptr(scales), po, pp, _dtype_code(x),
                                  _ptr(x), _ptr(y), _stream_ptr(stream)), "darb_spmv_i8")
+        _used_on(stream, y)
         return y
 
     def spmm_i8(self, codes, scales, X, offsets=None, packed=None, Y=None, stream=None):
@@ -542,10 +570,11 @@ class Plan:
         _require_cuda(codes, scales, X)
         self._check_i8(codes, scales)
         po, pp = self._i8_offsets(offsets, packed)
-        B, ldx, Y, ldy = self._matrix_out(X, Y)
+        B, ldx, Y, ldy = self._matrix_out(X, Y, stream)
         _check(_lib.darb_spmm_i8(self._h, _ptr(codes), _ptr(scales), po, pp, _dtype_code(X), B,
                                  _ptr(X), ldx, _ptr(Y), ldy, _stream_ptr(stream)),
                "darb_spmm_i8")
+        _used_on(stream, Y)
         return Y
 
     # -- gradients ----------------------------------------------------------------------
@@ -648,23 +677,25 @@ class Plan:
         torch = _torch()
         _check_format(packed, self.packed_words, "packed", (torch.int32,))
 
-    def _vector_out(self, x, y):
+    def _vector_out(self, x, y, stream):
         torch = _torch()
         if x.dim() != 1 or x.shape[0] != self.N or not x.is_contiguous():
             raise ValueError(f"x must be a contiguous [{self.N}] tensor")
         if y is None:
-            y = torch.empty(self.M, dtype=torch.float32, device=x.device)
+            with _memory_of(stream):
+                y = torch.empty(self.M, dtype=torch.float32, device=x.device)
         _check_format(y, self.M, "y", (torch.float32,))
         return y
 
-    def _matrix_out(self, X, Y):
+    def _matrix_out(self, X, Y, stream):
         torch = _torch()
         if X.dim() != 2 or X.shape[0] != self.N:
             raise ValueError(f"X must be [{self.N}, B]")
         B = X.shape[1]
         ldx = _row_major_ld(X, self.N, B, "X")
         if Y is None:
-            Y = torch.empty((self.M, B), dtype=torch.float32, device=X.device)
+            with _memory_of(stream):
+                Y = torch.empty((self.M, B), dtype=torch.float32, device=X.device)
         if Y.dtype != torch.float32:
             raise TypeError("Y must be fp32")
         ldy = _row_major_ld(Y, self.M, B, "Y")
@@ -686,14 +717,16 @@ def prune_counts(W, k: int, counts=None, workspace=None, stream=None):
     code = _dtype_code(W)
     need = ctypes.c_int64()
     _check(_lib.darb_prune_workspace(M, N, code, ctypes.byref(need)), "darb_prune_workspace")
-    if workspace is None:
-        workspace = torch.empty(need.value, dtype=torch.uint8, device=W.device)
-    if counts is None:
-        counts = torch.empty(M, dtype=torch.int64, device=W.device)
+    with _memory_of(stream):
+        if workspace is None:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=W.device)
+        if counts is None:
+            counts = torch.empty(M, dtype=torch.int64, device=W.device)
     _check_format(counts, M, "counts", (torch.int64,))
     _check_format(workspace, need.value, "workspace", (torch.uint8,))
     _check(_lib.darb_prune_counts(M, N, code, _ptr(W), ldw, int(k), _ptr(counts), _ptr(workspace),
                                   workspace.numel(), _stream_ptr(stream)), "darb_prune_counts")
+    _used_on(stream, counts, workspace)
     return counts
 
 
@@ -715,15 +748,16 @@ def lstm_layer(wih: Tuple[Plan, object, object], whh: Tuple[Plan, object, object
     torch = _torch()
     H, T, Bt = hidden, seq_len, batch
     dev = x_seq.device
-    if h is None:
-        h = torch.zeros((H, Bt), dtype=torch.float32, device=dev)
-    if c is None:
-        c = torch.zeros((H, Bt), dtype=torch.float32, device=dev)
-    if h_seq is None:
-        h_seq = torch.empty((H, T * Bt), dtype=torch.float32, device=dev)
     need = lstm_workspace_floats(H, T, Bt)
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.float32, device=dev)
+    with _memory_of(stream):
+        if h is None:
+            h = torch.zeros((H, Bt), dtype=torch.float32, device=dev)
+        if c is None:
+            c = torch.zeros((H, Bt), dtype=torch.float32, device=dev)
+        if h_seq is None:
+            h_seq = torch.empty((H, T * Bt), dtype=torch.float32, device=dev)
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.float32, device=dev)
     for t in (x_seq, h, c, h_seq, workspace):
         if t.dtype != torch.float32 or not t.is_contiguous():
             raise ValueError("LSTM state and sequences must be contiguous fp32")
@@ -739,6 +773,7 @@ def lstm_layer(wih: Tuple[Plan, object, object], whh: Tuple[Plan, object, object
                                 _ptr(whh[1]), _ptr(whh[2]), _dtype_code(wih[1]), H, T, Bt,
                                 _ptr(x_seq), _ptr(h_seq), _ptr(h), _ptr(c), _ptr(workspace),
                                 workspace.numel(), _stream_ptr(stream)), "darb_lstm_layer")
+    _used_on(stream, h_seq, h, c, workspace)
     return h_seq, h, c
 
 

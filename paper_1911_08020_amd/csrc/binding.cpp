@@ -86,6 +86,10 @@ bool stream_of(PyObject *o, void **s) {
     return ok;
 }
 
+// A result to allocate for a call on a given stream, which takes that stream's memory: left to
+// the Python code.
+bool new_on_stream(PyObject *out, PyObject *stream) { return out == Py_None && stream != Py_None; }
+
 void *ptr(const at::Tensor &t) { return t.data_ptr(); }
 
 PyObject *none() { Py_RETURN_NONE; }
@@ -173,7 +177,7 @@ PyObject *vector_product(const PlanRef &p, PyObject *xo, PyObject *yo, PyObject 
     int xcode;
     void *s;
     if (!x || !float_code(*x, &xcode) || x->dim() != 1 || x->size(0) != p.N ||
-        !x->is_contiguous() || !stream_of(so, &s))
+        !x->is_contiguous() || new_on_stream(yo, so) || !stream_of(so, &s))
         return none();
     at::Tensor y;
     PyObject *res = vector_out(yo, p, *x, &y);
@@ -189,7 +193,8 @@ PyObject *matrix_product(const PlanRef &p, PyObject *xo, PyObject *yo, PyObject 
     const at::Tensor *X = tensor(xo);
     int xcode;
     void *s;
-    if (!X || !float_code(*X, &xcode) || X->dim() != 2 || !stream_of(so, &s)) return none();
+    if (!X || !float_code(*X, &xcode) || X->dim() != 2 || new_on_stream(yo, so) || !stream_of(so, &s))
+        return none();
     const int64_t B = X->size(1), ldx = leading(*X, p.N, B);
     if (ldx < 0) return none();
     at::Tensor Y;

@@ -13,8 +13,8 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple, Optional
 
-from . import (BF16, F16, F32, _AdamTensor, _as_stream, _check, _check_format, _lib, _memory_of,
-               _native, _ptr, _stream_ptr, _torch, _used_on)
+from . import (BF16, F16, F32, _AdamTensor, _after_current, _as_stream, _check, _check_format,
+               _lib, _memory_of, _native, _ptr, _stream_ptr, _torch, _used_on)
 
 
 class TokenLogprobs(NamedTuple):
@@ -300,10 +300,7 @@ class AdamW:
             table[i] = self._entry(i, p, t, s, float(decay[i]))
         self.workspace = _workspace(_lib.darb_adamw_workspace, "darb_adamw_workspace", dev, None,
                                     table, count)
-        if stream is not None:
-            # the masters and zeros above are the current stream's work; darb_adamw_create waits
-            # for the given one
-            _as_stream(stream).wait_stream(torch.cuda.current_stream())
+        _after_current(stream)              # the masters and zeros above
         h = ctypes.c_void_p()
         with torch.cuda.device(dev):
             _check(_lib.darb_adamw_create(table, count, self.state_bits, _ptr(self.workspace),
