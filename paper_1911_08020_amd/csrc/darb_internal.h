@@ -87,6 +87,21 @@ void clear_error();
 int check_uploaded(const darb_plan *p);
 int launched(hipError_t e, const char *what);
 
+// A launch of 2^32 threads or more runs some of its workgroups and reports no error.
+constexpr int64_t kMostThreads = (int64_t(1) << 32) - 1;
+inline bool one_launch(int64_t blocks, int threads) { return blocks <= kMostThreads / threads; }
+
+// f(first workgroup, workgroups) for every launch of `blocks` workgroups in all.
+template <typename F> hipError_t over_blocks(int64_t blocks, int threads, F &&f) {
+    const int64_t most = (int64_t(1) << 31) / threads;
+    for (int64_t first = 0; first < blocks; first += most) {
+        f(first, unsigned(blocks - first < most ? blocks - first : most));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // kernel launchers (return hipError_t of the launch)
 hipError_t launch_encode(const darb_plan &p, int wdtype, const void *W, int64_t ldw,
                          void *values, uint8_t *offsets, hipStream_t s);

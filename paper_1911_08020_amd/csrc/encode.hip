@@ -198,7 +198,7 @@ __device__ __forceinline__ void small_blocks_all(const Vec<Bits, VEC> (&v)[UNROL
 template <typename Bits>
 __global__ __launch_bounds__(kEncodeThreads) void encode_kernel(
     const Bits *__restrict__ W, int64_t ldw, int64_t N, const int64_t *__restrict__ rowinfo,
-    uint32_t chunks_per_row, uint32_t total_chunks, Bits *__restrict__ values,
+    uint32_t chunks_per_row, uint32_t total_chunks, uint32_t first, Bits *__restrict__ values,
     uint8_t *__restrict__ offsets) {
     using Tr = EncodeTraits<Bits>;
     constexpr int VEC = Tr::VEC;
@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kEncodeThreads) void encode_kernel(
     // arrive from the per-row table while they are in flight.
     const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
     const int lane = int(threadIdx.x) & (kWave - 1);
-    const uint32_t item = blockIdx.x * uint32_t(kEncodeWaves) + uint32_t(wave);
+    const uint32_t item = (first + blockIdx.x) * uint32_t(kEncodeWaves) + uint32_t(wave);
     if (item >= total_chunks) return;                 // wave-uniform, no barrier below
     const uint32_t r = item / chunks_per_row;
     const int64_t q = int64_t(item - r * chunks_per_row);
@@ -264,10 +264,11 @@ hipError_t launch_encode_t(const darb_plan &p, const void *W, int64_t ldw, void 
     const int64_t total = p.M * chunks;
     const int64_t blocks = (total + kEncodeWaves - 1) / kEncodeWaves;
     if (blocks > 0x3FFFFFFF) return hipErrorInvalidConfiguration;   // total fits 32 bits
-    hipLaunchKernelGGL((encode_kernel<Bits>), dim3(unsigned(blocks)), dim3(kEncodeThreads), 0, s,
-                       static_cast<const Bits *>(W), ldw, p.N, p.d_rowinfo, uint32_t(chunks),
-                       uint32_t(total), static_cast<Bits *>(values), offsets);
-    return hipGetLastError();
+    return over_blocks(blocks, kEncodeThreads, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL((encode_kernel<Bits>), dim3(n), dim3(kEncodeThreads), 0, s,
+                           static_cast<const Bits *>(W), ldw, p.N, p.d_rowinfo, uint32_t(chunks),
+                           uint32_t(total), uint32_t(first), static_cast<Bits *>(values), offsets);
+    });
 }
 
 }  // namespace

@@ -13,9 +13,10 @@ constexpr int kThreads = 256;
 template <typename Bits>
 __global__ __launch_bounds__(kThreads) void decode_kernel(
     const Bits *__restrict__ values, const uint8_t *__restrict__ offsets, Bits *__restrict__ W,
-    int64_t ldw, int64_t N, const int32_t *__restrict__ perm, BinTable bins, int64_t col_blocks) {
-    const int64_t i = blockIdx.x / col_blocks;
-    const int64_t c = (blockIdx.x - i * col_blocks) * int64_t(kThreads) + threadIdx.x;
+    int64_t ldw, int64_t N, const int32_t *__restrict__ perm, BinTable bins, int64_t col_blocks,
+    int64_t first) {
+    const int64_t block = first + blockIdx.x, i = block / col_blocks;
+    const int64_t c = (block - i * col_blocks) * int64_t(kThreads) + threadIdx.x;
     if (c >= N) return;
     int g = 0;
     while (g + 1 < bins.nbins && i >= bins.first_row[g + 1]) ++g;
@@ -107,11 +108,11 @@ hipError_t launch_decode_t(const darb_plan &p, const void *values, const uint8_t
                            void *W, int64_t ldw, hipStream_t s) {
     const int64_t col_blocks = (p.N + kThreads - 1) / kThreads;
     const int64_t blocks = p.M * col_blocks;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((decode_kernel<Bits>), dim3(unsigned(blocks)), dim3(kThreads), 0, s,
-                       static_cast<const Bits *>(values), offsets, static_cast<Bits *>(W), ldw,
-                       p.N, p.d_perm, p.bins, col_blocks);
-    return hipGetLastError();
+    return over_blocks(blocks, kThreads, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL((decode_kernel<Bits>), dim3(n), dim3(kThreads), 0, s,
+                           static_cast<const Bits *>(values), offsets, static_cast<Bits *>(W), ldw,
+                           p.N, p.d_perm, p.bins, col_blocks, first);
+    });
 }
 
 }  // namespace
@@ -127,7 +128,7 @@ hipError_t launch_lstm_cell(int64_t H, int64_t batch, const float *G, const floa
                             hipStream_t s) {
     const int64_t n = H * batch;
     const int64_t blocks = (n + kThreads - 1) / kThreads;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    if (!one_launch(blocks, kThreads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(lstm_cell_kernel, dim3(unsigned(blocks)), dim3(kThreads), 0, s, H, batch,
                        G, U, ldu, h, c, h_seq, ld_seq);
     return hipGetLastError();
@@ -136,7 +137,7 @@ hipError_t launch_lstm_cell(int64_t H, int64_t batch, const float *G, const floa
 hipError_t launch_stream_read(const void *buf, int64_t bytes, float *sink, hipStream_t s) {
     const int64_t n16 = bytes / 16;
     const int64_t blocks = (n16 + kReadUnroll * kThreads - 1) / (kReadUnroll * kThreads);
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    if (!one_launch(blocks, kThreads)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL(stream_read_kernel, dim3(unsigned(blocks)), dim3(kThreads), 0, s,
                        static_cast<const f32x4 *>(buf), n16, sink);
     return hipGetLastError();
@@ -147,7 +148,7 @@ hipError_t launch_stream_read_shape(const void *buf, int64_t bytes, int threads,
     const int64_t n16 = bytes / 16;
     const int64_t per_block = int64_t(threads) * vectors;
     const int64_t blocks = (n16 + per_block - 1) / per_block;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+    if (!one_launch(blocks, threads)) return hipErrorInvalidConfiguration;
     const f32x4 *b = static_cast<const f32x4 *>(buf);
 #define DARB_READ_SHAPE(T, V)                                                               \
     if (threads == T && vectors == V) {                                                     \

@@ -34,8 +34,9 @@ __device__ __forceinline__ T pick(const T (&a)[kMaxBins], int g) {
 // floor(32w / l) ... floor((32w + 31) / l) of the run.
 __global__ __launch_bounds__(kThreads) void pack_kernel(const uint8_t *__restrict__ offsets,
                                                         uint32_t *__restrict__ packed,
-                                                        int64_t words, BinTable bins) {
-    const int64_t wi = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+                                                        int64_t words, BinTable bins,
+                                                        int64_t first) {
+    const int64_t wi = (first + blockIdx.x) * kThreads + threadIdx.x;
     if (wi >= words) return;
     const int g = owning_group(bins.first_word, bins.nbins, wi);
     const int l = pick(bins.log2b, g);                   // >= 1: this group has words
@@ -62,8 +63,9 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const uint8_t *__restric
 // One thread per retained weight.
 __global__ __launch_bounds__(kThreads) void unpack_kernel(const uint32_t *__restrict__ packed,
                                                           uint8_t *__restrict__ offsets,
-                                                          int64_t nnz, BinTable bins) {
-    const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+                                                          int64_t nnz, BinTable bins,
+                                                          int64_t first) {
+    const int64_t i = (first + blockIdx.x) * kThreads + threadIdx.x;
     if (i >= nnz) return;
     const int g = owning_group(bins.first_elem, bins.nbins, i);
     const int l = pick(bins.log2b, g);
@@ -82,19 +84,19 @@ hipError_t launch_pack_offsets(const darb_plan &p, const uint8_t *offsets, uint3
                                hipStream_t s) {
     if (p.packed_words == 0) return hipSuccess;
     const int64_t blocks = (p.packed_words + kThreads - 1) / kThreads;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(pack_kernel, dim3(unsigned(blocks)), dim3(kThreads), 0, s, offsets, packed,
-                       p.packed_words, p.bins);
-    return hipGetLastError();
+    return over_blocks(blocks, kThreads, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL(pack_kernel, dim3(n), dim3(kThreads), 0, s, offsets, packed,
+                           p.packed_words, p.bins, first);
+    });
 }
 
 hipError_t launch_unpack_offsets(const darb_plan &p, const uint32_t *packed, uint8_t *offsets,
                                  hipStream_t s) {
     const int64_t blocks = (p.nnz + kThreads - 1) / kThreads;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(unpack_kernel, dim3(unsigned(blocks)), dim3(kThreads), 0, s, packed,
-                       offsets, p.nnz, p.bins);
-    return hipGetLastError();
+    return over_blocks(blocks, kThreads, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL(unpack_kernel, dim3(n), dim3(kThreads), 0, s, packed, offsets, p.nnz,
+                           p.bins, first);
+    });
 }
 
 }  // namespace darb

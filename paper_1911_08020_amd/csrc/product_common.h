@@ -1650,6 +1650,15 @@ hipError_t launch_spmm_t(const darb_plan &p, const void *values, const uint8_t *
                          const uint32_t *packed, int64_t B, const void *X, int64_t ldx, float *Y,
                          int64_t ldy, const float *scales, hipStream_t st) {
     constexpr int CPL = 16 / int(sizeof(Tx));
+    // more workgroups than a launch takes: the batch in two halves of whole slabs
+    auto halves = [&] {
+        const int64_t half = (B / 2 + 511) / 512 * 512;
+        if (half >= B) return hipErrorInvalidConfiguration;
+        const hipError_t e = launch_spmm_t<Tw, Tx, PK>(p, values, offsets, packed, half, X, ldx, Y, ldy, scales, st);
+        if (e != hipSuccess) return e;
+        return launch_spmm_t<Tw, Tx, PK>(p, values, offsets, packed, B - half, static_cast<const Tx *>(X) + half, ldx,
+                                         Y + half, ldy, scales, st);
+    };
     if constexpr (std::is_same<Tx, float>::value && !kScaled<Tw>) {
         // the LDS-slab kernel is chosen from the plan and B alone (rows in whole steps
         // of 16 weights, slabs that fit, enough of them), so every alignment of the
@@ -1661,10 +1670,9 @@ hipError_t launch_spmm_t(const darb_plan &p, const void *values, const uint8_t *
                 lgl = -1;
         if (lgl >= 0) {
             ProductSchedule s;
-            if (!spmm_schedule(p, B, CPL, s))
-                return hipErrorInvalidConfiguration;
+            if (!spmm_schedule(p, B, CPL, s)) return halves();
             const int64_t slabs = (B + (int64_t(4) << lgl) - 1) / (int64_t(4) << lgl);
-            if (slabs > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
+            if (!one_launch(slabs, kXldsThreads)) return halves();
             const Tw *v = static_cast<const Tw *>(values);
             const float *x = static_cast<const float *>(X);
             const void *offs = offset_source(p, offsets, packed);
@@ -1728,8 +1736,8 @@ hipError_t launch_spmm_t(const darb_plan &p, const void *values, const uint8_t *
         else wide_lgl = B <= 8 && fills(8) ? 3 : B <= 16 && fills(16) ? 4 : 6;
     }
     ProductSchedule s;
-    if (!spmm_schedule(p, B, cpl, s, wide_lgl))
-        return hipErrorInvalidConfiguration;
+    if (!spmm_schedule(p, B, cpl, s, wide_lgl) || !one_launch(s.block_begin[s.nbins], kSpmmThreads))
+        return halves();
     if (s.block_begin[s.nbins] == 0) return hipSuccess;
     const Tw *v = static_cast<const Tw *>(values);
     const void *offs = offset_source(p, offsets, packed);

@@ -24,8 +24,8 @@ __device__ __forceinline__ float value_f32(const Tw *v, int64_t i) { return to_f
 template <typename Tw>
 __global__ __launch_bounds__(kQuantThreads) void quantize_i8_kernel(
     const Tw *__restrict__ values, int8_t *__restrict__ codes, float *__restrict__ scales,
-    const int32_t *__restrict__ perm, int64_t M, BinTable bins) {
-    const int64_t i = int64_t(blockIdx.x) * (kQuantThreads / kWave) + threadIdx.x / kWave;
+    const int32_t *__restrict__ perm, int64_t M, BinTable bins, int64_t first) {
+    const int64_t i = (first + blockIdx.x) * (kQuantThreads / kWave) + threadIdx.x / kWave;
     if (i >= M) return;                                   // wave-uniform, no barrier below
     const int lane = int(threadIdx.x) & (kWave - 1);
     int g = 0;
@@ -73,11 +73,11 @@ hipError_t launch_quantize_t(const darb_plan &p, const void *values, int8_t *cod
                              float *scales, hipStream_t s) {
     constexpr int rows_per_block = kQuantThreads / kWave;
     const int64_t blocks = (p.M + rows_per_block - 1) / rows_per_block;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
-    if (blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL((quantize_i8_kernel<Tw>), dim3(unsigned(blocks)), dim3(kQuantThreads), 0,
-                       s, static_cast<const Tw *>(values), codes, scales, p.d_perm, p.M, p.bins);
-    return hipGetLastError();
+    return over_blocks(blocks, kQuantThreads, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL((quantize_i8_kernel<Tw>), dim3(n), dim3(kQuantThreads), 0, s,
+                           static_cast<const Tw *>(values), codes, scales, p.d_perm, p.M, p.bins,
+                           first);
+    });
 }
 
 }  // namespace
