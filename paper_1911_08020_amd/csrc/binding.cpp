@@ -86,9 +86,13 @@ bool stream_of(PyObject *o, void **s) {
     return ok;
 }
 
-// A result to allocate for a call on a given stream, which takes that stream's memory: left to
-// the Python code.
-bool new_on_stream(PyObject *out, PyObject *stream) { return out == Py_None && stream != Py_None; }
+// The given stream is not the current one.
+bool elsewhere(PyObject *o, void *s) {
+    return o != Py_None && s != static_cast<void *>(c10::hip::getCurrentHIPStream().stream());
+}
+
+// A result to allocate for a call on another stream, whose memory it takes: left to the Python code.
+bool new_elsewhere(PyObject *out, PyObject *o, void *s) { return out == Py_None && elsewhere(o, s); }
 
 void *ptr(const at::Tensor &t) { return t.data_ptr(); }
 
@@ -177,7 +181,7 @@ PyObject *vector_product(const PlanRef &p, PyObject *xo, PyObject *yo, PyObject 
     int xcode;
     void *s;
     if (!x || !float_code(*x, &xcode) || x->dim() != 1 || x->size(0) != p.N ||
-        !x->is_contiguous() || new_on_stream(yo, so) || !stream_of(so, &s))
+        !x->is_contiguous() || !stream_of(so, &s) || new_elsewhere(yo, so, s))
         return none();
     at::Tensor y;
     PyObject *res = vector_out(yo, p, *x, &y);
@@ -193,7 +197,7 @@ PyObject *matrix_product(const PlanRef &p, PyObject *xo, PyObject *yo, PyObject 
     const at::Tensor *X = tensor(xo);
     int xcode;
     void *s;
-    if (!X || !float_code(*X, &xcode) || X->dim() != 2 || new_on_stream(yo, so) || !stream_of(so, &s))
+    if (!X || !float_code(*X, &xcode) || X->dim() != 2 || !stream_of(so, &s) || new_elsewhere(yo, so, s))
         return none();
     const int64_t B = X->size(1), ldx = leading(*X, p.N, B);
     if (ldx < 0) return none();
@@ -333,11 +337,11 @@ PyObject *encode(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 // ---- evaluating and retraining a layer -------------------------------------------------
 //
-// These allocate outputs and workspaces, which belong to the current stream: a call on a given
-// stream is left to the Python code, which tells the allocator so.
+// These allocate outputs and workspaces, which belong to the current stream: a call on another
+// one is left to the Python code, which takes that stream's memory.
 
-// The current stream's handle, for None.
-bool current(PyObject *o, void **s) { return o == Py_None && stream_of(o, s); }
+// The current stream's handle, for None or the stream itself.
+bool current(PyObject *o, void **s) { return stream_of(o, s) && !elsewhere(o, *s); }
 
 bool any_float_code(const at::Tensor &t, int *code) {
     if (t.scalar_type() != at::kBFloat16) return float_code(t, code);

@@ -104,3 +104,16 @@ def test_plans_made_for_a_given_stream(darb, busy, pair):  # noqa: F811
     got_v = again.encode(fa["W"])[0]
     torch.cuda.synchronize()
     assert same(got_b, want_b) and torch.equal(got_v, want_v) and same(planned(darb, fa), want_a)
+
+
+def test_the_current_stream_named(darb, pair):  # noqa: F811
+    """Given as an argument, the current stream is what it is without."""
+    for name in sorted(CALLS):
+        want = copies(CALLS[name](darb, pair[0]))
+        assert same(flat(CALLS[name](darb, pair[0], stream=torch.cuda.current_stream())), want), name
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            got = flat(CALLS[name](darb, pair[0], stream=st))
+        st.synchronize()
+        assert same(got, want), name

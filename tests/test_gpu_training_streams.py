@@ -157,3 +157,16 @@ def test_adamw_dropped_before_its_step_is_done(darb, busy, given):  # noqa: F811
         t.fill_(85)
     torch.cuda.synchronize()
     assert same(p, want)
+
+
+def test_the_current_stream_named(darb, pair):  # noqa: F811
+    """Given as an argument, the current stream is what it is without."""
+    for name in sorted(CALLS):
+        want = copies(CALLS[name](darb, pair[0]))
+        assert same(flat(CALLS[name](darb, pair[0], stream=torch.cuda.current_stream())), want), name
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            got = flat(CALLS[name](darb, pair[0], stream=st))
+        st.synchronize()
+        assert same(got, want), name
