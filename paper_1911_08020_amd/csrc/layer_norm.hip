@@ -10,10 +10,11 @@
 // columns: each workgroup sums the columns it takes, rows of partial sums go to the workspace,
 // and a last launch adds them in a fixed order.
 //
-// Measured on MI355X, among other calls: forward 1024 x 32 fp32 6.3 us (latency of one round of
+// Measured on MI355X, among other calls: forward 1024 x 32 fp32 6.6 us (latency of one round of
 // loads and two sums), 4096 x 4096 27 (4.9 TB/s); gradients of 1024 x 6400 fp32 feature-major
 // 25.8 (3.1 TB/s: all loads, then the sums, then all stores), of 9216 x 2047 token-major bf16 35.4
-// (3.2 TB/s; partial rows are a sixth of it) and fp32 43 (5.3 TB/s).
+// (3.2 TB/s; partial rows are a sixth of it) and fp32 54 (4.2 TB/s; 43 out of the cache); forward of
+// the same bf16 16.4 (4.6 TB/s).
 #include <type_traits>
 
 #include "darb_internal.h"

@@ -10,8 +10,8 @@
 // segments whose maximum reaches it are read again.
 //
 // Measured on MI355X, among other calls: 10 000 x 700 fp32 feature-major 11.9 us (2.4 TB/s, two
-// launches of 8 and 3), 131 072 x 512 bf16 token-major 25.8 us (5.2 TB/s) and 32.2 with 20
-// alternatives, one row of 10 000 with five 8.0; the gradients of 10 000 x 700 fp32 11.1 (5.0
+// launches of 8 and 3) and 16.3 with five alternatives, 131 072 x 512 bf16 token-major 27.1 us (5.0
+// TB/s) and 32.1 with 20, one row of 10 000 with five 8.2; the gradients of 10 000 x 700 fp32 11.1 (5.0
 // TB/s) and of 50 001 x 1023 fp16 40 (5.1 TB/s).  Bound by memory where there are rows for the
 // whole card, by the chain of one workgroup's loads and sums where there are few.
 #include <type_traits>
@@ -38,6 +38,9 @@ struct Stat {
     float m, s, u;                      // s = 0 and u = 0 where every logit is -inf
 };
 
+// The hardware's exponential of a rounded product: off by up to (|x| + 2) 2^-23 of the term.  x is
+// 0 at the greatest term and a term's share falls as e^x, so that a log sum stays within a few
+// 2^-23 (and results below the smallest normal number are 0).
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 __device__ __forceinline__ Stat join(Stat a, Stat b) {
@@ -519,8 +522,10 @@ __global__ __launch_bounds__(kColThreads) void columns_kernel(Args a) {
         float m[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) m[j] = -kInf;
-        // fp32: all loads of a run under way at once (10 000 x 700: 11.5 -> 10.4 us); eight tokens
-        // of 16 bits a lane would take the registers of other waves (32 000 x 2048: 35 -> 42 us)
+        // fp32: all loads of a run under way at once, which few tokens gain from (in one graph, 8
+        // and 16 at once: 10 000 x 128 8.6 and 8.0 us, x 700 10.4 and 10.2, x 5000 42.8 and 41.5,
+        // but 50 001 x 700 28.1 and 29.5); eight tokens of 16 bits a lane would take the registers
+        // of other waves (32 000 x 2048: 35 -> 42 us)
         constexpr int kAtOnce = sizeof(T) == 4 ? kColRun : kColRun / 2;
 #pragma unroll 1
         for (int r0 = 0; r0 < kColRun; r0 += kAtOnce) {
@@ -773,12 +778,19 @@ Cut cut_of(int dtype, int64_t V, int64_t B, bool contiguous, int64_t top) {
     c.rows = contiguous && V >= c.vec;
     if (c.rows) {
         c.lanes = 0;
-        // a wave has at least four runs, or one where rows are few; a long row several parts
+        // A wave has at least four runs, or one where rows are few (one and four, fp32: 10 000 x 16
+        // 4.3 and 4.5 us, x 512 6.6 and 6.4, x 1024 11.1 and 10.4; all times here in one graph).
         const int64_t run = c.vec * kWave, runs = (V + run - 1) / run, each = B < 256 ? 1 : 4;
         c.threads = 256;
         while (c.threads < 1024 && runs >= 2 * each * c.threads / kWave) c.threads *= 2;
         const int64_t step = int64_t(c.vec) * c.threads;            // one round of a workgroup
         const int64_t rounds = (V + step - 1) / step;
+        // A long row several parts, two workgroups a CU in all (256, 512 and 1024 workgroups: 131 072 x
+        // 64 fp32 with 5 alternatives 13.4, 12.6 and 12.6 us, without, x 256, 24.1, 26.0 and 25.5),
+        // of four rounds at least: a short row's join costs more than its parts win (parts of one,
+        // two and four rounds: 10 000 x 128 fp32 8.2, 4.5 and 4.5; 50 001 x 255 bf16 14.4, 14.2 and
+        // 7.5; one row of 131 072 fp32 5.8, 5.8 and 5.7, with 5 alternatives 13.2, 9.9 and 8.8; one of
+        // 2^20 bf16 6.2, 5.5 and 6.7, with them 29.9, 19.4 and 14.4).
         int64_t parts = (512 + B - 1) / B;
         if (parts > rounds / 4) parts = rounds / 4;
         const int64_t least = top ? (rounds + kPartRounds - 1) / kPartRounds : 1;
@@ -794,6 +806,8 @@ Cut cut_of(int dtype, int64_t V, int64_t B, bool contiguous, int64_t top) {
         const int64_t step = kColThreads / c.lanes * kColRun;     // one round of a workgroup
         const int64_t rounds = (V + step - 1) / step;
         const int64_t tiles = (B + c.lanes * c.vec - 1) / (c.lanes * c.vec);
+        // four workgroups a CU (512, 1024 and 2048 in all: 10 000 x 1500 fp32 16.8, 17.5 and 17.5 us, x
+        // 5000 45.7, 41.5 and 39.4, 32 000 x 2048 bf16 37.3, 34.8 and 35.3)
         int64_t parts = (1024 + tiles - 1) / tiles;
         if (parts > rounds) parts = rounds;
         c.part_len = (rounds + parts - 1) / parts * step;
