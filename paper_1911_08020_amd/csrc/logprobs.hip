@@ -733,12 +733,12 @@ __global__ __launch_bounds__(kGradThreads) void grad_columns_kernel(GradArgs a, 
     }
 }
 
-constexpr int64_t kMaxGridY = 32768;             // and a launch has below 2^32 threads
-
-// One launch per kMaxGridY rows or tiles.
-template <typename A, typename F> hipError_t over_grid_y(A a, int64_t n, F &&launch) {
-    for (a.first = 0; a.first < n; a.first += kMaxGridY) {
-        launch(a, unsigned(n - a.first < kMaxGridY ? n - a.first : kMaxGridY));
+// One launch per 2^15 rows or tiles of `threads` threads each, or as many as stay below 2^32 threads.
+template <typename A, typename F> hipError_t over_grid_y(A a, int64_t n, int64_t threads, F &&launch) {
+    constexpr int64_t kMaxGridY = 32768;
+    const int64_t most = kMostThreads / threads < kMaxGridY ? kMostThreads / threads : kMaxGridY;
+    for (a.first = 0; a.first < n; a.first += most) {
+        launch(a, unsigned(n - a.first < most ? n - a.first : most));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -844,7 +844,7 @@ hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, bool rows, const voi
         using T = decltype(type);
         hipError_t e;
         if (c.rows) {
-            e = over_grid_y(a, B, [&](const Args &part, unsigned n) {
+            e = over_grid_y(a, B, c.nparts * c.threads, [&](const Args &part, unsigned n) {
                 const dim3 grid(unsigned(c.nparts), n);
                 if (c.threads == 256)
                     hipLaunchKernelGGL((rows_kernel<T, 256>), grid, dim3(256), 0, s, part);
@@ -860,7 +860,7 @@ hipError_t launch_logprobs(int dtype, int64_t V, int64_t B, bool rows, const voi
                 constexpr int V1 = decltype(vec)::value;
                 return with_lanes<V1>(c.lanes, [&](auto lanes) {
                     constexpr int L = decltype(lanes)::value;
-                    return over_grid_y(a, tiles, [&](const Args &part, unsigned n) {
+                    return over_grid_y(a, tiles, c.nparts * kColThreads, [&](const Args &part, unsigned n) {
                         hipLaunchKernelGGL((columns_kernel<T, V1, L>),
                                            dim3(unsigned(c.nparts), n), dim3(kColThreads), 0, s,
                                            part);
@@ -900,11 +900,10 @@ hipError_t launch_logprobs_grad(int dtype, int64_t V, int64_t B, bool rows, cons
         auto launch = [&](auto with_entropy) {
             constexpr bool E = decltype(with_entropy)::value;
             if (rows) {
-                const int64_t each = kGradThreads * 4 * VT;
-                return over_grid_y(a, B, [&](const GradArgs &part, unsigned n) {
-                    hipLaunchKernelGGL((grad_rows_kernel<T, E>),
-                                       dim3(unsigned((V + each - 1) / each), n),
-                                       dim3(kGradThreads), 0, s, part);
+                const int64_t each = kGradThreads * 4 * VT, blocks = (V + each - 1) / each;
+                return over_grid_y(a, B, blocks * kGradThreads, [&](const GradArgs &part, unsigned n) {
+                    hipLaunchKernelGGL((grad_rows_kernel<T, E>), dim3(unsigned(blocks), n), dim3(kGradThreads), 0,
+                                       s, part);
                 });
             }
             const int64_t vec = B < VT ? 1 : VT, vecs = (B + vec - 1) / vec;
