@@ -72,3 +72,22 @@ def test_rows_of_dy_far_apart(darb, B, ld):  # noqa: F811
     wv, sv, wX, sX = want(rows, cols, host(v), X, dY, N)
     compare(host(dv), wv, sv, 1e-5, f"dvalues B={B}")
     compare(host(dX), wX, sX, 1e-5, f"dX B={B}")
+
+
+@pytest.mark.parametrize("M", [256, 257])
+@pytest.mark.parametrize("B", [1, 64, 260])
+def test_rows_of_dy_to_4_gib(darb, M, B):  # noqa: F811
+    """The last dY whose byte offsets take 32 bits, and the first that does not."""
+    ld = (1 << 22) - 1
+    assert (M * ld < 1 << 30) == (M == 256)
+    say(f"spmm_grad: {M} rows of batch {B}, leading dimension {ld}")
+    rng = np.random.default_rng(M + B)
+    N = 90
+    plan, v, o, rows, cols = make(darb, rng, M, N, [4, 16])
+    X, dY = rng.standard_normal((N, B)).astype(np.float32), rng.standard_normal((M, B)).astype(np.float32)
+    far = torch.empty(M * ld, device="cuda").view(M, ld)[:, ld - B:]             # to its very end
+    far.copy_(dev(dY))
+    dv, dX = plan.spmm_grad(plan.transpose(o), v, dev(X), far)
+    wv, sv, wX, sX = want(rows, cols, host(v), X, dY, N)
+    compare(host(dv), wv, sv, 1e-5, f"dvalues M={M} B={B}")
+    compare(host(dX), wX, sX, 1e-5, f"dX M={M} B={B}")
