@@ -28,7 +28,9 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kRange = 128;      // columns of one wave while the index is built: whole blocks
 constexpr int kScanThreads = 1024;
-// Elements of dY from which it is cut into tiles of the batch.
+// Elements of dY (3 MB) from which it is cut into tiles of the batch.  In one graph, whole and cut:
+// 2000 rows x 160 24.7 and 33.6 us, 4096 x 160 61.9 and 72.6, 10 000 x 80 (3.1 MB) 43.9 and 51.1, but
+// 2000 x 384 (2.9 MB) 78 and 52, 4096 x 384 (6 MB) 186 and 121.
 constexpr int64_t kSplitFrom = (3 << 20) / 4;
 
 struct Entry {
@@ -726,6 +728,10 @@ hipError_t launch_spmm_grad(const darb_plan &p, const void *index, int wdtype, c
     const IndexParts x = parts_of(p, const_cast<void *>(index));
     const GradArgs a{x.starts, x.entries, values, X, dY, dvalues, dX, p.N, B, ldx, ldy, lddx, wdtype, xdtype, 0};
     if (is_split(p.M, B)) return launch_split(p, a, workspace, s);
+    // 16 bytes a lane and few lanes to a weight, so that a wave has many weights' rows under way.
+    // (4096 x 9216 with 1.2 M weights, so and with twice the lanes or a column a lane: batch 16 18.6 and
+    // 27.0 us, 32 21.2 and 22.2, 64 29.4 and 38.0, 192 65.1 and 84.6, though 128 52.5 and 48.8; 2000 x
+    // 3000: batch 8 8.8 and 10.0, 32 10.1 and 11.6, 128 19.9 and 20.8.)
     if (B == 1) return launch_grad_t<1, 1, 1>(a, p.M, p.nnz, s);
     if (B < 4) return launch_grad_t<4, 1, 1>(a, p.M, p.nnz, s);
     if (B == 4) return launch_grad_t<1, 4, 1>(a, p.M, p.nnz, s);
