@@ -13,6 +13,7 @@
 
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
+#include <c10/hip/HIPCachingAllocator.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -86,13 +87,31 @@ bool stream_of(PyObject *o, void **s) {
     return ok;
 }
 
-// The given stream is not the current one.
-bool elsewhere(PyObject *o, void *s) {
-    return o != Py_None && s != static_cast<void *>(c10::hip::getCurrentHIPStream().stream());
-}
+// What a call allocates, while this lives, for its stream.  On another stream than the current one
+// that is the other's memory: blocks of the current stream may still be in use by work queued there.
+// Results (new or given) are then held until both streams are done with them.
+class Memory {
+  public:
+    Memory(PyObject *o, void *s) : here_(c10::hip::getCurrentHIPStream()), there_(here_) {
+        if (o == Py_None || s == static_cast<void *>(here_.stream())) return;
+        there_ = c10::hip::getStreamFromExternal(static_cast<hipStream_t>(s), here_.device_index());
+        other_ = true;
+        c10::hip::setCurrentHIPStream(there_);
+    }
+    ~Memory() {
+        if (other_) c10::hip::setCurrentHIPStream(here_);
+    }
+    Memory(const Memory &) = delete;
+    Memory &operator=(const Memory &) = delete;
+    void result(const at::Tensor &t) const {
+        if (!other_ || !t.defined()) return;
+        for (const auto &s : {here_, there_}) c10::hip::HIPCachingAllocator::recordStream(t.storage().data_ptr(), s);
+    }
 
-// A result to allocate for a call on another stream, whose memory it takes: left to the Python code.
-bool new_elsewhere(PyObject *out, PyObject *o, void *s) { return out == Py_None && elsewhere(o, s); }
+  private:
+    c10::hip::HIPStream here_, there_;
+    bool other_ = false;
+};
 
 void *ptr(const at::Tensor &t) { return t.data_ptr(); }
 
@@ -181,11 +200,13 @@ PyObject *vector_product(const PlanRef &p, PyObject *xo, PyObject *yo, PyObject 
     int xcode;
     void *s;
     if (!x || !float_code(*x, &xcode) || x->dim() != 1 || x->size(0) != p.N ||
-        !x->is_contiguous() || !stream_of(so, &s) || new_elsewhere(yo, so, s))
+        !x->is_contiguous() || !stream_of(so, &s))
         return none();
+    const Memory memory(so, s);
     at::Tensor y;
     PyObject *res = vector_out(yo, p, *x, &y);
     if (!res) return none();
+    memory.result(y);
     const void *xp = ptr(*x);
     float *yp = static_cast<float *>(ptr(y));
     return finish(res, where, [&] { return call(xcode, xp, yp, s); });
@@ -197,14 +218,15 @@ PyObject *matrix_product(const PlanRef &p, PyObject *xo, PyObject *yo, PyObject 
     const at::Tensor *X = tensor(xo);
     int xcode;
     void *s;
-    if (!X || !float_code(*X, &xcode) || X->dim() != 2 || !stream_of(so, &s) || new_elsewhere(yo, so, s))
-        return none();
+    if (!X || !float_code(*X, &xcode) || X->dim() != 2 || !stream_of(so, &s)) return none();
     const int64_t B = X->size(1), ldx = leading(*X, p.N, B);
     if (ldx < 0) return none();
+    const Memory memory(so, s);
     at::Tensor Y;
     int64_t ldy;
     PyObject *res = matrix_out(yo, p, *X, &Y, &ldy);
     if (!res) return none();
+    memory.result(Y);
     const void *xp = ptr(*X);
     float *yp = static_cast<float *>(ptr(Y));
     return finish(res, where, [&] { return call(xcode, B, xp, ldx, yp, ldy, s); });
@@ -336,12 +358,6 @@ PyObject *encode(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 // ---- evaluating and retraining a layer -------------------------------------------------
-//
-// These allocate outputs and workspaces, which belong to the current stream: a call on another
-// one is left to the Python code, which takes that stream's memory.
-
-// The current stream's handle, for None or the stream itself.
-bool current(PyObject *o, void **s) { return stream_of(o, s) && !elsewhere(o, *s); }
 
 bool any_float_code(const at::Tensor &t, int *code) {
     if (t.scalar_type() != at::kBFloat16) return float_code(t, code);
@@ -420,7 +436,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (n != 4) return none();
         const at::Tensor *z = matrix(a[0]);
         if (!z || !any_float_code(*z, &code) || !optional(a[1], z->size(1), at::kLong, &t) ||
-            !PyLong_CheckExact(a[2]) || !current(a[3], &s))
+            !PyLong_CheckExact(a[2]) || !stream_of(a[3], &s))
             return none();
         const int64_t V = z->size(0), B = z->size(1), fs = z->stride(0), bs = z->stride(1);
         const long long top = PyLong_AsLongLong(a[2]);
@@ -429,6 +445,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
             PyErr_Clear();
             return none();
         }
+        const Memory memory(a[3], s);
         const auto f32 = z->options().dtype(at::kFloat);
         at::Tensor out[5], workspace;
         for (int i = 0; i < 3; ++i) out[i] = at::empty({B}, f32);
@@ -437,6 +454,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
             out[4] = at::empty({B, int64_t(top)}, z->options().dtype(at::kLong));
         }
         if (bytes) workspace = at::empty({bytes}, z->options().dtype(at::kByte));
+        for (const at::Tensor &t : out) memory.result(t);
         const void *zp = ptr(*z);
         float *p[4];
         for (int i = 0; i < 4; ++i) p[i] = out[i].defined() ? static_cast<float *>(ptr(out[i])) : nullptr;
@@ -465,12 +483,14 @@ PyObject *token_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int64_t V = z->size(0), B = z->size(1);
         if (!optional(a[1], B, at::kLong, &t) || !optional(a[2], B, at::kFloat, &lse) || !lse ||
             !optional(a[3], B, at::kFloat, &g) || !optional(a[4], B, at::kFloat, &h) ||
-            !optional(a[5], B, at::kFloat, &gh) || !current(a[7], &s))
+            !optional(a[5], B, at::kFloat, &gh) || !stream_of(a[7], &s))
             return none();
+        const Memory memory(a[7], s);
         at::Tensor dz;
         PyObject *res = given_or(a[6], &dz, [&](PyObject *o) { return matrix_like(o, *z); },
                                  [&] { return dense_like(*z); });
         if (!res) return none();
+        memory.result(dz);
         const void *zp = ptr(*z);
         void *dp = ptr(dz);
         return finish(res, "darb_token_logprobs_grad", [&] {
@@ -504,7 +524,7 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!x || !any_float_code(*x, &code)) return none();
         const int64_t H = x->size(0), B = x->size(1);
         if (!norm_weight(a[1], *x, H, code, &wcode, &w) || !norm_weight(a[2], *x, H, code, &wcode, &b) ||
-            !PyFloat_CheckExact(a[3]) || !current(a[7], &s))
+            !PyFloat_CheckExact(a[3]) || !stream_of(a[7], &s))
             return none();
         const double eps = PyFloat_AS_DOUBLE(a[3]);
         const auto f32 = x->options().dtype(at::kFloat);
@@ -512,6 +532,7 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
             const at::Tensor *t = buffer(o, B, at::kFloat);
             return t && here(*t) ? t : nullptr;
         };
+        const Memory memory(a[7], s);
         at::Tensor y, mean, rstd;
         Held held;
         if (!(held.o[0] = given_or(a[4], &y, [&](PyObject *o) { return matrix_like(o, *x); },
@@ -519,6 +540,7 @@ PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
             !(held.o[1] = given_or(a[5], &mean, vector, [&] { return at::empty({B}, f32); })) ||
             !(held.o[2] = given_or(a[6], &rstd, vector, [&] { return at::empty({B}, f32); })))
             return none();
+        for (const at::Tensor &t : {y, mean, rstd}) memory.result(t);
         const void *xp = ptr(*x);
         void *yp = ptr(y);
         float *mp = static_cast<float *>(ptr(mean)), *rp = static_cast<float *>(ptr(rstd));
@@ -544,12 +566,14 @@ PyObject *layer_norm_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int64_t H = x->size(0), B = x->size(1);
         int64_t bytes;
         if (!dy || !optional(a[2], B, at::kFloat, &mean) || !mean || !optional(a[3], B, at::kFloat, &rstd) ||
-            !rstd || !norm_weight(a[4], *x, H, code, &wcode, &w) || !current(a[5], &s) ||
+            !rstd || !norm_weight(a[4], *x, H, code, &wcode, &w) || !stream_of(a[5], &s) ||
             darb_layer_norm_workspace(H, B, &bytes) != DARB_OK)
             return none();
+        const Memory memory(a[5], s);
         const auto f32 = x->options().dtype(at::kFloat);
         at::Tensor dx = dense_like(*x), dw = at::empty({H}, f32), db = at::empty({H}, f32);
         at::Tensor workspace = at::empty({bytes}, x->options().dtype(at::kByte));
+        for (const at::Tensor &t : {dx, dw, db}) memory.result(t);
         Held held;
         held.o[0] = THPVariable_Wrap(dx);
         held.o[1] = THPVariable_Wrap(dw);
@@ -578,13 +602,16 @@ PyObject *spmm_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const at::Tensor *index = buffer(a[1], need, at::kByte), *values = values_of(a[2], p->nnz, &wcode);
         const at::Tensor *X = tensor(a[3]), *dY = tensor(a[4]);
         if (!index || !values || !X || !dY || !float_code(*X, &xcode) || dY->scalar_type() != at::kFloat ||
-            dY->dim() != 2 || !current(a[5], &s))
+            dY->dim() != 2 || !stream_of(a[5], &s))
             return none();
         const int64_t B = dY->size(1), ldy = leading(*dY, p->M, B), ldx = leading(*X, p->N, B);
         if (ldy < 0 || ldx < 0 || darb_spmm_grad_workspace(p->plan, B, &bytes) != DARB_OK) return none();
+        const Memory memory(a[5], s);
         const auto f32 = dY->options();
         at::Tensor dv = at::empty({p->nnz}, f32), dX = at::empty({p->N, B}, f32), workspace;
         if (bytes) workspace = at::empty({bytes}, f32.dtype(at::kByte));
+        memory.result(dv);
+        memory.result(dX);
         Held held;
         held.o[0] = THPVariable_Wrap(dv);
         held.o[1] = THPVariable_Wrap(dX);

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from tests._gpu import darb, dev, say, torch  # noqa: F401
-from tests._streams import Busy, copies, flat, same
+from tests._streams import Busy, copies, flat, same, without_native
 
 pytestmark = pytest.mark.gpu
 
@@ -61,9 +61,12 @@ def pair(darb):  # noqa: F811
     return inputs(darb, 1), inputs(darb, 2)
 
 
+@pytest.mark.parametrize("path", ["native", "python"])
 @pytest.mark.parametrize("name", sorted(CALLS))
-def test_memory_of_two_streams(darb, busy, pair, name):  # noqa: F811
-    say(f"memory of two streams: {name}")
+def test_memory_of_two_streams(darb, busy, pair, monkeypatch, name, path):  # noqa: F811
+    say(f"memory of two streams: {name} {path}")
+    if path == "python":                             # nothing that the native module takes
+        without_native(monkeypatch, darb)
     call, (fa, fb) = CALLS[name], pair
     want_a, want_b = copies(call(darb, fa)), copies(call(darb, fb))
     assert not same(want_a, want_b)
