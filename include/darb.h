@@ -55,8 +55,8 @@ extern "C" {
 #define DARB_E_NOMEM (-5)        /* host allocation failed */
 #define DARB_E_WORKSPACE (-6)    /* workspace too small */
 
-/* DARB_BF16 is taken by the evaluation and retraining calls only (logits, layer norm,
- * parameters and their gradients); the format and its products are fp32 or fp16. */
+/* DARB_BF16 is taken by the evaluation and retraining calls only (logits, layer norm, the gated
+ * recurrence, parameters and their gradients); the format and its products are fp32 or fp16. */
 typedef enum { DARB_F32 = 0, DARB_F16 = 1, DARB_BF16 = 2 } darb_dtype;
 
 /* Rounding of a row density to a power-of-two fraction (section 3.2). */
@@ -541,6 +541,161 @@ int darb_adamw_step(const darb_adamw *adamw, const void *const *grads, const int
 int darb_adamw_moments(const darb_adamw *adamw, float *const *m, float *const *v, int64_t count,
                        void *stream);
 void darb_adamw_destroy(darb_adamw *adamw);
+
+/*
+ * A gated linear recurrence over sequences, the recurrent layer that is retrained here: column
+ * t * batch + n of an operand [H x T*batch] is step t of sequence n, as in darb_lstm_layer.
+ *   DARB_RECURRENCE_GATE    f = sigmoid(gate),  h_t = f_t h_{t-1} + (1 - f_t) x_t
+ *   DARB_RECURRENCE_LINEAR  f = gate,           h_t = f_t h_{t-1} + x_t
+ * elementwise, from h_{-1} = h0.  T = 1 is the single step of a program that generates: h0 and
+ * h_last may be the same buffer.
+ *   dtype     type of gate, x and h: DARB_F32, DARB_F16 or DARB_BF16; the state between steps
+ *             and h0, h_last are fp32
+ *   gate, x   device [H x T*batch], any order, one for all such operands (strides as above)
+ *   resets    device uint8 [T*batch] or NULL: where it is not 0 a sequence starts, and the state
+ *             before it counts as 0, whatever it was (packed texts)
+ *   h0        device fp32 [H x batch], either order, or NULL (zeros)
+ *   h         device [H x T*batch] of dtype, receives every state; may be gate or x itself
+ *   h_last    device fp32 [H x batch], either order, or NULL: the state after the last step
+ * Steps are joined as maps h -> a h + b, a being a product of gates: gates above 1 in magnitude
+ * (linear form) are right as long as no product of consecutive ones leaves the range of fp32.  A
+ * state that is not finite makes those after it not finite, up to the next start.
+ *   workspace device, 256-byte aligned, >= darb_gated_recurrence_workspace's bytes (back: 0, or
+ *             1 for the gradients); NULL where those are 0
+ * H, T, batch >= 1, H < 2^31, T * batch < 2^31.
+ *
+ * Gradients, from dh [H x T*batch] (by every state) and dh_last (by the last one; NULL: zeros),
+ * with g_t = dh_t + f_{t+1} g_{t+1} (nothing from a start), g_{T-1} = dh_{T-1} + dh_last:
+ *   gate form    dgate_t = (h_{t-1} - x_t) g_t f_t (1 - f_t),  dx_t = (1 - f_t) g_t
+ *   linear form  dgate_t = h_{t-1} g_t,                        dx_t = g_t   (x is not read: NULL)
+ *   dh0 = f_0 g_0 (zeros where step 0 is a start)
+ *   h          as darb_gated_recurrence returned it; h0 as it was given
+ *   dgate, dx  device [H x T*batch] of dtype; each may be dh, gate or x itself, neither may be h
+ *   dh0        device fp32 [H x batch], either order, or NULL; may be dh_last or h0 itself
+ * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_WORKSPACE, DARB_E_HIP.
+ */
+typedef enum { DARB_RECURRENCE_GATE = 0, DARB_RECURRENCE_LINEAR = 1 } darb_recurrence;
+
+/* A device matrix: element (f, b) at p + f * feature_stride + b * batch_stride (elements). */
+typedef struct {
+    void *p;
+    int64_t feature_stride, batch_stride;
+} darb_matrix;
+
+int darb_gated_recurrence_workspace(int dtype, int back, int64_t H, int64_t T, int64_t batch,
+                                    int64_t *bytes);
+int darb_gated_recurrence(int dtype, int form, int64_t H, int64_t T, int64_t batch,
+                          const darb_matrix *gate, const darb_matrix *x, const uint8_t *resets,
+                          const darb_matrix *h0, const darb_matrix *h, const darb_matrix *h_last,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+int darb_gated_recurrence_grad(int dtype, int form, int64_t H, int64_t T, int64_t batch,
+                               const darb_matrix *dh, const darb_matrix *gate,
+                               const darb_matrix *x, const darb_matrix *h, const uint8_t *resets,
+                               const darb_matrix *h0, const darb_matrix *dh_last,
+                               const darb_matrix *dgate, const darb_matrix *dx,
+                               const darb_matrix *dh0, void *workspace, int64_t workspace_bytes,
+                               void *stream);
+
+/*
+ * The clipped policy loss over token log probabilities (darb_token_logprobs), and its gradients,
+ * which darb_token_logprobs_grad takes: with r = e^(logprob - old), q = ref - logprob,
+ *   L_b = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (e^q - 1 - q)
+ *         - entropy_coef entropy,
+ *   loss = sum_b weight_b L_b,  kl = sum_b weight_b (e^q - 1 - q),
+ *   clipped = sum of the weights of the tokens whose ratio's part is the clipped one (and so has
+ *   no gradient),
+ *   grad_logprob = weight (-r A where not clipped, - kl_coef (e^q - 1)),
+ *   grad_entropy = -weight entropy_coef.
+ * A token of weight 0 adds nothing and has gradient 0, whatever its other values are.
+ *   logprob, old, advantage   device fp32 [B], 1 <= B < 2^31
+ *   weight        device fp32 [B], or NULL (1 / B each)
+ *   ref           device fp32 [B], or NULL (kl is 0; kl_coef must be 0 then)
+ *   entropy       device fp32 [B], with grad_entropy, or NULL both (entropy_coef 0)
+ *   clip_low, clip_high   >= 0 (clip_low of 1 or more: no lower bound); kl_coef >= 0
+ *   stats         device fp32 [3]: loss, kl, clipped
+ *   grad_logprob, grad_entropy   device fp32 [B]; may be any of the inputs of that size
+ *   workspace     device, 256-byte aligned, >= darb_policy_loss_workspace's bytes; NULL where
+ *                 those are 0
+ * Errors: DARB_E_INVALID, DARB_E_WORKSPACE, DARB_E_HIP.
+ */
+int darb_policy_loss_workspace(int64_t B, int64_t *bytes);
+int darb_policy_loss(int64_t B, const float *logprob, const float *old, const float *advantage,
+                     const float *weight, const float *ref, const float *entropy,
+                     double clip_low, double clip_high, double kl_coef, double entropy_coef,
+                     float *stats, float *grad_logprob, float *grad_entropy, void *workspace,
+                     int64_t workspace_bytes, void *stream);
+
+/*
+ * The preference loss of `pairs` pairs of sequences over token log probabilities, and its gradient.
+ * Sequences 0 ... P-1 are the preferred ones, P ... 2P-1 the others of the same pairs.  With
+ * s = a sequence's sum of logprob - ref, m_p = beta (s_p - s_{P+p}),
+ *   loss = sum_p weight_p (-(1 - smoothing) log sigma(m_p) - smoothing log sigma(-m_p)),
+ *   grad_logprob = weight_p beta (smoothing - sigma(-m_p)) for the tokens of sequence p, the
+ *   negative for those of P + p.
+ *   starts        NULL: B = T * 2P, token t of sequence s at t * 2P + s (the columns of an operand
+ *                 [V x T*batch] with batch 2P; a padded place has logprob and ref 0).  Or device
+ *                 int64 [2P + 1], never decreasing: sequence s holds the tokens starts[s] ...
+ *                 starts[s + 1] - 1; tokens before the first and behind the last sequence have
+ *                 gradient 0.  What lies outside [0, B] is taken as 0 or B.
+ *   logprob       device fp32 [B], 1 <= B < 2^31; ref device fp32 [B], or NULL (zeros)
+ *   weight        device fp32 [P], or NULL (1 / P each); a pair of weight 0 adds nothing and has
+ *                 gradient 0, whatever its margin is
+ *   beta          finite, >= 0; smoothing in [0, 1)
+ *   loss          device fp32 [1]; margin device fp32 [P] (m_p)
+ *   grad_logprob  device fp32 [B]; may be logprob or ref itself
+ * 1 <= P < 2^30.
+ * Errors: DARB_E_INVALID, DARB_E_HIP.
+ */
+int darb_preference_loss(int64_t pairs, int64_t B, const float *logprob, const float *ref,
+                         const int64_t *starts, const float *weight, double beta,
+                         double smoothing, float *loss, float *margin, float *grad_logprob,
+                         void *stream);
+
+/*
+ * The orthogonalised update of weight matrices: a matrix u is divided by its norm and its singular
+ * values taken towards 1 by steps of a quintic, X = u / (|u| + eps) (Frobenius norm),
+ *   X = a X + (b A + c A A) X,  A = X X^T (X with at most as many rows as columns),
+ *   (a, b, c) = (3.4445, -4.7750, 2.0315),
+ * after five of which those from 0.01 of |u| up lie between 0.68 and 1.21.
+ * darb_orthogonalize writes that X of each matrix; darb_muon_step makes one optimizer step with
+ *   m = momentum m + (1 - momentum) g,  u = momentum m + (1 - momentum) g  (nesterov; else m)
+ *   p = p (1 - lr decay) - lr scale X.
+ * Sums and m are fp32 or more.  An fp32 result (or master) is as accurate as fp32 products make
+ * it; one of 16 bits has its products in fp16 (X itself in more), off by 1 to 3 10^-3 of its norm.
+ * A matrix that holds an infinity or NaN becomes NaN; zeros stay zeros.
+ *   dtype, gdtype   DARB_F32, DARB_F16 or DARB_BF16, of param and of grad
+ *   param       device [rows x cols], unit column stride, leading dimension ld_param >= cols
+ *               (darb_orthogonalize: receives X; may be grad itself)
+ *   master      device fp32 [rows x cols] at the same leading dimension, or NULL: a copy that the
+ *               step updates and rounds into param
+ *   grad        device [rows x cols], unit column stride, leading dimension ld_grad >= cols;
+ *               NULL (darb_muon_step): the tensor is left as it is
+ *   momentum    device fp32 [rows x cols], contiguous (darb_orthogonalize: NULL)
+ *   scale, decay  finite, decay >= 0
+ *   rows, cols  1 <= rows, cols < 2^20
+ *   tensors     host array of `count` >= 1, read during the call; no memory overlaps
+ *   steps       1 ... 16;  momentum in [0, 1), lr >= 0, eps > 0 (finite)
+ *   grad_scale  device fp32 [1] that multiplies every gradient, or NULL (1)
+ *   workspace   device, 256-byte aligned, >= darb_muon_workspace's bytes for these tensors; it
+ *               grows with the largest group of tensors that is taken at once
+ * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_WORKSPACE, DARB_E_HIP.
+ */
+typedef struct {
+    void *param;
+    float *master;
+    const void *grad;
+    float *momentum;
+    int64_t rows, cols, ld_param, ld_grad;
+    double scale, decay;
+    int32_t dtype, gdtype;
+} darb_muon_tensor;
+
+int darb_muon_workspace(const darb_muon_tensor *tensors, int64_t count, int64_t *bytes);
+int darb_muon_step(const darb_muon_tensor *tensors, int64_t count, double lr, double momentum,
+                   int nesterov, int steps, double eps, const float *grad_scale, void *workspace,
+                   int64_t workspace_bytes, void *stream);
+int darb_orthogonalize(const darb_muon_tensor *tensors, int64_t count, int steps, double eps,
+                       void *workspace, int64_t workspace_bytes, void *stream);
 
 /*
  * Measurement helpers (not part of DARB).  darb_stream_read reads `bytes`

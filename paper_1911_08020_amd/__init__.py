@@ -81,6 +81,19 @@ class _AdamTensor(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class _Matrix(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("feature_stride", ctypes.c_int64),
+                ("batch_stride", ctypes.c_int64)]
+
+
+class _MuonTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("momentum", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld_param", ctypes.c_int64), ("ld_grad", ctypes.c_int64),
+                ("scale", ctypes.c_double), ("decay", ctypes.c_double), ("dtype", ctypes.c_int32),
+                ("gdtype", ctypes.c_int32)]
+
+
 def _load_library():
     # torch carries its own HIP runtime (same soname as /opt/rocm's).  Loading it
     # first makes libdarb.so bind to that one, so the process has a single HIP
@@ -137,6 +150,16 @@ def _load_library():
         "darb_adamw_step": ([P, P, P, I64] + [ctypes.c_double] * 4 + [I64, P, ctypes.c_uint32, P], I),
         "darb_adamw_moments": ([P, P, P, I64, P], I),
         "darb_adamw_destroy": ([P], None),
+        "darb_gated_recurrence_workspace": ([I, I, I64, I64, I64, ctypes.POINTER(I64)], I),
+        "darb_gated_recurrence": ([I, I, I64, I64, I64, P, P, P, P, P, P, P, I64, P], I),
+        "darb_gated_recurrence_grad": ([I, I, I64, I64, I64] + [P] * 11 + [I64, P], I),
+        "darb_policy_loss_workspace": ([I64, ctypes.POINTER(I64)], I),
+        "darb_policy_loss": ([I64] + [P] * 6 + [ctypes.c_double] * 4 + [P] * 4 + [I64, P], I),
+        "darb_preference_loss": ([I64, I64] + [P] * 4 + [ctypes.c_double] * 2 + [P] * 4, I),
+        "darb_muon_workspace": ([P, I64, ctypes.POINTER(I64)], I),
+        "darb_muon_step": ([P, I64, ctypes.c_double, ctypes.c_double, I, I, ctypes.c_double, P, P,
+                            I64, P], I),
+        "darb_orthogonalize": ([P, I64, I, ctypes.c_double, P, I64, P], I),
         "darb_stream_read": ([P, I64, P, P], I),
         "darb_stream_read_shape": ([P, I64, I, I, P, P], I),
         "darb_stream_copy": ([P, P, I64, P], I),
@@ -162,7 +185,10 @@ EXPORTED = ("darb_plan_create", "darb_plan_create_counts", "darb_plan_device_wor
             "darb_layer_norm_grad", "darb_transpose_bytes", "darb_transpose",
             "darb_spmm_grad_workspace", "darb_spmm_grad",
             "darb_adamw_workspace", "darb_adamw_create", "darb_adamw_step", "darb_adamw_moments",
-            "darb_adamw_destroy", "darb_stream_read", "darb_stream_read_shape", "darb_stream_copy", "darb_strerror",
+            "darb_adamw_destroy", "darb_gated_recurrence_workspace", "darb_gated_recurrence",
+            "darb_gated_recurrence_grad", "darb_policy_loss_workspace", "darb_policy_loss",
+            "darb_preference_loss", "darb_muon_workspace", "darb_muon_step", "darb_orthogonalize",
+            "darb_stream_read", "darb_stream_read_shape", "darb_stream_copy", "darb_strerror",
             "darb_last_error", "darb_version")
 
 
@@ -790,5 +816,7 @@ def stream_copy(dst, src, stream=None):
            "darb_stream_copy")
 
 
-from .training import (AdamW, TokenLogprobs, layer_norm, layer_norm_grad,  # noqa: E402,F401
-                       token_logprobs, token_logprobs_grad)
+from .training import (AdamW, Muon, PolicyLoss, PreferenceLoss, TokenLogprobs,  # noqa: E402,F401
+                       gated_recurrence, gated_recurrence_grad, layer_norm, layer_norm_grad,
+                       orthogonalize, policy_loss, preference_loss, token_logprobs,
+                       token_logprobs_grad)

@@ -140,6 +140,50 @@ template <typename F> int over_tensors(const darb_adamw &a, int64_t most, F &&f)
     return DARB_OK;
 }
 
+// Whether the result's own type asks for fp32 products.
+bool muon_full(const darb_muon_tensor &t) { return t.dtype == DARB_F32 || t.master; }
+
+// The groups of tensors that go through the launches together: consecutive ones of one accuracy,
+// up to kMuonTensors and 2^28 elements of theirs (or a single one).  A tensor that is left out
+// (`skip`: without a gradient) counts in its group all the same, so that no step's groups take
+// more than those of all tensors.  f(group, its bytes).
+template <typename F>
+int over_groups(const darb_muon_tensor *t, int64_t count, bool skip, double lr, F &&f) {
+    constexpr int64_t kMostElements = int64_t(1) << 28;
+    for (int full = 0; full < 2; ++full) {
+        MuonCall c{};
+        c.full = full != 0;
+        int members = 0;
+        int64_t elements = 0;
+        for (int64_t i = 0; i <= count; ++i) {
+            const bool end = i == count;
+            if (!end && muon_full(t[i]) != c.full) continue;
+            const int64_t n = end ? 0 : t[i].rows * t[i].cols;
+            if (members && (end || members == kMuonTensors || elements + n > kMostElements)) {
+                if (c.count) {
+                    const int64_t bytes = muon_group(c);
+                    const int rc = f(c, bytes);
+                    if (rc) return rc;
+                }
+                members = c.count = 0;
+                elements = 0;
+            }
+            if (end) break;
+            ++members;
+            elements += n;
+            if (skip && !t[i].grad) continue;
+            MuonTensor &to = c.t[c.count++];
+            to = {};
+            to.param = t[i].param, to.master = t[i].master, to.grad = t[i].grad, to.momentum = t[i].momentum;
+            to.ld_in = t[i].ld_grad, to.ld_out = t[i].ld_param;
+            to.rows = int32_t(t[i].rows), to.cols = int32_t(t[i].cols);
+            to.dtype = t[i].dtype, to.gdtype = t[i].gdtype;
+            to.scale = float(lr * t[i].scale), to.keep = float(1.0 - lr * t[i].decay);
+        }
+    }
+    return DARB_OK;
+}
+
 }  // namespace
 }  // namespace darb
 
@@ -466,5 +510,257 @@ int darb_adamw_moments(const darb_adamw *a, float *const *m, float *const *v, in
 }
 
 void darb_adamw_destroy(darb_adamw *a) { delete a; }
+
+static bool recurrence_sizes(int64_t H, int64_t T, int64_t batch) {
+    return H >= 1 && H < kMax && T >= 1 && batch >= 1 && T < kMax && batch < kMax && T * batch < kMax;
+}
+
+static int check_recurrence(int dtype, int form, int64_t H, int64_t T, int64_t batch) {
+    if (!recurrence_sizes(H, T, batch))
+        return fail(DARB_E_INVALID, "H, T and batch must be >= 1, H and T * batch below 2^31");
+    if (!float_dtype(dtype)) return fail(DARB_E_DTYPE, "unknown dtype");
+    if (form != DARB_RECURRENCE_GATE && form != DARB_RECURRENCE_LINEAR)
+        return fail(DARB_E_INVALID, "unknown form");
+    return DARB_OK;
+}
+
+static int64_t recurrence_bytes(int dtype, bool back, int64_t H, int64_t T, int64_t batch) {
+    const int64_t a = recurrence_workspace_bytes(dtype, back, false, H, T, batch);
+    const int64_t b = recurrence_workspace_bytes(dtype, back, true, H, T, batch);
+    return a > b ? a : b;
+}
+
+// A state [H x batch] of either order; `read`: its elements may coincide.
+static int check_state(const darb_matrix *m, bool read, int64_t H, int64_t batch, const char *name,
+                       RecurrenceMatrix *out) {
+    if (!m || !m->p) return DARB_OK;
+    if (!aligned(m->p, 4)) return fail(DARB_E_INVALID, std::string(name) + " is not aligned to its elements");
+    const Strides s{m->feature_stride, m->batch_stride};
+    if (s.feature < 0 || s.batch < 0 ||
+        (!read && !as_rows(s, H, batch, 1) && !as_columns(s, H, batch, 1)))
+        return fail(DARB_E_INVALID, std::string(name) + ": one stride must be 1 and the other at least that axis' length");
+    *out = {m->p, s.feature, s.batch};
+    return DARB_OK;
+}
+
+// The operands [H x T*batch], all in one order; `reads` of them are only read.
+static int check_sequences(RecurrenceMatrix *const *to, const darb_matrix *const *m, int count, int reads, int64_t H,
+                           int64_t columns, int dtype, const char *where, bool *rows) {
+    Strides s[6];
+    for (int i = 0; i < count; ++i) {
+        if (!m[i] || !m[i]->p) return fail(DARB_E_INVALID, "NULL buffer");
+        if (!aligned(m[i]->p, size_of(dtype))) return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
+        s[i] = {m[i]->feature_stride, m[i]->batch_stride};
+    }
+    const int rc = common_order(s, count, reads, H, columns, where, rows);
+    if (rc) return rc;
+    for (int i = 0; i < count; ++i) *to[i] = {m[i]->p, s[i].feature, s[i].batch};
+    return DARB_OK;
+}
+
+int darb_gated_recurrence_workspace(int dtype, int back, int64_t H, int64_t T, int64_t batch, int64_t *bytes) {
+    clear_error();
+    if (!bytes) return fail(DARB_E_INVALID, "bytes is NULL");
+    const int rc = check_recurrence(dtype, DARB_RECURRENCE_GATE, H, T, batch);
+    if (rc) return rc;
+    *bytes = recurrence_bytes(dtype, back != 0, H, T, batch);
+    return DARB_OK;
+}
+
+int darb_gated_recurrence(int dtype, int form, int64_t H, int64_t T, int64_t batch, const darb_matrix *gate,
+                          const darb_matrix *x, const uint8_t *resets, const darb_matrix *h0, const darb_matrix *h,
+                          const darb_matrix *h_last, void *workspace, int64_t workspace_bytes, void *stream) {
+    clear_error();
+    int rc = check_recurrence(dtype, form, H, T, batch);
+    if (rc) return rc;
+    RecurrenceCall c;
+    const darb_matrix *const m[] = {gate, x, h};
+    RecurrenceMatrix *const to[] = {&c.gate, &c.x, &c.out};
+    if ((rc = check_sequences(to, m, 3, 2, H, T * batch, dtype, "gate, x, h", &c.rows)) ||
+        (rc = check_state(h0, true, H, batch, "h0", &c.in)) ||
+        (rc = check_state(h_last, false, H, batch, "h_last", &c.last)))
+        return rc;
+    const int64_t need = recurrence_bytes(dtype, false, H, T, batch);
+    if (need > 0 && (rc = check_workspace(workspace, workspace_bytes, need))) return rc;
+    c.dtype = dtype, c.form = form, c.back = false;
+    c.H = H, c.T = T, c.batch = batch;
+    c.resets = resets, c.workspace = workspace;
+    return launched(launch_recurrence(c, static_cast<hipStream_t>(stream)), "gated recurrence launch");
+}
+
+int darb_gated_recurrence_grad(int dtype, int form, int64_t H, int64_t T, int64_t batch, const darb_matrix *dh,
+                               const darb_matrix *gate, const darb_matrix *x, const darb_matrix *h,
+                               const uint8_t *resets, const darb_matrix *h0, const darb_matrix *dh_last,
+                               const darb_matrix *dgate, const darb_matrix *dx, const darb_matrix *dh0,
+                               void *workspace, int64_t workspace_bytes, void *stream) {
+    clear_error();
+    int rc = check_recurrence(dtype, form, H, T, batch);
+    if (rc) return rc;
+    RecurrenceCall c;
+    const bool with_x = form == DARB_RECURRENCE_GATE;
+    const darb_matrix *const m[] = {dh, gate, h, with_x ? x : gate, dgate, dx};
+    RecurrenceMatrix *const to[] = {&c.dh, &c.gate, &c.h, &c.x, &c.out, &c.out2};
+    if ((rc = check_sequences(to, m, 6, 4, H, T * batch, dtype, "dh, gate, x, h, dgate, dx", &c.rows)) ||
+        (rc = check_state(h0, true, H, batch, "h0", &c.h0)) ||
+        (rc = check_state(dh_last, true, H, batch, "dh_last", &c.in)) ||
+        (rc = check_state(dh0, false, H, batch, "dh0", &c.last)))
+        return rc;
+    if (dgate->p == h->p || dx->p == h->p || dgate->p == dx->p)
+        return fail(DARB_E_INVALID, "dgate, dx and h must be different buffers");
+    const int64_t need = recurrence_bytes(dtype, true, H, T, batch);
+    if (need > 0 && (rc = check_workspace(workspace, workspace_bytes, need))) return rc;
+    c.dtype = dtype, c.form = form, c.back = true;
+    c.H = H, c.T = T, c.batch = batch;
+    c.resets = resets, c.workspace = workspace;
+    return launched(launch_recurrence(c, static_cast<hipStream_t>(stream)), "gated recurrence gradient launch");
+}
+
+int darb_policy_loss_workspace(int64_t B, int64_t *bytes) {
+    clear_error();
+    if (!bytes) return fail(DARB_E_INVALID, "bytes is NULL");
+    if (B < 1 || B >= kMax) return fail(DARB_E_INVALID, "B must be in [1, 2^31)");
+    *bytes = policy_workspace_bytes(B);
+    return DARB_OK;
+}
+
+int darb_policy_loss(int64_t B, const float *logprob, const float *old, const float *advantage, const float *weight,
+                     const float *ref, const float *entropy, double clip_low, double clip_high, double kl_coef,
+                     double entropy_coef, float *stats, float *grad_logprob, float *grad_entropy, void *workspace,
+                     int64_t workspace_bytes, void *stream) {
+    clear_error();
+    if (B < 1 || B >= kMax) return fail(DARB_E_INVALID, "B must be in [1, 2^31)");
+    if (!logprob || !old || !advantage || !stats || !grad_logprob) return fail(DARB_E_INVALID, "NULL buffer");
+    if ((entropy == nullptr) != (grad_entropy == nullptr))
+        return fail(DARB_E_INVALID, "pass entropy and grad_entropy, or neither");
+    if (!(clip_low >= 0.0) || !(clip_high >= 0.0) || !std::isfinite(clip_low) || !std::isfinite(clip_high))
+        return fail(DARB_E_INVALID, "clip_low and clip_high must be finite and >= 0");
+    if (!(kl_coef >= 0.0) || !std::isfinite(kl_coef) || !std::isfinite(entropy_coef))
+        return fail(DARB_E_INVALID, "kl_coef must be finite and >= 0, entropy_coef finite");
+    if ((!ref && kl_coef != 0.0) || (!entropy && entropy_coef != 0.0))
+        return fail(DARB_E_INVALID, "a coefficient without its values");
+    for (const void *p : {static_cast<const void *>(logprob), static_cast<const void *>(old),
+                          static_cast<const void *>(advantage), static_cast<const void *>(weight),
+                          static_cast<const void *>(ref), static_cast<const void *>(entropy),
+                          static_cast<const void *>(stats), static_cast<const void *>(grad_logprob),
+                          static_cast<const void *>(grad_entropy)})
+        if (!aligned(p, 4)) return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
+    if (grad_logprob == grad_entropy) return fail(DARB_E_INVALID, "the gradients must be different buffers");
+    const int64_t need = policy_workspace_bytes(B);
+    int rc;
+    if (need > 0 && (rc = check_workspace(workspace, workspace_bytes, need))) return rc;
+    PolicyCall c{};
+    c.B = B;
+    c.lp = logprob, c.old = old, c.advantage = advantage, c.weight = weight, c.ref = ref, c.entropy = entropy;
+    c.grad = grad_logprob, c.grad_entropy = grad_entropy, c.stats = stats;
+    c.partial = static_cast<double *>(workspace);
+    c.even = float(1.0 / double(B));
+    c.low = float(1.0 - clip_low), c.high = float(1.0 + clip_high);
+    c.kl_coef = float(kl_coef), c.entropy_coef = float(entropy_coef);
+    c.log_low = clip_low < 1.0 ? std::log1p(-clip_low) : -HUGE_VAL;
+    c.log_high = std::log1p(clip_high);
+    return launched(launch_policy(c, static_cast<hipStream_t>(stream)), "policy loss launch");
+}
+
+int darb_preference_loss(int64_t pairs, int64_t B, const float *logprob, const float *ref, const int64_t *starts,
+                         const float *weight, double beta, double smoothing, float *loss, float *margin,
+                         float *grad_logprob, void *stream) {
+    clear_error();
+    if (pairs < 1 || pairs >= kMax / 2) return fail(DARB_E_INVALID, "pairs must be in [1, 2^30)");
+    if (B < 1 || B >= kMax) return fail(DARB_E_INVALID, "B must be in [1, 2^31)");
+    if (!starts && B % (2 * pairs) != 0) return fail(DARB_E_INVALID, "B must be a multiple of 2 * pairs");
+    if (!logprob || !loss || !margin || !grad_logprob) return fail(DARB_E_INVALID, "NULL buffer");
+    if (!(beta >= 0.0) || !std::isfinite(beta)) return fail(DARB_E_INVALID, "beta must be finite and >= 0");
+    if (!(smoothing >= 0.0 && smoothing < 1.0)) return fail(DARB_E_INVALID, "smoothing must be in [0, 1)");
+    if (!aligned(logprob, 4) || !aligned(ref, 4) || !aligned(starts, 8) || !aligned(weight, 4) || !aligned(loss, 4) ||
+        !aligned(margin, 4) || !aligned(grad_logprob, 4))
+        return fail(DARB_E_INVALID, "a buffer is not aligned to its elements");
+    PreferenceCall c{};
+    c.P = pairs, c.B = B, c.L = B / (2 * pairs);
+    c.lp = logprob, c.ref = ref, c.weight = weight, c.starts = starts;
+    c.loss = loss, c.margin = margin, c.grad = grad_logprob;
+    c.even = float(1.0 / double(pairs)), c.beta = float(beta), c.smoothing = float(smoothing);
+    return launched(launch_preference(c, static_cast<hipStream_t>(stream)), "preference loss launch");
+}
+
+static int check_muon(const darb_muon_tensor *t, int64_t count, bool buffers, bool update) {
+    if (!t) return fail(DARB_E_INVALID, "tensors is NULL");
+    if (count < 1 || count >= kMax) return fail(DARB_E_INVALID, "count must be in [1, 2^31)");
+    for (int64_t i = 0; i < count; ++i) {
+        const std::string name = "tensor " + std::to_string(i) + ": ";
+        if (t[i].rows < 1 || t[i].rows >= int64_t(1) << 20 || t[i].cols < 1 || t[i].cols >= int64_t(1) << 20)
+            return fail(DARB_E_INVALID, name + "rows and cols must be in [1, 2^20)");
+        if (!float_dtype(t[i].dtype)) return fail(DARB_E_DTYPE, name + "unknown dtype");
+        if (!buffers) continue;
+        if (t[i].ld_param < t[i].cols) return fail(DARB_E_INVALID, name + "a leading dimension is below cols");
+        if (!t[i].param || (update && !t[i].momentum)) return fail(DARB_E_INVALID, name + "NULL buffer");
+        if (!update && !t[i].grad) return fail(DARB_E_INVALID, name + "NULL buffer");
+        if (!aligned(t[i].param, size_of(t[i].dtype)) || !aligned(t[i].master, 4) || !aligned(t[i].momentum, 4))
+            return fail(DARB_E_INVALID, name + "a buffer is not aligned to its elements");
+        if (update && (!std::isfinite(t[i].scale) || !(t[i].decay >= 0.0) || !std::isfinite(t[i].decay)))
+            return fail(DARB_E_INVALID, name + "scale must be finite, decay finite and >= 0");
+        if (!t[i].grad) continue;
+        if (!float_dtype(t[i].gdtype)) return fail(DARB_E_DTYPE, name + "unknown gradient dtype");
+        if (t[i].ld_grad < t[i].cols) return fail(DARB_E_INVALID, name + "a leading dimension is below cols");
+        if (!aligned(t[i].grad, size_of(t[i].gdtype)))
+            return fail(DARB_E_INVALID, name + "a buffer is not aligned to its elements");
+    }
+    return DARB_OK;
+}
+
+int darb_muon_workspace(const darb_muon_tensor *tensors, int64_t count, int64_t *bytes) {
+    clear_error();
+    if (!bytes) return fail(DARB_E_INVALID, "bytes is NULL");
+    int rc = check_muon(tensors, count, false, false);
+    if (rc) return rc;
+    *bytes = 0;
+    return over_groups(tensors, count, false, 0.0, [&](MuonCall &, int64_t need) {
+        if (need > *bytes) *bytes = need;
+        return int(DARB_OK);
+    });
+}
+
+static int muon(const darb_muon_tensor *tensors, int64_t count, bool update, double lr, double momentum, int nesterov,
+                int steps, double eps, const float *grad_scale, void *workspace, int64_t workspace_bytes,
+                void *stream) {
+    if (steps < 1 || steps > 16) return fail(DARB_E_INVALID, "steps must be in [1, 16]");
+    if (!(eps > 0.0) || !std::isfinite(eps)) return fail(DARB_E_INVALID, "eps must be finite and > 0");
+    if (!(lr >= 0.0) || !std::isfinite(lr)) return fail(DARB_E_INVALID, "lr must be finite and >= 0");
+    if (!(momentum >= 0.0 && momentum < 1.0)) return fail(DARB_E_INVALID, "momentum must be in [0, 1)");
+    if (!aligned(grad_scale, 4)) return fail(DARB_E_INVALID, "grad_scale is not aligned");
+    int rc = check_muon(tensors, count, true, update);
+    if (rc) return rc;
+    rc = check_workspace(workspace, workspace_bytes, 0);
+    if (rc) return rc;
+    auto group = [&](MuonCall &c, int64_t bytes) {
+        if (bytes > workspace_bytes)
+            return fail(DARB_E_WORKSPACE, "workspace needs " + std::to_string(bytes) + " bytes");
+        return int(DARB_OK);
+    };
+    if ((rc = over_groups(tensors, count, update, lr, group))) return rc;       // all, before the first launch
+    return over_groups(tensors, count, update, lr, [&](MuonCall &c, int64_t) {
+        c.update = update;
+        c.nesterov = nesterov != 0;
+        c.steps = steps;
+        c.mu = float(momentum), c.one_mu = float(1.0 - momentum);
+        c.eps = eps;
+        c.grad_scale = grad_scale;
+        c.workspace = workspace;
+        return launched(launch_muon(c, static_cast<hipStream_t>(stream)), "orthogonalised update launch");
+    });
+}
+
+int darb_muon_step(const darb_muon_tensor *tensors, int64_t count, double lr, double momentum, int nesterov,
+                   int steps, double eps, const float *grad_scale, void *workspace, int64_t workspace_bytes,
+                   void *stream) {
+    clear_error();
+    return muon(tensors, count, true, lr, momentum, nesterov, steps, eps, grad_scale, workspace, workspace_bytes,
+                stream);
+}
+
+int darb_orthogonalize(const darb_muon_tensor *tensors, int64_t count, int steps, double eps, void *workspace,
+                       int64_t workspace_bytes, void *stream) {
+    clear_error();
+    return muon(tensors, count, false, 0.0, 0.0, 0, steps, eps, nullptr, workspace, workspace_bytes, stream);
+}
 
 }  // extern "C"

@@ -700,6 +700,254 @@ PyObject *adamw_moments(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+darb_matrix as_matrix(const at::Tensor &t) { return {ptr(t), t.stride(0), t.stride(1)}; }
+
+// A state fp32 [H, batch] on the current device; None is none.
+bool state(PyObject *o, int64_t H, int64_t batch, darb_matrix *m, const darb_matrix **p) {
+    *p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *t = tensor(o);
+    if (!t || t->scalar_type() != at::kFloat || t->dim() != 2 || t->size(0) != H || t->size(1) != batch || !here(*t))
+        return false;
+    *m = as_matrix(*t);
+    *p = m;
+    return true;
+}
+
+at::Tensor state_like(const at::Tensor &x, int64_t H, int64_t batch) {
+    const auto f32 = x.options().dtype(at::kFloat);
+    if (x.stride(0) == 1 && H > 1 && x.size(1) > 1) return at::empty_strided({H, batch}, {1, H}, f32);
+    return at::empty({H, batch}, f32);
+}
+
+// What both directions of the recurrence share.
+struct Sequences {
+    int code = 0, form = 0;
+    int64_t H = 0, T = 0, batch = 0;
+    const uint8_t *resets = nullptr;
+    bool take(const at::Tensor &x, PyObject *batch_, PyObject *resets_, PyObject *form_) {
+        if (!any_float_code(x, &code) || !PyLong_CheckExact(batch_) || !PyLong_CheckExact(form_)) return false;
+        batch = PyLong_AsLongLong(batch_);
+        form = int(PyLong_AsLong(form_));
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            return false;
+        }
+        if (batch < 1 || x.size(1) % batch != 0 || form < 0) return false;
+        H = x.size(0);
+        T = x.size(1) / batch;
+        if (resets_ == Py_None) return true;
+        const at::Tensor *r = tensor(resets_);
+        if (!r || (r->scalar_type() != at::kBool && r->scalar_type() != at::kByte) || r->dim() != 1 ||
+            r->size(0) != x.size(1) || !r->is_contiguous() || !here(*r))
+            return false;
+        resets = static_cast<const uint8_t *>(ptr(*r));
+        return true;
+    }
+};
+
+// A new state, or the one given.
+PyObject *state_or(PyObject *o, const at::Tensor &x, const Sequences &q, at::Tensor *out) {
+    return given_or(o, out,
+                    [&](PyObject *g) -> const at::Tensor * {
+                        darb_matrix m;
+                        const darb_matrix *p;
+                        return state(g, q.H, q.batch, &m, &p) && p ? tensor(g) : nullptr;
+                    },
+                    [&] { return state_like(x, q.H, q.batch); });
+}
+
+// (gate, x, batch, h0, resets, form, h, h_last, stream): (h, h_last)
+PyObject *gated_recurrence(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Sequences q;
+        void *s;
+        darb_matrix m0;
+        const darb_matrix *h0;
+        int64_t bytes;
+        if (n != 9) return none();
+        const at::Tensor *x = matrix(a[1]);
+        if (!x) return none();
+        const at::Tensor *gate = matrix_like(a[0], *x);
+        if (!gate || !q.take(*x, a[2], a[4], a[5]) || !state(a[3], q.H, q.batch, &m0, &h0) || !stream_of(a[8], &s) ||
+            darb_gated_recurrence_workspace(q.code, 0, q.H, q.T, q.batch, &bytes) != DARB_OK)
+            return none();
+        const Memory memory(a[8], s);
+        at::Tensor h, last, workspace;
+        Held held;
+        if (!(held.o[0] = given_or(a[6], &h, [&](PyObject *o) { return matrix_like(o, *x); },
+                                   [&] { return dense_like(*x); })) ||
+            !(held.o[1] = state_or(a[7], *x, q, &last)))
+            return none();
+        if (bytes) workspace = at::empty({bytes}, x->options().dtype(at::kByte));
+        memory.result(h);
+        memory.result(last);
+        const darb_matrix gm = as_matrix(*gate), xm = as_matrix(*x), hm = as_matrix(h), lm = as_matrix(last);
+        void *w = bytes ? ptr(workspace) : nullptr;
+        PyObject *res = held.tuple(2);
+        if (!res) return nullptr;
+        return finish(res, "darb_gated_recurrence", [&] {
+            return darb_gated_recurrence(q.code, q.form, q.H, q.T, q.batch, &gm, &xm, q.resets, h0, &hm, &lm, w, bytes,
+                                         s);
+        });
+    });
+}
+
+// (dh, gate, x, h, batch, h0, resets, dh_last, form, dgate, dx, dh0, stream): (dgate, dx, dh0)
+PyObject *gated_recurrence_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        Sequences q;
+        void *s;
+        darb_matrix m0, ml, xm;
+        const darb_matrix *h0, *dl;
+        int64_t bytes;
+        if (n != 13) return none();
+        const at::Tensor *gate = matrix(a[1]);
+        if (!gate) return none();
+        const at::Tensor *dh = matrix_like(a[0], *gate), *h = matrix_like(a[3], *gate);
+        const at::Tensor *x = a[2] == Py_None ? nullptr : matrix_like(a[2], *gate);
+        if (!dh || !h || (!x && a[2] != Py_None) || !q.take(*gate, a[4], a[6], a[8]) ||
+            (!x && q.form != DARB_RECURRENCE_LINEAR) || !state(a[5], q.H, q.batch, &m0, &h0) ||
+            !state(a[7], q.H, q.batch, &ml, &dl) || !stream_of(a[12], &s) ||
+            darb_gated_recurrence_workspace(q.code, 1, q.H, q.T, q.batch, &bytes) != DARB_OK)
+            return none();
+        const Memory memory(a[12], s);
+        at::Tensor dgate, dx, dh0, workspace;
+        Held held;
+        auto like = [&](PyObject *o) { return matrix_like(o, *gate); };
+        auto dense = [&] { return dense_like(*gate); };
+        if (!(held.o[0] = given_or(a[9], &dgate, like, dense)) || !(held.o[1] = given_or(a[10], &dx, like, dense)) ||
+            !(held.o[2] = state_or(a[11], *gate, q, &dh0)))
+            return none();
+        if (bytes) workspace = at::empty({bytes}, gate->options().dtype(at::kByte));
+        for (const at::Tensor &t : {dgate, dx, dh0}) memory.result(t);
+        const darb_matrix dm = as_matrix(*dh), gm = as_matrix(*gate), hm = as_matrix(*h), zm = as_matrix(dgate),
+                          dxm = as_matrix(dx), d0m = as_matrix(dh0);
+        if (x) xm = as_matrix(*x);
+        void *w = bytes ? ptr(workspace) : nullptr;
+        PyObject *res = held.tuple(3);
+        if (!res) return nullptr;
+        return finish(res, "darb_gated_recurrence_grad", [&] {
+            return darb_gated_recurrence_grad(q.code, q.form, q.H, q.T, q.batch, &dm, &gm, x ? &xm : nullptr, &hm,
+                                              q.resets, h0, dl, &zm, &dxm, &d0m, w, bytes, s);
+        });
+    });
+}
+
+// fp32 [n] on the current device; None is none.
+bool tokens(PyObject *o, int64_t n, const float **p) {
+    *p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *t = buffer(o, n, at::kFloat);
+    if (!t || t->dim() != 1 || t->size(0) != n || !here(*t)) return false;
+    *p = static_cast<const float *>(ptr(*t));
+    return true;
+}
+
+PyObject *tokens_or(PyObject *o, int64_t n, const at::TensorOptions &f32, at::Tensor *out) {
+    return given_or(o, out,
+                    [&](PyObject *g) -> const at::Tensor * {
+                        const float *p;
+                        return tokens(g, n, &p) && p ? tensor(g) : nullptr;
+                    },
+                    [&] { return at::empty({n}, f32); });
+}
+
+// (logprob, old, advantage, weight, low, high, ref, kl_coef, entropy, entropy_coef, grad_logprob,
+// grad_entropy, stream): (loss, kl, clipped, grad_logprob, grad_entropy)
+PyObject *policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        void *s;
+        const float *lp, *old, *adv, *w, *ref, *ent;
+        double k[4];
+        int64_t bytes;
+        if (n != 13) return none();
+        const at::Tensor *t = tensor(a[0]);
+        if (!t) return none();
+        const int64_t B = t->numel();
+        const int at_[4] = {4, 5, 7, 9};
+        for (int i = 0; i < 4; ++i) {
+            if (!PyFloat_CheckExact(a[at_[i]])) return none();
+            k[i] = PyFloat_AS_DOUBLE(a[at_[i]]);
+        }
+        if (!tokens(a[0], B, &lp) || !tokens(a[1], B, &old) || !tokens(a[2], B, &adv) || !old || !adv ||
+            !tokens(a[3], B, &w) || !tokens(a[6], B, &ref) || !tokens(a[8], B, &ent) || !stream_of(a[12], &s) ||
+            darb_policy_loss_workspace(B, &bytes) != DARB_OK)
+            return none();
+        const Memory memory(a[12], s);
+        const auto f32 = t->options();
+        at::Tensor stats = at::empty({3}, f32), grad, gent, workspace;
+        Held held;
+        if (!(held.o[0] = tokens_or(a[10], B, f32, &grad))) return none();
+        if (ent && !(held.o[1] = tokens_or(a[11], B, f32, &gent))) return none();
+        if (bytes) workspace = at::empty({bytes}, f32.dtype(at::kByte));
+        for (const at::Tensor &r : {stats, grad, gent}) memory.result(r);
+        float *sp = static_cast<float *>(ptr(stats)), *gp = static_cast<float *>(ptr(grad));
+        float *ep = ent ? static_cast<float *>(ptr(gent)) : nullptr;
+        void *ws = bytes ? ptr(workspace) : nullptr;
+        PyObject *res = PyTuple_New(5);
+        if (!res) return nullptr;
+        for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(res, i, THPVariable_Wrap(stats.select(0, i)));
+        for (int i = 0; i < 2; ++i) {
+            PyTuple_SET_ITEM(res, 3 + i, held.o[i] ? held.o[i] : (Py_INCREF(Py_None), Py_None));
+            held.o[i] = nullptr;
+        }
+        return finish(res, "darb_policy_loss", [&] {
+            return darb_policy_loss(B, lp, old, adv, w, ref, ent, k[0], k[1], k[2], k[3], sp, gp, ep, ws, bytes, s);
+        });
+    });
+}
+
+// (logprob, ref, batch, starts, beta, smoothing, weight, grad_logprob, stream): (loss, margin,
+// grad_logprob)
+PyObject *preference_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject * {
+        void *s;
+        const float *lp, *ref, *w;
+        if (n != 9) return none();
+        const at::Tensor *t = tensor(a[0]);
+        if (!t || !PyFloat_CheckExact(a[4]) || !PyFloat_CheckExact(a[5]) || (a[2] == Py_None) == (a[3] == Py_None))
+            return none();
+        const int64_t B = t->numel();
+        const int64_t *starts = nullptr;
+        int64_t sequences;
+        if (a[3] != Py_None) {
+            const at::Tensor *st = tensor(a[3]);
+            if (!st || st->scalar_type() != at::kLong || st->dim() != 1 || !st->is_contiguous() || !here(*st))
+                return none();
+            sequences = st->size(0) - 1;
+            starts = static_cast<const int64_t *>(ptr(*st));
+        } else {
+            if (!PyLong_CheckExact(a[2])) return none();
+            sequences = PyLong_AsLongLong(a[2]);
+            if (PyErr_Occurred()) {
+                PyErr_Clear();
+                return none();
+            }
+            if (sequences > 0 && B % sequences != 0) return none();
+        }
+        if (sequences < 2 || sequences % 2 != 0 || !tokens(a[0], B, &lp) || !tokens(a[1], B, &ref) ||
+            !tokens(a[6], sequences / 2, &w) || !stream_of(a[8], &s))
+            return none();
+        const int64_t P = sequences / 2;
+        const double beta = PyFloat_AS_DOUBLE(a[4]), smoothing = PyFloat_AS_DOUBLE(a[5]);
+        const Memory memory(a[8], s);
+        at::Tensor out = at::empty({1 + P}, t->options()), grad;
+        Held held;
+        if (!(held.o[2] = tokens_or(a[7], B, t->options(), &grad))) return none();
+        memory.result(out);
+        memory.result(grad);
+        held.o[0] = THPVariable_Wrap(out.select(0, 0));
+        held.o[1] = THPVariable_Wrap(out.narrow(0, 1, P));
+        float *op = static_cast<float *>(ptr(out)), *gp = static_cast<float *>(ptr(grad));
+        PyObject *res = held.tuple(3);
+        if (!res) return nullptr;
+        return finish(res, "darb_preference_loss", [&] {
+            return darb_preference_loss(P, B, lp, ref, starts, w, beta, smoothing, op, op + 1, gp, s);
+        });
+    });
+}
+
 // (handle, M, N, nnz, packed words): what the functions above take as the plan
 PyObject *plan_ref(PyObject *, PyObject *args) {
     unsigned long long h;
@@ -735,6 +983,8 @@ PyMethodDef methods[] = {
     DARB_FAST(token_logprobs), DARB_FAST(token_logprobs_grad),
     DARB_FAST(layer_norm), DARB_FAST(layer_norm_grad),
     DARB_FAST(adamw_step), DARB_FAST(adamw_moments),
+    DARB_FAST(gated_recurrence), DARB_FAST(gated_recurrence_grad),
+    DARB_FAST(policy_loss), DARB_FAST(preference_loss),
     {"plan_ref", plan_ref, METH_VARARGS, nullptr},
     {"current_stream", current_stream, METH_NOARGS, nullptr},
     {"set_check", set_check, METH_O, nullptr},

@@ -244,6 +244,73 @@ hipError_t launch_adamw(int bits, const AdamTensor *tensors, const AdamTile *til
 hipError_t launch_moments(int bits, const AdamTensor *tensors, const AdamTile *tiles,
                           int64_t ntiles, int first_tensor, int count, float *const *m,
                           float *const *v, hipStream_t s);
+// The gated linear recurrence: forward (gate, x, out = h, in = h0, last = h_last) or, with `back`,
+// its gradients (also h, dh, h0; out = dgate, out2 = dx, in = dh_last, last = dh0).  The operands
+// [H x T*batch] of `dtype` lie in one order (`rows` as above); states are fp32 [H x batch] with any
+// strides, and may be null.  workspace: recurrence_workspace_bytes, 256-byte aligned.
+struct RecurrenceMatrix {
+    void *p = nullptr;
+    int64_t feature = 0, batch = 0;     // strides; of an operand [H x T*batch] the columns'
+};
+struct RecurrenceCall {
+    int dtype, form;
+    bool back, rows;
+    int64_t H, T, batch;
+    RecurrenceMatrix gate, x, h, dh, out, out2, in, last, h0;
+    const uint8_t *resets;
+    void *workspace;
+};
+struct PolicyCall {
+    int64_t B;
+    const float *lp, *old, *advantage, *weight, *ref, *entropy;
+    float *grad, *grad_entropy, *stats;
+    double *partial;                    // the workspace
+    float even;                         // the weight where there are none
+    float low, high, kl_coef, entropy_coef;
+    double log_low, log_high;
+};
+int64_t policy_workspace_bytes(int64_t B);
+hipError_t launch_policy(PolicyCall c, hipStream_t s);
+struct PreferenceCall {
+    int64_t P, B, L;                    // pairs, tokens, a strided sequence's tokens
+    const float *lp, *ref, *weight;
+    const int64_t *starts;
+    float *loss, *margin, *grad;
+    float even, beta, smoothing;
+};
+hipError_t launch_preference(const PreferenceCall &c, hipStream_t s);
+// The orthogonalised update of up to kMuonTensors matrices at once: u (a gradient, or its momentum's
+// update) is divided by its norm, taken through `steps` steps and written out, or into a parameter.
+constexpr int kMuonTensors = 28;
+struct MuonTensor {
+    void *param;                        // written: p, or where the result goes
+    float *master;                      // fp32 copy of p, or null
+    const void *grad;
+    float *momentum;                    // null: u is the gradient
+    int64_t ld_in, ld_out;              // of grad and param, elements a row
+    int64_t base;                       // filled in: the tensor's part of the workspace
+    int32_t rows, cols;
+    int32_t dtype, gdtype;              // of param, of grad
+    float scale, keep;                  // p = p keep - scale O
+    int32_t m, n;                       // filled in: min and max of rows and cols, padded
+};
+struct MuonCall {
+    MuonTensor t[kMuonTensors];
+    int count;
+    bool update;                        // into parameters (else the result itself)
+    bool full;                          // as accurate as fp32
+    bool nesterov;
+    int steps;
+    float mu, one_mu;
+    double eps;
+    const float *grad_scale;
+    void *workspace;
+};
+// The bytes of `count` matrices' group; fills in what the launch needs.
+int64_t muon_group(MuonCall &c);
+hipError_t launch_muon(const MuonCall &c, hipStream_t s);
+int64_t recurrence_workspace_bytes(int dtype, bool back, bool rows, int64_t H, int64_t T, int64_t batch);
+hipError_t launch_recurrence(const RecurrenceCall &c, hipStream_t s);
 hipError_t launch_stream_read(const void *buf, int64_t bytes, float *sink, hipStream_t s);
 hipError_t launch_stream_read_shape(const void *buf, int64_t bytes, int threads, int vectors,
                                    float *sink, hipStream_t s);

@@ -1,4 +1,5 @@
-"""Evaluating and retraining a DARB layer: token log probabilities, layer norm, AdamW.
+"""Evaluating and retraining a DARB layer: token log probabilities and the losses over them, layer
+norm, a gated recurrence, AdamW and the orthogonalised update.
 
 Argument marshalling for the calls of include/darb.h.  Activations are [features, batch] in
 either memory order: contiguous along the batch, as the products' X and Y are, or along the
@@ -11,10 +12,12 @@ are the caller's to have ready for that stream, and to keep until it is done wit
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import NamedTuple, Optional
 
-from . import (BF16, F16, F32, _AdamTensor, _after_current, _as_stream, _check, _check_format,
-               _lib, _memory_of, _native, _ptr, _stream_ptr, _torch, _used_on)
+from . import (BF16, F16, F32, _AdamTensor, _Matrix, _MuonTensor, _after_current, _as_stream,
+               _check, _check_format, _lib, _memory_of, _native, _ptr, _stream_ptr, _torch,
+               _used_on)
 
 
 class TokenLogprobs(NamedTuple):
@@ -407,3 +410,396 @@ class AdamW:
                "darb_adamw_moments")
         _used_on(stream, *out[0], *out[1])
         return out
+
+
+# ---- gated recurrence ------------------------------------------------------------------
+
+FORMS = {"gate": 0, "linear": 1}
+
+
+def _as_matrix(t, name: str, like=None):
+    _require_cuda(t)
+    fs, bs = _matrix(t, name, like)
+    return _Matrix(t.data_ptr(), fs, bs)
+
+
+def _as_state(t, H: int, batch: int, name: str):
+    if t is None:
+        return None
+    torch = _torch()
+    _require_cuda(t)
+    if t.dtype != torch.float32 or tuple(t.shape) != (H, batch):
+        raise ValueError(f"{name} must be fp32 [{H}, {batch}], got {t.dtype} {tuple(t.shape)}")
+    return ctypes.byref(_Matrix(t.data_ptr(), *t.stride()))
+
+
+def _sequences(x, batch, form, resets):
+    """Checks what both directions share; returns (dtype code, form, H, T, batch, resets)."""
+    torch = _torch()
+    code = _float_code(x, "x")
+    if form not in FORMS:
+        raise ValueError(f"form must be one of {tuple(FORMS)}, got {form!r}")
+    batch = int(batch)
+    H, columns = x.shape
+    if batch < 1 or columns % batch:
+        raise ValueError(f"{columns} columns are not a multiple of the batch ({batch})")
+    if resets is None:
+        return code, FORMS[form], H, columns // batch, batch, None
+    _require_cuda(resets)
+    if resets.dim() != 1 or resets.shape[0] != columns:
+        raise ValueError(f"resets must be [{columns}], got {tuple(resets.shape)}")
+    _check_format(resets, columns, "resets", (torch.bool, torch.uint8))
+    return code, FORMS[form], H, columns // batch, batch, _ptr(resets)
+
+
+def _state_like(x, H: int, batch: int):
+    """A new fp32 state [H, batch] in x's memory order."""
+    torch = _torch()
+    if x.stride(0) == 1 and H > 1 and x.shape[1] > 1:
+        return torch.empty((batch, H), dtype=torch.float32, device=x.device).t()
+    return torch.empty((H, batch), dtype=torch.float32, device=x.device)
+
+
+def gated_recurrence(gate, x, batch: int = 1, h0=None, resets=None, form: str = "gate", h=None,
+                     h_last=None, workspace=None, stream=None):
+    """(h, h_last): h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(gate) (``form`` "gate"), or
+    h_t = gate_t h_{t-1} + x_t ("linear"), over the sequences of gate and x [H, T * batch] (fp32,
+    fp16 or bf16; column t * batch + n is step t of sequence n).
+
+    ``h0``, ``h_last``: fp32 [H, batch], the states before and after; they may be one tensor.
+    ``resets``: bool or uint8 [T * batch], where a new sequence starts.  ``h`` may be gate or x.
+    T = 1 is the step of a program that generates.  See darb_gated_recurrence."""
+    if workspace is None:
+        done = _native.gated_recurrence(gate, x, batch, h0, resets, FORMS.get(form, -1), h, h_last, stream)
+        if done is not None:
+            return done
+    _require_cuda(gate, x)
+    xm = _as_matrix(x, "x")
+    gm = _as_matrix(gate, "gate", x)
+    code, kind, H, T, batch, rp = _sequences(x, batch, form, resets)
+    with _memory_of(stream):
+        workspace = _workspace(_lib.darb_gated_recurrence_workspace, "darb_gated_recurrence_workspace",
+                               x.device, workspace, code, 0, H, T, batch)
+        if h is None:
+            h = _empty_like(x)
+        if h_last is None:
+            h_last = _state_like(x, H, batch)
+    hm = _as_matrix(h, "h", x)
+    _check(_lib.darb_gated_recurrence(
+        code, kind, H, T, batch, ctypes.byref(gm), ctypes.byref(xm), rp,
+        _as_state(h0, H, batch, "h0"), ctypes.byref(hm), _as_state(h_last, H, batch, "h_last"),
+        None if workspace is None else _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream_ptr(stream)), "darb_gated_recurrence")
+    _used_on(stream, h, h_last, workspace)
+    return h, h_last
+
+
+def gated_recurrence_grad(dh, gate, x, h, batch: int = 1, h0=None, resets=None, dh_last=None,
+                          form: str = "gate", dgate=None, dx=None, dh0=None, workspace=None,
+                          stream=None):
+    """(dgate, dx, dh0) of ``gated_recurrence`` from dh, by every state, and dh_last (fp32
+    [H, batch] or None), by the last one; ``h`` as it was returned.  ``x`` may be None in the linear
+    form.  ``dgate`` and ``dx`` may be dh, gate or x, not h; ``dh0`` (fp32 [H, batch]) may be
+    dh_last."""
+    if workspace is None:
+        done = _native.gated_recurrence_grad(dh, gate, x, h, batch, h0, resets, dh_last, FORMS.get(form, -1),
+                                             dgate, dx, dh0, stream)
+        if done is not None:
+            return done
+    _require_cuda(dh, gate, h)
+    gm = _as_matrix(gate, "gate")
+    dm, hm = _as_matrix(dh, "dh", gate), _as_matrix(h, "h", gate)
+    if x is None and form != "linear":
+        raise ValueError("x is needed in this form")
+    xm = None if x is None else ctypes.byref(_as_matrix(x, "x", gate))
+    code, kind, H, T, batch, rp = _sequences(gate, batch, form, resets)
+    with _memory_of(stream):
+        workspace = _workspace(_lib.darb_gated_recurrence_workspace, "darb_gated_recurrence_workspace",
+                               gate.device, workspace, code, 1, H, T, batch)
+        if dgate is None:
+            dgate = _empty_like(gate)
+        if dx is None:
+            dx = _empty_like(gate)
+        if dh0 is None:
+            dh0 = _state_like(gate, H, batch)
+    ggm, dxm = _as_matrix(dgate, "dgate", gate), _as_matrix(dx, "dx", gate)
+    _check(_lib.darb_gated_recurrence_grad(
+        code, kind, H, T, batch, ctypes.byref(dm), ctypes.byref(gm), xm, ctypes.byref(hm), rp,
+        _as_state(h0, H, batch, "h0"), _as_state(dh_last, H, batch, "dh_last"), ctypes.byref(ggm),
+        ctypes.byref(dxm), _as_state(dh0, H, batch, "dh0"),
+        None if workspace is None else _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream_ptr(stream)),
+        "darb_gated_recurrence_grad")
+    _used_on(stream, dgate, dx, dh0, workspace)
+    return dgate, dx, dh0
+
+
+# ---- losses over token log probabilities -----------------------------------------------
+
+class PolicyLoss(NamedTuple):
+    loss: object                        # fp32 [], as kl and clipped
+    kl: object
+    clipped: object
+    grad_logprob: object                # fp32 [B]
+    grad_entropy: Optional[object]      # fp32 [B]
+
+
+class PreferenceLoss(NamedTuple):
+    loss: object                        # fp32 []
+    margin: object                      # fp32 [P]
+    grad_logprob: object                # fp32 [B]
+
+
+def _tokens(t, n: int, name: str):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name} must be [{n}], got {tuple(t.shape)}")
+    return _vector(t, n, name)
+
+
+def policy_loss(logprob, old_logprob, advantage, weight=None, clip=0.2, ref_logprob=None,
+                kl_coef: float = 0.0, entropy=None, entropy_coef: float = 0.0, grad_logprob=None,
+                grad_entropy=None, workspace=None, stream=None) -> PolicyLoss:
+    """The clipped policy loss of tokens with log probabilities ``logprob`` (fp32 [B],
+    ``token_logprobs``'), sampled at ``old_logprob``, and its gradients, which
+    ``token_logprobs_grad`` takes: sum of weight * (-min(r A, clip(r) A) + kl_coef (e^q - 1 - q)
+    - entropy_coef entropy) with r = e^(logprob - old), q = ref_logprob - logprob.
+
+    ``weight``: fp32 [B], 0 for tokens that do not count (None: 1 / B each).  ``clip``: one bound, or
+    (below, above).  See darb_policy_loss."""
+    low, high = clip if hasattr(clip, "__len__") else (clip, clip)
+    low, high, kl_coef, entropy_coef = float(low), float(high), float(kl_coef), float(entropy_coef)
+    if workspace is None:
+        done = _native.policy_loss(logprob, old_logprob, advantage, weight, low, high, ref_logprob,
+                                   kl_coef, entropy, entropy_coef, grad_logprob, grad_entropy, stream)
+        if done is not None:
+            return PolicyLoss(*done)
+    torch = _torch()
+    _require_cuda(logprob)
+    B = logprob.numel()
+    lp = _tokens(logprob, B, "logprob")
+    old, adv = _tokens(old_logprob, B, "old_logprob"), _tokens(advantage, B, "advantage")
+    if old is None or adv is None:
+        raise ValueError("old_logprob and advantage are needed")
+    w, ref = _tokens(weight, B, "weight"), _tokens(ref_logprob, B, "ref_logprob")
+    ent = _tokens(entropy, B, "entropy")
+    kind = dict(dtype=torch.float32, device=logprob.device)
+    with _memory_of(stream):
+        workspace = _workspace(_lib.darb_policy_loss_workspace, "darb_policy_loss_workspace",
+                               logprob.device, workspace, B)
+        stats = torch.empty(3, **kind)
+        if grad_logprob is None:
+            grad_logprob = torch.empty(B, **kind)
+        if entropy is None:
+            grad_entropy = None
+        elif grad_entropy is None:
+            grad_entropy = torch.empty(B, **kind)
+    _check(_lib.darb_policy_loss(B, lp, old, adv, w, ref, ent, low, high, kl_coef, entropy_coef,
+                                 _ptr(stats), _tokens(grad_logprob, B, "grad_logprob"),
+                                 _tokens(grad_entropy, B, "grad_entropy"),
+                                 None if workspace is None else _ptr(workspace),
+                                 0 if workspace is None else workspace.numel(),
+                                 _stream_ptr(stream)), "darb_policy_loss")
+    _used_on(stream, stats, grad_logprob, grad_entropy, workspace)
+    return PolicyLoss(stats[0], stats[1], stats[2], grad_logprob, grad_entropy)
+
+
+def preference_loss(logprob, ref_logprob=None, batch: Optional[int] = None, starts=None,
+                    beta: float = 0.1, label_smoothing: float = 0.0, weight=None,
+                    grad_logprob=None, stream=None) -> PreferenceLoss:
+    """The preference loss of pairs of sequences over token log probabilities (fp32 [B],
+    ``token_logprobs``'), and its gradient, which ``token_logprobs_grad`` takes.  The first half of the
+    sequences are the preferred ones, the second half the others of the same pairs.  With a
+    sequence's s = sum(logprob - ref_logprob) and m = beta (s_preferred - s_other):
+    sum of weight * (-(1 - label_smoothing) log sigmoid(m) - label_smoothing log sigmoid(-m)).
+
+    Either ``batch``, the number of sequences, token t of sequence s being at t * batch + s; or
+    ``starts``, int64 [sequences + 1], for packed ones.  ``weight``: fp32 [pairs] (None: 1 / pairs
+    each).  See darb_preference_loss."""
+    beta, smoothing = float(beta), float(label_smoothing)
+    done = _native.preference_loss(logprob, ref_logprob, batch, starts, beta, smoothing, weight, grad_logprob, stream)
+    if done is not None:
+        return PreferenceLoss(*done)
+    torch = _torch()
+    _require_cuda(logprob)
+    B = logprob.numel()
+    lp, ref = _tokens(logprob, B, "logprob"), _tokens(ref_logprob, B, "ref_logprob")
+    if (batch is None) == (starts is None):
+        raise ValueError("pass batch or starts")
+    sp = None
+    if starts is not None:
+        if starts.dim() != 1:
+            raise ValueError("starts must be 1-D")
+        sequences = starts.shape[0] - 1
+        sp = _vector(starts, sequences + 1, "starts", torch.int64)
+    else:
+        sequences = int(batch)
+    if sequences < 2 or sequences % 2:
+        raise ValueError(f"the sequences must be pairs, got {sequences}")
+    P = sequences // 2
+    if starts is None and B % sequences:
+        raise ValueError(f"{B} tokens are not a multiple of the batch ({sequences})")
+    kind = dict(dtype=torch.float32, device=logprob.device)
+    with _memory_of(stream):
+        out = torch.empty(1 + P, **kind)
+        if grad_logprob is None:
+            grad_logprob = torch.empty(B, **kind)
+    _check(_lib.darb_preference_loss(P, B, lp, ref, sp, _tokens(weight, P, "weight"), beta, smoothing,
+                                     _ptr(out), ctypes.c_void_p(out.data_ptr() + 4),
+                                     _tokens(grad_logprob, B, "grad_logprob"), _stream_ptr(stream)),
+           "darb_preference_loss")
+    _used_on(stream, out, grad_logprob)
+    return PreferenceLoss(out[0], out[1:], grad_logprob)
+
+
+# ---- the orthogonalised update ---------------------------------------------------------
+
+def _unit_columns(t, name: str) -> int:
+    """The leading dimension of a non-empty matrix with unit column stride."""
+    if t.dim() != 2 or t.numel() == 0:
+        raise ValueError(f"{name} must be a matrix that is not empty, got {tuple(t.shape)}")
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ValueError(f"{name} must have unit column stride")
+    return t.stride(0) if rows > 1 else cols
+
+
+def _muon_workspace(table, count: int, device, workspace):
+    return _workspace(_lib.darb_muon_workspace, "darb_muon_workspace", device, workspace, table, count)
+
+
+def orthogonalize(G, steps: int = 5, eps: float = 1e-7, out=None, workspace=None, stream=None):
+    """G [m, n], or each matrix of G [k, m, n] (fp32, fp16 or bf16; one of the last two strides 1),
+    with its singular values taken towards 1: G / (|G| + eps) through ``steps`` steps of a quintic
+    (darb_orthogonalize).  ``out`` may be G."""
+    torch = _torch()
+    _require_cuda(G)
+    code = _float_code(G, "G")
+    if G.dim() not in (2, 3) or G.numel() == 0:
+        raise ValueError(f"G must be [m, n] or [k, m, n] and not empty, got {tuple(G.shape)}")
+    turned = G.stride(-1) != 1 and G.shape[-1] > 1      # its transpose has the transposed result
+    with _memory_of(stream):
+        if out is None:
+            out = torch.empty(G.mT.shape, dtype=G.dtype, device=G.device).mT if turned else \
+                torch.empty(G.shape, dtype=G.dtype, device=G.device)
+    _require_cuda(out)
+    if out.shape != G.shape or out.dtype != G.dtype:
+        raise ValueError(f"out must be {G.dtype} {tuple(G.shape)}")
+    a, b = (G.mT, out.mT) if turned else (G, out)
+    a, b = (a, b) if G.dim() == 3 else (a[None], b[None])
+    count, rows, cols = a.shape
+    lda, ldb = _unit_columns(a[0], "G"), _unit_columns(b[0], "out")
+    if count > 1 and b.stride(0) < (rows - 1) * ldb + cols:
+        raise ValueError("the matrices of out must not overlap")
+    table = (_MuonTensor * count)()
+    size = G.element_size()
+    for i in range(count):
+        table[i] = _MuonTensor(b.data_ptr() + i * b.stride(0) * size, None,
+                               a.data_ptr() + i * a.stride(0) * size, None, rows, cols, ldb, lda,
+                               1.0, 0.0, code, code)
+    with _memory_of(stream):
+        workspace = _muon_workspace(table, count, G.device, workspace)
+    _check(_lib.darb_orthogonalize(table, count, int(steps), float(eps), _ptr(workspace),
+                                   workspace.numel(), _stream_ptr(stream)), "darb_orthogonalize")
+    _used_on(stream, out, workspace)
+    return out
+
+
+class Muon:
+    """An optimizer of weight matrices whose update is the momentum's, orthogonalised
+    (darb_muon_step): m = momentum m + (1 - momentum) g, u = momentum m + (1 - momentum) g
+    (``nesterov``, else m), p = p (1 - lr decay) - lr scale orthogonalize(u).
+
+    ``params``: contiguous device matrices, fp32, fp16 or bf16; updated in place.  ``masters``: True
+    keeps fp32 copies of the 16-bit ones, which the step updates and rounds into the parameters;
+    or a list of fp32 tensors (or None) to use.  ``scale``: one number or one per matrix (None:
+    sqrt(max(1, rows / cols))); ``weight_decay`` as well.  ``state``: momenta to go on from, fp32
+    of the matrices' shapes (``momenta`` has them).
+
+    The tensors must not overlap.  The optimizer keeps references to them, and its workspace, of
+    some 16 bytes an element of the largest group of up to 28 matrices; a step reads the gradients
+    at their addresses of that call.  Steps on different streams share the workspace: the caller
+    orders them, replays of captured ones among them."""
+
+    def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay=0.0, steps: int = 5, eps: float = 1e-7, scale=None, masters=None,
+                 state=None, stream=None):
+        torch = _torch()
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("no parameters")
+        self.lr, self.momentum, self.nesterov = float(lr), float(momentum), bool(nesterov)
+        self.ns_steps, self.eps = int(steps), float(eps)
+        count, dev = len(self.params), self.params[0].device
+        for i, p in enumerate(self.params):
+            _require_cuda(p)
+            _float_code(p, f"parameter {i}")
+            if p.dim() != 2 or p.numel() == 0 or not p.is_contiguous():
+                raise ValueError(f"parameter {i} must be a contiguous matrix that is not empty")
+            if p.device != dev:
+                raise ValueError("the parameters must be on one device")
+
+        def each(given, what):
+            given = list(given) if hasattr(given, "__len__") else [given] * count
+            if len(given) != count:
+                raise ValueError(f"{what} must have one entry per tensor ({count})")
+            return given
+        scales = each(scale, "scale")
+        decays = each(weight_decay, "weight_decay")
+        if masters is True:
+            masters = [p.detach().float() if p.dtype != torch.float32 else None for p in self.params]
+        self.masters = each(None if masters is False else masters, "masters")
+        if state is None:
+            state = [torch.zeros(p.shape, dtype=torch.float32, device=dev) for p in self.params]
+        self.momenta = each(state, "state")
+        self._table = (_MuonTensor * count)()
+        for i, (p, t, m) in enumerate(zip(self.params, self.masters, self.momenta)):
+            rows, cols = p.shape
+            for name, s in (("master", t), ("state", m)):
+                if s is not None and tuple(s.shape) != (rows, cols):
+                    raise ValueError(f"{name} {i} must be [{rows}, {cols}]")
+            self._table[i] = _MuonTensor(
+                p.data_ptr(), None if t is None else _vector(t, p.numel(), f"master {i}").value, None,
+                _vector(m, p.numel(), f"state {i}").value, rows, cols, cols, cols,
+                math.sqrt(max(1.0, rows / cols)) if scales[i] is None else float(scales[i]),
+                float(decays[i]), _float_code(p, f"parameter {i}"), 0)
+        _after_current(stream)              # the masters and zeros above
+        self.workspace = _muon_workspace(self._table, count, dev, None)
+        self._streams = set()               # that _hold_on was told of
+        self._hold_on(stream)
+
+    def _hold_on(self, stream):
+        """The workspace, momenta, masters and parameters are in use on this stream (None: the
+        current one): dropping the optimizer does not hand them out before its work there is done."""
+        at = _native.current_stream() if stream is None else stream.cuda_stream
+        if at not in self._streams:
+            s = _torch().cuda.current_stream() if stream is None else _as_stream(stream)
+            for t in [self.workspace, *self.params, *self.masters, *self.momenta]:
+                if t is not None:
+                    t.record_stream(s)
+            self._streams.add(at)
+
+    def step(self, grads, lr: Optional[float] = None, grad_scale=None, stream=None):
+        """One step with the gradients (fp32, fp16 or bf16 matrices of the parameters' shapes with
+        unit column stride; None leaves a matrix and its momentum as they are).  ``grad_scale``: a
+        device fp32 tensor whose first element multiplies every gradient."""
+        count = len(self.params)
+        if len(grads) != count:
+            raise ValueError(f"one gradient per tensor ({count}), got {len(grads)}")
+        _require_cuda(self.params[0])
+        for i, (g, p, row) in enumerate(zip(grads, self.params, self._table)):
+            row.grad = None
+            if g is None:
+                continue
+            _require_cuda(g)
+            row.gdtype = _float_code(g, f"gradient {i}")
+            if g.shape != p.shape:
+                raise ValueError(f"gradient {i} must be {tuple(p.shape)}, got {tuple(g.shape)}")
+            row.ld_grad = _unit_columns(g, f"gradient {i}")
+            row.grad = g.data_ptr()
+        self._hold_on(stream)
+        _check(_lib.darb_muon_step(self._table, count, self.lr if lr is None else float(lr), self.momentum,
+                                   int(self.nesterov), self.ns_steps, self.eps,
+                                   _optional(grad_scale, 1, "grad_scale"), _ptr(self.workspace),
+                                   self.workspace.numel(), _stream_ptr(stream)), "darb_muon_step")
