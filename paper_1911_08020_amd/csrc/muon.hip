@@ -33,8 +33,8 @@ namespace {
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kScaleX = 0x1p15f, kScaleB = 0x1p14f;       // of X and A; of b A + c A A
-constexpr int kNormBlocks = 256;        // at most, a matrix
-constexpr int kNormTile = 8192;
+constexpr int kNormBlocks = 1024;       // at most, a matrix
+constexpr int kNormTile = 4096;
 constexpr int kNormThreads = 256;
 constexpr int kCutTile = 64;
 constexpr int kDepth = 32;              // columns of P and Q in LDS at a time
@@ -55,23 +55,56 @@ struct Places {
     __host__ __device__ int64_t all() const { return 8 * mn + 4 * mm; }
 };
 
-// The partial sums of every matrix lie before the matrices.
+// Matrices are cut into blocks of 16 rows by kDepth columns (1 KB), row of blocks by row of blocks: a
+// wave's load to LDS takes one block as it lies.  In a block, the 16-byte pieces of a row are moved
+// so that the rows that a read of LDS takes together use different banks.
+__device__ __forceinline__ int piece(int row, int k) { return k ^ ((row >> 1 & 3) ^ (row >> 3 & 1)); }
+__device__ __forceinline__ int64_t place_of(int row, int col, int cols) {
+    return (int64_t(row >> 4) * (cols / kDepth) + col / kDepth) * (16 * kDepth) + (row & 15) * kDepth +
+           piece(row & 15, col % kDepth / 8) * 8 + col % 8;
+}
+
+// The partial sums of every matrix' norm lie before the matrices.
 __host__ __device__ constexpr int64_t norms_bytes() { return int64_t(kMuonTensors) * kNormBlocks * 8; }
 
 __device__ __forceinline__ half_t *matrices(const MuonCall &c, const MuonTensor &t) {
     return reinterpret_cast<half_t *>(static_cast<char *>(c.workspace) + norms_bytes()) + t.base;
 }
-
 __device__ __forceinline__ float load_typed(int type, const void *p, int64_t at) {
     if (type == DARB_F32) return static_cast<const float *>(p)[at];
     if (type == DARB_F16) return float(static_cast<const half_t *>(p)[at]);
     return float(static_cast<const bf16_t *>(p)[at]);
 }
 
-__device__ __forceinline__ void store_typed(int type, void *p, int64_t at, float x) {
-    if (type == DARB_F32) static_cast<float *>(p)[at] = x;
-    else if (type == DARB_F16) static_cast<half_t *>(p)[at] = half_t(x);
-    else static_cast<bf16_t *>(p)[at] = bf16_t(x);
+// n (1 ... 4) elements from `at` on, and as much of 4 as there is.
+template <typename T> __device__ __forceinline__ void load4_as(const T *p, int n, float (&f)[4]) {
+    if (n == 4) {
+        const Loaded<T, 4> x = load_vec<T, 4>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = x[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = i < n ? float(p[i]) : 0.0f;
+    }
+}
+__device__ __forceinline__ void load4(int type, const void *p, int64_t at, int n, float (&f)[4]) {
+    if (type == DARB_F32) load4_as(static_cast<const float *>(p) + at, n, f);
+    else if (type == DARB_F16) load4_as(static_cast<const half_t *>(p) + at, n, f);
+    else load4_as(static_cast<const bf16_t *>(p) + at, n, f);
+}
+template <typename T> __device__ __forceinline__ void store4_as(T *p, int n, const float (&f)[4]) {
+    if (n == 4) {
+        store_vec<T, 4>(p, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) p[i] = T(f[i]);
+    }
+}
+__device__ __forceinline__ void store4(int type, void *p, int64_t at, int n, const float (&f)[4]) {
+    if (type == DARB_F32) store4_as(static_cast<float *>(p) + at, n, f);
+    else if (type == DARB_F16) store4_as(static_cast<half_t *>(p) + at, n, f);
+    else store4_as(static_cast<bf16_t *>(p) + at, n, f);
 }
 
 // ---- momentum and norm -----------------------------------------------------------------
@@ -88,17 +121,31 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(MuonCall c) {
     const int blocks = norm_blocks(t);
     if (int(blockIdx.x) >= blocks) return;
     const float gs = c.grad_scale ? *c.grad_scale : 1.0f;
-    const int64_t n = int64_t(t.rows) * t.cols;
+    const int64_t n = int64_t(t.rows) * t.cols, stride = int64_t(blocks) * kNormThreads * 4;
+    const bool dense = t.ld_in == t.cols;
     double sum = 0.0;
-    for (int64_t e = int64_t(blockIdx.x) * kNormThreads + threadIdx.x; e < n; e += int64_t(blocks) * kNormThreads) {
-        const int64_t at = t.ld_in == t.cols ? e : e / t.cols * t.ld_in + e % t.cols;
-        float u = load_typed(t.gdtype, t.grad, at) * gs;
-        if (t.momentum) {
-            const float m = c.mu * t.momentum[e] + c.one_mu * u;
-            t.momentum[e] = m;
-            u = c.nesterov ? c.mu * m + c.one_mu * u : m;
+#pragma unroll 2
+    for (int64_t e = (int64_t(blockIdx.x) * kNormThreads + threadIdx.x) * 4; e < n; e += stride) {
+        const int some = n - e < 4 ? int(n - e) : 4;
+        float u[4], m[4];
+        if (dense) {
+            load4(t.gdtype, t.grad, e, some, u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                u[i] = i < some ? load_typed(t.gdtype, t.grad, (e + i) / t.cols * t.ld_in + (e + i) % t.cols) : 0.0f;
         }
-        sum += double(u) * double(u);
+        if (t.momentum) load4(DARB_F32, t.momentum, e, some, m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u[i] *= gs;
+            if (t.momentum) {
+                m[i] = c.mu * m[i] + c.one_mu * u[i];
+                u[i] = c.nesterov ? c.mu * m[i] + c.one_mu * u[i] : m[i];
+            }
+            if (i < some) sum += double(u[i]) * double(u[i]);
+        }
+        if (t.momentum) store4(DARB_F32, t.momentum, e, some, m);
     }
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
@@ -136,7 +183,8 @@ __global__ __launch_bounds__(256) void cut_kernel(MuonCall c, int first_block) {
     const MuonTensor &t = c.t[which];
     const int tid = int(threadIdx.x), R = padded_rows(t), C = padded_cols(t);
     const int r0 = block / (C / kCutTile) * kCutTile, c0 = block % (C / kCutTile) * kCutTile;
-    double sum = tid < norm_blocks(t) ? static_cast<const double *>(c.workspace)[which * kNormBlocks + tid] : 0.0;
+    double sum = 0.0;
+    for (int i = tid; i < norm_blocks(t); i += 256) sum += static_cast<const double *>(c.workspace)[which * kNormBlocks + i];
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
     if (lane_id() == 0) room[wave_id()] = sum;
@@ -150,28 +198,50 @@ __global__ __launch_bounds__(256) void cut_kernel(MuonCall c, int first_block) {
     const bool turned = t.rows > t.cols;                    // X is u^T
     half_t *nh = base + (turned ? at.xt(0, 0) : at.x(0, 0)), *nl = base + (turned ? at.xt(0, 1) : at.x(0, 1));
     half_t *fh = base + (turned ? at.x(0, 0) : at.xt(0, 0)), *fl = base + (turned ? at.x(0, 1) : at.xt(0, 1));
-    const int col = tid % kCutTile;
-    for (int row = tid / kCutTile; row < kCutTile; row += 256 / kCutTile) {
-        const int r = r0 + row, q = c0 + col;
-        float x = 0.0f;
-        if (r < t.rows && q < t.cols) {
-            float u = load_typed(t.gdtype, t.grad, r * t.ld_in + q) * gs;
-            if (t.momentum) {
-                const float m = t.momentum[int64_t(r) * t.cols + q];
-                u = c.nesterov ? c.mu * m + c.one_mu * u : m;
-            }
-            x = float(double(u) * inverse);
+    const int col = tid % 16 * 4;
+    float u[kCutTile / 16][4], m[kCutTile / 16][4];
+#pragma unroll
+    for (int k = 0; k < kCutTile / 16; ++k) {
+        const int r = r0 + k * 16 + tid / 16, q = c0 + col, some = r < t.rows ? t.cols - q < 4 ? t.cols - q : 4 : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[k][i] = m[k][i] = 0.0f;
+        if (some > 0) {
+            load4(t.gdtype, t.grad, r * t.ld_in + q, some, u[k]);
+            if (t.momentum) load4(DARB_F32, t.momentum, int64_t(r) * t.cols + q, some, m[k]);
         }
-        tile[row][col] = x;
-        const Split s = split(x);
-        nh[int64_t(r) * C + q] = s.hi;
-        nl[int64_t(r) * C + q] = s.lo;
+    }
+#pragma unroll
+    for (int k = 0; k < kCutTile / 16; ++k) {
+        const int row = k * 16 + tid / 16;
+        Half4 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float x = u[k][i] * gs;
+            if (t.momentum) x = c.nesterov ? c.mu * m[k][i] + c.one_mu * x : m[k][i];
+            x = float(double(x) * inverse);
+            tile[row][col + i] = x;
+            const Split s = split(x);
+            hi[i] = s.hi;
+            lo[i] = s.lo;
+        }
+        const int64_t to = place_of(r0 + row, c0 + col, C);
+        *reinterpret_cast<Half4 *>(nh + to) = hi;
+        *reinterpret_cast<Half4 *>(nl + to) = lo;
     }
     __syncthreads();
-    for (int row = tid / kCutTile; row < kCutTile; row += 256 / kCutTile) {
-        const Split s = split(tile[col][row]);
-        fh[int64_t(c0 + row) * R + r0 + col] = s.hi;
-        fl[int64_t(c0 + row) * R + r0 + col] = s.lo;
+#pragma unroll
+    for (int k = 0; k < kCutTile / 16; ++k) {
+        const int row = k * 16 + tid / 16;
+        Half4 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const Split s = split(tile[col + i][row]);
+            hi[i] = s.hi;
+            lo[i] = s.lo;
+        }
+        const int64_t to = place_of(c0 + row, r0 + col, R);
+        *reinterpret_cast<Half4 *>(fh + to) = hi;
+        *reinterpret_cast<Half4 *>(fl + to) = lo;
     }
 }
 
@@ -185,12 +255,37 @@ __host__ __device__ __forceinline__ int tiles_of(const MuonTensor &t, int mode, 
     return mode == kGram || mode == kSquare ? q * (q + 1) / 2 : q * (t.n / tile);
 }
 
-// Place of a 16-byte piece in its row of kDepth halves: rows that a read takes together use
-// different banks.
-__device__ __forceinline__ int piece(int row, int k) { return k ^ ((row >> 1 & 3) ^ (row >> 3 & 1)); }
+// 16 bytes from each lane's address to LDS, lane after lane from `to` (the same in all lanes).
+// In assembly: behind the builtin the compiler lets every read of LDS wait for all such loads,
+// those of the other buffer among them (2.1 us a stage of 256 x 256 then).  It has no result in
+// registers; `arrived` waits for it.  (Nothing else of these kernels uses m0.)
+__device__ __forceinline__ void load_lds(const half_t *from, half_t *to) {
+    const uint32_t place = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) half_t *)to));
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off"
+                 :: "v"(from), "s"(__builtin_amdgcn_readfirstlane(int(place))) : "memory");
+}
 
-typedef __attribute__((address_space(1))) const void GlobalPtr;
-typedef __attribute__((address_space(3))) void LdsPtr;
+// The workgroup's loads to LDS are there, and its reads of LDS are done.
+__device__ __forceinline__ void arrived() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Lane q of four holds a column's rows 0 ... 3; afterwards row q's columns 0 ... 3.
+template <int CTRL> __device__ __forceinline__ uint32_t lane_xor(uint32_t x) { return dpp_all<CTRL>(x); }
+__device__ __forceinline__ void turn4(uint32_t (&v)[4]) {
+    const int lane = lane_id();
+    auto swap = [&](uint32_t &a, uint32_t &b, bool odd, auto other) {
+        const uint32_t got = other(odd ? a : b);
+        (odd ? a : b) = got;
+    };
+    const bool one = lane & 1, two = lane & 2;
+    auto x1 = [](uint32_t x) { return lane_xor<kDppXor1>(x); };
+    auto x2 = [](uint32_t x) { return lane_xor<kDppXor2>(x); };
+    swap(v[0], v[1], one, x1);
+    swap(v[2], v[3], one, x1);
+    swap(v[0], v[2], two, x2);
+    swap(v[1], v[3], two, x2);
+}
 
 template <int TILE, int WAVES, int PRODUCTS, int MODE>
 __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int step, int first_block, int blocks) {
@@ -198,6 +293,7 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
     constexpr int kWaveRows = 2, kWaveCols = WAVES / kWaveRows;
     constexpr int kRows = TILE / kWaveRows / 16, kCols = TILE / kWaveCols / 16;     // 16 x 16 tiles of a wave
     constexpr int kPanel = TILE * kDepth;                   // halves of a panel
+    constexpr bool kTriangle = MODE == kGram || MODE == kSquare;
     __shared__ __attribute__((aligned(16))) half_t lds[2][2 * kParts][kPanel];
 
     // neighbouring tiles on one XCD
@@ -211,39 +307,43 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
     const MuonTensor &t = c.t[which];
     half_t *base = matrices(c, t);
     const Places place(t);
-    const int m = t.m, n = t.n;
-    int ti, tj;
-    if (MODE == kGram || MODE == kSquare) {
-        ti = int((sqrtf(8.0f * float(id) + 1.0f) - 1.0f) * 0.5f);
-        while (ti * (ti + 1) / 2 > id) --ti;
-        while ((ti + 1) * (ti + 2) / 2 <= id) ++ti;
-        tj = id - ti * (ti + 1) / 2;
-    } else {
-        // four tiles of rows at a time
-        const int rows = m / TILE, cols = n / TILE, band = id / (4 * cols), first = band * 4;
-        const int height = rows - first < 4 ? rows - first : 4;
-        ti = first + (id - band * 4 * cols) % height;
-        tj = (id - band * 4 * cols) / height;
+    const int m = t.m, n = t.n, K = MODE == kGram ? n : m;
+    // four rows of tiles at a time, column by column, and what is on and below the diagonal last
+    int ti, tj, top = 0, height;
+    for (;; top += 4) {
+        height = m / TILE - top < 4 ? m / TILE - top : 4;
+        const int band = kTriangle ? height * top + height * (height + 1) / 2 : height * (n / TILE);
+        if (id < band) break;
+        id -= band;
     }
-    const int K = MODE == kGram ? n : m;
+    if (!kTriangle || id < height * top) {
+        ti = top + id % height;
+        tj = id / height;
+    } else {
+        id -= height * top;
+        ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : 3;
+        tj = top + id - ti * (ti + 1) / 2;
+        ti += top;
+    }
+    const int lane = lane_id(), w = wave_id();
+    const int wr = w / kWaveCols * (kRows * 16), wc = w % kWaveCols * (kCols * 16);
+    const int mine = (lane & 15) * kDepth + piece(lane & 15, lane >> 4) * 8;
+    auto part_of = [&](int buffer, int part, int at) {
+        return *reinterpret_cast<const Half8 *>(&lds[buffer][part][at * kDepth + mine]);
+    };
     const int64_t ph = MODE == kGram ? place.x(step, 0) : MODE == kSquare ? place.a(0) : place.b(0);
     const int64_t pl = MODE == kGram ? place.x(step, 1) : MODE == kSquare ? place.a(1) : place.b(1);
-    const int64_t qh = MODE == kGram ? ph : MODE == kSquare ? ph : place.xt(step, 0);
-    const int64_t ql = MODE == kGram ? pl : MODE == kSquare ? pl : place.xt(step, 1);
-    const int lane = lane_id(), w = wave_id();
-
-    // A wave's load takes 16 rows of a panel: lane l brings the piece that stands at l.
-    const int row = lane >> 2, k8 = piece(row, lane & 3) * 8;
-    const int64_t po = int64_t(ti) * TILE * K + int64_t(row) * K + k8, qo = int64_t(tj) * TILE * K + int64_t(row) * K + k8;
+    const int64_t qh = kTriangle ? ph : place.xt(step, 0);
+    const int64_t ql = kTriangle ? pl : place.xt(step, 1);
+    const int64_t po = int64_t(ti) * TILE * K + lane * 8, qo = int64_t(tj) * TILE * K + lane * 8;
     auto fetch = [&](int buffer, int k) {
 #pragma unroll
         for (int part = 0; part < 2 * kParts; ++part) {
-            const half_t *from = base + (part == 0 ? ph + po : part == 1 ? qh + qo : part == 2 ? pl + po : ql + qo) + k;
+            const half_t *from = base + (part == 0 ? ph + po : part == 1 ? qh + qo : part == 2 ? pl + po : ql + qo) + int64_t(k) * 16;
 #pragma unroll
             for (int q = 0; q < TILE / 16 / WAVES; ++q) {
                 const int rows = (q * WAVES + w) * 16;
-                __builtin_amdgcn_global_load_lds((GlobalPtr *)(from + int64_t(rows) * K),
-                                                 (LdsPtr *)&lds[buffer][part][rows * kDepth], 16, 0, 0);
+                load_lds(from + int64_t(rows) * K, &lds[buffer][part][rows * kDepth]);
             }
         }
     };
@@ -252,52 +352,92 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
     for (int i = 0; i < kRows; ++i)
 #pragma unroll
         for (int j = 0; j < kCols; ++j) acc[i][j] = Float4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int wr = w / kWaveCols * (kRows * 16), wc = w % kWaveCols * (kCols * 16);
-    const int mine = (lane & 15) * kDepth + piece(lane & 15, lane >> 4) * 8;
-    auto part_of = [&](int buffer, int part, int at) {
-        return *reinterpret_cast<const Half8 *>(&lds[buffer][part][at * kDepth + mine]);
-    };
-    fetch(0, 0);
-    int buffer = 0;
-    for (int k = 0; k < K; k += kDepth, buffer ^= 1) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();                                    // this buffer is there, the other one read
-        if (k + kDepth < K) fetch(buffer ^ 1, k + kDepth);
-        Half8 qh_[kCols], ql_[kParts == 2 ? kCols : 1];
+    int buffer = 0, k = 0;
+    Half8 qh_[kCols], ql_[kCols], hi, lo;
+    auto columns = [&](int buffer) {
 #pragma unroll
         for (int j = 0; j < kCols; ++j) {
             qh_[j] = part_of(buffer, 1, wc + j * 16);
             if (kParts == 2) ql_[j] = part_of(buffer, 3, wc + j * 16);
         }
+    };
+    auto rows = [&](int buffer, int i) {
+        hi = part_of(buffer, 0, wr + i * 16);
+        if (kParts == 2) lo = part_of(buffer, 2, wr + i * 16);
+    };
+    fetch(0, k);
+    arrived();
+    if (k + kDepth < K) fetch(1, k + kDepth);
+    columns(0);
+    rows(0, 0);
+    for (; k < K; k += kDepth, buffer ^= 1) {
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const Half8 hi = part_of(buffer, 0, wr + i * 16);
+            const Half8 h = hi, l = lo;
+            Half8 ch[kCols], cl[kCols];
 #pragma unroll
-            for (int j = 0; j < kCols; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, qh_[j], acc[i][j], 0, 0, 0);
+            for (int j = 0; j < kCols; ++j) ch[j] = qh_[j], cl[j] = ql_[j];
+            if (i + 1 < kRows) {
+                rows(buffer, i + 1);
+            } else if (k + kDepth < K) {
+                // The last rows of this stage are in registers: the next stage's first reads and
+                // the loads of the one after it run beside their products.
+                arrived();
+                if (k + 2 * kDepth < K) fetch(buffer, k + 2 * kDepth);
+                columns(buffer ^ 1);
+                rows(buffer ^ 1, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, ch[j], acc[i][j], 0, 0, 0);
             if (kParts == 2) {
-                const Half8 lo = part_of(buffer, 2, wr + i * 16);
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, ql_[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qh_[j], acc[i][j], 0, 0, 0);
-                }
+                for (int j = 0; j < kCols; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, cl[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < kCols; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(l, ch[j], acc[i][j], 0, 0, 0);
             }
         }
     }
-    // A lane holds rows 4 (l / 16) to + 3 of column l % 16 of each 16 x 16 tile.
+    // A lane holds rows 4 (l / 16) to + 3 of column l % 16 of each 16 x 16 tile, and after turn4
+    // columns 4 (l % 16 / 4) to + 3 of row 4 (l / 16) + l % 4.
     const int r0 = ti * TILE + wr + (lane >> 4) * 4, c0 = tj * TILE + wc + (lane & 15);
+    const int r1 = ti * TILE + wr + (lane >> 4) * 4 + (lane & 3), c1 = tj * TILE + wc + (lane & 12);
 #pragma unroll
     for (int i = 0; i < kRows; ++i)
 #pragma unroll
         for (int j = 0; j < kCols; ++j) {
-            const int r = r0 + i * 16, q = c0 + j * 16;
+            const int r = r0 + i * 16, q = c0 + j * 16, rt = r1 + i * 16, qt = c1 + j * 16;
             float v[4];
-            if (MODE == kGram || MODE == kSquare) {
-                // the value times its scale; of a symmetric matrix [q][r] stands for [r][q]
+            // [q][r ... r + 3] of X^T or a symmetric matrix
+            const int64_t to = place_of(q, r, m);
+            // both orders of a matrix, hi and lo
+            auto write = [&](half_t *th, half_t *tl, half_t *nh, half_t *nl, int ld, bool low) {
+                Half4 hi, lo;
+                uint32_t both[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const Split s = split(v[e]);
+                    hi[e] = s.hi;
+                    lo[e] = s.lo;
+                    both[e] = uint32_t(__builtin_bit_cast(uint16_t, s.hi)) |
+                              uint32_t(__builtin_bit_cast(uint16_t, s.lo)) << 16;
+                }
+                *reinterpret_cast<Half4 *>(th + to) = hi;
+                *reinterpret_cast<Half4 *>(tl + to) = lo;
+                if (!nh) return;
+                turn4(both);
+                const int64_t at2 = place_of(rt, qt, ld);
+                typedef uint32_t U2 __attribute__((ext_vector_type(2)));
+                *reinterpret_cast<U2 *>(nh + at2) = U2{(both[0] & 0xFFFF) | both[1] << 16, (both[2] & 0xFFFF) | both[3] << 16};
+                if (low)
+                    *reinterpret_cast<U2 *>(nl + at2) =
+                        U2{both[0] >> 16 | (both[1] & 0xFFFF0000), both[2] >> 16 | (both[3] & 0xFFFF0000)};
+            };
+            if (kTriangle) {
+                // the value times its scale
                 half_t *th = base + (MODE == kGram ? place.a(0) : place.b(0));
                 half_t *tl = base + (MODE == kGram ? place.a(1) : place.b(1));
-                const int64_t to = int64_t(q) * m + r;
                 if (MODE == kGram) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * (1.0f / kScaleX);
@@ -309,60 +449,46 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
                         v[e] = kB * (kScaleB / kScaleX) * (float(ah[e]) + float(al[e])) +
                                kC * (kScaleB / kScaleX / kScaleX) * acc[i][j][e];
                 }
-                Half4 hi, lo;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const Split s = split(v[e]);
-                    hi[e] = s.hi;
-                    lo[e] = s.lo;
-                }
-                *reinterpret_cast<Half4 *>(th + to) = hi;
-                *reinterpret_cast<Half4 *>(tl + to) = lo;
-                if (ti != tj) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        th[int64_t(r + e) * m + q] = hi[e];
-                        tl[int64_t(r + e) * m + q] = lo[e];
-                    }
-                }
+                write(th, tl, ti != tj ? th : nullptr, tl, m, true);
             } else {
-                const int64_t to = int64_t(q) * m + r;      // in X^T
                 const Half4 xh = *reinterpret_cast<const Half4 *>(base + place.xt(step, 0) + to);
                 const Half4 xl = *reinterpret_cast<const Half4 *>(base + place.xt(step, 1) + to);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)                 // times kScaleX
+                for (int e = 0; e < 4; ++e)             // times kScaleX
                     v[e] = kA * (float(xh[e]) + float(xl[e])) + acc[i][j][e] * (1.0f / kScaleB);
                 if (MODE == kApply) {
-                    half_t *xr = base + place.x(step + 1, 0), *xrl = base + place.x(step + 1, 1);
-                    Half4 hi, lo;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const Split s = split(v[e]);
-                        hi[e] = s.hi;
-                        lo[e] = s.lo;
-                        xr[int64_t(r + e) * n + q] = s.hi;
-                        if (kParts == 2) xrl[int64_t(r + e) * n + q] = s.lo;
-                    }
-                    *reinterpret_cast<Half4 *>(base + place.xt(step + 1, 0) + to) = hi;
-                    *reinterpret_cast<Half4 *>(base + place.xt(step + 1, 1) + to) = lo;
+                    write(base + place.xt(step + 1, 0), base + place.xt(step + 1, 1), base + place.x(step + 1, 0),
+                          base + place.x(step + 1, 1), n, kParts == 2);
                 } else {
                     const bool turned = t.rows > t.cols;
+                    if (!turned) {
+                        uint32_t u[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int pr = turned ? q : r + e, pc = turned ? r + e : q;
-                        if (pr >= t.rows || pc >= t.cols) continue;
+                        for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(v[e]);
+                        turn4(u);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(u[e]);
+                    }
+                    const int pr = turned ? q : rt, pc = turned ? r : qt;
+                    const int some = pr < t.rows ? t.cols - pc < 4 ? t.cols - pc : 4 : 0;
+                    if (some > 0) {
                         const int64_t p = pr * t.ld_out + pc;
-                        float o = v[e] * (1.0f / kScaleX);
-                        if (c.update) {
-                            o = (t.master ? t.master[p] : load_typed(t.dtype, t.param, p)) * t.keep - t.scale * o;
-                            if (t.master) t.master[p] = o;
+                        float o[4];
+                        if (c.update) load4(t.master ? int(DARB_F32) : t.dtype, t.master ? t.master : t.param, p, some, o);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            v[e] *= 1.0f / kScaleX;
+                            if (c.update) v[e] = o[e] * t.keep - t.scale * v[e];
                         }
-                        store_typed(t.dtype, t.param, p, o);
+                        if (c.update && t.master) store4(DARB_F32, t.master, p, some, v);
+                        store4(t.dtype, t.param, p, some, v);
                     }
                 }
             }
         }
 }
+
+constexpr int kSmall = 128, kLarge = 256;
 
 template <int TILE, int WAVES, int PRODUCTS, int MODE>
 hipError_t product(const MuonCall &c, int step, hipStream_t s) {
@@ -385,8 +511,6 @@ template <int TILE, int WAVES, int PRODUCTS> hipError_t steps(const MuonCall &c,
     }
     return hipSuccess;
 }
-
-constexpr int kSmall = 128, kLarge = 256;
 
 // Large tiles read least, and are taken where there are enough of them for the device.
 int tile_of(const MuonCall &c) {

@@ -132,7 +132,11 @@ def test_layouts(darb):
     g = torch.from_numpy(np.random.default_rng(5).normal(size=(3, 70, 130))).float().cuda()
     one = [darb.orthogonalize(x) for x in g]
     got = darb.orthogonalize(g)
-    assert got.shape == g.shape and all(torch.equal(a, b) for a, b in zip(got, one))
+    # a matrix among others is summed in other places: each is within the bound of the exact result
+    assert got.shape == g.shape
+    for x, a, b in zip(g, got, one):
+        off = np.linalg.norm(wide(a) - wide(b))
+        assert off <= 2 * (bound(wide(x), 5, 1e-7, True) + U * np.linalg.norm(wide(a)))
     turned = darb.orthogonalize(g.mT)
     assert turned.stride() == (70 * 130, 1, 130) and torch.equal(turned.mT, got)
     assert torch.equal(darb.orthogonalize(g[0].t().contiguous()), one[0].t())
@@ -247,10 +251,12 @@ def test_grad_scale_and_state(darb):
     a.step(grads, lr=0.05)
     c.step(grads, lr=0.05)
     assert all(torch.equal(x, y) for x, y in zip(a.params, c.params))
-    # one alone gives the same bits as among others
+    # one alone gives the same as among others, but for the places its sums are cut at: each is within
+    # the bound of the exact step, 0.1 of the result's and two roundings of values below 1.2
     d = darb.Muon([torch.ones(shapes[60], device="cuda")], lr=0.1)
     d.step([grads[60]])
-    assert torch.equal(d.params[0], b.params[60])
+    off = np.linalg.norm(wide(d.params[0]) - wide(b.params[60]))
+    assert off <= 2 * (0.1 * bound(wide(b.momenta[60]), 5, 1e-7, True) + 2 * 1.2 * U * math.sqrt(d.params[0].numel()))
     # strided gradients
     e = make()
     e.step([torch.cat([g, g], 1)[:, :g.shape[1]] for g in grads])
