@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libdarb.so")
 CALL_MODULE = os.path.join(HERE, "_darbcall.so")
 SOURCES = ["api.cpp", "encode.hip", "product.hip", "product_i8.hip", "lstm_seq.hip",
            "packed.hip", "prune.hip", "plan.hip", "misc.hip", "api_train.cpp", "logprobs.hip",
-           "layer_norm.hip", "adamw.hip", "spmm_grad.hip", "recurrence.hip", "losses.hip", "muon.hip"]
+           "layer_norm.hip", "adamw.hip", "spmm_grad.hip", "recurrence_f32.hip", "recurrence_f16.hip", "recurrence_bf16.hip", "losses.hip", "muon.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -22,9 +22,13 @@
 // be read in short pieces; such rows are staged whole through LDS.
 //
 // Memory-bound: forward 3 arrays, gradients 6 (5).
+#pragma once
+
 #include "darb_internal.h"
 #include "float_io.h"
 #include "wave.h"
+
+#include <type_traits>
 
 namespace darb {
 namespace {
@@ -64,7 +68,7 @@ struct Args {
     uint8_t *cuts;                      // [slabs][series]
 };
 
-template <int V> struct Map {
+template <int V, bool CUTS> struct Map {
     float a[V], b[V];
     uint32_t cut;                       // bit v: restarted
     __device__ __forceinline__ void none() {
@@ -76,72 +80,54 @@ template <int V> struct Map {
     __device__ __forceinline__ void after(const Map &m) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            b[v] = (cut >> v) & 1 ? b[v] : a[v] * m.b[v] + b[v];
+            b[v] = CUTS && (cut >> v) & 1 ? b[v] : a[v] * m.b[v] + b[v];
             a[v] *= m.a[v];
         }
-        cut |= m.cut;
+        if (CUTS) cut |= m.cut;
     }
     __device__ __forceinline__ float of(int v, float s) const {
-        return (cut >> v) & 1 ? b[v] : a[v] * s + b[v];
+        return CUTS && (cut >> v) & 1 ? b[v] : a[v] * s + b[v];
     }
 };
 
-template <int V> __device__ __forceinline__ Map<V> map_up(const Map<V> &m, int lanes) {
-    Map<V> r;
+template <int V, bool CUTS> __device__ __forceinline__ Map<V, CUTS> map_up(const Map<V, CUTS> &m, int lanes) {
+    Map<V, CUTS> r;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         r.a[v] = __shfl_up(m.a[v], lanes);
         r.b[v] = __shfl_up(m.b[v], lanes);
     }
-    r.cut = uint32_t(__shfl_up(int(m.cut), lanes));
+    r.cut = CUTS ? uint32_t(__shfl_up(int(m.cut), lanes)) : 0;
     return r;
 }
 
-// sigmoid(z) and 1 - sigmoid(z), each to a few units in its last place: the smaller of the two is
-// s = e^-|z| / (1 + e^-|z|), kept with the sign bit set where it is 1 - sigmoid(z); the other is
-// 1 - s.
-__device__ __forceinline__ float gate_share(float z) {
-    const float e = expf(-fabsf(z));
-    const float s = e * __builtin_amdgcn_rcpf(1.0f + e);
-    return z >= 0.0f ? -s : s;          // a NaN stays one
+// f = sigmoid(z) = 1 / (1 + e^-z) and u = 1 - f, each to a few units in its last place (e^-z is off
+// by |z| units where |z| is large, as is the smaller of the two): u is e^-z f where that is the
+// smaller one.
+__device__ __forceinline__ void gates(float z, float &f, float &u) {
+    const float e = __builtin_amdgcn_exp2f(z * -1.44269504f);
+    f = __builtin_amdgcn_rcpf(1.0f + e);
+    u = z < 0.0f ? 1.0f - f : e * f;
 }
-__device__ __forceinline__ float gate_f(float s) { return __float_as_int(s) < 0 ? 1.0f + s : s; }
-__device__ __forceinline__ float gate_u(float s) { return __float_as_int(s) < 0 ? -s : 1.0f - s; }
 
-// V elements, or the first n of them (a whole vector where ALL: the address of the others is
-// valid too).
 template <typename T, int V> struct Raw {
     typename VecOf<T, V>::Type v;
-    __device__ __forceinline__ void load(const T *p, int n, bool whole) {
-        if (whole) {
-            v = *reinterpret_cast<const typename VecOf<T, V>::Type *>(p);
-        } else if constexpr (V > 1) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = i < n ? p[i] : T(0);
-        }
-    }
+    __device__ __forceinline__ void load(const T *p) { v = *reinterpret_cast<const typename VecOf<T, V>::Type *>(p); }
     __device__ __forceinline__ float operator[](int i) const {
         if constexpr (V == 1) return float(v);
         else return float(v[i]);
     }
 };
 
-template <typename T, int V> __device__ __forceinline__ void store_n(T *p, int n, const float (&f)[V]) {
-    if (n == V) {
-        store_vec<T, V>(p, f);
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < n) p[v] = T(f[v]);
-    }
-}
-
 // LDS place of element i: rows of 32 are moved on by one word, so that chunks that start on
 // multiples of 8 spread over the banks.
 __device__ __forceinline__ int staged_at(int i) { return i + (i >> 5); }
 
-template <typename T, int V, int C, bool GATE, bool BACK, bool STAGED>
-__global__ __launch_bounds__(kThreads) void recurrence_kernel(Args k) {
+enum { kDirect, kStaged, kAlong };      // see the top of the file
+
+template <typename T, int V, int C, bool GATE, bool BACK, bool RESETS, int LAYOUT>
+__global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
+    constexpr bool STAGED = LAYOUT == kStaged, ALONG = LAYOUT == kAlong;
     constexpr int kArrays = BACK ? (GATE ? 4 : 3) : 2;      // staged: z, x; z, dh, h, x
     constexpr int kRoom = STAGED ? kThreads * C + kThreads * C / 32 : 1;
     __shared__ T staged[STAGED ? kArrays : 1][kRoom];
@@ -151,26 +137,19 @@ __global__ __launch_bounds__(kThreads) void recurrence_kernel(Args k) {
     const int lanes = k.lanes, chunks = kThreads / lanes;
     const int tid = int(threadIdx.x), g = tid & (lanes - 1), c = tid / lanes;
     const int lane = tid & (kWave - 1), w = wave_id();
-    const int64_t per = (k.W + V - 1) / V;                  // groups of an o
-    const int64_t blocks = STAGED ? k.O : (k.groups + lanes - 1) / lanes;
+    const int64_t per = k.W / V;                            // groups of an o
+    const int64_t blocks = STAGED || ALONG ? k.O : (k.groups + lanes - 1) / lanes;
     const int64_t number = k.first_block + blockIdx.x;
     const int slab = int(number / blocks);
     const int64_t block = number - slab * blocks;
-    const int64_t group = STAGED ? 0 : block * lanes + g;
-    const int64_t o = STAGED ? block : group / per;
-    const int64_t i = STAGED ? g : (group - o * per) * V;
-    // the series of this thread: none, some or all of V
-    const int64_t left = STAGED ? k.W - g : group < k.groups ? k.W - i : 0;
-    const int n = left <= 0 ? 0 : left < V ? int(left) : V;
-
-    // A thread without series reads those of the first group, whole, and writes nothing; where a
-    // wave has a group that is not whole, all its loads go element by element.
-    const bool whole = k.W >= V && __ballot(n != V && n != 0) == 0;
-    const int64_t lo = n ? o : 0, li = n ? i : 0;
-    const T *z = static_cast<const T *>(k.z.p) + lo * k.z.so + li;
-    const T *x = static_cast<const T *>(k.x.p) + lo * k.x.so + li;
-    const T *h = BACK ? static_cast<const T *>(k.h.p) + lo * k.h.so + li : nullptr;
-    const T *dh = BACK ? static_cast<const T *>(k.dh.p) + lo * k.dh.so + li : nullptr;
+    // threads behind the last group read with it, and write nothing
+    const int64_t group = STAGED || ALONG ? 0 : block * lanes + g < k.groups ? block * lanes + g : k.groups - 1;
+    const int64_t o = STAGED || ALONG ? block : group / per;
+    const int64_t i = STAGED || ALONG ? g : (group - o * per) * V;
+    const bool mine = STAGED || ALONG ? g < k.W : block * lanes + g < k.groups;
+    const int n = mine ? V : 0;                             // the thread's series
+    // the thread's series at step 0
+    auto series_of = [&](const Operand &q) { return static_cast<const T *>(q.p) + o * q.so + i; };
     const bool first_launch = k.maps && !k.out.p;           // only the slabs' maps
     const int64_t t0 = slab * k.slab_steps;
     const int64_t steps = k.T - t0 < k.slab_steps ? k.T - t0 : k.slab_steps;
@@ -180,30 +159,40 @@ __global__ __launch_bounds__(kThreads) void recurrence_kernel(Args k) {
     float state[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
-        state[v] = v < n && k.in.p ? k.in.p[o * k.in.so + (i + v) * k.in.si] : 0.0f;
+        state[v] = mine && k.in.p ? k.in.p[o * k.in.so + (i + v) * k.in.si] : 0.0f;
     if (first_launch && c == 0 && slab == (BACK ? k.slabs - 1 : 0)) {
         // the second launch may write h_last where h0 is
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < n) k.enters[at + v] = state[v];
+            if (mine) k.enters[at + v] = state[v];
     }
     if (k.maps && !first_launch) {
         const int before = BACK ? k.slabs - 1 - slab : slab;
 #pragma unroll 4
         for (int q = 0; q < before; ++q) {
-            const int64_t from = int64_t(BACK ? k.slabs - 1 - q : q) * series + (n ? at : 0);
+            const int64_t from = int64_t(BACK ? k.slabs - 1 - q : q) * series + at;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int64_t e = from + (v < n ? v : 0);
+                const int64_t e = from + v;
                 const float a = k.maps[e], b = k.maps[e + k.slabs * series];
-                state[v] = k.cuts[e] ? b : a * state[v] + b;
+                state[v] = RESETS && k.cuts[e] ? b : a * state[v] + b;
             }
         }
     }
-    Map<V> all;                                             // first launch: the slab's map
+    Map<V, RESETS> all;                                             // first launch: the slab's map
     all.none();
 
     const int64_t tile = int64_t(chunks) * C;
+    // kDirect: where the chunk's first step is (in the direction of the scan), and how far a step takes
+    const int64_t begin = BACK ? t0 + steps - 1 - c * C : t0 + c * C, way = BACK ? -1 : 1;
+    struct Cursor {
+        const T *p;
+        int64_t st;
+    };
+    auto cursor = [&](const Operand &q) { return Cursor{series_of(q) + begin * q.st, q.st * way}; };
+    Cursor zc = cursor(k.z), xc = cursor(k.x), hc = cursor(k.h), gc = cursor(k.dh);
+    auto writer = [&](const Result &q) { return cursor({q.p, q.so, q.st}); };
+    Cursor oc = writer(k.out), oc2 = writer(k.out2);
     int turn = 0;
     for (int64_t done = 0; done < steps; done += tile, turn ^= 1) {
         // Scan position p = done + c * C + j is step t0 + p, or counted from the slab's end.
@@ -215,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void recurrence_kernel(Args k) {
             return BACK ? tsteps - 1 - p : p;
         };
         const int live = n > 0 ? tsteps - p0 : 0;           // steps j < live are the thread's
-        float f[C][V], b[C][V];                             // f (its share, for both uses) and b
+        float f[C][V], b[C][V], u[BACK && GATE ? C : 1][V]; // f, what a step adds or dh, 1 - f
         Raw<T, V> y[BACK ? C : 1], xs[BACK && GATE ? C : 1];
         float y0[BACK ? V : 1];                             // the state before the first step
         uint64_t cuts = 0;
@@ -229,103 +218,159 @@ __global__ __launch_bounds__(kThreads) void recurrence_kernel(Args k) {
             auto row = [&](const Operand &q) { return static_cast<const T *>(q.p) + o * q.so + ta * k.W; };
             const T *zr = row(k.z), *xr = row(k.x), *hr = row(k.h), *gr = row(k.dh);
             const bool start = BACK && ta == 0;             // h at -1 is h0
-            for (int e = tid; e < count; e += kThreads) {
-                const int s = staged_at(e);
-                staged[0][s] = zr[e];
-                if constexpr (!BACK) {
-                    staged[1][s] = xr[e];
-                } else {
-                    staged[1][s] = gr[e];
-                    if (!first_launch) {
-                        staged[2][s] = start && e < k.W ? T(0) : hr[e - k.W];
-                        if constexpr (GATE) staged[kArrays - 1][s] = xr[e];
+            auto bring = [&](T *to, const T *from) {
+                for (int e = tid * 4; e < count; e += kThreads * 4) {
+                    if (e + 4 <= count) {
+                        Raw<T, 4> v;
+                        v.load(from + e);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) to[staged_at(e + q)] = v.v[q];
+                    } else {
+                        for (int q = e; q < count; ++q) to[staged_at(q)] = from[q];
                     }
+                }
+            };
+            bring(staged[0], zr);
+            bring(staged[1], BACK ? gr : xr);
+            if constexpr (BACK) {
+                if (!first_launch) {
+                    if (start) {
+                        for (int e = tid; e < count; e += kThreads) staged[2][staged_at(e)] = e < k.W ? T(0) : hr[e - k.W];
+                    } else {
+                        bring(staged[2], hr - k.W);
+                    }
+                    if constexpr (GATE) bring(staged[kArrays - 1], xr);
                 }
             }
             __syncthreads();
         }
         Raw<T, V> rz[C], rb[C];
+        if constexpr (ALONG) {
+            // the chunk's steps lie side by side: ascending, or backwards from `low` up
+            const int64_t low = ta + (BACK ? tsteps - p0 - C : p0);
+            auto bring = [&](Raw<T, V> (&to)[C], const T *from, int64_t at) {
+                if (live >= C && at >= 0) {
+                    const Loaded<T, C> v = load_vec<T, C>(from + at);
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            const int tj = step(j);
-            const int64_t t = ta + tj;
-            if constexpr (STAGED) {
-                if constexpr (V == 1) {
-                    const int s = staged_at(n ? int(tj * k.W) + g : 0);
-                    rz[j].v = staged[0][s];
-                    rb[j].v = staged[1][s];
-                    if constexpr (BACK) {
-                        if (!first_launch) {
-                            y[j].v = staged[2][s];
-                            if constexpr (GATE) xs[j].v = staged[kArrays - 1][s];
-                        }
+                    for (int j = 0; j < C; ++j) to[j].v = v.raw[BACK ? C - 1 - j : j];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < C; ++j) {
+                        const int64_t t = at - low + ta + step(j);
+                        to[j].v = j < live && t >= 0 ? from[t] : T(0);
                     }
                 }
-            } else {
-                rz[j].load(z + t * k.z.st, n, whole);
-                if constexpr (!BACK) {
-                    rb[j].load(x + t * k.x.st, n, whole);
-                } else {
-                    rb[j].load(dh + t * k.dh.st, n, whole);
+            };
+            bring(rz, series_of(k.z), low);
+            bring(rb, series_of(BACK ? k.dh : k.x), low);
+            if constexpr (BACK) {
+                if (!first_launch) {
+                    bring(y, series_of(k.h), low - 1);
+                    if constexpr (GATE) bring(xs, series_of(k.x), low);
+                }
+            }
+        } else if constexpr (STAGED) {
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                const int s = staged_at(mine ? step(j) * int(k.W) + g : 0);
+                rz[j].v = staged[0][s];
+                rb[j].v = staged[1][s];
+                if constexpr (BACK) {
                     if (!first_launch) {
-                        y[j].load(h + (t > 0 ? t - 1 : 0) * k.h.st, n, whole);
-                        if constexpr (GATE) xs[j].load(x + t * k.x.st, n, whole);
+                        y[j].v = staged[2][s];
+                        if constexpr (GATE) xs[j].v = staged[kArrays - 1][s];
                     }
                 }
             }
+        } else {
+            // all loads before the first use; steps that are not there read the tile's last one
+            auto bring = [&](auto whole) {
+#pragma unroll
+                for (int j = 0; j < C; ++j) {
+                    const int64_t d = whole ? j : p0 + j < tsteps ? j : tsteps - 1 - p0;
+                    rz[j].load(zc.p + d * zc.st);
+                    if constexpr (!BACK) {
+                        rb[j].load(xc.p + d * xc.st);
+                    } else {
+                        rb[j].load(gc.p + d * gc.st);
+                        if (!first_launch) {
+                            // the state before; step 0's is not in h
+                            y[j].load(hc.p + (whole || ta + step(j) > 0 ? d + 1 : d) * hc.st);
+                            if constexpr (GATE) xs[j].load(xc.p + d * xc.st);
+                        }
+                    }
+                }
+            };
+            if (tsteps == tile && (!BACK || ta > 0)) bring(std::true_type{});
+            else bring(std::false_type{});
         }
         if (BACK && !first_launch && k.h0.p && ta == 0) {
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                if (v < n) y0[v] = k.h0.p[o * k.h0.so + (i + v) * k.h0.si];
+                if (mine) y0[v] = k.h0.p[o * k.h0.so + (i + v) * k.h0.si];
         }
         if (k.resets) {
 #pragma unroll
             for (int j = 0; j < C; ++j) {
-                const uint8_t *r = k.resets + (ta + step(j)) * k.rt + lo * k.ro;
+                const uint8_t *r = k.resets + (ta + step(j)) * k.rt + o * k.ro;
+                if (k.ri == 0) {                            // one sequence: all its features
+                    if (r[0]) cuts |= uint64_t((1u << V) - 1) << (j * V);
+                } else {
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (j < live && v < n && r[(li + v) * k.ri]) cuts |= uint64_t(1) << (j * V + v);
+                    for (int v = 0; v < V; ++v)
+                        if (r[i + v]) cuts |= uint64_t(1) << (j * V + v);
+                }
             }
         }
-        // the chunk's map
-        Map<V> m;
-        m.none();
+        if (RESETS && live < C) cuts &= live > 0 ? (uint64_t(1) << (live * V)) - 1 : 0;   // the steps that are there
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            const uint32_t cut = uint32_t(cuts >> (j * V)) & ((1u << V) - 1);
+        for (int j = 0; j < C; ++j)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 f[j][v] = rz[j][v];
                 b[j][v] = rb[j][v];
                 if constexpr (GATE) {
-                    f[j][v] = gate_share(f[j][v]);
-                    if constexpr (!BACK) {
-                        b[j][v] *= gate_u(f[j][v]);
-                        f[j][v] = gate_f(f[j][v]);
-                    }
-                }
-                const float fv = BACK && GATE ? gate_f(f[j][v]) : f[j][v];
-                // backwards b holds dh, and the map is f (dh + s)
-                const float in = BACK ? fv * b[j][v] : b[j][v];
-                const bool reset = (cut >> v) & 1;
-                if (j < live) {
-                    m.b[v] = reset ? (BACK ? 0.0f : in) : fv * m.b[v] + in;
-                    m.a[v] *= fv;
+                    float share;
+                    gates(f[j][v], f[j][v], share);
+                    if constexpr (BACK) u[j][v] = share;
+                    else b[j][v] *= share;
                 }
             }
-            m.cut |= cut;
+        if (tsteps < tile) {                                // steps that are not there change nothing
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+                if (j >= live) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) f[j][v] = 1.0f, b[j][v] = 0.0f;
+                }
+        }
+        // the chunk's map; backwards b holds dh, and a step is f (dh + s)
+        Map<V, RESETS> m;
+        m.none();
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const uint32_t cut = RESETS ? uint32_t(cuts >> (j * V)) & ((1u << V) - 1) : 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float in = BACK ? f[j][v] * b[j][v] : b[j][v];
+                const bool reset = RESETS && (cut >> v) & 1;
+                m.b[v] = reset ? (BACK ? 0.0f : in) : f[j][v] * m.b[v] + in;
+                m.a[v] *= f[j][v];
+            }
+            if (RESETS) m.cut |= cut;
         }
         // joined over the wave's chunks, then over the waves
         float enter[V];
         if (chunks == 1) {
 #pragma unroll
             for (int v = 0; v < V; ++v) enter[v] = state[v], state[v] = m.of(v, state[v]);
-            m.after(all);
-            all = m;
+            if (first_launch) {
+                m.after(all);
+                all = m;
+            }
         } else {
             for (int d = lanes; d < kWave; d <<= 1) {
-                const Map<V> up = map_up(m, d);
+                const Map<V, RESETS> up = map_up(m, d);
                 if (lane >= d) m.after(up);
             }
             // a wave holds `lanes` groups, or 64 of them
@@ -335,37 +380,44 @@ __global__ __launch_bounds__(kThreads) void recurrence_kernel(Args k) {
                     total[turn][w][0][v][lane] = m.a[v];
                     total[turn][w][1][v][lane] = m.b[v];
                 }
-                total_cut[turn][w][lane] = m.cut;
+                if (RESETS) total_cut[turn][w][lane] = m.cut;
             }
-            Map<V> before;
+            Map<V, RESETS> before;
             before.none();
             if (lanes < kWave) {
-                const Map<V> up = map_up(m, lanes);
+                const Map<V, RESETS> up = map_up(m, lanes);
                 if (lane >= lanes) before = up;
             }
             __syncthreads();
             const int apart = lanes <= kWave ? 1 : lanes / kWave, mine = lanes < kWave ? kWave - lanes + g : lane;
             const int from = lanes <= kWave ? 0 : w & (apart - 1);
             for (int q = from; q < kWaves; q += apart) {
-                Map<V> t;
+                Map<V, RESETS> t;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     t.a[v] = total[turn][q][0][v][mine];
                     t.b[v] = total[turn][q][1][v][mine];
                 }
-                t.cut = total_cut[turn][q][mine];
+                t.cut = RESETS ? total_cut[turn][q][mine] : 0;
                 if (q == w) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) enter[v] = before.of(v, state[v]);
                 }
 #pragma unroll
                 for (int v = 0; v < V; ++v) state[v] = t.of(v, state[v]);
-                t.after(all);
-                all = t;
+                if (first_launch) {
+                    t.after(all);
+                    all = t;
+                }
             }
         }
         if (first_launch) {
-            if constexpr (STAGED) __syncthreads();                    // the tile is read
+            if constexpr (STAGED) __syncthreads();          // the tile is read
+            if constexpr (LAYOUT == kDirect) {
+                zc.p += tile * zc.st;
+                xc.p += tile * xc.st;
+                gc.p += tile * gc.st;
+            }
             continue;
         }
         // the steps again, from the state that enters the chunk
@@ -374,38 +426,66 @@ __global__ __launch_bounds__(kThreads) void recurrence_kernel(Args k) {
             if (j < live) {
                 const int tj = step(j);
                 const int64_t t = ta + tj;
-                const uint32_t cut = uint32_t(cuts >> (j * V)) & ((1u << V) - 1);
+                const uint32_t cut = RESETS ? uint32_t(cuts >> (j * V)) & ((1u << V) - 1) : 0;
                 float r[V], r2[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const bool reset = (cut >> v) & 1;
+                    const bool reset = RESETS && (cut >> v) & 1;
                     if constexpr (!BACK) {
                         enter[v] = reset ? b[j][v] : f[j][v] * enter[v] + b[j][v];
                         r[v] = enter[v];
                     } else {
                         const float gr = b[j][v] + enter[v];
                         const float past = reset ? 0.0f : t > 0 ? y[j][v] : y0[v];
-                        const float fv = GATE ? gate_f(f[j][v]) : f[j][v];
                         if constexpr (GATE) {
-                            const float u = gate_u(f[j][v]);
-                            r[v] = (past - xs[j][v]) * gr * (fv * u);
-                            r2[v] = u * gr;
+                            r[v] = (past - xs[j][v]) * gr * (f[j][v] * u[j][v]);
+                            r2[v] = u[j][v] * gr;
                         } else {
                             r[v] = past * gr;
                             r2[v] = gr;
                         }
-                        enter[v] = reset ? 0.0f : fv * gr;
+                        enter[v] = reset ? 0.0f : f[j][v] * gr;
                     }
                 }
                 if constexpr (STAGED) {
                     const int s = staged_at(int(tj * k.W) + g);
                     staged[0][s] = T(r[0]);
                     if constexpr (BACK) staged[1][s] = T(r2[0]);
+                } else if constexpr (ALONG) {
+                    f[j][0] = r[0];
+                    if constexpr (BACK) b[j][0] = r2[0];
                 } else {
-                    store_n<T, V>(static_cast<T *>(k.out.p) + o * k.out.so + i + t * k.out.st, n, r);
-                    if constexpr (BACK)
-                        store_n<T, V>(static_cast<T *>(k.out2.p) + o * k.out2.so + i + t * k.out2.st, n, r2);
+                    store_vec<T, V>(const_cast<T *>(oc.p + j * oc.st), r);
+                    if constexpr (BACK) store_vec<T, V>(const_cast<T *>(oc2.p + j * oc2.st), r2);
                 }
+            }
+        }
+        if constexpr (ALONG) {
+            const int64_t low = ta + (BACK ? tsteps - p0 - C : p0);
+            auto put = [&](void *p, int64_t so, float (&from)[C][V]) {
+                T *to = static_cast<T *>(p) + o * so;
+                if (live >= C) {
+                    float v[C];
+#pragma unroll
+                    for (int j = 0; j < C; ++j) v[BACK ? C - 1 - j : j] = from[j][0];
+                    store_vec<T, C>(to + low, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < C; ++j)
+                        if (j < live) to[ta + step(j)] = T(from[j][0]);
+                }
+            };
+            put(k.out.p, k.out.so, f);
+            if constexpr (BACK) put(k.out2.p, k.out2.so, b);
+        }
+        if constexpr (LAYOUT == kDirect) {
+            zc.p += tile * zc.st;
+            xc.p += tile * xc.st;
+            oc.p += tile * oc.st;
+            if constexpr (BACK) {
+                hc.p += tile * hc.st;
+                gc.p += tile * gc.st;
+                oc2.p += tile * oc2.st;
             }
         }
         if constexpr (STAGED) {
@@ -425,46 +505,49 @@ __global__ __launch_bounds__(kThreads) void recurrence_kernel(Args k) {
         const int64_t to = int64_t(slab) * series;
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < n) {
+            if (mine) {
                 k.maps[to + at + v] = all.a[v];
                 k.maps[to + k.slabs * series + at + v] = all.b[v];
-                k.cuts[to + at + v] = uint8_t((all.cut >> v) & 1);
+                if (RESETS) k.cuts[to + at + v] = uint8_t((all.cut >> v) & 1);
             }
     } else if (k.last.p && slab == (BACK ? 0 : k.slabs - 1)) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < n) k.last.p[o * k.last.so + (i + v) * k.last.si] = state[v];
+            if (mine) k.last.p[o * k.last.so + (i + v) * k.last.si] = state[v];
     }
 }
 
 // How a call is cut: see the top of the file.
 struct Cut {
-    bool staged;
+    int layout, vector;
     int lanes, slabs;
     int64_t groups, slab_steps;
 };
 
-template <typename T, bool BACK> constexpr int kV = sizeof(T) == 4 ? 4 : 8;
-template <typename T, bool BACK> constexpr int kSteps = !BACK && sizeof(T) == 4 ? 8 : 4;
-constexpr int kStagedSteps = 8;
+template <typename T, bool BACK> constexpr int kV = 2;
+template <typename T, bool BACK> constexpr int kSteps = BACK ? 4 : 8;
+constexpr int kRowSteps = 8;
 
-Cut cut_of(int V, int C, int size, bool rows, int64_t T, int64_t W, int64_t O) {
+inline Cut cut_of(int V, int C, int size, bool rows, int64_t T, int64_t W, int64_t O) {
     Cut k;
-    // feature-major rows that are read in pieces of less than 64 bytes, unless they are short
-    k.staged = !rows && W * size < 64 && T >= 64;
-    if (k.staged) {
+    if (W % V != 0) V = 1;
+    // feature-major rows that would be read in pieces of less than 64 bytes, unless they are short
+    k.layout = rows || W * size >= 64 || T < 64 ? kDirect : W == 1 ? kAlong : kStaged;
+    if (k.layout != kDirect) {
         V = 1;
-        C = kStagedSteps;
+        C = kRowSteps;
     }
+    // lanes side by side take at least a line of 128 bytes
     int chunks = 1;
-    while (chunks < 32 && int64_t(chunks) * C < T) chunks *= 2;
+    while (chunks < 2 * V * size && int64_t(chunks) * C < T) chunks *= 2;
     k.lanes = kThreads / chunks;
-    if (k.staged) {
+    if (k.layout != kDirect) {
         k.lanes = 1;
         while (k.lanes < W) k.lanes *= 2;
     }
-    k.groups = k.staged ? O : O * ((W + V - 1) / V);
-    const int64_t blocks = k.staged ? O : (k.groups + k.lanes - 1) / k.lanes;
+    k.groups = k.layout != kDirect ? O : O * (W / V);
+    k.vector = V;
+    const int64_t blocks = k.layout != kDirect ? O : (k.groups + k.lanes - 1) / k.lanes;
     const int64_t tile = int64_t(kThreads / k.lanes) * C;
     int64_t slabs = blocks < 512 ? (1024 + blocks - 1) / blocks : 1;
     if (slabs > kSlabs) slabs = kSlabs;
@@ -475,7 +558,7 @@ Cut cut_of(int V, int C, int size, bool rows, int64_t T, int64_t W, int64_t O) {
     return k;
 }
 
-int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+inline int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 template <typename T, bool GATE, bool BACK>
 hipError_t launch(const RecurrenceCall &c, hipStream_t s) {
@@ -514,17 +597,21 @@ hipError_t launch(const RecurrenceCall &c, hipStream_t s) {
     k.lanes = cut.lanes;
     k.slabs = cut.slabs;
     k.slab_steps = cut.slab_steps;
-    const int64_t blocks = cut.staged ? O : (cut.groups + cut.lanes - 1) / cut.lanes;
+    const int64_t blocks = cut.layout != kDirect ? O : (cut.groups + cut.lanes - 1) / cut.lanes;
     auto go = [&](const Args &a) {
         return over_blocks(blocks * cut.slabs, kThreads, [&](int64_t first, unsigned n) {
             Args b = a;
             b.first_block = first;
-            if (cut.staged)
-                hipLaunchKernelGGL((recurrence_kernel<T, 1, kStagedSteps, GATE, BACK, true>), dim3(n),
-                                   dim3(kThreads), 0, s, b);
-            else
-                hipLaunchKernelGGL((recurrence_kernel<T, V, C, GATE, BACK, false>), dim3(n), dim3(kThreads), 0, s,
-                                   b);
+            auto run = [&](auto resets) {
+                constexpr bool kResets = decltype(resets)::value;
+                auto kernel = recurrence_kernel<T, V, C, GATE, BACK, kResets, kDirect>;
+                if (cut.layout == kStaged) kernel = recurrence_kernel<T, 1, kRowSteps, GATE, BACK, kResets, kStaged>;
+                else if (cut.layout == kAlong) kernel = recurrence_kernel<T, 1, kRowSteps, GATE, BACK, kResets, kAlong>;
+                else if (cut.vector == 1) kernel = recurrence_kernel<T, 1, C, GATE, BACK, kResets, kDirect>;
+                hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, s, b);
+            };
+            if (c.resets) run(std::true_type{});
+            else run(std::false_type{});
         });
     };
     if (cut.slabs > 1) {
@@ -541,26 +628,12 @@ hipError_t launch(const RecurrenceCall &c, hipStream_t s) {
     return go(k);
 }
 
+// A call of type T, in the source file of that type.
+template <typename T> hipError_t launch_type(const RecurrenceCall &c, hipStream_t s) {
+    const bool gate = c.form == DARB_RECURRENCE_GATE;
+    if (c.back) return gate ? launch<T, true, true>(c, s) : launch<T, false, true>(c, s);
+    return gate ? launch<T, true, false>(c, s) : launch<T, false, false>(c, s);
+}
+
 }  // namespace
-
-int64_t recurrence_workspace_bytes(int dtype, bool back, bool rows, int64_t H, int64_t T, int64_t batch) {
-    const int size = dtype == DARB_F32 ? 4 : 2;
-    const int V = size == 4 ? kV<float, false> : kV<half_t, false>;
-    const int C = size == 4 ? (back ? kSteps<float, true> : kSteps<float, false>)
-                            : (back ? kSteps<half_t, true> : kSteps<half_t, false>);
-    const Cut k = cut_of(V, C, size, rows, T, rows ? H : batch, rows ? batch : H);
-    if (k.slabs == 1) return 0;
-    const int64_t series = H * batch;
-    return padded(8 * series * k.slabs) + padded(4 * series) + padded(series * k.slabs);
-}
-
-hipError_t launch_recurrence(const RecurrenceCall &c, hipStream_t s) {
-    return with_type(c.dtype, [&](auto t) {
-        using T = decltype(t);
-        const bool gate = c.form == DARB_RECURRENCE_GATE;
-        if (c.back) return gate ? launch<T, true, true>(c, s) : launch<T, false, true>(c, s);
-        return gate ? launch<T, true, false>(c, s) : launch<T, false, false>(c, s);
-    });
-}
-
 }  // namespace darb
