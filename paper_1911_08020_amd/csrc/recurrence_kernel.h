@@ -193,11 +193,31 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
     Cursor zc = cursor(k.z), xc = cursor(k.x), hc = cursor(k.h), gc = cursor(k.dh);
     auto writer = [&](const Result &q) { return cursor({q.p, q.so, q.st}); };
     Cursor oc = writer(k.out), oc2 = writer(k.out2);
+    // kDirect: z and x (or dh) of a tile of `ts` steps, `ahead` tiles from the cursors; steps that are
+    // not there read the tile's last one
+    Raw<T, V> rz[C], rb[C];
+    auto bring = [&](int ts, int ahead) {
+        const Cursor &second = BACK ? gc : xc;
+        const T *zp = zc.p + ahead * tile * zc.st, *bp = second.p + ahead * tile * second.st;
+        auto all_of = [&](auto whole) {
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+                const int64_t d = whole || c * C + j < ts ? j : ts - 1 - c * C;
+                rz[j].load(zp + d * zc.st);
+                rb[j].load(bp + d * second.st);
+            }
+        };
+        if (ts == tile) all_of(std::true_type{});
+        else all_of(std::false_type{});
+    };
+    auto steps_of = [&](int64_t done) { return int(steps - done < tile ? steps - done : tile); };
+    constexpr bool kAhead = LAYOUT == kDirect && !BACK;     // the gradients hold too much for it: 35.5 -> 41 us
+    if constexpr (kAhead) bring(steps_of(0), 0);
     int turn = 0;
     for (int64_t done = 0; done < steps; done += tile, turn ^= 1) {
         // Scan position p = done + c * C + j is step t0 + p, or counted from the slab's end.
         const int p0 = c * C;
-        const int tsteps = int(steps - done < tile ? steps - done : tile);
+        const int tsteps = steps_of(done);
         const int64_t ta = BACK ? t0 + steps - done - tsteps : t0 + done;  // the tile's first step
         auto step = [&](int j) {                            // in the tile, kept inside it
             const int p = p0 + j < tsteps ? p0 + j : tsteps - 1;
@@ -244,7 +264,6 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
             }
             __syncthreads();
         }
-        Raw<T, V> rz[C], rb[C];
         if constexpr (ALONG) {
             // the chunk's steps lie side by side: ascending, or backwards from `low` up
             const int64_t low = ta + (BACK ? tsteps - p0 - C : p0);
@@ -282,44 +301,41 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
                     }
                 }
             }
-        } else {
-            // all loads before the first use; steps that are not there read the tile's last one
-            auto bring = [&](auto whole) {
+        } else if constexpr (BACK) {
+            bring(tsteps, 0);
+            if (!first_launch) {
+                auto rest = [&](auto whole) {
 #pragma unroll
-                for (int j = 0; j < C; ++j) {
-                    const int64_t d = whole ? j : p0 + j < tsteps ? j : tsteps - 1 - p0;
-                    rz[j].load(zc.p + d * zc.st);
-                    if constexpr (!BACK) {
-                        rb[j].load(xc.p + d * xc.st);
-                    } else {
-                        rb[j].load(gc.p + d * gc.st);
-                        if (!first_launch) {
-                            // the state before; step 0's is not in h
-                            y[j].load(hc.p + (whole || ta + step(j) > 0 ? d + 1 : d) * hc.st);
-                            if constexpr (GATE) xs[j].load(xc.p + d * xc.st);
-                        }
+                    for (int j = 0; j < C; ++j) {
+                        const int64_t d = whole || p0 + j < tsteps ? j : tsteps - 1 - p0;
+                        // the state before; step 0's is not in h
+                        y[j].load(hc.p + (whole || ta + step(j) > 0 ? d + 1 : d) * hc.st);
+                        if constexpr (GATE) xs[j].load(xc.p + d * xc.st);
                     }
-                }
-            };
-            if (tsteps == tile && (!BACK || ta > 0)) bring(std::true_type{});
-            else bring(std::false_type{});
+                };
+                if (tsteps == tile && ta > 0) rest(std::true_type{});
+                else rest(std::false_type{});
+            }
         }
         if (BACK && !first_launch && k.h0.p && ta == 0) {
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 if (mine) y0[v] = k.h0.p[o * k.h0.so + (i + v) * k.h0.si];
         }
-        if (k.resets) {
+        if constexpr (RESETS) {
+            const uint8_t *r = k.resets + ta * k.rt + o * k.ro + (mine ? i * k.ri : 0);
+            if (V == 1 || k.ri == 0) {                      // one sequence: all its features
+                uint8_t first[C];
 #pragma unroll
-            for (int j = 0; j < C; ++j) {
-                const uint8_t *r = k.resets + (ta + step(j)) * k.rt + o * k.ro;
-                if (k.ri == 0) {                            // one sequence: all its features
-                    if (r[0]) cuts |= uint64_t((1u << V) - 1) << (j * V);
-                } else {
+                for (int j = 0; j < C; ++j) first[j] = r[step(j) * k.rt];
+#pragma unroll
+                for (int j = 0; j < C; ++j) cuts |= first[j] ? uint64_t((1u << V) - 1) << (j * V) : 0;
+            } else {
+#pragma unroll
+                for (int j = 0; j < C; ++j)
 #pragma unroll
                     for (int v = 0; v < V; ++v)
-                        if (r[i + v]) cuts |= uint64_t(1) << (j * V + v);
-                }
+                        cuts |= r[step(j) * k.rt + v] ? uint64_t(1) << (j * V + v) : 0;
             }
         }
         if (RESETS && live < C) cuts &= live > 0 ? (uint64_t(1) << (live * V)) - 1 : 0;   // the steps that are there
@@ -336,6 +352,9 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
                     else b[j][v] *= share;
                 }
             }
+        if constexpr (kAhead) {                             // the next tile's loads beside this one's scan
+            if (done + tile < steps) bring(steps_of(done + tile), 1);
+        }
         if (tsteps < tile) {                                // steps that are not there change nothing
 #pragma unroll
             for (int j = 0; j < C; ++j)
