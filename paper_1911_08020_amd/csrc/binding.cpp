@@ -11,6 +11,7 @@
 // calls.
 #include <Python.h>
 
+#include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
 #include <c10/hip/HIPCachingAllocator.h>
@@ -887,7 +888,11 @@ PyObject *policy_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
         void *ws = bytes ? ptr(workspace) : nullptr;
         PyObject *res = PyTuple_New(5);
         if (!res) return nullptr;
-        for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(res, i, THPVariable_Wrap(stats.select(0, i)));
+        {
+            // views of a result of no gradient: nothing for automatic differentiation to record
+            const at::AutoDispatchBelowADInplaceOrView plain;
+            for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(res, i, THPVariable_Wrap(stats.select(0, i)));
+        }
         for (int i = 0; i < 2; ++i) {
             PyTuple_SET_ITEM(res, 3 + i, held.o[i] ? held.o[i] : (Py_INCREF(Py_None), Py_None));
             held.o[i] = nullptr;
@@ -937,8 +942,11 @@ PyObject *preference_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (!(held.o[2] = tokens_or(a[7], B, t->options(), &grad))) return none();
         memory.result(out);
         memory.result(grad);
-        held.o[0] = THPVariable_Wrap(out.select(0, 0));
-        held.o[1] = THPVariable_Wrap(out.narrow(0, 1, P));
+        {
+            const at::AutoDispatchBelowADInplaceOrView plain;
+            held.o[0] = THPVariable_Wrap(out.select(0, 0));
+            held.o[1] = THPVariable_Wrap(out.slice(0, 1, 1 + P));
+        }
         float *op = static_cast<float *>(ptr(out)), *gp = static_cast<float *>(ptr(grad));
         PyObject *res = held.tuple(3);
         if (!res) return nullptr;

@@ -23,20 +23,34 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBig = 1024;              // threads of a workgroup that is alone
 constexpr int kV = 4;
-constexpr int kTile = kThreads * kV * 4;
+constexpr int kTile = kThreads * kV;     // policy tokens of a workgroup: 4 and 16 a thread take longer
 constexpr int kAlone = 8192;            // tokens that one workgroup takes
 
-// The workgroup's sum of each thread's x, in thread 0 (`room`: a double a wave).
-template <int THREADS> __device__ __forceinline__ double block_sum(double x, double *room) {
+// The workgroup's sums of each thread's x, in thread 0 (`room`: a double a wave for each).
+template <int THREADS, int N> __device__ __forceinline__ void block_sums(double (&x)[N], double (&room)[N][THREADS / kWave]) {
+    constexpr int kWaves = THREADS / kWave;
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
-    __syncthreads();                    // the room may be in use
-    if (lane_id() == 0) room[wave_id()] = x;
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) x[i] += __shfl_xor(x[i], d);
+        if (lane_id() == 0) room[i][wave_id()] = x[i];
+    }
     __syncthreads();
-    x = 0.0;
-    if (threadIdx.x == 0)
-        for (int w = 0; w < THREADS / kWave; ++w) x += room[w];
-    return x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = room[i][threadIdx.x % kWaves];
+#pragma unroll
+        for (int d = 1; d < kWaves; d <<= 1) x[i] += __shfl_xor(x[i], d);
+    }
+}
+
+// e^x, off by about 2 units: 2^t with t = x log2 e, whose rounding is put right in the result.
+__device__ __forceinline__ float exp_of(float x) {
+    constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
+    const float t = x * kLog2E;
+    const float e = __builtin_amdgcn_exp2f(t);
+    const float r = fmaf(x, kLog2E, -t) * kLn2;
+    return fabsf(t) < 126.0f ? fmaf(e, r, e) : e;           // not where t or e is infinite
 }
 
 // ---- policy ----------------------------------------------------------------------------
@@ -45,19 +59,21 @@ struct Sums {
     double loss = 0.0, kl = 0.0, cut = 0.0;
 };
 
-// e^q - 1 - q without its cancellation near 0.
-__device__ __forceinline__ float excess(float q) {
-    if (fabsf(q) < 0.25f) {
-        float p = 1.0f / 40320.0f;
-        p = p * q + 1.0f / 5040.0f;
-        p = p * q + 1.0f / 720.0f;
-        p = p * q + 1.0f / 120.0f;
-        p = p * q + 1.0f / 24.0f;
-        p = p * q + 1.0f / 6.0f;
-        p = p * q + 0.5f;
-        return p * q * q;
-    }
-    return expm1f(q) - q;
+// e^q - 1 - q without its cancellation near 0, and e^q - 1.
+__device__ __forceinline__ float excess(float q, float &grown) {
+    float p = 1.0f / 362880.0f;
+    p = p * q + 1.0f / 40320.0f;
+    p = p * q + 1.0f / 5040.0f;
+    p = p * q + 1.0f / 720.0f;
+    p = p * q + 1.0f / 120.0f;
+    p = p * q + 1.0f / 24.0f;
+    p = p * q + 1.0f / 6.0f;
+    p = p * q + 0.5f;
+    p = p * q * q;
+    const float e = exp_of(q) - 1.0f;
+    const bool near = fabsf(q) < 0.5f;
+    grown = near ? p + q : e;
+    return near ? p : e - q;
 }
 
 struct PolicyToken {
@@ -67,7 +83,7 @@ struct PolicyToken {
 __device__ __forceinline__ float policy_token(const PolicyCall &c, const PolicyToken &t, Sums &s) {
     if (t.w == 0.0f) return 0.0f;       // whatever stands there
     const double d = double(t.lp) - double(t.old);
-    const float ra = expf(float(d)) * t.A;
+    const float ra = exp_of(float(d)) * t.A;
     float loss = -ra, grad = -ra;
     if (t.A > 0.0f && d > c.log_high) {
         loss = -(c.high * t.A);
@@ -80,10 +96,11 @@ __device__ __forceinline__ float policy_token(const PolicyCall &c, const PolicyT
     }
     if (c.ref) {
         const float q = float(double(t.ref) - double(t.lp));
-        const float k = excess(q);
+        float grown;
+        const float k = excess(q, grown);
         s.kl += double(t.w) * double(k);
         loss += c.kl_coef * k;
-        grad -= c.kl_coef * expm1f(q);
+        grad -= c.kl_coef * grown;
     }
     if (c.entropy) loss -= c.entropy_coef * t.h;
     s.loss += double(t.w) * double(loss);
@@ -116,7 +133,7 @@ __device__ __forceinline__ void store4(float *p, int64_t at, int n, const float 
 
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void policy_kernel(PolicyCall c, int64_t first_block, int64_t blocks, int64_t tile) {
-    __shared__ double room[THREADS / kWave];
+    __shared__ double room[3][THREADS / kWave];
     Sums s;
     const int64_t block = first_block + blockIdx.x, end = (block + 1) * tile < c.B ? (block + 1) * tile : c.B;
     for (int64_t at = block * tile + int64_t(threadIdx.x) * kV; at < end; at += THREADS * kV) {
@@ -136,27 +153,28 @@ __global__ __launch_bounds__(THREADS) void policy_kernel(PolicyCall c, int64_t f
         store4(c.grad, at, n, g);
         if (c.grad_entropy) store4(c.grad_entropy, at, n, gh);
     }
-    const double loss = block_sum<THREADS>(s.loss, room), kl = block_sum<THREADS>(s.kl, room),
-                 cut = block_sum<THREADS>(s.cut, room);
+    double x[3] = {s.loss, s.kl, s.cut};
+    block_sums<THREADS>(x, room);
     if (threadIdx.x != 0) return;
-    if (blocks == 1) {
-        c.stats[0] = float(loss);
-        c.stats[1] = float(kl);
-        c.stats[2] = float(cut);
-    } else {
-        c.partial[block] = loss;
-        c.partial[blocks + block] = kl;
-        c.partial[2 * blocks + block] = cut;
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        if (blocks == 1) c.stats[q] = float(x[q]);
+        else c.partial[q * blocks + block] = x[q];
     }
 }
 
-__global__ __launch_bounds__(kBig) void policy_sum_kernel(const double *partial, int64_t blocks, float *stats) {
-    __shared__ double room[kBig / kWave];
-    for (int q = 0; q < 3; ++q) {
-        double x = 0.0;
-        for (int64_t i = threadIdx.x; i < blocks; i += kBig) x += partial[q * blocks + i];
-        x = block_sum<kBig>(x, room);
-        if (threadIdx.x == 0) stats[q] = float(x);
+__global__ __launch_bounds__(kThreads) void policy_sum_kernel(const double *partial, int64_t blocks, float *stats) {
+    __shared__ double room[3][kThreads / kWave];
+    double x[3] = {};
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < blocks; i += kThreads) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) x[q] += partial[q * blocks + i];
+    }
+    block_sums<kThreads>(x, room);
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) stats[q] = float(x[q]);
     }
 }
 
@@ -184,7 +202,11 @@ __global__ __launch_bounds__(THREADS) void preference_kernel(PreferenceCall c, i
     // strided: lanes lie side by side over the sequences; packed: over the tokens
     const int which = c.starts ? int(threadIdx.x) / kTeam : q, at = c.starts ? int(threadIdx.x) % kTeam : team;
     const int64_t pair = block * PAIRS + which % PAIRS, s = which < PAIRS ? pair : c.P + pair;
-    int64_t from = 0, count = 0, stride = 1;
+    int64_t from = 0, count = 0, stride = 1, head = 0, tail = 0;
+    if (c.starts) {
+        head = c.starts[0];
+        tail = c.starts[S];
+    }
     if (pair < c.P) {
         if (c.starts) {
             int64_t a = c.starts[s], b = c.starts[s + 1];
@@ -199,10 +221,22 @@ __global__ __launch_bounds__(THREADS) void preference_kernel(PreferenceCall c, i
         }
     }
     double sum = 0.0;
-#pragma unroll 4
-    for (int64_t t = at; t < count; t += kTeam) {
-        const int64_t e = from + t * stride;
-        sum += double(c.lp[e]) - (c.ref ? double(c.ref[e]) : 0.0);
+    if (c.starts) {
+#pragma unroll 2
+        for (int64_t t = int64_t(at) * kV; t < count; t += kTeam * kV) {
+            const int n = count - t < kV ? int(count - t) : kV;
+            float lp[kV], ref[kV];
+            load4(c.lp, from + t, n, 0.0f, lp);
+            load4(c.ref, from + t, n, 0.0f, ref);
+#pragma unroll
+            for (int i = 0; i < kV; ++i) sum += double(lp[i]) - double(ref[i]);
+        }
+    } else {
+#pragma unroll 8
+        for (int64_t t = at; t < count; t += kTeam) {
+            const int64_t e = from + t * stride;
+            sum += double(c.lp[e]) - (c.ref ? double(c.ref[e]) : 0.0);
+        }
     }
     // each sequence's parts by neighbouring lanes, whichever way they were read
     room[which][at] = sum;
@@ -233,11 +267,16 @@ __global__ __launch_bounds__(THREADS) void preference_kernel(PreferenceCall c, i
     __syncthreads();
     if (pair < c.P) {
         const float d = coef[which];
-        for (int64_t t = at; t < count; t += kTeam) c.grad[from + t * stride] = d;
+        if (c.starts) {
+            const float all[kV] = {d, d, d, d};
+            for (int64_t t = int64_t(at) * kV; t < count; t += kTeam * kV)
+                store4(c.grad, from + t, count - t < kV ? int(count - t) : kV, all);
+        } else {
+            for (int64_t t = at; t < count; t += kTeam) c.grad[from + t * stride] = d;
+        }
     }
     if (c.starts) {
         // tokens of no sequence have no gradient: each workgroup clears a share
-        int64_t head = c.starts[0], tail = c.starts[S];
         head = head < 0 ? 0 : head > c.B ? c.B : head;
         tail = tail < head ? head : tail > c.B ? c.B : tail;
         const int64_t none = head + c.B - tail, all = (c.P + PAIRS - 1) / PAIRS;
@@ -255,12 +294,12 @@ __global__ __launch_bounds__(THREADS) void preference_kernel(PreferenceCall c, i
 }
 
 __global__ __launch_bounds__(kBig) void preference_sum_kernel(PreferenceCall c) {
-    __shared__ double room[kBig / kWave];
-    double x = 0.0;
+    __shared__ double room[1][kBig / kWave];
+    double x[1] = {0.0};
     for (int64_t p = threadIdx.x; p < c.P; p += kBig)
-        x += double(pair_loss(c, c.margin[p], c.weight ? c.weight[p] : c.even));
-    x = block_sum<kBig>(x, room);
-    if (threadIdx.x == 0) *c.loss = float(x);
+        x[0] += double(pair_loss(c, c.margin[p], c.weight ? c.weight[p] : c.even));
+    block_sums<kBig>(x, room);
+    if (threadIdx.x == 0) *c.loss = float(x[0]);
 }
 
 }  // namespace
@@ -280,7 +319,7 @@ hipError_t launch_policy(PolicyCall c, hipStream_t s) {
         hipLaunchKernelGGL((policy_kernel<kThreads>), dim3(n), dim3(kThreads), 0, s, c, first, blocks, int64_t(kTile));
     });
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(kBig), 0, s, c.partial, blocks, c.stats);
+    hipLaunchKernelGGL(policy_sum_kernel, dim3(1), dim3(kThreads), 0, s, c.partial, blocks, c.stats);
     return hipGetLastError();
 }
 
