@@ -140,8 +140,11 @@ template <typename F> int over_tensors(const darb_adamw &a, int64_t most, F &&f)
     return DARB_OK;
 }
 
-// Whether the result's own type asks for fp32 products.
-bool muon_full(const darb_muon_tensor &t) { return t.dtype == DARB_F32 || t.master; }
+// Whether the result's own type asks for products as accurate as fp32.  Those of small matrices are,
+// whatever the type: in fp16 the sums of few terms are further off, and they take no longer.
+bool muon_full(const darb_muon_tensor &t) {
+    return t.dtype == DARB_F32 || t.master || (t.rows < t.cols ? t.rows : t.cols) < 64;
+}
 
 // The groups of tensors that go through the launches together: consecutive ones of one accuracy,
 // up to kMuonTensors and 2^28 elements of theirs (or a single one).  A tensor that is left out

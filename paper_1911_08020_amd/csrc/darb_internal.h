@@ -305,6 +305,7 @@ struct MuonCall {
     double eps;
     const float *grad_scale;
     void *workspace;
+    uint8_t order[2][kMuonTensors];     // filled in: the tensors by m and by n
 };
 // The bytes of `count` matrices' group; fills in what the launch needs.
 int64_t muon_group(MuonCall &c);

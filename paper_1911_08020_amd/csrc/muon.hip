@@ -64,8 +64,13 @@ __device__ __forceinline__ int64_t place_of(int row, int col, int cols) {
            piece(row & 15, col % kDepth / 8) * 8 + col % 8;
 }
 
-// The partial sums of every matrix' norm lie before the matrices.
-__host__ __device__ constexpr int64_t norms_bytes() { return int64_t(kMuonTensors) * kNormBlocks * 8; }
+// Before the matrices lie the call itself, which the first launch leaves there (launches that carry
+// its 3 KB along cost the host more than their kernels), and the partial sums of the norms.
+__host__ __device__ constexpr int64_t call_bytes() { return (int64_t(sizeof(MuonCall)) + 255) / 256 * 256; }
+__host__ __device__ constexpr int64_t norms_bytes() { return call_bytes() + int64_t(kMuonTensors) * kNormBlocks * 8; }
+__device__ __forceinline__ double *norms(const MuonCall &c, int which) {
+    return reinterpret_cast<double *>(static_cast<char *>(c.workspace) + call_bytes()) + which * kNormBlocks;
+}
 
 __device__ __forceinline__ half_t *matrices(const MuonCall &c, const MuonTensor &t) {
     return reinterpret_cast<half_t *>(static_cast<char *>(c.workspace) + norms_bytes()) + t.base;
@@ -117,6 +122,9 @@ __host__ __device__ __forceinline__ int norm_blocks(const MuonTensor &t) {
 __global__ __launch_bounds__(kNormThreads) void norm_kernel(MuonCall c) {
     __shared__ double room[kNormThreads / kWave];
     const int which = int(blockIdx.y);
+    if (blockIdx.x == 0 && which == 0)
+        for (int i = threadIdx.x; i < int(sizeof(MuonCall) / 4); i += kNormThreads)
+            static_cast<uint32_t *>(c.workspace)[i] = reinterpret_cast<const uint32_t *>(&c)[i];
     const MuonTensor &t = c.t[which];
     const int blocks = norm_blocks(t);
     if (int(blockIdx.x) >= blocks) return;
@@ -153,7 +161,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(MuonCall c) {
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int w = 1; w < kNormThreads / kWave; ++w) sum += room[w];
-        static_cast<double *>(c.workspace)[which * kNormBlocks + blockIdx.x] = sum;
+        norms(c, which)[blockIdx.x] = sum;
     }
 }
 
@@ -167,24 +175,29 @@ __device__ __forceinline__ Split split(float scaled) {
     return {hi, half_t(scaled - float(hi))};
 }
 
-// Padded to whole tiles of the natural orientation.
+// Padded, in the natural orientation.
 __host__ __device__ __forceinline__ int padded_rows(const MuonTensor &t) { return t.rows <= t.cols ? t.m : t.n; }
 __host__ __device__ __forceinline__ int padded_cols(const MuonTensor &t) { return t.rows <= t.cols ? t.n : t.m; }
 
-__global__ __launch_bounds__(256) void cut_kernel(MuonCall c, int first_block) {
+__host__ __device__ __forceinline__ int cut_tiles(const MuonTensor &t) {
+    return ((t.m + kCutTile - 1) / kCutTile) * ((t.n + kCutTile - 1) / kCutTile);
+}
+
+__global__ __launch_bounds__(256) void cut_kernel(const MuonCall *__restrict__ call, int first_block) {
+    const MuonCall &c = *call;
     __shared__ float tile[kCutTile][kCutTile + 1];
     __shared__ double room[256 / kWave];
     int block = first_block + int(blockIdx.x), which = 0;
     for (;; ++which) {
-        const int blocks = (padded_rows(c.t[which]) / kCutTile) * (padded_cols(c.t[which]) / kCutTile);
+        const int blocks = cut_tiles(c.t[which]);
         if (block < blocks) break;
         block -= blocks;
     }
     const MuonTensor &t = c.t[which];
     const int tid = int(threadIdx.x), R = padded_rows(t), C = padded_cols(t);
-    const int r0 = block / (C / kCutTile) * kCutTile, c0 = block % (C / kCutTile) * kCutTile;
+    const int across = (C + kCutTile - 1) / kCutTile, r0 = block / across * kCutTile, c0 = block % across * kCutTile;
     double sum = 0.0;
-    for (int i = tid; i < norm_blocks(t); i += 256) sum += static_cast<const double *>(c.workspace)[which * kNormBlocks + i];
+    for (int i = tid; i < norm_blocks(t); i += 256) sum += norms(c, which)[i];
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
     if (lane_id() == 0) room[wave_id()] = sum;
@@ -224,6 +237,7 @@ __global__ __launch_bounds__(256) void cut_kernel(MuonCall c, int first_block) {
             hi[i] = s.hi;
             lo[i] = s.lo;
         }
+        if (r0 + row >= R || c0 + col >= C) continue;
         const int64_t to = place_of(r0 + row, c0 + col, C);
         *reinterpret_cast<Half4 *>(nh + to) = hi;
         *reinterpret_cast<Half4 *>(nl + to) = lo;
@@ -239,6 +253,7 @@ __global__ __launch_bounds__(256) void cut_kernel(MuonCall c, int first_block) {
             hi[i] = s.hi;
             lo[i] = s.lo;
         }
+        if (c0 + row >= C || r0 + col >= R) continue;
         const int64_t to = place_of(c0 + row, r0 + col, R);
         *reinterpret_cast<Half4 *>(fh + to) = hi;
         *reinterpret_cast<Half4 *>(fl + to) = lo;
@@ -249,10 +264,10 @@ __global__ __launch_bounds__(256) void cut_kernel(MuonCall c, int first_block) {
 
 enum { kGram, kSquare, kApply, kResult };                   // A; b A + c A A; X; the last X
 
-// Tiles on and below the diagonal of q x q, or all of them.
-__host__ __device__ __forceinline__ int tiles_of(const MuonTensor &t, int mode, int tile) {
-    const int q = t.m / tile;
-    return mode == kGram || mode == kSquare ? q * (q + 1) / 2 : q * (t.n / tile);
+// Tiles on and below the diagonal, or all of them; the last ones may hang over.
+__host__ __device__ __forceinline__ int tiles_of(const MuonTensor &t, int mode, int rows, int cols) {
+    const int a = (t.m + rows - 1) / rows;
+    return mode == kGram || mode == kSquare ? a * (a + 1) / 2 : a * ((t.n + cols - 1) / cols);
 }
 
 // 16 bytes from each lane's address to LDS, lane after lane from `to` (the same in all lanes).
@@ -287,20 +302,24 @@ __device__ __forceinline__ void turn4(uint32_t (&v)[4]) {
     swap(v[1], v[3], two, x2);
 }
 
-template <int TILE, int WAVES, int PRODUCTS, int MODE>
-__global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int step, int first_block, int blocks) {
-    constexpr int kParts = PRODUCTS == 1 ? 1 : 2;
-    constexpr int kWaveRows = 2, kWaveCols = WAVES / kWaveRows;
-    constexpr int kRows = TILE / kWaveRows / 16, kCols = TILE / kWaveCols / 16;     // 16 x 16 tiles of a wave
-    constexpr int kPanel = TILE * kDepth;                   // halves of a panel
+// C tiles of TM x TN by WR x WC waves.
+template <int TM, int TN, int WR, int WC, int PRODUCTS, int MODE>
+__global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *__restrict__ call, int step,
+                                                                int first_block, int blocks) {
+    constexpr int kParts = PRODUCTS == 1 ? 1 : 2, kWaves = WR * WC;
+    constexpr int kRows = TM / WR / 16, kCols = TN / WC / 16;                       // 16 x 16 tiles of a wave
+    constexpr int kBlocks = (TM + TN) / 16, kBlock = 16 * kDepth;                   // of a stage, P's first
     constexpr bool kTriangle = MODE == kGram || MODE == kSquare;
-    __shared__ __attribute__((aligned(16))) half_t lds[2][2 * kParts][kPanel];
+    static_assert(!kTriangle || TM == TN, "the diagonal runs through whole tiles");
+    __shared__ __attribute__((aligned(16))) half_t lds[2][kParts][kBlocks * kBlock];
+    const MuonCall &c = *call;
 
-    // neighbouring tiles on one XCD
+    // neighbouring tiles on one XCD, the longest products first
     const int b = first_block + int(blockIdx.x), share = blocks / 8, rest = blocks % 8, xcd = b % 8;
     int id = (xcd < rest ? xcd * (share + 1) : rest + xcd * share) + b / 8, which = 0;
-    for (;; ++which) {
-        const int n = tiles_of(c.t[which], MODE, TILE);
+    for (int i = 0;; ++i) {
+        which = c.order[MODE == kGram][i];
+        const int n = tiles_of(c.t[which], MODE, TM, TN);
         if (id < n) break;
         id -= n;
     }
@@ -309,10 +328,11 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
     const Places place(t);
     const int m = t.m, n = t.n, K = MODE == kGram ? n : m;
     // four rows of tiles at a time, column by column, and what is on and below the diagonal last
+    const int down = (m + TM - 1) / TM, across = kTriangle ? 0 : (n + TN - 1) / TN;
     int ti, tj, top = 0, height;
     for (;; top += 4) {
-        height = m / TILE - top < 4 ? m / TILE - top : 4;
-        const int band = kTriangle ? height * top + height * (height + 1) / 2 : height * (n / TILE);
+        height = down - top < 4 ? down - top : 4;
+        const int band = kTriangle ? height * top + height * (height + 1) / 2 : height * across;
         if (id < band) break;
         id -= band;
     }
@@ -326,7 +346,7 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
         ti += top;
     }
     const int lane = lane_id(), w = wave_id();
-    const int wr = w / kWaveCols * (kRows * 16), wc = w % kWaveCols * (kCols * 16);
+    const int wr = w / WC * (kRows * 16), wc = w % WC * (kCols * 16);
     const int mine = (lane & 15) * kDepth + piece(lane & 15, lane >> 4) * 8;
     auto part_of = [&](int buffer, int part, int at) {
         return *reinterpret_cast<const Half8 *>(&lds[buffer][part][at * kDepth + mine]);
@@ -335,17 +355,21 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
     const int64_t pl = MODE == kGram ? place.x(step, 1) : MODE == kSquare ? place.a(1) : place.b(1);
     const int64_t qh = kTriangle ? ph : place.xt(step, 0);
     const int64_t ql = kTriangle ? pl : place.xt(step, 1);
-    const int64_t po = int64_t(ti) * TILE * K + lane * 8, qo = int64_t(tj) * TILE * K + lane * 8;
+    // rows of blocks: behind the last one its own are read again, and not used
+    const int plast = m / 16 - 1, qlast = (kTriangle ? m : n) / 16 - 1;
     auto fetch = [&](int buffer, int k) {
 #pragma unroll
-        for (int part = 0; part < 2 * kParts; ++part) {
-            const half_t *from = base + (part == 0 ? ph + po : part == 1 ? qh + qo : part == 2 ? pl + po : ql + qo) + int64_t(k) * 16;
+        for (int part = 0; part < kParts; ++part)
 #pragma unroll
-            for (int q = 0; q < TILE / 16 / WAVES; ++q) {
-                const int rows = (q * WAVES + w) * 16;
-                load_lds(from + int64_t(rows) * K, &lds[buffer][part][rows * kDepth]);
+            for (int i = 0; i < (kBlocks + kWaves - 1) / kWaves; ++i) {
+                const int at = i * kWaves + w;
+                if (kBlocks % kWaves != 0 && at >= kBlocks) break;
+                const bool p = at < TM / 16;
+                int r = p ? ti * (TM / 16) + at : tj * (TN / 16) + at - TM / 16;
+                r = p ? (r < plast ? r : plast) : (r < qlast ? r : qlast);
+                const half_t *from = base + (p ? (part ? pl : ph) : (part ? ql : qh)) + int64_t(r) * 16 * K + int64_t(k) * 16;
+                load_lds(from + lane * 8, &lds[buffer][part][at * kBlock]);
             }
-        }
     };
     Float4 acc[kRows][kCols];
 #pragma unroll
@@ -357,13 +381,13 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
     auto columns = [&](int buffer) {
 #pragma unroll
         for (int j = 0; j < kCols; ++j) {
-            qh_[j] = part_of(buffer, 1, wc + j * 16);
-            if (kParts == 2) ql_[j] = part_of(buffer, 3, wc + j * 16);
+            qh_[j] = part_of(buffer, 0, TM + wc + j * 16);
+            if (kParts == 2) ql_[j] = part_of(buffer, 1, TM + wc + j * 16);
         }
     };
     auto rows = [&](int buffer, int i) {
         hi = part_of(buffer, 0, wr + i * 16);
-        if (kParts == 2) lo = part_of(buffer, 2, wr + i * 16);
+        if (kParts == 2) lo = part_of(buffer, 1, wr + i * 16);
     };
     fetch(0, k);
     arrived();
@@ -401,13 +425,15 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
     }
     // A lane holds rows 4 (l / 16) to + 3 of column l % 16 of each 16 x 16 tile, and after turn4
     // columns 4 (l % 16 / 4) to + 3 of row 4 (l / 16) + l % 4.
-    const int r0 = ti * TILE + wr + (lane >> 4) * 4, c0 = tj * TILE + wc + (lane & 15);
-    const int r1 = ti * TILE + wr + (lane >> 4) * 4 + (lane & 3), c1 = tj * TILE + wc + (lane & 12);
+    const int r0 = ti * TM + wr + (lane >> 4) * 4, c0 = tj * TN + wc + (lane & 15);
+    const int r1 = ti * TM + wr + (lane >> 4) * 4 + (lane & 3), c1 = tj * TN + wc + (lane & 12);
 #pragma unroll
     for (int i = 0; i < kRows; ++i)
 #pragma unroll
         for (int j = 0; j < kCols; ++j) {
             const int r = r0 + i * 16, q = c0 + j * 16, rt = r1 + i * 16, qt = c1 + j * 16;
+            // 16 rows or columns at a time are there or not, for all lanes
+            if (ti * TM + wr + i * 16 > plast * 16 || tj * TN + wc + j * 16 > qlast * 16) continue;
             float v[4];
             // [q][r ... r + 3] of X^T or a symmetric matrix
             const int64_t to = place_of(q, r, m);
@@ -488,53 +514,100 @@ __global__ __launch_bounds__(WAVES *kWave) void product_kernel(MuonCall c, int s
         }
 }
 
-constexpr int kSmall = 128, kLarge = 256;
+// The tiles that a product may go by: rows, columns, and the rate of a compute unit that is full
+// of them, of that of the largest.  4096 x 9216 in fp32, us a product:  TABLE
+struct Tile {
+    int rows, cols;
+    float rate;
+};
+constexpr Tile kTiles[] = {{256, 256, 1.0f}, {256, 192, 0.95f}, {192, 192, 0.92f}, {128, 128, 0.75f}, {64, 64, 0.3f}};
+constexpr int kTileKinds = 5;
+constexpr int kUnits = 256;             // compute units
 
-template <int TILE, int WAVES, int PRODUCTS, int MODE>
+int depth_of(const MuonTensor &t, int mode) { return mode == kGram ? t.n : t.m; }
+
+// How long a product of all matrices takes by tiles of one kind, in stages of the largest: rounds of
+// tiles over the compute units, or, where tiles are of unlike lengths, what they come to together and
+// half of the shortest.
+float cost_of(const MuonCall &c, int mode, const Tile &k) {
+    int64_t tiles = 0, all = 0;
+    int least = 1 << 30, most = 0;
+    for (int i = 0; i < c.count; ++i) {
+        const int n = tiles_of(c.t[i], mode, k.rows, k.cols), depth = depth_of(c.t[i], mode);
+        tiles += n;
+        all += int64_t(n) * depth;
+        least = depth < least ? depth : least;
+        most = depth > most ? depth : most;
+    }
+    float rounds = least == most ? float((tiles + kUnits - 1) / kUnits) * most : float(all) / kUnits + 0.5f * least;
+    rounds = rounds > most ? rounds : most;
+    return rounds * k.rows * k.cols / k.rate;
+}
+
+int tile_of(const MuonCall &c, int mode) {
+    int best = 0;
+    float cost = 0.0f;
+    for (int i = 0; i < kTileKinds; ++i) {
+        if ((mode == kGram || mode == kSquare) && kTiles[i].rows != kTiles[i].cols) continue;
+        const float x = cost_of(c, mode, kTiles[i]);
+        if (cost == 0.0f || x < cost) cost = x, best = i;
+    }
+    return best;
+}
+
+template <int TM, int TN, int WR, int WC, int PRODUCTS, int MODE>
 hipError_t product(const MuonCall &c, int step, hipStream_t s) {
     int blocks = 0;
-    for (int i = 0; i < c.count; ++i) blocks += tiles_of(c.t[i], MODE, TILE);
-    return over_blocks(blocks, WAVES * kWave, [&](int64_t first, unsigned n) {
-        hipLaunchKernelGGL((product_kernel<TILE, WAVES, PRODUCTS, MODE>), dim3(n), dim3(WAVES * kWave), 0, s, c,
-                           step, int(first), blocks);
+    for (int i = 0; i < c.count; ++i) blocks += tiles_of(c.t[i], MODE, TM, TN);
+    return over_blocks(blocks, WR * WC * kWave, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL((product_kernel<TM, TN, WR, WC, PRODUCTS, MODE>), dim3(n), dim3(WR * WC * kWave), 0, s,
+                           static_cast<const MuonCall *>(c.workspace), step, int(first), blocks);
     });
 }
 
-template <int TILE, int WAVES, int PRODUCTS> hipError_t steps(const MuonCall &c, hipStream_t s) {
+template <int PRODUCTS, int MODE> hipError_t product(const MuonCall &c, int kind, int step, hipStream_t s) {
+    if (kind == 0) return product<256, 256, 2, 4, PRODUCTS, MODE>(c, step, s);
+    if constexpr (MODE == kApply || MODE == kResult) {
+        if (kind == 1) return product<256, 192, 2, 4, PRODUCTS, MODE>(c, step, s);
+    }
+    if (kind == 2) return product<192, 192, 2, 2, PRODUCTS, MODE>(c, step, s);
+    if (kind == 3) return product<128, 128, 2, 2, PRODUCTS, MODE>(c, step, s);
+    return product<64, 64, 2, 2, PRODUCTS, MODE>(c, step, s);
+}
+
+template <int PRODUCTS> hipError_t steps(const MuonCall &c, hipStream_t s) {
+    const int gram = tile_of(c, kGram), square = tile_of(c, kSquare), apply = tile_of(c, kApply);
     for (int k = 0; k < c.steps; ++k) {
-        hipError_t e = product<TILE, WAVES, PRODUCTS, kGram>(c, k, s);
-        if (e == hipSuccess) e = product<TILE, WAVES, 3, kSquare>(c, k, s);
+        hipError_t e = product<PRODUCTS, kGram>(c, gram, k, s);
+        if (e == hipSuccess) e = product<3, kSquare>(c, square, k, s);
         if (e == hipSuccess)
-            e = k + 1 < c.steps ? product<TILE, WAVES, PRODUCTS, kApply>(c, k, s)
-                                : product<TILE, WAVES, PRODUCTS, kResult>(c, k, s);
+            e = k + 1 < c.steps ? product<PRODUCTS, kApply>(c, apply, k, s) : product<PRODUCTS, kResult>(c, apply, k, s);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
-// Large tiles read least, and are taken where there are enough of them for the device.
-int tile_of(const MuonCall &c) {
-    int64_t tiles = 0;
-    for (int i = 0; i < c.count; ++i) {
-        const int64_t a = (c.t[i].rows + kLarge - 1) / kLarge, b = (c.t[i].cols + kLarge - 1) / kLarge;
-        tiles += a * b;
-    }
-    return tiles >= 256 ? kLarge : kSmall;
-}
-
 }  // namespace
 
 int64_t muon_group(MuonCall &c) {
-    const int tile = tile_of(c);
     int64_t at = 0;
     for (int i = 0; i < c.count; ++i) {
         MuonTensor &t = c.t[i];
-        const int a = (t.rows + tile - 1) / tile * tile, b = (t.cols + tile - 1) / tile * tile;
+        const int a = (t.rows + kDepth - 1) / kDepth * kDepth, b = (t.cols + kDepth - 1) / kDepth * kDepth;
         t.m = t.rows <= t.cols ? a : b;
         t.n = t.rows <= t.cols ? b : a;
         t.base = at;
         at += Places(t).all();
     }
+    // by length of the products' sums, longest first
+    for (int gram = 0; gram < 2; ++gram)
+        for (int i = 0; i < c.count; ++i) {
+            int j = i;
+            const int depth = depth_of(c.t[i], gram ? kGram : kSquare);
+            for (; j > 0 && depth_of(c.t[c.order[gram][j - 1]], gram ? kGram : kSquare) < depth; --j)
+                c.order[gram][j] = c.order[gram][j - 1];
+            c.order[gram][j] = uint8_t(i);
+        }
     return norms_bytes() + 2 * at;
 }
 
@@ -543,17 +616,17 @@ hipError_t launch_muon(const MuonCall &c, hipStream_t s) {
     for (int i = 0; i < c.count; ++i) {
         const int n = norm_blocks(c.t[i]);
         most = n > most ? n : most;
-        cuts += (c.t[i].m / kCutTile) * (c.t[i].n / kCutTile);
+        cuts += cut_tiles(c.t[i]);
     }
     hipLaunchKernelGGL(norm_kernel, dim3(most, c.count), dim3(kNormThreads), 0, s, c);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     e = over_blocks(cuts, 256, [&](int64_t first, unsigned n) {
-        hipLaunchKernelGGL(cut_kernel, dim3(n), dim3(256), 0, s, c, int(first));
+        hipLaunchKernelGGL(cut_kernel, dim3(n), dim3(256), 0, s,
+                           static_cast<const MuonCall *>(c.workspace), int(first));
     });
     if (e != hipSuccess) return e;
-    if (tile_of(c) == kLarge) return c.full ? steps<kLarge, 8, 3>(c, s) : steps<kLarge, 8, 1>(c, s);
-    return c.full ? steps<kSmall, 4, 3>(c, s) : steps<kSmall, 4, 1>(c, s);
+    return c.full ? steps<3>(c, s) : steps<1>(c, s);
 }
 
 }  // namespace darb
