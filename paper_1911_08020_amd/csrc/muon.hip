@@ -58,7 +58,7 @@ struct Places {
 // Matrices are cut into blocks of 16 rows by kDepth columns (1 KB), row of blocks by row of blocks: a
 // wave's load to LDS takes one block as it lies.  In a block, the 16-byte pieces of a row are moved
 // so that the rows that a read of LDS takes together use different banks.
-__device__ __forceinline__ int piece(int row, int k) { return k ^ ((row >> 1 & 3) ^ (row >> 3 & 1)); }
+__device__ __forceinline__ int piece(int row, int k) { return k ^ (4 - (row >> 2) & 3); }
 __device__ __forceinline__ int64_t place_of(int row, int col, int cols) {
     return (int64_t(row >> 4) * (cols / kDepth) + col / kDepth) * (16 * kDepth) + (row & 15) * kDepth +
            piece(row & 15, col % kDepth / 8) * 8 + col % 8;
@@ -270,6 +270,12 @@ __host__ __device__ __forceinline__ int tiles_of(const MuonTensor &t, int mode, 
     return mode == kGram || mode == kSquare ? a * (a + 1) / 2 : a * ((t.n + cols - 1) / cols);
 }
 
+// The first and the number of the tiles, of n of the i-th matrix, that an XCD takes.
+__host__ __device__ __forceinline__ int2 share_of(int n, int xcd, int i) {
+    const int x = (xcd + 3 * i) % 8, first = int(int64_t(n) * x / 8);
+    return {first, int(int64_t(n) * (x + 1) / 8) - first};
+}
+
 // 16 bytes from each lane's address to LDS, lane after lane from `to` (the same in all lanes).
 // In assembly: behind the builtin the compiler lets every read of LDS wait for all such loads,
 // those of the other buffer among them (2.1 us a stage of 256 x 256 then).  It has no result in
@@ -280,9 +286,9 @@ __device__ __forceinline__ void load_lds(const half_t *from, half_t *to) {
                  :: "v"(from), "s"(__builtin_amdgcn_readfirstlane(int(place))) : "memory");
 }
 
-// The workgroup's loads to LDS are there, and its reads of LDS are done.
-__device__ __forceinline__ void arrived() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// The workgroup's loads to LDS but each wave's last LEFT ones are there, its reads of LDS are done.
+template <int LEFT> __device__ __forceinline__ void arrived() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 
 // Lane q of four holds a column's rows 0 ... 3; afterwards row q's columns 0 ... 3.
@@ -302,26 +308,33 @@ __device__ __forceinline__ void turn4(uint32_t (&v)[4]) {
     swap(v[1], v[3], two, x2);
 }
 
-// C tiles of TM x TN by WR x WC waves.
-template <int TM, int TN, int WR, int WC, int PRODUCTS, int MODE>
+// C tiles of TM x TN by WR x WC waves, BUFS stages of them in LDS or on their way there.
+template <int TM, int TN, int WR, int WC, int BUFS, int PRODUCTS, int MODE>
 __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *__restrict__ call, int step,
-                                                                int first_block, int blocks) {
+                                                                int first_block) {
     constexpr int kParts = PRODUCTS == 1 ? 1 : 2, kWaves = WR * WC;
     constexpr int kRows = TM / WR / 16, kCols = TN / WC / 16;                       // 16 x 16 tiles of a wave
     constexpr int kBlocks = (TM + TN) / 16, kBlock = 16 * kDepth;                   // of a stage, P's first
     constexpr bool kTriangle = MODE == kGram || MODE == kSquare;
+    constexpr int kLoads = (kBlocks + kWaves - 1) / kWaves * kParts;                // of a wave, a stage
     static_assert(!kTriangle || TM == TN, "the diagonal runs through whole tiles");
-    __shared__ __attribute__((aligned(16))) half_t lds[2][kParts][kBlocks * kBlock];
+    static_assert(BUFS == 2 || kBlocks % kWaves == 0, "waiting counts the loads of each wave");
+    static_assert((BUFS - 1) * kLoads < 64, "what s_waitcnt counts");
+    __shared__ __attribute__((aligned(16))) half_t lds[BUFS][kParts][kBlocks * kBlock];
     const MuonCall &c = *call;
 
-    // neighbouring tiles on one XCD, the longest products first
-    const int b = first_block + int(blockIdx.x), share = blocks / 8, rest = blocks % 8, xcd = b % 8;
-    int id = (xcd < rest ? xcd * (share + 1) : rest + xcd * share) + b / 8, which = 0;
-    for (int i = 0;; ++i) {
+    // the longest products first; of each matrix a share of neighbouring tiles on one XCD
+    const int b = first_block + int(blockIdx.x), xcd = b % 8;
+    int id = b / 8, which = 0, i = 0;
+    for (;; ++i) {
+        if (i == c.count) return;                           // this XCD's shares are fewer
         which = c.order[MODE == kGram][i];
-        const int n = tiles_of(c.t[which], MODE, TM, TN);
-        if (id < n) break;
-        id -= n;
+        const int2 part = share_of(tiles_of(c.t[which], MODE, TM, TN), xcd, i);
+        if (id < part.y) {
+            id += part.x;
+            break;
+        }
+        id -= part.y;
     }
     const MuonTensor &t = c.t[which];
     half_t *base = matrices(c, t);
@@ -376,8 +389,11 @@ __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *
     for (int i = 0; i < kRows; ++i)
 #pragma unroll
         for (int j = 0; j < kCols; ++j) acc[i][j] = Float4{0.0f, 0.0f, 0.0f, 0.0f};
-    int buffer = 0, k = 0;
-    Half8 qh_[kCols], ql_[kCols], hi, lo;
+    // Rows are read two steps ahead, columns a stage: the barrier stands before the last two rows'
+    // products, beside which the next stage's first reads run.
+    constexpr int kAhead = 2;
+    static_assert(kRows >= kAhead, "rows ahead");
+    Half8 qh_[kCols], ql_[kCols], hi[kAhead], lo[kAhead];
     auto columns = [&](int buffer) {
 #pragma unroll
         for (int j = 0; j < kCols; ++j) {
@@ -386,30 +402,37 @@ __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *
         }
     };
     auto rows = [&](int buffer, int i) {
-        hi = part_of(buffer, 0, wr + i * 16);
-        if (kParts == 2) lo = part_of(buffer, 1, wr + i * 16);
+        hi[i % kAhead] = part_of(buffer, 0, wr + i * 16);
+        if (kParts == 2) lo[i % kAhead] = part_of(buffer, 1, wr + i * 16);
     };
-    fetch(0, k);
-    arrived();
-    if (k + kDepth < K) fetch(1, k + kDepth);
+    // behind the last stage that one is loaded again, so that the loads on their way stay as many
+#pragma unroll
+    for (int q = 0; q < BUFS; ++q) fetch(q, q * kDepth < K ? q * kDepth : K - kDepth);
+    arrived<(BUFS - 1) * kLoads>();
     columns(0);
-    rows(0, 0);
-    for (; k < K; k += kDepth, buffer ^= 1) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) rows(0, i);
+    int buffer = 0;
+    for (int k = 0; k < K; k += kDepth) {
+        const int next = buffer + 1 == BUFS ? 0 : buffer + 1;
+        Half8 ch[kCols], cl[kCols];
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) ch[j] = qh_[j], cl[j] = ql_[j];
+        Half8 nh[kAhead], nl[kAhead];                       // the next stage's first rows
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const Half8 h = hi, l = lo;
-            Half8 ch[kCols], cl[kCols];
+            const Half8 h = hi[i % kAhead], l = lo[i % kAhead];
+            if (i + kAhead < kRows) {
+                rows(buffer, i + kAhead);
+            } else if (i + kAhead == kRows && k + kDepth < K) {
+                arrived<(BUFS - 2) * kLoads>();
+                fetch(buffer, k + BUFS * kDepth < K ? k + BUFS * kDepth : K - kDepth);
+                columns(next);
 #pragma unroll
-            for (int j = 0; j < kCols; ++j) ch[j] = qh_[j], cl[j] = ql_[j];
-            if (i + 1 < kRows) {
-                rows(buffer, i + 1);
-            } else if (k + kDepth < K) {
-                // The last rows of this stage are in registers: the next stage's first reads and
-                // the loads of the one after it run beside their products.
-                arrived();
-                if (k + 2 * kDepth < K) fetch(buffer, k + 2 * kDepth);
-                columns(buffer ^ 1);
-                rows(buffer ^ 1, 0);
+                for (int r = 0; r < kAhead; ++r) {
+                    nh[r] = part_of(next, 0, wr + r * 16);
+                    if (kParts == 2) nl[r] = part_of(next, 1, wr + r * 16);
+                }
             }
 #pragma unroll
             for (int j = 0; j < kCols; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(h, ch[j], acc[i][j], 0, 0, 0);
@@ -422,7 +445,11 @@ __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *
                     acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(l, ch[j], acc[i][j], 0, 0, 0);
             }
         }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) hi[i] = nh[i], lo[i] = nl[i];
+        buffer = next;
     }
+    arrived<0>();                                           // loads to LDS end before the workgroup does
     // A lane holds rows 4 (l / 16) to + 3 of column l % 16 of each 16 x 16 tile, and after turn4
     // columns 4 (l % 16 / 4) to + 3 of row 4 (l / 16) + l % 4.
     const int r0 = ti * TM + wr + (lane >> 4) * 4, c0 = tj * TN + wc + (lane & 15);
@@ -520,7 +547,7 @@ struct Tile {
     int rows, cols;
     float rate;
 };
-constexpr Tile kTiles[] = {{256, 256, 1.0f}, {256, 192, 0.95f}, {192, 192, 0.92f}, {128, 128, 0.75f}, {64, 64, 0.3f}};
+constexpr Tile kTiles[] = {{256, 256, 1.0f}, {256, 192, 0.9f}, {192, 192, 0.87f}, {128, 128, 0.8f}, {64, 64, 0.5f}};
 constexpr int kTileKinds = 5;
 constexpr int kUnits = 256;             // compute units
 
@@ -555,24 +582,30 @@ int tile_of(const MuonCall &c, int mode) {
     return best;
 }
 
-template <int TM, int TN, int WR, int WC, int PRODUCTS, int MODE>
+template <int TM, int TN, int WR, int WC, int BUFS, int PRODUCTS, int MODE>
 hipError_t product(const MuonCall &c, int step, hipStream_t s) {
-    int blocks = 0;
-    for (int i = 0; i < c.count; ++i) blocks += tiles_of(c.t[i], MODE, TM, TN);
-    return over_blocks(blocks, WR * WC * kWave, [&](int64_t first, unsigned n) {
-        hipLaunchKernelGGL((product_kernel<TM, TN, WR, WC, PRODUCTS, MODE>), dim3(n), dim3(WR * WC * kWave), 0, s,
-                           static_cast<const MuonCall *>(c.workspace), step, int(first), blocks);
+    int most = 0;
+    for (int xcd = 0; xcd < 8; ++xcd) {
+        int n = 0;
+        for (int i = 0; i < c.count; ++i) n += share_of(tiles_of(c.t[c.order[MODE == kGram][i]], MODE, TM, TN), xcd, i).y;
+        most = n > most ? n : most;
+    }
+    return over_blocks(8 * int64_t(most), WR * WC * kWave, [&](int64_t first, unsigned n) {
+        hipLaunchKernelGGL((product_kernel<TM, TN, WR, WC, BUFS, PRODUCTS, MODE>), dim3(n), dim3(WR * WC * kWave), 0, s,
+                           static_cast<const MuonCall *>(c.workspace), step, int(first));
     });
 }
 
 template <int PRODUCTS, int MODE> hipError_t product(const MuonCall &c, int kind, int step, hipStream_t s) {
-    if (kind == 0) return product<256, 256, 2, 4, PRODUCTS, MODE>(c, step, s);
+    // as many stages as LDS holds beside another workgroup of the smaller tiles
+    constexpr bool kOne = PRODUCTS == 1;
+    if (kind == 0) return product<256, 256, 2, 4, kOne ? 4 : 2, PRODUCTS, MODE>(c, step, s);
     if constexpr (MODE == kApply || MODE == kResult) {
-        if (kind == 1) return product<256, 192, 2, 4, PRODUCTS, MODE>(c, step, s);
+        if (kind == 1) return product<256, 192, 2, 4, 2, PRODUCTS, MODE>(c, step, s);
     }
-    if (kind == 2) return product<192, 192, 2, 2, PRODUCTS, MODE>(c, step, s);
-    if (kind == 3) return product<128, 128, 2, 2, PRODUCTS, MODE>(c, step, s);
-    return product<64, 64, 2, 2, PRODUCTS, MODE>(c, step, s);
+    if (kind == 2) return product<192, 192, 2, 4, kOne ? 4 : 3, PRODUCTS, MODE>(c, step, s);
+    if (kind == 3) return product<128, 128, 2, 2, kOne ? 4 : 2, PRODUCTS, MODE>(c, step, s);
+    return product<64, 64, 2, 2, 4, PRODUCTS, MODE>(c, step, s);
 }
 
 template <int PRODUCTS> hipError_t steps(const MuonCall &c, hipStream_t s) {
