@@ -724,7 +724,7 @@ int darb_muon_workspace(const darb_muon_tensor *tensors, int64_t count, int64_t 
 
 static int muon(const darb_muon_tensor *tensors, int64_t count, bool update, double lr, double momentum, int nesterov,
                 int steps, double eps, const float *grad_scale, void *workspace, int64_t workspace_bytes,
-                void *stream) {
+                void *stream, const int *kinds = nullptr) {
     if (steps < 1 || steps > 16) return fail(DARB_E_INVALID, "steps must be in [1, 16]");
     if (!(eps > 0.0) || !std::isfinite(eps)) return fail(DARB_E_INVALID, "eps must be finite and > 0");
     if (!(lr >= 0.0) || !std::isfinite(lr)) return fail(DARB_E_INVALID, "lr must be finite and >= 0");
@@ -748,6 +748,7 @@ static int muon(const darb_muon_tensor *tensors, int64_t count, bool update, dou
         c.eps = eps;
         c.grad_scale = grad_scale;
         c.workspace = workspace;
+        for (int i = 0; kinds && i < 3; ++i) c.kind[i] = int8_t(kinds[i]);
         return launched(launch_muon(c, static_cast<hipStream_t>(stream)), "orthogonalised update launch");
     });
 }
@@ -764,6 +765,16 @@ int darb_orthogonalize(const darb_muon_tensor *tensors, int64_t count, int steps
                        int64_t workspace_bytes, void *stream) {
     clear_error();
     return muon(tensors, count, false, 0.0, 0.0, 0, steps, eps, nullptr, workspace, workspace_bytes, stream);
+}
+
+int darb_test_orthogonalize(const darb_muon_tensor *tensors, int64_t count, int steps, double eps, void *workspace,
+                            int64_t workspace_bytes, int gram, int square, int apply, void *stream) {
+    clear_error();
+    const int kinds[3] = {gram, square, apply};
+    for (int k : kinds)
+        if (k < 0 || k > 4) return fail(DARB_E_INVALID, "unknown tiles");
+    if (gram == 1 || square == 1) return fail(DARB_E_INVALID, "tiles on the diagonal are square");
+    return muon(tensors, count, false, 0.0, 0.0, 0, steps, eps, nullptr, workspace, workspace_bytes, stream, kinds);
 }
 
 }  // extern "C"

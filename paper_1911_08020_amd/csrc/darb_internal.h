@@ -306,6 +306,7 @@ struct MuonCall {
     const float *grad_scale;
     void *workspace;
     uint8_t order[2][kMuonTensors];     // filled in: the tensors by m and by n
+    int8_t kind[3] = {-1, -1, -1};      // the tiles of A, of b A + c A A and of X; -1: by the sizes
 };
 // The bytes of `count` matrices' group; fills in what the launch needs.
 int64_t muon_group(MuonCall &c);
@@ -320,8 +321,12 @@ hipError_t launch_stream_copy(void *dst, const void *src, int64_t bytes, hipStre
 }  // namespace darb
 
 // What the tests reach from outside (no part of the ABI): launch_lstm_seq with its waiting
-// and its exchange chosen, a plan's lstm_chunks, and whether the LSTM layer's time steps
-// would run as one launch.
+// and its exchange chosen, a plan's lstm_chunks, whether the LSTM layer's time steps would run as
+// one launch, and darb_orthogonalize with the tiles of its products chosen (0 ... 4, where those of A
+// and b A + c A A are square ones: not 1).
+extern "C" int darb_test_orthogonalize(const darb_muon_tensor *tensors, int64_t count, int steps, double eps,
+                                       void *workspace, int64_t workspace_bytes, int gram, int square, int apply,
+                                       void *stream);
 extern "C" int darb_test_lstm_seq(const darb_plan *whh, int wdtype, const void *values,
                                   const uint8_t *offsets, int64_t H, int64_t T, int64_t batch,
                                   const float *U, float *scratch, float *h_seq, float *h,

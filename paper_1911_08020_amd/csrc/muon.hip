@@ -316,9 +316,8 @@ __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *
     constexpr int kRows = TM / WR / 16, kCols = TN / WC / 16;                       // 16 x 16 tiles of a wave
     constexpr int kBlocks = (TM + TN) / 16, kBlock = 16 * kDepth;                   // of a stage, P's first
     constexpr bool kTriangle = MODE == kGram || MODE == kSquare;
-    constexpr int kLoads = (kBlocks + kWaves - 1) / kWaves * kParts;                // of a wave, a stage
+    constexpr int kLoads = kBlocks / kWaves * kParts;       // of a wave, a stage, at least
     static_assert(!kTriangle || TM == TN, "the diagonal runs through whole tiles");
-    static_assert(BUFS == 2 || kBlocks % kWaves == 0, "waiting counts the loads of each wave");
     static_assert((BUFS - 1) * kLoads < 64, "what s_waitcnt counts");
     __shared__ __attribute__((aligned(16))) half_t lds[BUFS][kParts][kBlocks * kBlock];
     const MuonCall &c = *call;
@@ -609,7 +608,8 @@ template <int PRODUCTS, int MODE> hipError_t product(const MuonCall &c, int kind
 }
 
 template <int PRODUCTS> hipError_t steps(const MuonCall &c, hipStream_t s) {
-    const int gram = tile_of(c, kGram), square = tile_of(c, kSquare), apply = tile_of(c, kApply);
+    auto kind = [&](int mode) { return c.kind[mode] >= 0 ? c.kind[mode] : tile_of(c, mode); };
+    const int gram = kind(kGram), square = kind(kSquare), apply = kind(kApply);
     for (int k = 0; k < c.steps; ++k) {
         hipError_t e = product<PRODUCTS, kGram>(c, gram, k, s);
         if (e == hipSuccess) e = product<3, kSquare>(c, square, k, s);

@@ -110,6 +110,68 @@ def test_orthogonalize(darb, dtype, kind):
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
+def test_every_tile(darb, dtype):
+    """Each kind of tile that a product may go by, where tiles hang over, and where the sums are shorter
+    than the stages that are loaded ahead."""
+    import ctypes
+    P, I64, I = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
+    call = darb.lib().darb_test_orthogonalize
+    call.argtypes, call.restype = [P, I64, I, ctypes.c_double, P, I64, I, I, I, P], I
+    code = {"f32": 0, "f16": 1, "bf16": 2}[dtype]
+    shapes = [(64, 64), (70, 900), (290, 300), (520, 270), (400, 590), (333, 1100)]
+    mats = [torch.from_numpy(matrix(*s, "flat", 70 + i)).to(TYPES[dtype]).cuda() for i, s in enumerate(shapes)]
+    want = [exact(wide(g), 5, 1e-7) for g in mats]
+    limit = [bound(wide(g), 5, 1e-7, dtype == "f32") for g in mats]
+    for kinds in ((0, 0, 0), (2, 2, 1), (2, 2, 2), (3, 3, 3), (4, 4, 4), (4, 0, 1)):
+        for only in (None, 3):
+            table = (darb._MuonTensor * len(mats))()
+            out = [torch.empty_like(g) for g in mats]
+            chosen = [i for i in range(len(mats)) if only in (None, i)]
+            for j, i in enumerate(chosen):
+                r, c = shapes[i]
+                table[j] = darb._MuonTensor(out[i].data_ptr(), None, mats[i].data_ptr(), None, r, c, c, c, 1.0, 0.0, code, code)
+            n = ctypes.c_int64()
+            assert darb.lib().darb_muon_workspace(table, len(chosen), ctypes.byref(n)) == 0
+            # what the call does not write itself would show as NaN
+            ws = torch.full((n.value // 4,), math.nan, device="cuda")
+            for again in range(2):
+                say(dtype, kinds, only, again)
+                assert call(table, len(chosen), 5, 1e-7, ws.data_ptr(), n.value, *kinds,
+                            torch.cuda.current_stream().cuda_stream) == 0
+                for i in chosen:
+                    got = wide(out[i])
+                    off = np.linalg.norm(got - want[i])
+                    rounded = ROUND[dtype][0] * np.linalg.norm(want[i]) + ROUND[dtype][1] * math.sqrt(got.size)
+                    assert off <= limit[i] + rounded, (kinds, shapes[i], off, limit[i])
+                    # no element is off by itself: a product's error is spread over a row and a column
+                    worst = np.abs(got - want[i]).max()
+                    assert worst <= 0.02 + ROUND[dtype][0] * np.abs(want[i]).max(), (kinds, shapes[i], worst)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_large(darb, dtype):
+    """Sizes that the rules give each kind of tile, against the steps in 64 bits."""
+    for rows, cols in ((1536, 4608), (2048, 2048), (4100, 1000)):
+        g = torch.randn(rows, cols, device="cuda", dtype=torch.float32).to(TYPES[dtype])
+        x = g.double()
+        x = x / (x.norm() + 1e-7)
+        x = x if rows <= cols else x.t().contiguous()
+        for _ in range(5):
+            a = x @ x.t()
+            x = A * x + (B * a + C * (a @ a)) @ x
+        x = x if rows <= cols else x.t()
+        for again in range(3):
+            got = darb.orthogonalize(g).double()
+            off = float((got - x).norm() / x.norm())
+            say(dtype, rows, cols, off)
+            # fp32: 22 bits an operand, sums of up to 4608 terms, stretched by less than 3.4445 a step while
+            # values are small: 2^-22 sqrt(3) 5 3.5; 16 bits: as the call's documentation has it, and its rounding
+            assert off <= (2.0 ** -22 * 31 if dtype == "f32" else 3e-3 + ROUND[dtype][0])
+            assert float((got - x).abs().max()) <= 40 * off * float(x.square().mean().sqrt()) + 1e-6 + \
+                ROUND[dtype][0] * float(x.abs().max())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
 def test_what_it_does(darb, dtype):
     """Singular values from 0.01 of the norm up land between 0.68 and 1.21, the vectors stay."""
     r = np.random.default_rng(2)
