@@ -141,7 +141,8 @@ template <typename F> int over_tensors(const darb_adamw &a, int64_t most, F &&f)
 }
 
 // Whether the result's own type asks for products as accurate as fp32.  Those of small matrices are,
-// whatever the type: in fp16 the sums of few terms are further off, and they take no longer.
+// whatever the type: with single products their results are up to 6 10^-3 of the norm off (3 10^-3 from
+// 64 on).  16 matrices of 48 x 48 take 127 us so instead of 123, of 48 x 2000 241 instead of 192.
 bool muon_full(const darb_muon_tensor &t) {
     return t.dtype == DARB_F32 || t.master || (t.rows < t.cols ? t.rows : t.cols) < 64;
 }

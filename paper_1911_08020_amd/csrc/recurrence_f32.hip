@@ -8,10 +8,7 @@ hipError_t launch_recurrence_bf16(const RecurrenceCall &c, hipStream_t s);
 
 int64_t recurrence_workspace_bytes(int dtype, bool back, bool rows, int64_t H, int64_t T, int64_t batch) {
     const int size = dtype == DARB_F32 ? 4 : 2;
-    const int V = size == 4 ? (back ? kV<float, true> : kV<float, false>)
-                            : (back ? kV<half_t, true> : kV<half_t, false>);
-    const int C = size == 4 ? (back ? kSteps<float, true> : kSteps<float, false>)
-                            : (back ? kSteps<half_t, true> : kSteps<half_t, false>);
+    const int V = kVector, C = back ? kSteps<true> : kSteps<false>;
     const Cut k = cut_of(V, C, size, rows, T, rows ? H : batch, rows ? batch : H);
     if (k.slabs == 1) return 0;
     const int64_t series = H * batch;

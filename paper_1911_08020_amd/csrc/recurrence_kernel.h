@@ -13,15 +13,22 @@
 //
 // Element (o, t, i) lies at o * so + t * st + i: features x columns with the columns contiguous
 // has a feature per o and a sequence per i, with the features contiguous the reverse.  A thread
-// takes kV series that lie side by side over kSteps steps, whose maps it holds in registers from
-// one read; the workgroup's 256 threads are `lanes` such groups by 256 / lanes chunks of time.
-// Chunks are joined by shuffles inside a wave and through LDS between waves, and the workgroup
-// goes on to the next steps with the state it has reached.  Few series cannot fill the device so:
-// time is then cut into slabs, a first launch writes each slab's map and a second one starts each
-// slab from the maps before it (inputs read twice).  Feature-major rows of few sequences would
-// be read in short pieces; such rows are staged whole through LDS.
+// takes V series that lie side by side over C steps, whose maps it holds in registers from one read
+// (V C = 16 forward, 8 for the gradients, which hold four values an element; at twice that registers
+// spill: 15.6 -> 16.9 us and 35.5 -> 45.6 in the case below); the workgroup's 256 threads are `lanes`
+// such groups by 256 / lanes chunks of time.  Chunks are joined by shuffles inside a wave and through
+// LDS between waves, and the workgroup goes on to the next steps with the state it has reached.  Few
+// series cannot fill the device so: time is then cut into slabs, a first launch writes each slab's
+// map and a second one starts each slab from the maps before it (inputs read twice).  Feature-major
+// rows of few sequences would be read in short pieces; such rows are staged whole through LDS, or,
+// one sequence's, read in vectors along time, a chunk a vector.
 //
-// Memory-bound: forward 3 arrays, gradients 6 (5).
+// Memory-bound: forward 3 arrays, gradients 6 (linear form 5).  Measured on MI355X: 200 steps of 32
+// sequences of 1024 fp32 features 15.6 us (5.1 TB/s), gradients 35.5 (4.4 TB/s: a tile's loads are not
+// under way while the one before is joined, and registers leave four waves a SIMD); 65536 steps of
+// 1024 bf16 features of one sequence, with restarts, 177 us (the inputs read twice 3.8 TB/s: each
+// slab's tiles follow one another); gradients of 1500 fp16 rows of 2999 steps, linear form, 14.6 us
+// (3.1 TB/s: rows of 1.5 tiles).
 #pragma once
 
 #include "darb_internal.h"
@@ -58,7 +65,7 @@ struct Args {
     const uint8_t *resets;
     int64_t rt, ro, ri;                 // its strides
     int64_t T, W, O;
-    int64_t groups;                     // groups of kV series
+    int64_t groups;                     // groups of V series
     int lanes;                          // groups of a workgroup, a power of two
     int slabs;
     int64_t slab_steps;
@@ -147,7 +154,6 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
     const int64_t o = STAGED || ALONG ? block : group / per;
     const int64_t i = STAGED || ALONG ? g : (group - o * per) * V;
     const bool mine = STAGED || ALONG ? g < k.W : block * lanes + g < k.groups;
-    const int n = mine ? V : 0;                             // the thread's series
     // the thread's series at step 0
     auto series_of = [&](const Operand &q) { return static_cast<const T *>(q.p) + o * q.so + i; };
     const bool first_launch = k.maps && !k.out.p;           // only the slabs' maps
@@ -179,7 +185,7 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
             }
         }
     }
-    Map<V, RESETS> all;                                             // first launch: the slab's map
+    Map<V, RESETS> all;                                     // first launch: the slab's map
     all.none();
 
     const int64_t tile = int64_t(chunks) * C;
@@ -223,7 +229,7 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
             const int p = p0 + j < tsteps ? p0 + j : tsteps - 1;
             return BACK ? tsteps - 1 - p : p;
         };
-        const int live = n > 0 ? tsteps - p0 : 0;           // steps j < live are the thread's
+        const int live = mine ? tsteps - p0 : 0;           // steps j < live are the thread's
         float f[C][V], b[C][V], u[BACK && GATE ? C : 1][V]; // f, what a step adds or dh, 1 - f
         Raw<T, V> y[BACK ? C : 1], xs[BACK && GATE ? C : 1];
         float y0[BACK ? V : 1];                             // the state before the first step
@@ -408,16 +414,16 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Args k) {
                 if (lane >= lanes) before = up;
             }
             __syncthreads();
-            const int apart = lanes <= kWave ? 1 : lanes / kWave, mine = lanes < kWave ? kWave - lanes + g : lane;
+            const int apart = lanes <= kWave ? 1 : lanes / kWave, last = lanes < kWave ? kWave - lanes + g : lane;
             const int from = lanes <= kWave ? 0 : w & (apart - 1);
             for (int q = from; q < kWaves; q += apart) {
                 Map<V, RESETS> t;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    t.a[v] = total[turn][q][0][v][mine];
-                    t.b[v] = total[turn][q][1][v][mine];
+                    t.a[v] = total[turn][q][0][v][last];
+                    t.b[v] = total[turn][q][1][v][last];
                 }
-                t.cut = RESETS ? total_cut[turn][q][mine] : 0;
+                t.cut = RESETS ? total_cut[turn][q][last] : 0;
                 if (q == w) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) enter[v] = before.of(v, state[v]);
@@ -543,14 +549,16 @@ struct Cut {
     int64_t groups, slab_steps;
 };
 
-template <typename T, bool BACK> constexpr int kV = 2;
-template <typename T, bool BACK> constexpr int kSteps = BACK ? 4 : 8;
+constexpr int kVector = 2;              // series of a thread, where W is a multiple of it
+template <bool BACK> constexpr int kSteps = BACK ? 4 : 8;
 constexpr int kRowSteps = 8;
 
 inline Cut cut_of(int V, int C, int size, bool rows, int64_t T, int64_t W, int64_t O) {
     Cut k;
     if (W % V != 0) V = 1;
-    // feature-major rows that would be read in pieces of less than 64 bytes, unless they are short
+    // Feature-major rows that would be read in pieces of less than 64 bytes, unless they are short: 200
+    // steps of 1024 fp32 features, 8 sequences 7.5 us through LDS and 11.7 directly (gradients 12.3 and
+    // 16.2), 16 sequences 11.9 and 9.6 (18.5 and 17.3); 48 steps of 8 sequences 6.3 and 5.5.
     k.layout = rows || W * size >= 64 || T < 64 ? kDirect : W == 1 ? kAlong : kStaged;
     if (k.layout != kDirect) {
         V = 1;
@@ -568,9 +576,13 @@ inline Cut cut_of(int V, int C, int size, bool rows, int64_t T, int64_t W, int64
     k.vector = V;
     const int64_t blocks = k.layout != kDirect ? O : (k.groups + k.lanes - 1) / k.lanes;
     const int64_t tile = int64_t(kThreads / k.lanes) * C;
-    int64_t slabs = blocks < 512 ? (1024 + blocks - 1) / blocks : 1;
-    if (slabs > kSlabs) slabs = kSlabs;
     const int64_t tiles = (T + tile - 1) / tile;
+    // Slabs where workgroups are fewer than compute units and have more than a few tiles each, which
+    // the second launch and the second reading have to earn: 2048 steps of 1024 fp32 features, one
+    // sequence (32 workgroups) 34.4 -> 12.6 us, gradients 67.6 -> 18.8; four 36.1 -> 33.0, 70.8 -> 46.1;
+    // eight (256 workgroups) 38.2 -> 59.6, 101 -> 94.5.  256 rows of 4096 steps (two tiles) 6.3 -> 9.2.
+    int64_t slabs = blocks < 256 && tiles > 4 ? (1024 + blocks - 1) / blocks : 1;
+    if (slabs > kSlabs) slabs = kSlabs;
     if (slabs > tiles) slabs = tiles;
     k.slab_steps = (tiles + slabs - 1) / slabs * tile;
     k.slabs = int((T + k.slab_steps - 1) / k.slab_steps);
@@ -581,7 +593,7 @@ inline int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
 template <typename T, bool GATE, bool BACK>
 hipError_t launch(const RecurrenceCall &c, hipStream_t s) {
-    constexpr int V = kV<T, BACK>, C = kSteps<T, BACK>;
+    constexpr int V = kVector, C = kSteps<BACK>;
     const int64_t W = c.rows ? c.H : c.batch, O = c.rows ? c.batch : c.H;
     const Cut cut = cut_of(V, C, int(sizeof(T)), c.rows, c.T, W, O);
     auto stride = [&](const RecurrenceMatrix &m, int64_t &so, int64_t &st) {

@@ -788,8 +788,8 @@ class Muon:
         if len(grads) != count:
             raise ValueError(f"one gradient per tensor ({count}), got {len(grads)}")
         _require_cuda(self.params[0])
-        for i, (g, p, row) in enumerate(zip(grads, self.params, self._table)):
-            row.grad = None
+        table = type(self._table).from_buffer_copy(self._table)
+        for i, (g, p, row) in enumerate(zip(grads, self.params, table)):
             if g is None:
                 continue
             _require_cuda(g)
@@ -799,7 +799,7 @@ class Muon:
             row.ld_grad = _unit_columns(g, f"gradient {i}")
             row.grad = g.data_ptr()
         self._hold_on(stream)
-        _check(_lib.darb_muon_step(self._table, count, self.lr if lr is None else float(lr), self.momentum,
+        _check(_lib.darb_muon_step(table, count, self.lr if lr is None else float(lr), self.momentum,
                                    int(self.nesterov), self.ns_steps, self.eps,
                                    _optional(grad_scale, 1, "grad_scale"), _ptr(self.workspace),
                                    self.workspace.numel(), _stream_ptr(stream)), "darb_muon_step")

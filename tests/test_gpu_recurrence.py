@@ -74,6 +74,55 @@ def test_backward(darb, dtype, form, order):
                 check(wide(g), w, b, f"{label} {name}")
 
 
+@pytest.mark.parametrize("H,T,batch,order", [(3, 20000, 1, "features"), (2, 9001, 3, "features"), (5, 3001, 1, "tokens"),
+                                             (2, 2500, 7, "tokens"), (4, 3000, 20, "features")])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_sequences(darb, dtype, H, T, batch, order):
+    """Time cut into slabs in every layout, a matrix of odd width, and what a replay finds in its workspace."""
+    for form in ("gate", "linear"):
+        z, x, h0, starts, r = data(H, T, batch, form, True, T, dtype)
+        starts[:] = r.random(T * batch) < 0.002
+        want, last, bound, lbound = forward(z, x, h0, starts, batch, form)
+        say(dtype, H, T, batch, order, form)
+        for again in range(2):
+            args = dict(batch=batch, h0=state(h0, order), resets=on(starts), form=form)
+            h, hl = darb.gated_recurrence(place(z, order, dtype), place(x, order, dtype), **args)
+            check(wide(h), want, bound + rounding(np.abs(want) + bound, dtype), "h")
+            check(wide(hl), last, lbound + 2.0 ** -24 * np.abs(last), "last")
+        hr = torch.from_numpy(want).to(TYPES[dtype]).double().numpy()
+        dh = torch.from_numpy(r.normal(size=z.shape)).to(TYPES[dtype]).double().numpy()
+        dl = r.normal(size=h0.shape).astype(np.float32)
+        dz, dx, d0, bz, bx, b0 = backward(dh, z, x, hr, h0, dl, starts, batch, form)
+        got = darb.gated_recurrence_grad(place(dh, order, dtype), place(z, order, dtype), place(x, order, dtype),
+                                         place(hr, order, dtype), dh_last=state(dl, order), **args)
+        for g, w, b, name in zip(got, (dz, dx, d0), (bz, bx, b0), ("dgate", "dx", "dh0")):
+            check(wide(g), w, b + rounding(np.abs(w) + b, dtype if name != "dh0" else "f32"), name)
+
+
+def test_offsets_past_32_bits(darb):
+    """Columns of one buffer 2^32 bytes and more apart."""
+    far = (1 << 30) + 16                    # fp32 elements between steps
+    H, T = 64, 3
+    room = torch.empty((T - 1) * far + 3 * H, device="cuda")
+    z, x, h = (room[k * H:].as_strided((H, T), (1, far)) for k in range(3))
+    r = np.random.default_rng(0)
+    a, b = r.normal(size=(2, H, T)).astype(np.float32)
+    z.copy_(torch.from_numpy(a))
+    x.copy_(torch.from_numpy(b))
+    z0 = np.zeros((H, 1), np.float32)
+    want, want_last, bound, lbound = forward(a, b, z0, None, 1, "gate")
+    got, last = darb.gated_recurrence(z, x, h=h)
+    assert got is h
+    check(wide(h), want, bound + 2.0 ** -24 * np.abs(want), "h")
+    check(wide(last), want_last, lbound + 2.0 ** -24 * np.abs(want_last), "last")
+    assert torch.equal(z.cpu(), torch.from_numpy(a)) and torch.equal(x.cpu(), torch.from_numpy(b))
+    dz, dx, d0, bz, bx, b0 = backward(b, a, b, wide(h), z0, z0, None, 1, "gate")
+    got = darb.gated_recurrence_grad(x, z, x, h, dgate=z, dx=x)
+    assert got[0] is z and got[1] is x
+    for g, w, e, name in zip(got, (dz, dx, d0), (bz, bx, b0), ("dgate", "dx", "dh0")):
+        check(wide(g), w, e + 2.0 ** -24 * np.abs(w), name)
+
+
 @pytest.mark.parametrize("form", ["gate", "linear"])
 def test_gradients_against_differences(darb, form):
     """Central differences of the definition in 64 bits: off by about the step squared."""
