@@ -23,6 +23,14 @@ Evaluating and retraining a layer (``training``; activations are [features, batc
     opt = AdamW([values, ...], lr=1e-3, state_bits=8)
     opt.step([dvalues, ...])
 
+Training a recurrent model around it:
+
+    h, state = gated_recurrence(gate, x, batch=B, h0=state)       # and gated_recurrence_grad
+    loss = policy_loss(lp.logprob, old, advantage)                # or preference_loss
+    dY = token_logprobs_grad(Y, targets, lp.lse, loss.grad_logprob)
+    muon = Muon([W, ...], lr=0.02)                                # dense matrices; orthogonalize
+    muon.step([dW, ...])
+
 The library must have been built (``python paper_1911_08020_amd/build.py`` or
 ``__graft_entry__.build()``); importing this package fails loudly otherwise.
 """
@@ -48,7 +56,7 @@ E_WORKSPACE = -6
 
 F32 = 0
 F16 = 1
-BF16 = 2                # logits, layer norm, parameters and gradients only
+BF16 = 2                # logits, layer norm, recurrence, parameters and gradients only
 ROUND_FLOOR = 0
 ROUND_PAPER = 1
 
