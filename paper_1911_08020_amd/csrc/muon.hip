@@ -30,7 +30,7 @@
 // (2.1 on zeros: it is the power).  Measured on MI355X: 4096 x 9216 in fp32 7.1 ms (1.1 10^15; X's
 // product 1.2, A's 1.1, A A's 1.0); the eight matrices of a 1500-wide model with its momentum's update,
 // fp32 masters of bf16, 4.4 ms (0.4 of it momentum, norm, first X and parameters, at 5 TB/s); eight
-// bf16 matrices of 256 x 1024 164 us (17 launches of 6 to 12 us: a tile's 32 stages one after
+// bf16 matrices of 256 x 1024 147 us (17 launches of 6 to 10 us: a tile's 32 stages one after
 // another).  Equal shares of all stages for each workgroup, cut tiles finished by the last to come,
 // took 11.9 ms, 10.4 ms and 377 us: workgroups at unlike places of their sums share nothing in L2.
 #include "darb_internal.h"
@@ -174,6 +174,15 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(MuonCall c) {
     }
 }
 
+// What the workgroups of a launch look for their matrix in.  It travels with the launch: out of the
+// call in memory each matrix on the way costs a load that the next one waits for (eight matrices of
+// 256 x 1024: 164 us instead of 147).
+struct Shares {
+    int count;
+    int tiles[kMuonTensors];
+    uint8_t which[kMuonTensors];
+};
+
 // ---- X of the first step ---------------------------------------------------------------
 
 struct Split {
@@ -192,28 +201,15 @@ __host__ __device__ __forceinline__ int cut_tiles(const MuonTensor &t) {
     return ((t.m + kCutTile - 1) / kCutTile) * ((t.n + kCutTile - 1) / kCutTile);
 }
 
-__global__ __launch_bounds__(256) void cut_kernel(const MuonCall *__restrict__ call, int first_block) {
+__global__ __launch_bounds__(256) void cut_kernel(const MuonCall *__restrict__ call, int first_block, Shares shares) {
     const MuonCall &c = *call;
     __shared__ float tile[kCutTile][kCutTile + 1];
     __shared__ double room[256 / kWave];
     int block = first_block + int(blockIdx.x), which = 0;
-    for (;; ++which) {
-        const int blocks = cut_tiles(c.t[which]);
-        if (block < blocks) break;
-        block -= blocks;
-    }
+    for (; which + 1 < shares.count && block >= shares.tiles[which]; ++which) block -= shares.tiles[which];
     const MuonTensor &t = c.t[which];
     const int tid = int(threadIdx.x), R = padded_rows(t), C = padded_cols(t);
     const int across = (C + kCutTile - 1) / kCutTile, r0 = block / across * kCutTile, c0 = block % across * kCutTile;
-    double sum = 0.0;
-    for (int i = tid; i < norm_blocks(t); i += 256) sum += norms(c, which)[i];
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
-    if (lane_id() == 0) room[wave_id()] = sum;
-    __syncthreads();
-    sum = 0.0;
-    for (int w = 0; w < 256 / kWave; ++w) sum += room[w];
-    const double inverse = double(kScaleX) / (sqrt(sum) + c.eps);
     const float gs = c.grad_scale ? *c.grad_scale : 1.0f;
     half_t *base = matrices(c, t);
     const Places at(t);
@@ -232,6 +228,16 @@ __global__ __launch_bounds__(256) void cut_kernel(const MuonCall *__restrict__ c
             if (t.momentum) load4(DARB_F32, t.momentum, int64_t(r) * t.cols + q, some, m[k]);
         }
     }
+    // the norm, beside those loads
+    double sum = 0.0;
+    for (int i = tid; i < norm_blocks(t); i += 256) sum += norms(c, which)[i];
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
+    if (lane_id() == 0) room[wave_id()] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < 256 / kWave; ++w) sum += room[w];
+    const double inverse = double(kScaleX) / (sqrt(sum) + c.eps);
 #pragma unroll
     for (int k = 0; k < kCutTile / 16; ++k) {
         const int row = k * 16 + tid / 16;
@@ -279,10 +285,10 @@ __host__ __device__ __forceinline__ int tiles_of(const MuonTensor &t, int mode, 
     return mode == kGram || mode == kSquare ? a * (a + 1) / 2 : a * ((t.n + cols - 1) / cols);
 }
 
-// The first and the number of the tiles, of n of the i-th matrix, that an XCD takes.
-__host__ __device__ __forceinline__ int2 share_of(int n, int xcd, int i) {
-    const int x = (xcd + 3 * i) % 8, first = int(int64_t(n) * x / 8);
-    return {first, int(int64_t(n) * (x + 1) / 8) - first};
+// The first and the number of the tiles, of n (below 2^29) of the i-th matrix, that an XCD takes.
+__host__ __device__ __forceinline__ int2 share_of(uint32_t n, int xcd, int i) {
+    const uint32_t x = uint32_t(xcd + 3 * i) % 8, first = n * x / 8;
+    return {int(first), int(n * (x + 1) / 8 - first)};
 }
 
 // 16 bytes from each lane's address to LDS, lane after lane from `to` (the same in all lanes).
@@ -320,7 +326,7 @@ __device__ __forceinline__ void turn4(uint32_t (&v)[4]) {
 // C tiles of TM x TN by WR x WC waves, BUFS stages of them in LDS or on their way there.
 template <int TM, int TN, int WR, int WC, int BUFS, int PRODUCTS, int MODE>
 __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *__restrict__ call, int step,
-                                                                int first_block) {
+                                                                int first_block, Shares shares) {
     constexpr int kParts = PRODUCTS == 1 ? 1 : 2, kWaves = WR * WC;
     constexpr int kRows = TM / WR / 16, kCols = TN / WC / 16;                       // 16 x 16 tiles of a wave
     constexpr int kBlocks = (TM + TN) / 16, kBlock = 16 * kDepth;                   // of a stage, P's first
@@ -333,17 +339,17 @@ __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *
 
     // the longest products first; of each matrix a share of neighbouring tiles on one XCD
     const int b = first_block + int(blockIdx.x), xcd = b % 8;
-    int id = b / 8, which = 0, i = 0;
-    for (;; ++i) {
-        if (i == c.count) return;                           // this XCD's shares are fewer
-        which = c.order[MODE == kGram][i];
-        const int2 part = share_of(tiles_of(c.t[which], MODE, TM, TN), xcd, i);
+    int id = b / 8, which = -1;
+    for (int i = 0; i < shares.count; ++i) {
+        const int2 part = share_of(shares.tiles[i], xcd, i);
         if (id < part.y) {
+            which = shares.which[i];
             id += part.x;
             break;
         }
         id -= part.y;
     }
+    if (which < 0) return;                                  // this XCD's shares are fewer
     const MuonTensor &t = c.t[which];
     half_t *base = matrices(c, t);
     const Places place(t);
@@ -555,7 +561,7 @@ __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *
 //                          64: 610 274 1192
 //   four of 1500 x 1500, four of 1500 x 6000, fp32 masters
 //                          256: 387 134 459   192: 259 157 454   128: 258 124 466
-//   eight of 256 x 1024 bf16   256: 33 30 28   192: 22 20 19   128: 17 17 15   64: 11 7 10
+//   eight of 256 x 1024 bf16   256: 33 30 28   192: 22 20 19   128: 17 17 15   64: 10 7 10
 struct Tile {
     int rows, cols;
     float rate;
@@ -597,15 +603,21 @@ int tile_of(const MuonCall &c, int mode) {
 
 template <int TM, int TN, int WR, int WC, int BUFS, int PRODUCTS, int MODE>
 hipError_t product(const MuonCall &c, int step, hipStream_t s) {
+    Shares shares{};
+    shares.count = c.count;
+    for (int i = 0; i < c.count; ++i) {
+        shares.which[i] = c.order[MODE == kGram][i];
+        shares.tiles[i] = tiles_of(c.t[shares.which[i]], MODE, TM, TN);
+    }
     int most = 0;
     for (int xcd = 0; xcd < 8; ++xcd) {
         int n = 0;
-        for (int i = 0; i < c.count; ++i) n += share_of(tiles_of(c.t[c.order[MODE == kGram][i]], MODE, TM, TN), xcd, i).y;
+        for (int i = 0; i < c.count; ++i) n += share_of(shares.tiles[i], xcd, i).y;
         most = n > most ? n : most;
     }
     return over_blocks(8 * int64_t(most), WR * WC * kWave, [&](int64_t first, unsigned n) {
         hipLaunchKernelGGL((product_kernel<TM, TN, WR, WC, BUFS, PRODUCTS, MODE>), dim3(n), dim3(WR * WC * kWave), 0, s,
-                           static_cast<const MuonCall *>(c.workspace), step, int(first));
+                           static_cast<const MuonCall *>(c.workspace), step, int(first), shares);
     });
 }
 
@@ -660,17 +672,20 @@ int64_t muon_group(MuonCall &c) {
 
 hipError_t launch_muon(const MuonCall &c, hipStream_t s) {
     int most = 0, cuts = 0;
+    Shares shares{};
+    shares.count = c.count;
     for (int i = 0; i < c.count; ++i) {
+        shares.tiles[i] = cut_tiles(c.t[i]);
         const int n = norm_blocks(c.t[i]);
         most = n > most ? n : most;
-        cuts += cut_tiles(c.t[i]);
+        cuts += shares.tiles[i];
     }
     hipLaunchKernelGGL(norm_kernel, dim3(most, c.count), dim3(kNormThreads), 0, s, c);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     e = over_blocks(cuts, 256, [&](int64_t first, unsigned n) {
         hipLaunchKernelGGL(cut_kernel, dim3(n), dim3(256), 0, s,
-                           static_cast<const MuonCall *>(c.workspace), int(first));
+                           static_cast<const MuonCall *>(c.workspace), int(first), shares);
     });
     if (e != hipSuccess) return e;
     return c.full ? steps<3>(c, s) : steps<1>(c, s);
