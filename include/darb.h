@@ -661,7 +661,9 @@ int darb_preference_loss(int64_t pairs, int64_t B, const float *logprob, const f
  *   m = momentum m + (1 - momentum) g,  u = momentum m + (1 - momentum) g  (nesterov; else m)
  *   p = p (1 - lr decay) - lr scale X.
  * Sums and m are fp32 or more.  An fp32 result (or master) is as accurate as fp32 products make
- * it; one of 16 bits has its products in fp16 (X itself in more), off by 1 to 3 10^-3 of its norm.
+ * it; one of 16 bits has its products in fp16 (X itself in more; all as for fp32 where a side is below
+ * 64), off by 1 to 3 10^-3 of its norm.  The same call gives the same bits; a matrix together with
+ * others may differ from it alone in how its sums are rounded.
  * A matrix that holds an infinity or NaN becomes NaN; zeros stay zeros.
  *   dtype, gdtype   DARB_F32, DARB_F16 or DARB_BF16, of param and of grad
  *   param       device [rows x cols], unit column stride, leading dimension ld_param >= cols
