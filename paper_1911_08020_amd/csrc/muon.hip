@@ -294,12 +294,17 @@ __host__ __device__ __forceinline__ int2 share_of(uint32_t n, int xcd, int i) {
 // 16 bytes from each lane's address to LDS, lane after lane from `to` (the same in all lanes).
 // In assembly: behind the builtin the compiler lets every read of LDS wait for all such loads,
 // those of the other buffer among them (2.1 us a stage of 256 x 256 then).  It has no result in
-// registers; `arrived` waits for it.  (Nothing else of these kernels uses m0.)
+// registers; `arrived` waits for it.  The load may read M0 only one wait state after it is written,
+// which the compiler looks after for the builtin but not inside of assembly: hence the s_nop.  M0
+// is listed as written, which a reserved register is warned of.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds(const half_t *from, half_t *to) {
     const uint32_t place = uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) half_t *)to));
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off"
-                 :: "v"(from), "s"(__builtin_amdgcn_readfirstlane(int(place))) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+                 :: "v"(from), "s"(__builtin_amdgcn_readfirstlane(int(place))) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // The workgroup's loads to LDS but each wave's last LEFT ones are there, its reads of LDS are done.
 template <int LEFT> __device__ __forceinline__ void arrived() {
