@@ -660,10 +660,9 @@ int darb_preference_loss(int64_t pairs, int64_t B, const float *logprob, const f
  * darb_orthogonalize writes that X of each matrix; darb_muon_step makes one optimizer step with
  *   m = momentum m + (1 - momentum) g,  u = momentum m + (1 - momentum) g  (nesterov; else m)
  *   p = p (1 - lr decay) - lr scale X.
- * Sums and m are fp32 or more.  An fp32 result (or master) is as accurate as fp32 products make
- * it; one of 16 bits has its products in fp16 (X itself in more; all as for fp32 where a side is below
- * 64), off by 1 to 3 10^-3 of its norm.  The same call gives the same bits; a matrix together with
- * others may differ from it alone in how its sums are rounded.
+ * Sums and m are fp32 or more.  A result is as accurate as fp32 products make it, whatever its type,
+ * and rounded to that type once.  The same call gives the same bits; a matrix together with others
+ * may differ from it alone in how its sums are rounded.
  * A matrix that holds an infinity or NaN becomes NaN; zeros stay zeros.
  *   dtype, gdtype   DARB_F32, DARB_F16 or DARB_BF16, of param and of grad
  *   param       device [rows x cols], unit column stride, leading dimension ld_param >= cols
@@ -674,6 +673,10 @@ int darb_preference_loss(int64_t pairs, int64_t B, const float *logprob, const f
  *               NULL (darb_muon_step): the tensor is left as it is
  *   momentum    device fp32 [rows x cols], contiguous (darb_orthogonalize: NULL)
  *   scale, decay  finite, decay >= 0
+ *   fp16_products   0; or 1: a result of 16 bits (without a master) may take its products from
+ *               operands of fp16, in less time: it is off by 1 to 3 10^-3 of its norm before it is
+ *               rounded.  Without effect on other results, and where a side is below 64.
+ *   reserved    0
  *   rows, cols  1 <= rows, cols < 2^20
  *   tensors     host array of `count` >= 1, read during the call; no memory overlaps
  *   steps       1 ... 16;  momentum in [0, 1), lr >= 0, eps > 0 (finite)
@@ -690,6 +693,7 @@ typedef struct {
     int64_t rows, cols, ld_param, ld_grad;
     double scale, decay;
     int32_t dtype, gdtype;
+    int32_t fp16_products, reserved;
 } darb_muon_tensor;
 
 int darb_muon_workspace(const darb_muon_tensor *tensors, int64_t count, int64_t *bytes);

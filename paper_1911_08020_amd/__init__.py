@@ -99,7 +99,8 @@ class _MuonTensor(ctypes.Structure):
                 ("momentum", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
                 ("ld_param", ctypes.c_int64), ("ld_grad", ctypes.c_int64),
                 ("scale", ctypes.c_double), ("decay", ctypes.c_double), ("dtype", ctypes.c_int32),
-                ("gdtype", ctypes.c_int32)]
+                ("gdtype", ctypes.c_int32), ("fp16_products", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 def _load_library():

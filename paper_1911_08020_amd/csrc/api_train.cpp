@@ -140,11 +140,12 @@ template <typename F> int over_tensors(const darb_adamw &a, int64_t most, F &&f)
     return DARB_OK;
 }
 
-// Whether the result's own type asks for products as accurate as fp32.  Those of small matrices are,
-// whatever the type: with single products their results are up to 6 10^-3 of the norm off (3 10^-3 from
-// 64 on).  16 matrices of 48 x 48 take 127 us so instead of 123, of 48 x 2000 241 instead of 192.
+// Whether products are as accurate as fp32: unless the caller takes those of fp16 operands for a 16-bit
+// result.  Small matrices are accurate all the same: with single products their results are up to
+// 6 10^-3 of the norm off (3 10^-3 from 64 on).  16 matrices of 48 x 48 take 127 us so instead of 123,
+// of 48 x 2000 241 instead of 192.
 bool muon_full(const darb_muon_tensor &t) {
-    return t.dtype == DARB_F32 || t.master || (t.rows < t.cols ? t.rows : t.cols) < 64;
+    return !t.fp16_products || t.dtype == DARB_F32 || t.master || (t.rows < t.cols ? t.rows : t.cols) < 64;
 }
 
 // The groups of tensors that go through the launches together: consecutive ones of one accuracy,
@@ -694,6 +695,8 @@ static int check_muon(const darb_muon_tensor *t, int64_t count, bool buffers, bo
         if (t[i].rows < 1 || t[i].rows >= int64_t(1) << 20 || t[i].cols < 1 || t[i].cols >= int64_t(1) << 20)
             return fail(DARB_E_INVALID, name + "rows and cols must be in [1, 2^20)");
         if (!float_dtype(t[i].dtype)) return fail(DARB_E_DTYPE, name + "unknown dtype");
+        if (t[i].fp16_products < 0 || t[i].fp16_products > 1 || t[i].reserved != 0)
+            return fail(DARB_E_INVALID, name + "fp16_products must be 0 or 1, reserved 0");
         if (!buffers) continue;
         if (t[i].ld_param < t[i].cols) return fail(DARB_E_INVALID, name + "a leading dimension is below cols");
         if (!t[i].param || (update && !t[i].momentum)) return fail(DARB_E_INVALID, name + "NULL buffer");

@@ -13,25 +13,27 @@
 // The products run on the matrix cores in fp16 with fp32 sums.  A matrix is kept as hi + lo, two
 // fp16 parts of its value times a power of two (22 bits; the greatest values, |x| <= 1.21,
 // |A| <= 1.46 and |b A + c A A| <= 2.81, stay in fp16's range), and a product as accurate as fp32
-// is hi hi + hi lo + lo hi.  A result of 16 bits takes hi hi alone for A and for the last product:
-// each element is then off by at most 2^-11 of itself, the result by 1 to 3 10^-3 of its norm (the
-// steps amplify what happens to small singular values as they do these), beside a rounding of
-// 2^-9.  A A is computed from both parts then too: A is close to a multiple of the identity
-// when m is well below n, and its one large diagonal's rounding would be half of the error.  a X is
-// added from both parts, so that what X has in no direction does not grow out of its rounding.
+// is hi hi + hi lo + lo hi.  A result of 16 bits may, where its caller asks for that, take hi hi alone
+// for A and for the last product: each element is then off by at most 2^-11 of itself, the result by 1
+// to 3 10^-3 of its norm (the steps amplify what happens to small singular values as they do these),
+// beside its rounding (2^-8 of an element in bf16, 2^-11 in fp16).  A A is computed from both parts
+// then too: A is close to a multiple of the identity when m is well below n, and its one large
+// diagonal's rounding would be half of the error.  a X is added from both parts, so that what X has in
+// no direction does not grow out of its rounding.
 //
 // Every product is rows by rows, C[i, j] = sum_k P[i, k] Q[j, k]: A from X, A A from A
 // (symmetric), and the last one from b A + c A A and X^T, so each step writes X in both
 // orders.  Buffers are padded with zeros to multiples of 32, which the steps keep.  All matrices of a
 // call go through one launch per product, the longest sums first.
 //
-// Bound by the matrix cores: 3 m m n + m m m operations a step (three times that for fp32 results),
+// Bound by the matrix cores: 3 (3 m m n + m m m) operations a step (of fp16 products 3 m m n + 3 m m m),
 // on whose random operands a large library product in fp16 reaches 1.4 to 1.5 10^15 a second here
-// (2.1 on zeros: it is the power).  Measured on MI355X: 4096 x 9216 in fp32 7.1 ms (1.1 10^15; X's
-// product 1.2, A's 1.1, A A's 1.0); the eight matrices of a 1500-wide model with its momentum's update,
-// fp32 masters of bf16, 4.4 ms (0.4 of it momentum, norm, first X and parameters, at 5 TB/s); eight
-// bf16 matrices of 256 x 1024 147 us (17 launches of 6 to 10 us: a tile's 32 stages one after
-// another).  Equal shares of all stages for each workgroup, cut tiles finished by the last to come,
+// (2.1 on zeros: it is the power).  Measured on MI355X: 4096 x 9216 in fp32 or 16 bits 7.0 ms
+// (1.1 10^15; X's product 1.2, A's 1.1, A A's 1.0), with fp16 products 3.8; the eight matrices of a
+// 1500-wide model with its momentum's update, fp32 masters of bf16, 4.4 ms (0.4 of it momentum, norm,
+// first X and parameters, at 5 TB/s), without masters 4.4, with fp16 products 2.7; eight bf16 matrices
+// of 256 x 1024 184 us, with fp16 products 150 (17 launches of 6 to 12 us: a tile's 32 stages one
+// after another).  Equal shares of all stages for each workgroup, cut tiles finished by the last to come,
 // took 11.9 ms, 10.4 ms and 377 us: workgroups at unlike places of their sums share nothing in L2.
 #include "darb_internal.h"
 #include "float_io.h"
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(MuonCall c) {
 
 // What the workgroups of a launch look for their matrix in.  It travels with the launch: out of the
 // call in memory each matrix on the way costs a load that the next one waits for (eight matrices of
-// 256 x 1024: 164 us instead of 147).
+// 256 x 1024, fp16 products: 164 us instead of 147).
 struct Shares {
     int count;
     int tiles[kMuonTensors];
@@ -566,7 +568,7 @@ __global__ __launch_bounds__(WR *WC *kWave) void product_kernel(const MuonCall *
 //                          64: 610 274 1192
 //   four of 1500 x 1500, four of 1500 x 6000, fp32 masters
 //                          256: 387 134 459   192: 259 157 454   128: 258 124 466
-//   eight of 256 x 1024 bf16   256: 33 30 28   192: 22 20 19   128: 17 17 15   64: 10 7 10
+//   eight of 256 x 1024, fp16 products   256: 33 30 28   192: 22 20 19   128: 17 17 15   64: 10 7 10
 struct Tile {
     int rows, cols;
     float rate;

@@ -669,10 +669,12 @@ def _muon_workspace(table, count: int, device, workspace):
     return _workspace(_lib.darb_muon_workspace, "darb_muon_workspace", device, workspace, table, count)
 
 
-def orthogonalize(G, steps: int = 5, eps: float = 1e-7, out=None, workspace=None, stream=None):
+def orthogonalize(G, steps: int = 5, eps: float = 1e-7, out=None, workspace=None, stream=None,
+                  fp16_products: bool = False):
     """G [m, n], or each matrix of G [k, m, n] (fp32, fp16 or bf16; one of the last two strides 1),
     with its singular values taken towards 1: G / (|G| + eps) through ``steps`` steps of a quintic
-    (darb_orthogonalize).  ``out`` may be G."""
+    (darb_orthogonalize).  ``out`` may be G.  ``fp16_products``: a 16-bit result may be off by 1 to
+    3 10^-3 of its norm beside its rounding, and takes less time."""
     torch = _torch()
     _require_cuda(G)
     code = _float_code(G, "G")
@@ -697,7 +699,7 @@ def orthogonalize(G, steps: int = 5, eps: float = 1e-7, out=None, workspace=None
     for i in range(count):
         table[i] = _MuonTensor(b.data_ptr() + i * b.stride(0) * size, None,
                                a.data_ptr() + i * a.stride(0) * size, None, rows, cols, ldb, lda,
-                               1.0, 0.0, code, code)
+                               1.0, 0.0, code, code, int(bool(fp16_products)))
     with _memory_of(stream):
         workspace = _muon_workspace(table, count, G.device, workspace)
     _check(_lib.darb_orthogonalize(table, count, int(steps), float(eps), _ptr(workspace),
@@ -715,7 +717,8 @@ class Muon:
     keeps fp32 copies of the 16-bit ones, which the step updates and rounds into the parameters;
     or a list of fp32 tensors (or None) to use.  ``scale``: one number or one per matrix (None:
     sqrt(max(1, rows / cols))); ``weight_decay`` as well.  ``state``: momenta to go on from, fp32
-    of the matrices' shapes (``momenta`` has them).
+    of the matrices' shapes (``momenta`` has them).  ``fp16_products``: the updates of 16-bit
+    parameters without masters may be off by 1 to 3 10^-3 of their norm, and take less time.
 
     The tensors must not overlap.  The optimizer keeps references to them, and its workspace, of
     some 16 bytes an element of the largest group of up to 28 matrices; a step reads the gradients
@@ -724,7 +727,7 @@ class Muon:
 
     def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
                  weight_decay=0.0, steps: int = 5, eps: float = 1e-7, scale=None, masters=None,
-                 state=None, stream=None):
+                 state=None, stream=None, fp16_products: bool = False):
         torch = _torch()
         self.params = list(params)
         if not self.params:
@@ -763,7 +766,7 @@ class Muon:
                 p.data_ptr(), None if t is None else _vector(t, p.numel(), f"master {i}").value, None,
                 _vector(m, p.numel(), f"state {i}").value, rows, cols, cols, cols,
                 math.sqrt(max(1.0, rows / cols)) if scales[i] is None else float(scales[i]),
-                float(decays[i]), _float_code(p, f"parameter {i}"), 0)
+                float(decays[i]), _float_code(p, f"parameter {i}"), 0, int(bool(fp16_products)))
         _after_current(stream)              # the masters and zeros above
         self.workspace = _muon_workspace(self._table, count, dev, None)
         self._streams = set()               # that _hold_on was told of
