@@ -87,7 +87,8 @@ struct PolicyToken {
 __device__ __forceinline__ float policy_token(const PolicyCall &c, const PolicyToken &t, Sums &s) {
     if (t.w == 0.0f) return 0.0f;       // whatever stands there
     const double d = double(t.lp) - double(t.old);
-    const float ra = exp_of(float(d)) * t.A;
+    // a finite ratio times 0, where fp32 holds the ratio as infinite too
+    const float ra = t.A == 0.0f && isfinite(d) ? 0.0f : exp_of(float(d)) * t.A;
     float loss = -ra, grad = -ra;
     if (t.A > 0.0f && d > c.log_high) {
         loss = -(c.high * t.A);
