@@ -609,9 +609,12 @@ int darb_gated_recurrence_grad(int dtype, int form, int64_t H, int64_t T, int64_
  * A token of weight 0 adds nothing and has gradient 0, whatever its other values are.
  *   logprob, old, advantage   device fp32 [B], 1 <= B < 2^31
  *   weight        device fp32 [B], or NULL (1 / B each)
- *   ref           device fp32 [B], or NULL (kl is 0; kl_coef must be 0 then)
+ *   ref           device fp32 [B], or NULL (kl is 0; kl_coef must be 0 then); with kl_coef 0 it
+ *                 changes kl alone, whatever it holds
  *   entropy       device fp32 [B], with grad_entropy, or NULL both (entropy_coef 0)
  *   clip_low, clip_high   >= 0 (clip_low of 1 or more: no lower bound); kl_coef >= 0
+ * r and e^q are formed in fp32: past its range (an exponent above 88.7) they count as infinite, but
+ * an A of 0 times a finite r is 0.
  *   stats         device fp32 [3]: loss, kl, clipped
  *   grad_logprob, grad_entropy   device fp32 [B]; may be any of the inputs of that size
  *   workspace     device, 256-byte aligned, >= darb_policy_loss_workspace's bytes; NULL where

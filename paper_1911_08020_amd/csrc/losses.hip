@@ -104,8 +104,10 @@ __device__ __forceinline__ float policy_token(const PolicyCall &c, const PolicyT
         float grown;
         const float k = excess(q, grown);
         s.kl += double(t.w) * double(k);
-        loss += c.kl_coef * k;
-        grad -= c.kl_coef * grown;
+        if (c.kl_coef != 0.0f) {        // 0: kl is only summed, whatever it comes to
+            loss += c.kl_coef * k;
+            grad -= c.kl_coef * grown;
+        }
     }
     if (c.entropy) loss -= c.entropy_coef * t.h;
     s.loss += double(t.w) * double(loss);

@@ -41,3 +41,18 @@ def test_what_is_not_finite_stays(darb):
     # a token of probability 0 now has a ratio of 0
     got = darb.policy_loss(on([-math.inf, -1.0]), on([-1.0, -1.0]), on([0.0, 1.0]))
     assert float(got.loss) == -0.5 and got.grad_logprob.tolist() == [0.0, -0.5]
+
+
+@pytest.mark.parametrize("n", [1, 700, 9001])
+@pytest.mark.parametrize("far", [89.0, 1e4, math.inf, -math.inf, math.nan])
+def test_kl_that_is_only_reported(darb, n, far):
+    """With a coefficient of 0 the reference changes kl, neither the loss nor its gradient."""
+    r, lp, old, A, w, ref, ent = tokens(n, n)
+    w = f32(w + 1e-3 / n)
+    ref[::7] = far
+    without = darb.policy_loss(on(lp), on(old), on(A), weight=on(w))
+    got = darb.policy_loss(on(lp), on(old), on(A), weight=on(w), ref_logprob=on(ref), kl_coef=0.0)
+    assert torch.isfinite(got.loss) and torch.equal(got.loss, without.loss) and torch.equal(got.clipped, without.clipped)
+    assert torch.equal(got.grad_logprob, without.grad_logprob)
+    # a reference of +inf has no value: e^q - 1 - q is infinity less infinity in the definition too
+    assert torch.isnan(got.kl) if math.isnan(far) or far == math.inf else float(got.kl) == math.inf
