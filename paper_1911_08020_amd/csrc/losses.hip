@@ -16,6 +16,7 @@
 // for 700 tokens (one launch) and 8.1 + 3.3 us for 1 M (24 MB from the Infinity Cache), preference
 // 6.1 + 2.1 us for 64 padded pairs' 512 tokens and 8.3 + 3.0 us for 1500 packed pairs of 2.1 M tokens.
 #include "darb_internal.h"
+#include "exp_of.h"
 #include "float_io.h"
 #include "wave.h"
 
@@ -46,15 +47,6 @@ template <int THREADS, int N> __device__ __forceinline__ void block_sums(double 
 #pragma unroll
         for (int d = 1; d < kWaves; d <<= 1) x[i] += __shfl_xor(x[i], d);
     }
-}
-
-// e^x, off by about 2 units: 2^t with t = x log2 e, whose rounding is put right in the result.
-__device__ __forceinline__ float exp_of(float x) {
-    constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
-    const float t = x * kLog2E;
-    const float e = __builtin_amdgcn_exp2f(t);
-    const float r = fmaf(x, kLog2E, -t) * kLn2;
-    return fabsf(t) < 126.0f ? fmaf(e, r, e) : e;           // not where t or e is infinite
 }
 
 // ---- policy ----------------------------------------------------------------------------
