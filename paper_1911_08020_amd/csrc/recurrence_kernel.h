@@ -32,6 +32,7 @@
 #pragma once
 
 #include "darb_internal.h"
+#include "exp_of.h"
 #include "float_io.h"
 #include "wave.h"
 
@@ -108,11 +109,10 @@ template <int V, bool CUTS> __device__ __forceinline__ Map<V, CUTS> map_up(const
     return r;
 }
 
-// f = sigmoid(z) = 1 / (1 + e^-z) and u = 1 - f, each to a few units in its last place (e^-z is off
-// by |z| units where |z| is large, as is the smaller of the two): u is e^-z f where that is the
-// smaller one.
+// f = sigmoid(z) = 1 / (1 + e^-z) and u = 1 - f, each off by at most 9 2^-24 of itself, however small
+// it is (down to 2^-126): u is e^-z f where that is the smaller one.
 __device__ __forceinline__ void gates(float z, float &f, float &u) {
-    const float e = __builtin_amdgcn_exp2f(z * -1.44269504f);
+    const float e = exp_of(-z);
     f = __builtin_amdgcn_rcpf(1.0f + e);
     u = z < 0.0f ? 1.0f - f : e * f;
 }
