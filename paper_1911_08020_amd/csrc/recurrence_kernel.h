@@ -24,11 +24,11 @@
 // one sequence's, read in vectors along time, a chunk a vector.
 //
 // Memory-bound: forward 3 arrays, gradients 6 (linear form 5).  Measured on MI355X: 200 steps of 32
-// sequences of 1024 fp32 features 15.6 us (5.1 TB/s), gradients 35.5 (4.4 TB/s: a tile's loads are not
+// sequences of 1024 fp32 features 16.0 us (4.9 TB/s), gradients 35.8 (4.4 TB/s: a tile's loads are not
 // under way while the one before is joined, and registers leave four waves a SIMD); 65536 steps of
-// 1024 bf16 features of one sequence, with restarts, 177 us (the inputs read twice 3.8 TB/s: each
-// slab's tiles follow one another); gradients of 1500 fp16 rows of 2999 steps, linear form, 14.6 us
-// (3.1 TB/s: rows of 1.5 tiles).
+// 1024 bf16 features of one sequence, with restarts, 187 us (the inputs read twice 3.6 TB/s: each
+// slab's tiles follow one another; 177 with gates off by |z| 2^-24 of themselves); gradients of 1500
+// fp16 rows of 2999 steps, linear form, 14.5 us (3.1 TB/s: rows of 1.5 tiles).
 #pragma once
 
 #include "darb_internal.h"
