@@ -684,8 +684,9 @@ int darb_preference_loss(int64_t pairs, int64_t B, const float *logprob, const f
  *   tensors     host array of `count` >= 1, read during the call; no memory overlaps
  *   steps       1 ... 16;  momentum in [0, 1), lr >= 0, eps > 0 (finite)
  *   grad_scale  device fp32 [1] that multiplies every gradient, or NULL (1)
- *   workspace   device, 256-byte aligned, >= darb_muon_workspace's bytes for these tensors; it
- *               grows with the largest group of tensors that is taken at once
+ *   workspace   device, 256-byte aligned, >= darb_muon_workspace's bytes for these tensors: 16 to 24
+ *               an element (16 + 8 shorter side / longer side, sides padded to multiples of 32) of
+ *               the largest group that is taken at once, of up to 28 tensors and 4 GiB or a single one
  * Errors: DARB_E_INVALID, DARB_E_DTYPE, DARB_E_WORKSPACE, DARB_E_HIP.
  */
 typedef struct {

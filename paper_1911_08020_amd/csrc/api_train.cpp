@@ -149,33 +149,33 @@ bool muon_full(const darb_muon_tensor &t) {
 }
 
 // The groups of tensors that go through the launches together: consecutive ones of one accuracy,
-// up to kMuonTensors and 2^28 elements of theirs (or a single one).  A tensor that is left out
+// up to kMuonTensors and 4 GiB of their buffers (or a single one).  A tensor that is left out
 // (`skip`: without a gradient) counts in its group all the same, so that no step's groups take
 // more than those of all tensors.  f(group, its bytes).
 template <typename F>
 int over_groups(const darb_muon_tensor *t, int64_t count, bool skip, double lr, F &&f) {
-    constexpr int64_t kMostElements = int64_t(1) << 28;
+    constexpr int64_t kMost = int64_t(1) << 32;
     for (int full = 0; full < 2; ++full) {
         MuonCall c{};
         c.full = full != 0;
         int members = 0;
-        int64_t elements = 0;
+        int64_t sum = 0;
         for (int64_t i = 0; i <= count; ++i) {
             const bool end = i == count;
             if (!end && muon_full(t[i]) != c.full) continue;
-            const int64_t n = end ? 0 : t[i].rows * t[i].cols;
-            if (members && (end || members == kMuonTensors || elements + n > kMostElements)) {
+            const int64_t n = end ? 0 : muon_bytes(t[i].rows, t[i].cols);
+            if (members && (end || members == kMuonTensors || sum + n > kMost)) {
                 if (c.count) {
                     const int64_t bytes = muon_group(c);
                     const int rc = f(c, bytes);
                     if (rc) return rc;
                 }
                 members = c.count = 0;
-                elements = 0;
+                sum = 0;
             }
             if (end) break;
             ++members;
-            elements += n;
+            sum += n;
             if (skip && !t[i].grad) continue;
             MuonTensor &to = c.t[c.count++];
             to = {};

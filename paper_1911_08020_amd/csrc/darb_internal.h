@@ -308,6 +308,8 @@ struct MuonCall {
     uint8_t order[2][kMuonTensors];     // filled in: the tensors by m and by n
     int8_t kind[3] = {-1, -1, -1};      // the tiles of A, of b A + c A A and of X; -1: by the sizes
 };
+// The bytes of one matrix' buffers.
+int64_t muon_bytes(int64_t rows, int64_t cols);
 // The bytes of `count` matrices' group; fills in what the launch needs.
 int64_t muon_group(MuonCall &c);
 hipError_t launch_muon(const MuonCall &c, hipStream_t s);

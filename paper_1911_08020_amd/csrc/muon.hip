@@ -655,13 +655,24 @@ template <int PRODUCTS> hipError_t steps(const MuonCall &c, hipStream_t s) {
 
 }  // namespace
 
+static void pad(MuonTensor &t) {
+    const int a = (t.rows + kDepth - 1) / kDepth * kDepth, b = (t.cols + kDepth - 1) / kDepth * kDepth;
+    t.m = t.rows <= t.cols ? a : b;
+    t.n = t.rows <= t.cols ? b : a;
+}
+
+int64_t muon_bytes(int64_t rows, int64_t cols) {
+    MuonTensor t{};
+    t.rows = int32_t(rows), t.cols = int32_t(cols);
+    pad(t);
+    return 2 * Places(t).all();
+}
+
 int64_t muon_group(MuonCall &c) {
     int64_t at = 0;
     for (int i = 0; i < c.count; ++i) {
         MuonTensor &t = c.t[i];
-        const int a = (t.rows + kDepth - 1) / kDepth * kDepth, b = (t.cols + kDepth - 1) / kDepth * kDepth;
-        t.m = t.rows <= t.cols ? a : b;
-        t.n = t.rows <= t.cols ? b : a;
+        pad(t);
         t.base = at;
         at += Places(t).all();
     }

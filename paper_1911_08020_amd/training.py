@@ -720,9 +720,10 @@ class Muon:
     of the matrices' shapes (``momenta`` has them).  ``fp16_products``: the updates of 16-bit
     parameters without masters may be off by 1 to 3 10^-3 of their norm, and take less time.
 
-    The tensors must not overlap.  The optimizer keeps references to them, and its workspace, of
-    some 16 bytes an element of the largest group of up to 28 matrices; a step reads the gradients
-    at their addresses of that call.  Steps on different streams share the workspace: the caller
+    The tensors must not overlap.  The optimizer keeps references to them, and its workspace: 16 to
+    24 bytes an element, square matrices the most, sides padded to multiples of 32, of the largest
+    group of up to 28 matrices and 4 GiB (or a single one).  A step reads the gradients at their
+    addresses of that call.  Steps on different streams share the workspace: the caller
     orders them, replays of captured ones among them."""
 
     def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
