@@ -673,7 +673,7 @@ def orthogonalize(G, steps: int = 5, eps: float = 1e-7, out=None, workspace=None
                   fp16_products: bool = False):
     """G [m, n], or each matrix of G [k, m, n] (fp32, fp16 or bf16; one of the last two strides 1),
     with its singular values taken towards 1: G / (|G| + eps) through ``steps`` steps of a quintic
-    (darb_orthogonalize).  ``out`` may be G.  ``fp16_products``: a 16-bit result may be off by 1 to
+    (darb_orthogonalize).  ``out``, in G's memory order, may be G.  ``fp16_products``: a 16-bit result may be off by 1 to
     3 10^-3 of its norm beside its rounding, and takes less time."""
     torch = _torch()
     _require_cuda(G)
@@ -692,7 +692,8 @@ def orthogonalize(G, steps: int = 5, eps: float = 1e-7, out=None, workspace=None
     a, b = (a, b) if G.dim() == 3 else (a[None], b[None])
     count, rows, cols = a.shape
     lda, ldb = _unit_columns(a[0], "G"), _unit_columns(b[0], "out")
-    if count > 1 and b.stride(0) < (rows - 1) * ldb + cols:
+    apart = b.stride(0)                     # of two matrices: one behind the other, or row by row in turn
+    if count > 1 and apart < (rows - 1) * ldb + cols and not (apart >= cols and ldb >= (count - 1) * apart + cols):
         raise ValueError("the matrices of out must not overlap")
     table = (_MuonTensor * count)()
     size = G.element_size()
