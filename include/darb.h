@@ -664,7 +664,8 @@ int darb_preference_loss(int64_t pairs, int64_t B, const float *logprob, const f
  *   m = momentum m + (1 - momentum) g,  u = momentum m + (1 - momentum) g  (nesterov; else m)
  *   p = p (1 - lr decay) - lr scale X.
  * Sums and m are fp32 or more.  A result is as accurate as fp32 products make it, whatever its type,
- * and rounded to that type once.  The same call gives the same bits; a matrix together with others
+ * and rounded to that type once; X is held to 2^-22 of each element, and not below 2^-40, so that of a
+ * matrix whose norm is far below eps (its X far below 1) less is left.  The same call gives the same bits; a matrix together with others
  * may differ from it alone in how its sums are rounded.
  * A matrix that holds an infinity or NaN becomes NaN; zeros stay zeros.
  *   dtype, gdtype   DARB_F32, DARB_F16 or DARB_BF16, of param and of grad

@@ -32,7 +32,7 @@
 // (1.1 10^15; X's product 1.2, A's 1.1, A A's 1.0), with fp16 products 3.8; the eight matrices of a
 // 1500-wide model with its momentum's update, fp32 masters of bf16, 4.4 ms (0.4 of it momentum, norm,
 // first X and parameters, at 5 TB/s), without masters 4.4, with fp16 products 2.7; eight bf16 matrices
-// of 256 x 1024 184 us, with fp16 products 150 (17 launches of 6 to 12 us: a tile's 32 stages one
+// of 256 x 1024 180 us, with fp16 products 150 (17 launches of 6 to 14 us: a tile's 32 stages one
 // after another).  Equal shares of all stages for each workgroup, cut tiles finished by the last to come,
 // took 11.9 ms, 10.4 ms and 377 us: workgroups at unlike places of their sums share nothing in L2.
 #include "darb_internal.h"

@@ -558,7 +558,9 @@ inline Cut cut_of(int V, int C, int size, bool rows, int64_t T, int64_t W, int64
     if (W % V != 0) V = 1;
     // Feature-major rows that would be read in pieces of less than 64 bytes, unless they are short: 200
     // steps of 1024 fp32 features, 8 sequences 7.5 us through LDS and 11.7 directly (gradients 12.3 and
-    // 16.2), 16 sequences 11.9 and 9.6 (18.5 and 17.3); 48 steps of 8 sequences 6.3 and 5.5.
+    // 16.2), 16 sequences 11.9 and 9.6 (18.5 and 17.3); 48 steps of 8 sequences 6.3 and 5.5.  Of fp16,
+    // 16 sequences 13.6 and 14.6 (20.3 and 17.9: the gradients would rather go directly), 32 sequences
+    // 24.1 and 14.1 (36.1 and 20.5).
     k.layout = rows || W * size >= 64 || T < 64 ? kDirect : W == 1 ? kAlong : kStaged;
     if (k.layout != kDirect) {
         V = 1;
